@@ -6,7 +6,7 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
-_SRC = os.path.join(_HERE, "csrc", "dynlp.hip")
+_SRC = [os.path.join(_HERE, "csrc", name) for name in ("dynlp.hip", "dynlp_train.hip")]
 _SO = os.path.join(_HERE, "libdynlp.so")
 
 
@@ -22,7 +22,7 @@ def build(verbose: bool = False) -> str:
         # packed-FP32 instruction selection is switched off for all device code
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_HERE, "csrc"),
-        "-o", _SO + ".tmp", _SRC,
+        "-o", _SO + ".tmp", *_SRC,
     ]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode != 0:

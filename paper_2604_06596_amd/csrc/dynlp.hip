@@ -36,6 +36,15 @@ namespace {
 
 thread_local std::string g_create_error;
 
+}  // namespace
+
+// The message of this thread's last failed call without a context, for the operators of dynlp_train.hip too.
+namespace dynlp {
+std::string& thread_error() { return g_create_error; }
+}  // namespace dynlp
+
+namespace {
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
