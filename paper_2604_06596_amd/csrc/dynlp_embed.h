@@ -180,50 +180,84 @@ __global__ __launch_bounds__(kBlock) void k_embed_items(TokenList t, const T* ta
         t.scale, out + b * out_ld);
 }
 
-constexpr int kFewTokens = 8192;     // list entries one workgroup can hold: 32 per thread
+constexpr int kFewTokens = 8192;     // 32 for each thread of a workgroup
 constexpr int kZeroRows = 8192;      // rows whose presence one workgroup notes at most
 
-// The gradient for few tokens, without a sort: workgroup i looks through all ids; if token i is the first with its id it lists the
-// others, in order, and adds their rows up.  The workgroups behind those zero the rows of ids that do not occur.
+// The gradient for few tokens, without a sort: workgroup i looks through all ids, each wave through a quarter of them.  If token i is the first
+// with its id, every wave adds up the rows of those it found, four at a time, and the waves' sums are joined in order.  The workgroups behind those zero the rows of
+// ids that do not occur.  One launch instead of the sort's ten; the ids are read count^2 times, from the L2.
 template <typename T, typename O, int V>
-__global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T* grad, int64_t ld, O* out, int64_t out_ld, int dim,
-                                                           int lanes_log2, int zero_rows) {
-    __shared__ int32_t list[kFewTokens];
-    __shared__ uint32_t smem[kBlock / kWave + 1];
-    const int n = (int)t.count;
+__global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T* grad, int64_t ld, O* out, int64_t out_ld, int dim, int zero_rows) {
+    constexpr int kWaves = kBlock / kWave;
+    __shared__ float part[kWaves][kWave * V];
+    __shared__ uint16_t list[kWaves][kFewTokens / kWaves];
+    __shared__ int found[kWaves];
+    __shared__ uint32_t present[kZeroRows / 32];
+    const int n = (int)t.count, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+    const int pieces = (dim + V - 1) / V;
     if ((int64_t)blockIdx.x < t.count) {
         const int me = (int)blockIdx.x;
         bool bad;
         const int32_t id = t.id(me, &bad);
         if (bad && threadIdx.x == 0 && t.rejected) atomicAdd(t.rejected, 1);
         if (id < 0) return;
-        const int per = (n + kBlock - 1) / kBlock;
-        uint32_t hits = 0;
+        const int from = (int)((int64_t)n * wave / kWaves), to = (int)((int64_t)n * (wave + 1) / kWaves);
         bool earlier = false;
-        for (int k = 0; k < per; ++k) {
-            const int i = (int)threadIdx.x * per + k;
-            if (i < n && t.id(i) == id) {
-                hits |= 1u << k;
-                earlier |= i < me;
-            }
+        int mine = 0;
+        for (int i0 = from; i0 < to; i0 += kWave) {
+            const int i = i0 + lane;
+            const bool hit = i < to && t.id(i) == id;
+            earlier |= hit && i < me;
+            const unsigned long long m = __ballot(hit);
+            if (hit) list[wave][mine + (int)__popcll(m & ((1ull << lane) - 1))] = (uint16_t)i;
+            mine += (int)__popcll(m);
         }
+        if (lane == 0) found[wave] = mine;
         if (__syncthreads_or(earlier)) return;
-        uint32_t total;
-        uint32_t at = block_exclusive_scan<uint32_t>((uint32_t)__popc(hits), smem, &total);
-        for (int k = 0; k < per; ++k)
-            if (hits >> k & 1) list[at++] = (int)threadIdx.x * per + k;
-        __syncthreads();
-        block_sum<T, O, V>(
-            grad, ld, dim, lanes_log2, total,
-            [&](int64_t i, float* w) -> int64_t {
-                const int pos = list[i];
-                *w = t.weights ? t.weights[pos] : 1.f;
-                return t.item(pos);
-            },
-            t.scale, out + (int64_t)id * out_ld);
+        int others = 0;
+        for (int w = 0; w < kWaves; ++w) others += w == wave ? 0 : found[w];
+        O* row = out + (int64_t)id * out_ld;
+        const bool alone = __syncthreads_and(mine == 0 || others == 0);
+        for (int c0 = 0; c0 < pieces; c0 += kWave) {
+            const bool inside = c0 + lane < pieces;
+            const int col = piece_column<V>(inside ? c0 + lane : pieces - 1, dim);
+            float acc[V] = {};
+            constexpr int U = 4;
+            for (int k = 0; k < mine; k += U) {
+                Lane<T, V> x[U];
+                float w[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int pos = list[wave][min(k + u, mine - 1)];
+                    const int64_t src = t.item(pos);
+                    const bool ok = k + u < mine && src >= 0;
+                    w[u] = t.weights ? t.weights[pos] : 1.f;
+                    w[u] = ok ? w[u] : 0.f;
+                    x[u].load(grad + max(src, (int64_t)0) * ld + col);
+                    x[u].keep(ok);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float f[V];
+                    x[u].get(f);
+                    for (int e = 0; e < V; ++e) acc[e] += w[u] * f[e];
+                }
+            }
+            if (!alone) {
+                for (int e = 0; e < V; ++e) part[wave][lane * V + e] = acc[e];
+                __syncthreads();
+                if (wave == 0)
+                    for (int w = 1; w < kWaves; ++w)
+                        for (int e = 0; e < V; ++e) acc[e] += part[w][lane * V + e];
+            }
+            if (inside && (alone ? mine > 0 : wave == 0)) {
+                for (int e = 0; e < V; ++e) acc[e] *= t.scale;
+                store_values<V>(row + col, acc);
+            }
+            if (!alone) __syncthreads();
+        }
         return;
     }
-    uint32_t* present = reinterpret_cast<uint32_t*>(list);
     const int64_t first = ((int64_t)blockIdx.x - t.count) * zero_rows;
     const int rows = (int)min((int64_t)zero_rows, t.limit - first);
     for (int k = threadIdx.x; k < (zero_rows + 31) / 32; k += kBlock) present[k] = 0;
@@ -233,7 +267,6 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T*
         if (r >= 0 && r < rows) atomicOr(&present[r >> 5], 1u << (r & 31));
     }
     __syncthreads();
-    const int pieces = (dim + V - 1) / V;
     float zero[V] = {};
     for (int64_t at = threadIdx.x; at < (int64_t)rows * pieces; at += kBlock) {
         const int r = (int)(at / pieces), c = (int)(at - (int64_t)r * pieces);
@@ -243,48 +276,91 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T*
 
 // ---- long lists: sums over pieces of the list, joined ----------------------------------------------------------------
 
-// key[i] = the item of token i (-1: none), src[i] = its id (-1: contributes nothing); the blocks behind those of the tokens zero the rows of items
-// without tokens.
-constexpr int kKeyTile = 1024;
+// Zeros in the rows of `out` from `first` on that the lanes ask for, 64 at most: lane l for row first + l.  From whole waves.
 template <typename T, int V>
-__global__ __launch_bounds__(kBlock) void k_item_keys(TokenList t, int32_t* key, int32_t* src, int token_blocks, T* out,
-                                                      int64_t out_ld, int dim) {
-    if ((int)blockIdx.x < token_blocks) {
-        __shared__ int64_t range[2];
-        const int64_t first = (int64_t)blockIdx.x * kKeyTile;
-        const int64_t last = min(first + kKeyTile, t.count) - 1;
-        if (threadIdx.x < 2) range[threadIdx.x] = t.item_from(threadIdx.x ? last : first, -1, t.items);
-        __syncthreads();
-        const int64_t lo = range[0], hi = max(range[1], lo);
-        for (int64_t i = first + threadIdx.x; i <= last; i += kBlock) {
-            const int64_t b = t.item_from(i, lo, hi);
-            key[i] = b < t.items ? (int32_t)b : -1;
-            bool bad;
-            src[i] = t.id(i, &bad);
-            count_rejected(t.rejected, bad);
-        }
-        return;
+__device__ inline void zero_rows_of_wave(bool mine, int64_t first, T* out, int64_t out_ld, int dim) {
+    const float zero[V] = {};
+    const int pieces = (dim + V - 1) / V;
+    for (unsigned long long m = __ballot(mine); m; m &= m - 1) {
+        T* row = out + (first + __ffsll(m) - 1) * out_ld;
+        for (int c = lane_id(); c < pieces; c += kWave) store_values<V>(row + piece_column<V>(c, dim), zero);
     }
-    const int64_t wave = ((int64_t)blockIdx.x - token_blocks) * (kBlock / kWave) + threadIdx.x / kWave;
-    const int64_t mine = wave * kWave + lane_id();
+}
+
+// Zeros in the rows of items without tokens: block `block` looks at kBlock items.
+template <typename T, int V>
+__device__ inline void zero_empty_items(const TokenList& t, int64_t block, T* out, int64_t out_ld, int dim) {
+    const int64_t first = block * kBlock + (threadIdx.x / kWave) * kWave, mine = first + lane_id();
     bool empty = false;
     if (mine < t.items) {
         int64_t begin, end;
         t.bounds(mine, &begin, &end);
         empty = begin == end;
     }
-    float zero[V] = {};
-    const int pieces = (dim + V - 1) / V;
-    for (unsigned long long m = __ballot(empty); m; m &= m - 1) {
-        T* row = out + (wave * kWave + __ffsll(m) - 1) * out_ld;
-        for (int c = lane_id(); c < pieces; c += kWave) store_values<V>(row + piece_column<V>(c, dim), zero);
+    zero_rows_of_wave<T, V>(empty, first, out, out_ld, dim);
+}
+
+// mark[i] = the item of token first + i, for a tile of TILE tokens of which n are there: -1 before the first item, t.items behind the last.  Each
+// item that begins in the tile is noted at its first token, and a running maximum carries it on.  From all threads of the workgroup.
+template <int TILE>
+__device__ inline void tile_items(const TokenList& t, int64_t first, int n, int32_t* mark, int32_t* range) {
+    constexpr int per = TILE / kBlock;
+    if (threadIdx.x < 2) range[threadIdx.x] = (int32_t)t.item_from(threadIdx.x ? first + n - 1 : first, -1, t.items);
+    __syncthreads();
+    const int32_t lo = range[0], hi = range[1];
+    for (int i = threadIdx.x; i < TILE; i += kBlock) mark[i] = lo;
+    __syncthreads();
+    for (int64_t b = (int64_t)lo + 1 + threadIdx.x; b <= hi; b += kBlock) {
+        const int64_t at = t.offsets[b] - first;
+        if (at >= 0 && at < n) atomicMax(&mark[at], (int32_t)b);
+    }
+    __syncthreads();
+    int32_t v[per], top = -1;
+    for (int k = 0; k < per; ++k) {
+        top = max(top, mark[threadIdx.x * per + k]);
+        v[k] = top;
+    }
+    // the largest of the threads before this one: over the wave, then over the waves
+    int32_t run = top;
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int32_t o = __shfl_up(run, d, kWave);
+        if (lane_id() >= d) run = max(run, o);
+    }
+    int32_t before = __shfl_up(run, 1, kWave);
+    if (lane_id() == 0) before = -1;
+    if (lane_id() == kWave - 1) range[2 + threadIdx.x / kWave] = run;
+    __syncthreads();
+    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) before = max(before, range[2 + w]);
+    for (int k = 0; k < per; ++k) mark[threadIdx.x * per + k] = max(v[k], before);
+    __syncthreads();
+}
+constexpr int kTileRange = 2 + kBlock / kWave;  // words of tile_items' `range`
+
+// For rows that are narrower than a wave: key[i] = the item of token i (-1: none), src[i] = its id (-1: contributes nothing); the blocks
+// behind those of the tokens zero the rows of items without tokens.
+constexpr int kKeyTile = 2048;
+template <typename T, int V>
+__global__ __launch_bounds__(kBlock) void k_item_keys(TokenList t, int32_t* key, int32_t* src, int token_blocks, T* out,
+                                                      int64_t out_ld, int dim) {
+    if ((int)blockIdx.x >= token_blocks) {
+        zero_empty_items<T, V>(t, (int64_t)blockIdx.x - token_blocks, out, out_ld, dim);
+        return;
+    }
+    __shared__ int32_t mark[kKeyTile], range[kTileRange];
+    const int64_t first = (int64_t)blockIdx.x * kKeyTile;
+    const int n = (int)min((int64_t)kKeyTile, t.count - first);
+    tile_items<kKeyTile>(t, first, n, mark, range);
+    for (int i = threadIdx.x; i < n; i += kBlock) {
+        key[first + i] = mark[i] < t.items ? mark[i] : -1;
+        bool bad;
+        src[first + i] = t.id(first + i, &bad);
+        count_rejected(t.rejected, bad);
     }
 }
 
 enum : uint8_t {
-    kHead = 1,     // the piece's first run began before it; its sum is head[piece]
-    kThrough = 2,  // and goes on behind it
-    kOpen = 4      // the piece's last run began in it and goes on behind it; its sum is tail[piece]
+    kHead = 1,    // the piece's first run began before it; its sum is head[piece]
+    kThrough = 2  // and goes on behind it
 };
 
 struct SumList {
@@ -293,24 +369,33 @@ struct SumList {
     const float* factor;   // or NULL
     float* part;           // [piece][head, tail][dim]
     uint8_t* flags;        // [piece]
+    int32_t* open;         // [piece] key of the piece's last run if that began in it and goes on behind it (its sum is tail[piece]); else -1
+    uint8_t* present;      // [out_rows] set for keys that occur, or NULL
     int64_t count;
     int64_t row_count, out_rows;
-    int piece;             // entries of a piece of the list, a multiple of 8
+    int piece;             // entries of a piece of the list
     float scale;
+
+    __device__ inline bool real(int32_t k) const { return k >= 0 && k < out_rows; }
+    // What a piece leaves beside its sums; by one lane.
+    __device__ inline void leave(int64_t g, uint8_t f, int32_t k) const {
+        flags[g] = f;
+        open[g] = k;
+        if (present && k >= 0) present[k] = 1;
+    }
 };
 
-// A group of lanes goes through one piece of the list with a running sum; lanes are across the columns (blockIdx.y: 2^lanes_log2 lane
-// columns each).  Eight rows are asked for at a time.  Runs that lie within the piece are written to `out`, the first and the last, where
+// For rows that are narrower than a wave: a group of lanes goes through one piece of the list with a running sum; lanes are across the
+// columns.  Eight rows are asked for at a time.  Runs that lie within the piece are written to `out`, the first and the last, where
 // they go on beyond it, to `part`.
 template <typename T, typename O, int V>
 __global__ __launch_bounds__(kBlock) void k_segment_sum(SumList s, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim,
                                                         int lanes_log2) {
     const int64_t g = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> lanes_log2;
     const int lane = threadIdx.x & ((1 << lanes_log2) - 1);
-    const int c = ((int)blockIdx.y << lanes_log2) + lane;
     const int64_t first = g * s.piece;
-    if (first >= s.count || c * V >= dim + V - 1 || (V > 1 && c * V >= dim)) return;
-    const int col = piece_column<V>(c, dim);
+    if (first >= s.count || lane * V >= dim) return;
+    const int col = piece_column<V>(lane, dim);
     const int64_t end = min(first + s.piece, s.count);
     rows += col;
     out += col;
@@ -323,10 +408,11 @@ __global__ __launch_bounds__(kBlock) void k_segment_sum(SumList s, const T* rows
         if (before) {
             store_values<V>(part, acc);
             flags |= kHead;
-        } else if (cur >= 0 && cur < s.out_rows) {
+        } else if (s.real(cur)) {
             float f[V];
             for (int k = 0; k < V; ++k) f[k] = acc[k] * s.scale;
             store_values<V>(out + (int64_t)cur * out_ld, f);
+            if (s.present && lane == 0) s.present[cur] = 1;
         }
     };
     constexpr int U = 8;
@@ -364,11 +450,137 @@ __global__ __launch_bounds__(kBlock) void k_segment_sum(SumList s, const T* rows
         flags |= kHead | kThrough;
     } else if (goes_on) {
         store_values<V>(part + dim, acc);
-        flags |= kOpen;
     } else {
         flush();
     }
-    if (c == 0) s.flags[g] = flags;
+    if (lane == 0) s.leave(g, flags, goes_on && !before && s.real(cur) ? cur : -1);
+}
+
+// For rows of 256 bytes and more: a wave goes through one piece of the list (E columns per lane, blockIdx.y: 64 E columns).  64 entries are
+// read at once, one per lane; each is then handed to all lanes through scalar registers, so that a row's address, the end of a run and
+// the branch over what contributes nothing cost the vector units nothing: per entry they unpack and add E columns.  Eight rows are
+// asked for at a time.  With ITEMS the keys are the items, whose bounds are read from the offsets as they come; the blocks behind those of the list
+// zero the rows of items without tokens.
+template <typename T, typename O, int E, bool ITEMS>
+__global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim,
+                                                     int sum_blocks) {
+    if (ITEMS && (int)blockIdx.x >= sum_blocks) {
+        if (blockIdx.y == 0) zero_empty_items<O, Piece<O>::n>(t, (int64_t)blockIdx.x - sum_blocks, out, out_ld, dim);
+        return;
+    }
+    const int64_t g = (int64_t)blockIdx.x * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t first = g * s.piece;
+    if (first >= s.count) return;
+    const int64_t end = min(first + s.piece, s.count);
+    const int lane = lane_id();
+    const int c = (int)blockIdx.y * (kWave * E) + lane * E;
+    const bool inside = c < dim;
+    const int col = min(c, dim - E);
+    const uint32_t off = (uint32_t)col * (uint32_t)sizeof(T);  // beside a row's address, which is the same for all lanes
+    out += col;
+    float* part = s.part + g * 2 * dim + col;
+    int64_t item = 0, next = 0;  // ITEMS: the item at hand and where it ends
+    int32_t cur;
+    bool before;
+    if (ITEMS) {
+        item = t.item_from(first, -1, t.items);
+        next = item < t.items ? t.offsets[item + 1] : INT64_MAX;
+        cur = item >= 0 && item < t.items ? (int32_t)item : -1;
+        before = cur >= 0 && t.offsets[item] < first;
+    } else {
+        cur = s.key[first];
+        before = first > 0 && s.key[first - 1] == cur;
+    }
+    uint8_t flags = 0;
+    float acc[E] = {};
+    auto flush = [&]() {
+        if (before) {
+            if (inside) store_values<E>(part, acc);
+            flags |= kHead;
+        } else if (s.real(cur)) {
+            float f[E];
+            for (int k = 0; k < E; ++k) f[k] = acc[k] * s.scale;
+            if (inside) store_values<E>(out + (int64_t)cur * out_ld, f);
+            if (!ITEMS && s.present && c == 0) s.present[cur] = 1;
+        }
+        before = false;
+        for (int k = 0; k < E; ++k) acc[k] = 0.f;
+    };
+    constexpr int U = 8;
+    for (int64_t base = first; base < end; base += kWave) {
+        const int64_t at = base + lane;
+        const int n = (int)min((int64_t)kWave, end - base);
+        int32_t src = -1, key = cur;
+        float w = 0.f;
+        unsigned long long ends = 0;  // sorted lists: entries that begin another run
+        if (ITEMS) {
+            bool bad = false;
+            if (lane < n) {
+                src = t.id(at, &bad);
+                if (src >= 0) w = t.weights ? t.weights[at] : 1.f;
+            }
+            if (blockIdx.y == 0) count_rejected(t.rejected, bad);
+        } else {
+            if (lane < n) {
+                key = s.key[at];
+                src = s.src[at];
+                if (!s.real(key) || src >= s.row_count) src = -1;
+                if (src >= 0) w = s.factor ? s.factor[at] : 1.f;
+            }
+            int32_t last = __shfl_up(key, 1, kWave);
+            if (lane == 0) last = cur;
+            ends = __ballot(lane < n && key != last);
+        }
+        for (int j = 0; j < n; j += U) {
+            Columns<T, E> x[U];
+            const int stop = ITEMS && next < end ? (int)(next - base) - j : kWave;  // where the item ends, among the eight
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t from = __builtin_amdgcn_readlane(src, j + u);
+                if (from >= 0)
+                    x[u].load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(rows + (int64_t)from * ld) + off));
+                else
+                    x[u].zero();
+            }
+            if (ITEMS ? stop >= U : (ends >> j & 255) == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j + u));
+                    for (int e = 0; e < E; ++e) acc[e] += f * x[u].get(e);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (ITEMS) {
+                        if (base + j + u == next && next < end) {
+                            flush();
+                            do {
+                                ++item;
+                            } while (item < t.items && t.offsets[item + 1] <= base + j + u);
+                            next = item < t.items ? t.offsets[item + 1] : INT64_MAX;
+                            cur = item < t.items ? (int32_t)item : -1;
+                        }
+                    } else if (ends >> (j + u) & 1) {
+                        flush();
+                        cur = __builtin_amdgcn_readlane(key, j + u);
+                    }
+                    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j + u));
+                    for (int e = 0; e < E; ++e) acc[e] += f * x[u].get(e);
+                }
+            }
+        }
+    }
+    const bool goes_on = end < s.count && (ITEMS ? next > end : s.key[end] == cur);
+    const bool opens = goes_on && !before;
+    if (goes_on && before) {
+        if (inside) store_values<E>(part, acc);
+        flags |= kHead | kThrough;
+    } else if (goes_on) {
+        if (inside) store_values<E>(part + dim, acc);
+    } else {
+        flush();
+    }
+    if (c == 0) s.leave(g, flags, opens && s.real(cur) ? cur : -1);
 }
 
 // Runs that several pieces share: the wave of the piece in which such a run begins adds up its parts, in their order within each group of
@@ -376,9 +588,9 @@ __global__ __launch_bounds__(kBlock) void k_segment_sum(SumList s, const T* rows
 template <typename O, int V>
 __global__ __launch_bounds__(kBlock) void k_segment_join(SumList s, int64_t pieces, O* out, int64_t out_ld, int dim, int lanes_log2) {
     const int64_t p = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kWave;
-    if (p >= pieces || !(s.flags[p] & kOpen)) return;
-    const int32_t key = s.key[(p + 1) * s.piece - 1];
-    if (key < 0 || key >= s.out_rows) return;
+    if (p >= pieces) return;
+    const int32_t key = s.open[p];
+    if (key < 0) return;
     int64_t last = p + 1;  // the piece in which the run ends
     for (;; last += kWave) {
         const int64_t at = last + lane_id();
@@ -407,7 +619,7 @@ __global__ __launch_bounds__(kBlock) void k_segment_join(SumList s, int64_t piec
     }
 }
 
-// Rows of zeros, for the gradient of ids that do not occur.
+// Rows of zeros, for the gradient of no tokens at all.
 template <typename O, int V>
 __global__ __launch_bounds__(kBlock) void k_zero_rows(O* out, int64_t out_ld, int64_t rows, int dim, int pieces) {
     const float zero[V] = {};
@@ -417,11 +629,19 @@ __global__ __launch_bounds__(kBlock) void k_zero_rows(O* out, int64_t out_ld, in
     }
 }
 
+// Zeros in the rows of ids that do not occur.
+template <typename O, int V>
+__global__ __launch_bounds__(kBlock) void k_zero_absent(const uint8_t* present, O* out, int64_t out_ld, int64_t rows, int dim) {
+    const int64_t first = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kWave * kWave, mine = first + lane_id();
+    zero_rows_of_wave<O, V>(mine < rows && !present[mine], first, out, out_ld, dim);
+}
+
 // ---- stable radix sort of (id, item, weight) by id -------------------------------------------------------------------
 
 constexpr int kSortTile = 4096;                       // entries per workgroup
 constexpr int kSortItems = kSortTile / kBlock;        // per thread
 constexpr int kDigits = 256;
+constexpr int kClear = kBlock * 16;                   // bytes a workgroup clears
 
 struct SortPass {
     const int32_t* key;  // NULL in the first pass: ids are read from the list
@@ -443,7 +663,13 @@ __device__ inline int32_t sort_key(const TokenList& t, const SortPass& p, int64_
     return id < 0 ? (int32_t)t.limit : id;
 }
 
-__global__ __launch_bounds__(kBlock) void k_sort_count(TokenList t, SortPass p) {
+// The blocks behind those of the tiles (first pass) clear the notes of which ids occur.
+__global__ __launch_bounds__(kBlock) void k_sort_count(TokenList t, SortPass p, uint8_t* present) {
+    if ((int)blockIdx.x >= p.tiles) {
+        const int64_t at = ((int64_t)blockIdx.x - p.tiles) * kClear + threadIdx.x * 16;
+        if (at < t.limit) *reinterpret_cast<u32x4*>(present + at) = u32x4{0u, 0u, 0u, 0u};  // its end is padded to 256 bytes
+        return;
+    }
     __shared__ uint32_t count[kDigits];
     count[threadIdx.x] = 0;
     __syncthreads();
@@ -481,30 +707,42 @@ __global__ __launch_bounds__(kBlock) void k_sort_offsets(SortPass p) {
 }
 
 // Each wave ranks its 1,024 consecutive entries 64 at a time among those of the same digit (lanes of one digit are found by a ballot
-// per bit), the ranks are made the tile's, the entries are put in order in shared memory and written out as runs.
+// per bit), the ranks are made the tile's, and keys, sources and factors are put in order in shared memory, one after the other in the same 16 KB, and
+// written out as runs.
 __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p) {
     constexpr int kWaves = kBlock / kWave;
     __shared__ uint32_t count[kWaves][kDigits];
-    __shared__ uint32_t begin[kDigits];  // of each digit within the tile
-    __shared__ uint32_t to[kDigits];     // of each digit's entries of this tile in the output
+    __shared__ uint32_t to[kDigits];  // place of a digit's entries of this tile in the output, less their place in the tile
     __shared__ uint32_t smem[kWaves + 1];
-    __shared__ int32_t keys[kSortTile], srcs[kSortTile];
-    __shared__ float factors[kSortTile];
-    __shared__ int64_t range[2];
+    __shared__ int32_t range[kTileRange];
+    __shared__ int32_t order[kSortTile];
     const int wave = threadIdx.x / kWave, lane = lane_id();
     const uint32_t mask = (1u << p.bits) - 1;
     const int64_t first = (int64_t)blockIdx.x * kSortTile;
     const int n = (int)min((int64_t)kSortTile, t.count - first);
     for (int k = 0; k < kWaves; ++k) count[k][threadIdx.x] = 0;
-    if (!p.key && t.offsets && threadIdx.x < 2) range[threadIdx.x] = t.item_from(threadIdx.x ? first + n - 1 : first, -1, t.items);
-    __syncthreads();
-    int32_t key[kSortItems];
+    const int mine = wave * (kSortTile / kWaves) + lane;  // entry mine + 64 r of the tile
+    int32_t key[kSortItems], src[kSortItems];
     uint32_t rank[kSortItems];
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int at = wave * (kSortTile / kWaves) + r * kWave + lane;
-        const bool in = at < n;
-        key[r] = in ? sort_key(t, p, first + at) : 0;
+        const int at = mine + r * kWave;
+        key[r] = at < n ? sort_key(t, p, first + at) : 0;
+        if (p.key) src[r] = at < n ? p.src[first + at] : 0;
+    }
+    if (!p.key) {
+        if (t.offsets) tile_items<kSortTile>(t, first, n, order, range);
+#pragma unroll
+        for (int r = 0; r < kSortItems; ++r) {
+            const int at = mine + r * kWave;
+            src[r] = t.offsets ? order[at] : (int32_t)(first + at);
+            if (src[r] >= t.items) src[r] = -1;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const bool in = mine + r * kWave < n;
         const uint32_t d = ((uint32_t)key[r] >> p.shift) & mask;
         unsigned long long same = __ballot(in);
         for (int b = 0; b < p.bits; ++b) {
@@ -521,46 +759,53 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p
     {
         const uint32_t d = threadIdx.x;
         uint32_t sum = 0;
+        for (int k = 0; k < kWaves; ++k) sum += count[k][d];
+        uint32_t ignored;
+        uint32_t begin = block_exclusive_scan<uint32_t>(sum, smem, &ignored);
+        const uint32_t all = block_exclusive_scan<uint32_t>(d <= mask ? p.totals[d] : 0u, smem, &ignored);
+        to[d] = all + (d <= mask ? p.hist[(int64_t)d * p.tiles + blockIdx.x] : 0u) - begin;
         for (int k = 0; k < kWaves; ++k) {
             const uint32_t v = count[k][d];
-            count[k][d] = sum;
-            sum += v;
+            count[k][d] = begin;
+            begin += v;
         }
-        uint32_t ignored;
-        begin[d] = block_exclusive_scan<uint32_t>(sum, smem, &ignored);
-        const uint32_t all = block_exclusive_scan<uint32_t>(d <= mask ? p.totals[d] : 0u, smem, &ignored);
-        to[d] = all + (d <= mask ? p.hist[(int64_t)d * p.tiles + blockIdx.x] : 0u);
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int at = wave * (kSortTile / kWaves) + r * kWave + lane;
-        if (at < n) {
-            const uint32_t d = ((uint32_t)key[r] >> p.shift) & mask;
-            const uint32_t pos = begin[d] + count[wave][d] + rank[r];
-            keys[pos] = key[r];
-            if (p.key) {
-                srcs[pos] = p.src[first + at];
-                if (p.factor_out) factors[pos] = p.factor[first + at];
-            } else {
-                const int64_t i = first + at;
-                int64_t b = i;
-                if (t.offsets) {
-                    b = t.item_from(i, range[0], max(range[0], range[1]));
-                    if (b >= t.items) b = -1;
-                }
-                srcs[pos] = (int32_t)b;
-                if (p.factor_out) factors[pos] = t.weights[i];
-            }
-        }
+        rank[r] += count[wave][((uint32_t)key[r] >> p.shift) & mask];
+        if (mine + r * kWave < n) order[rank[r]] = key[r];
     }
     __syncthreads();
-    for (int at = threadIdx.x; at < n; at += kBlock) {
-        const uint32_t d = ((uint32_t)keys[at] >> p.shift) & mask;
-        const uint32_t pos = to[d] + (uint32_t)at - begin[d];
-        p.key_out[pos] = keys[at];
-        p.src_out[pos] = srcs[at];
-        if (p.factor_out) p.factor_out[pos] = factors[at];
+    uint32_t place[kSortItems];
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const int at = (int)threadIdx.x + r * kBlock;
+        const int32_t k = at < n ? order[at] : 0;
+        place[r] = to[((uint32_t)k >> p.shift) & mask] + (uint32_t)at;
+        if (at < n) p.key_out[place[r]] = k;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r)
+        if (mine + r * kWave < n) order[rank[r]] = src[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const int at = (int)threadIdx.x + r * kBlock;
+        if (at < n) p.src_out[place[r]] = order[at];
+    }
+    if (!p.factor_out) return;
+    __syncthreads();
+    const float* factor = p.key ? p.factor : t.weights;
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r)
+        if (mine + r * kWave < n) order[rank[r]] = __float_as_int(factor[first + mine + r * kWave]);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const int at = (int)threadIdx.x + r * kBlock;
+        if (at < n) p.factor_out[place[r]] = __int_as_float(order[at]);
     }
 }
 

@@ -127,10 +127,15 @@ int lanes_log2(int pieces) {
 
 constexpr int64_t kFewPerItem = 2048;  // tokens up to which each item has a workgroup
 
-// Entries of a piece of the list.  Pieces enough for 8,192 waves (32 for each CU), where the list has so many; not below 16 entries, so that
-// the parts a piece leaves are few against the rows it reads, and not above 512, so that a run over many pieces is joined soon.
-int piece_length(int64_t count, int dim) {
+// Rows of 256 bytes and more have waves of their own (k_wave_sum).
+bool wide_rows(int32_t type, int dim) { return (int64_t)dim * type_size(type) >= 256; }
+
+// Entries of a piece of the list.  Pieces enough for 16,384 waves, or groups of lanes for 8,192, where the list has so many entries (32 waves fit
+// each of the 256 CUs); not so few entries that the two parts a piece may leave weigh much against the rows it reads, and not above 512, so that a run
+// over many pieces is joined soon.
+int piece_length(int64_t count, int dim, bool wide) {
     const int64_t lanes = std::min<int64_t>(ceil_div(dim, 8), 64);
+    if (wide) return (int)std::min<int64_t>(std::max<int64_t>(round_up(ceil_div(count, 16384), 64), 64), 512);
     return (int)std::min<int64_t>(std::max<int64_t>(round_up(ceil_div(count * lanes, 8192 * 64), 8), 16), 512);
 }
 
@@ -141,29 +146,43 @@ struct SumSpace {
     float* factor2;
     uint32_t *hist, *totals;
     float* part;
-    uint8_t* flags;
+    uint8_t *flags, *present;
+    int32_t* open;
     int piece;
     int64_t pieces, tiles;
 };
 
-int64_t sum_space(char* base, int64_t count, int dim, bool sorted, SumSpace* s) {
+// sorted: rows of the gradient that is asked for, or -1.
+int64_t sum_space(char* base, int64_t count, int dim, bool wide, int64_t sorted, SumSpace* s) {
     Carve c{base};
-    s->piece = piece_length(count, dim);
+    s->piece = piece_length(count, dim, wide);
     s->pieces = ceil_div(count, s->piece);
     s->tiles = ceil_div(count, kSortTile);
-    s->key = c.take<int32_t>(count);
-    s->src = c.take<int32_t>(count);
-    if (sorted) {
+    if (sorted >= 0 || !wide) {
+        s->key = c.take<int32_t>(count);
+        s->src = c.take<int32_t>(count);
+    }
+    if (sorted >= 0) {
         s->factor = c.take<float>(count);
         s->key2 = c.take<int32_t>(count);
         s->src2 = c.take<int32_t>(count);
         s->factor2 = c.take<float>(count);
         s->hist = c.take<uint32_t>(kDigits * s->tiles);
         s->totals = c.take<uint32_t>(kDigits);
+        s->present = c.take<uint8_t>(sorted);
     }
     s->part = c.take<float>(s->pieces * 2 * dim);
     s->flags = c.take<uint8_t>(s->pieces);
+    s->open = c.take<int32_t>(s->pieces);
     return c.used;
+}
+
+// Whatever the type: rows of dim elements may be wide or not.
+int64_t sum_space_bytes(int64_t count, int dim, int64_t sorted) {
+    SumSpace s{};
+    const int64_t narrow = wide_rows(DYNLP_BFLOAT16, dim) ? 0 : sum_space(nullptr, count, dim, false, sorted, &s);
+    const int64_t wide = wide_rows(DYNLP_FLOAT32, dim) ? sum_space(nullptr, count, dim, true, sorted, &s) : 0;
+    return std::max(narrow, wide);
 }
 
 TokenList token_list(const dynlp_tokens* t, int64_t table_rows) {
@@ -171,12 +190,29 @@ TokenList token_list(const dynlp_tokens* t, int64_t table_rows) {
 }
 
 template <typename T, typename O, int V>
-void launch_sums(const SumList& s, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim, hipStream_t stream) {
-    const int pieces = (int)ceil_div(dim, V), l = lanes_log2(pieces);
+void launch_narrow(const SumList& s, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim, hipStream_t stream) {
+    const int l = lanes_log2((int)ceil_div(dim, V));
     const int64_t n = ceil_div(s.count, s.piece);
-    const unsigned across = (unsigned)ceil_div(pieces, 1 << l);
-    k_segment_sum<T, O, V><<<dim3((unsigned)ceil_div(n << l, kBlock), across), kBlock, 0, stream>>>(s, rows, ld, out, out_ld, dim, l);
-    k_segment_join<O, V><<<dim3((unsigned)ceil_div(n * kWave, kBlock), across), kBlock, 0, stream>>>(s, n, out, out_ld, dim, l);
+    k_segment_sum<T, O, V><<<(unsigned)ceil_div(n << l, kBlock), kBlock, 0, stream>>>(s, rows, ld, out, out_ld, dim, l);
+    k_segment_join<O, V><<<(unsigned)ceil_div(n * kWave, kBlock), kBlock, 0, stream>>>(s, n, out, out_ld, dim, l);
+}
+
+// A lane takes as many columns as a row needs for 64 lanes, 4 to 16 bytes of them.
+template <typename T, typename O, bool ITEMS>
+void launch_wide(const SumList& s, const TokenList& t, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim, hipStream_t stream) {
+    const int64_t n = ceil_div(s.count, s.piece), blocks = ceil_div(n, kBlock / kWave);
+    const unsigned grid = (unsigned)(blocks + (ITEMS ? ceil_div(t.items, kBlock) : 0));
+    constexpr int e = 4 / (int)sizeof(T);
+    auto sum = [&](auto width) {
+        constexpr int E = decltype(width)::v;
+        k_wave_sum<T, O, E, ITEMS><<<dim3(grid, (unsigned)ceil_div(dim, kWave * E)), kBlock, 0, stream>>>(s, t, rows, ld, out, out_ld, dim, (int)blocks);
+    };
+    if (dim <= kWave * e) sum(Width<e>());
+    else if (dim <= kWave * 2 * e) sum(Width<2 * e>());
+    else sum(Width<4 * e>());
+    constexpr int V = Piece<O>::n;
+    const int pieces = (int)ceil_div(dim, V), l = lanes_log2(pieces);
+    k_segment_join<O, V><<<dim3((unsigned)ceil_div(n * kWave, kBlock), (unsigned)ceil_div(pieces, 1 << l)), kBlock, 0, stream>>>(s, n, out, out_ld, dim, l);
 }
 
 template <typename O>
@@ -196,8 +232,7 @@ extern "C" {
 int64_t dynlp_embed_workspace(int64_t count, int64_t items, int32_t dim) {
     (void)items;
     if (count <= kFewPerItem || count > kMostRows || dim < 1) return 0;
-    SumSpace s;
-    return sum_space(nullptr, count, dim, false, &s);
+    return sum_space_bytes(count, dim, -1);
 }
 
 dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, const dynlp_matrix* out, const dynlp_call* call) {
@@ -225,12 +260,17 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
         } else if (!pieces) {
             k_embed_items<T, V><<<(unsigned)t.items, kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, lanes_log2((int)n));
         } else {
-            SumSpace s;
-            sum_space(static_cast<char*>(call->workspace), t.count, dim, false, &s);
-            const int64_t tiles = ceil_div(t.count, kKeyTile);
-            k_item_keys<T, V><<<(unsigned)(tiles + ceil_div(t.items, kBlock)), kBlock, 0, stream>>>(t, s.key, s.src, (int)tiles, to, out->stride, dim);
-            launch_sums<T, T, V>(SumList{s.key, s.src, t.weights, s.part, s.flags, t.count, table->rows, t.items, s.piece, t.scale}, rows,
-                                 table->stride, to, out->stride, dim, stream);
+            SumSpace s{};
+            const bool wide = wide_rows(table->type, dim);
+            sum_space(static_cast<char*>(call->workspace), t.count, dim, wide, -1, &s);
+            const SumList list{s.key, s.src, t.weights, s.part, s.flags, s.open, nullptr, t.count, table->rows, t.items, s.piece, t.scale};
+            if (wide) {
+                launch_wide<T, T, true>(list, t, rows, table->stride, to, out->stride, dim, stream);
+            } else {
+                const int64_t tiles = ceil_div(t.count, kKeyTile);
+                k_item_keys<T, V><<<(unsigned)(tiles + ceil_div(t.items, kBlock)), kBlock, 0, stream>>>(t, s.key, s.src, (int)tiles, to, out->stride, dim);
+                launch_narrow<T, T, V>(list, rows, table->stride, to, out->stride, dim, stream);
+            }
         }
     });
     return launched();
@@ -238,10 +278,8 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
 
 int64_t dynlp_embed_grad_workspace(int64_t count, int64_t items, int32_t dim, int64_t table_rows) {
     (void)items;
-    (void)table_rows;
-    if (count <= kFewTokens || count > kMostRows || dim < 1) return 0;
-    SumSpace s;
-    return sum_space(nullptr, count, dim, true, &s);
+    if (count <= kFewTokens || count > kMostRows || dim < 1 || table_rows < 0) return 0;
+    return sum_space_bytes(count, dim, table_rows);
 }
 
 dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* tokens, const dynlp_matrix* out, const dynlp_call* call) {
@@ -269,11 +307,11 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
             // zero rows: workgroups enough for the chip, 64 rows at least for the look through the ids
             const int zero_rows = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(out->rows, 1024), 64), kZeroRows);
             k_embed_grad_few<T, O, V><<<(unsigned)(count + ceil_div(out->rows, zero_rows)), kBlock, 0, stream>>>(
-                t, rows, grad->stride, to, out->stride, dim, lanes_log2((int)ceil_div(dim, V)), zero_rows);
+                t, rows, grad->stride, to, out->stride, dim, zero_rows);
         } else {
-            SumSpace s;
-            sum_space(static_cast<char*>(call->workspace), count, dim, true, &s);
-            launch_zeros(to, out->stride, out->rows, dim, stream);
+            SumSpace s{};
+            const bool wide = wide_rows(grad->type, dim);
+            sum_space(static_cast<char*>(call->workspace), count, dim, wide, out->rows, &s);
             int bits = 1;
             while (bits < 31 && (out->rows >> bits) != 0) ++bits;
             const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes;
@@ -291,12 +329,17 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
                 p.tiles = (int)s.tiles;
                 p.shift = k * per;
                 p.bits = std::min(per, bits - k * per);
-                k_sort_count<<<(unsigned)s.tiles, kBlock, 0, stream>>>(t, p);
+                k_sort_count<<<(unsigned)(s.tiles + (k == 0 ? ceil_div(out->rows, kClear) : 0)), kBlock, 0, stream>>>(t, p, s.present);
                 k_sort_offsets<<<1u << p.bits, kBlock, 0, stream>>>(p);
                 k_sort_scatter<<<(unsigned)s.tiles, kBlock, 0, stream>>>(t, p);
             }
-            launch_sums<T, O, V>(SumList{p.key_out, p.src_out, p.factor_out, s.part, s.flags, count, t.items, out->rows, s.piece, t.scale}, rows,
-                                 grad->stride, to, out->stride, dim, stream);
+            const SumList list{p.key_out, p.src_out, p.factor_out, s.part, s.flags, s.open, s.present, count, t.items, out->rows, s.piece, t.scale};
+            if (wide)
+                launch_wide<T, O, false>(list, t, rows, grad->stride, to, out->stride, dim, stream);
+            else
+                launch_narrow<T, O, V>(list, rows, grad->stride, to, out->stride, dim, stream);
+            constexpr int Z = V == 1 ? 1 : Piece<O>::n;
+            k_zero_absent<O, Z><<<(unsigned)ceil_div(out->rows, kBlock), kBlock, 0, stream>>>(s.present, to, out->stride, out->rows, dim);
         }
     };
     by_type(grad->type, dim, [&](auto type, auto width) {

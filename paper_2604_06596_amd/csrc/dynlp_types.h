@@ -57,34 +57,41 @@ __device__ inline void widen(u32x4 p, float (&f)[8], f16) {
     for (int k = 0; k < 8; ++k) f[k] = (float)h[k];
 }
 
-// V float32 values rounded to the type of the array and stored at p (any element alignment).
-template <int V>
-__device__ inline void store_values(float* p, const float (&f)[V]) {
-    static_assert(V == 1 || V % 4 == 0, "one value, or whole pieces");
-    if constexpr (V == 1) {
-        *p = f[0];
-    } else {
-        for (int k = 0; k < V; k += 4) {
-            u32x4 v;
-            for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(f[k + j]);
-            store_piece(p + k, v);
-        }
-    }
-}
+// V float32 values (1, 2 or a multiple of 4) rounded to the type of the array and stored at p (any element alignment).
 template <int V, typename T>
 __device__ inline void store_values(T* p, const float (&f)[V]) {
-    static_assert(sizeof(T) == 2 && (V == 1 || V % 4 == 0), "one value, or half a piece and more");
-    if constexpr (V == 1) {
+    constexpr int n = V < 4 ? V : 4;
+    static_assert(V % n == 0 && n != 3, "one value, two, or fours");
+    if constexpr (n == 1) {
         *p = (T)f[0];
     } else {
-        for (int k = 0; k < V; k += 4) {
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            typedef t4 t4_any __attribute__((aligned(2)));
-            t4 v;
-            for (int j = 0; j < 4; ++j) v[j] = (T)f[k + j];
-            *reinterpret_cast<t4_any*>(p + k) = v;
+        typedef T vec __attribute__((ext_vector_type(n)));
+        typedef vec vec_any __attribute__((aligned(sizeof(T))));
+        for (int k = 0; k < V; k += n) {
+            vec v;
+            for (int j = 0; j < n; ++j) v[j] = (T)f[k + j];
+            *reinterpret_cast<vec_any*>(p + k) = v;
         }
     }
 }
+
+// E consecutive elements of a row (4, 8 or 16 bytes) as they are in memory.
+template <typename T, int E>
+struct Columns {
+    static constexpr int words = E * (int)sizeof(T) / 4;
+    uint32_t d[words];
+    __device__ inline void load(const T* p) {
+        __builtin_memcpy(d, p, sizeof d);  // one access, at any element alignment
+    }
+    __device__ inline void zero() {
+        for (int k = 0; k < words; ++k) d[k] = 0u;
+    }
+    __device__ inline float get(int e) const {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(d[e]);
+        else
+            return to_float(__builtin_bit_cast(T, (uint16_t)(d[e / 2] >> (16 * (e & 1)))));
+    }
+};
 
 }  // namespace dynlp
