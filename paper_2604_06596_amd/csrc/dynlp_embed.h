@@ -531,32 +531,47 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
             if (lane == 0) last = cur;
             ends = __ballot(lane < n && key != last);
         }
+        const unsigned long long real = __ballot(src >= 0);
+        const uint64_t address = reinterpret_cast<uint64_t>(rows + (int64_t)max(src, 0) * ld);
+        uint32_t low = (uint32_t)address, high = (uint32_t)(address >> 32), factor = __float_as_uint(w);
         for (int j = 0; j < n; j += U) {
             Columns<T, E> x[U];
-            const int stop = ITEMS && next < end ? (int)(next - base) - j : kWave;  // where the item ends, among the eight
+            float f[U];
+            auto ask = [&](int u) {
+                x[u].load((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, u) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, u), off);
+            };
+            if ((real >> j & 255) == 255) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t from = __builtin_amdgcn_readlane(src, j + u);
-                if (from >= 0)
-                    x[u].load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(rows + (int64_t)from * ld) + off));
-                else
-                    x[u].zero();
-            }
-            if (ITEMS ? stop >= U : (ends >> j & 255) == 0) {
+                for (int u = 0; u < U; ++u) ask(u);
+            } else {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j + u));
-                    for (int e = 0; e < E; ++e) acc[e] += f * x[u].get(e);
+                    if (real >> (j + u) & 1)
+                        ask(u);
+                    else
+                        x[u].zero();
                 }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) f[u] = __uint_as_float(__builtin_amdgcn_readlane(factor, u));
+            // the next eight entries to the first lanes
+            low = __shfl_down(low, U, kWave);
+            high = __shfl_down(high, U, kWave);
+            factor = __shfl_down(factor, U, kWave);
+            const int64_t pos = base + j;
+            if (ITEMS ? next >= end || next >= pos + U : (ends >> j & 255) == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    for (int e = 0; e < E; ++e) acc[e] += f[u] * x[u].get(e);
             } else {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (ITEMS) {
-                        if (base + j + u == next && next < end) {
+                        if (pos + u == next && next < end) {
                             flush();
                             do {
                                 ++item;
-                            } while (item < t.items && t.offsets[item + 1] <= base + j + u);
+                            } while (item < t.items && t.offsets[item + 1] <= pos + u);
                             next = item < t.items ? t.offsets[item + 1] : INT64_MAX;
                             cur = item < t.items ? (int32_t)item : -1;
                         }
@@ -564,8 +579,7 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
                         flush();
                         cur = __builtin_amdgcn_readlane(key, j + u);
                     }
-                    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j + u));
-                    for (int e = 0; e < E; ++e) acc[e] += f * x[u].get(e);
+                    for (int e = 0; e < E; ++e) acc[e] += f[u] * x[u].get(e);
                 }
             }
         }

@@ -75,13 +75,34 @@ __device__ inline void store_values(T* p, const float (&f)[V]) {
     }
 }
 
+// Words at an address that is a multiple of 2 or 4 bytes only, in global memory.
+template <int WORDS, int ALIGN>
+struct Words;
+#define DYNLP_WORDS(n, a)                                                     \
+    template <>                                                               \
+    struct Words<n, a> {                                                      \
+        typedef uint32_t vec __attribute__((ext_vector_type(n), aligned(a))); \
+    };
+DYNLP_WORDS(1, 2)
+DYNLP_WORDS(2, 2)
+DYNLP_WORDS(4, 2)
+DYNLP_WORDS(1, 4)
+DYNLP_WORDS(2, 4)
+DYNLP_WORDS(4, 4)
+#undef DYNLP_WORDS
+
 // E consecutive elements of a row (4, 8 or 16 bytes) as they are in memory.
 template <typename T, int E>
 struct Columns {
     static constexpr int words = E * (int)sizeof(T) / 4;
     uint32_t d[words];
-    __device__ inline void load(const T* p) {
-        __builtin_memcpy(d, p, sizeof d);  // one access, at any element alignment
+    // From `offset` bytes behind an address that is the same for all lanes (scalar registers hold it).
+    __device__ inline void load(uint64_t address, uint32_t offset) {
+        typedef typename Words<words, (int)sizeof(T)>::vec vec;
+        typedef const __attribute__((address_space(1))) char* bytes;
+        typedef const __attribute__((address_space(1))) vec* vecs;
+        const vec v = *(vecs)((bytes)address + offset);
+        for (int k = 0; k < words; ++k) d[k] = v[k];
     }
     __device__ inline void zero() {
         for (int k = 0; k < words; ++k) d[k] = 0u;
