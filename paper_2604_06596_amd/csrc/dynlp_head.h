@@ -67,30 +67,122 @@ __device__ inline void store_columns(T* row, int col, int dim, const float (&f)[
     }
 }
 
-// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.
-template <typename T, int CT, int NT>
-__device__ inline void head_logits(const Head& a, int64_t first, f32x4 (&z)[NT][CT]) {
+// Four columns of a row: 16 bytes or 8.
+template <typename T>
+using Quad = Columns<T, 4>;
+template <typename T>
+__device__ inline Quad<T> load_quad(const T* row, int col, int dim) {
+    Quad<T> v;
+    if (col + 4 <= dim) {
+        __builtin_memcpy(v.d, row + col, sizeof v.d);
+        return v;
+    }
+    v.zero();
+    for (int k = 0; k < 4; ++k)
+        if (col + k < dim) {
+            if constexpr (sizeof(T) == 2)
+                v.d[k / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, row[col + k]) << (16 * (k & 1));
+            else
+                v.d[k] = __float_as_uint(row[col + k]);
+        }
+    return v;
+}
+template <typename T>
+__device__ inline void store_quad(T* row, int col, int dim, const float (&f)[4]) {
+    if (col + 4 <= dim) {
+        store_values<4>(row + col, f);
+    } else {
+        for (int k = 0; k < 4; ++k)
+            if (col + k < dim) row[col + k] = (T)f[k];
+    }
+}
+// Column t of eight rows' quads, as an operand with these rows for k.
+__device__ inline u32x4 column_of(const Quad<bf16> (&x)[8], int t) {
+    u32x4 v;
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(x[2 * j + 1].d[t >> 1], x[2 * j].d[t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+    return v;
+}
+
+// The head's rows where they are, or a copy in shared memory that is padded with zeros to whole tiles of classes and columns.
+template <typename T>
+struct WeightRows {
+    const T* w;
+    int64_t ld;
+    int dim, classes;
+    __device__ inline u32x4 piece(int c, int col) const {
+        return c < classes && col < dim ? load_columns(w + (int64_t)c * ld, col, dim) : u32x4{0u, 0u, 0u, 0u};
+    }
+    __device__ inline Quad<T> quad(int c, int col) const {
+        if (c < classes && col < dim) return load_quad(w + (int64_t)c * ld, col, dim);
+        Quad<T> v;
+        v.zero();
+        return v;
+    }
+};
+template <typename T>
+struct SharedWeight {
+    const T* w;
+    int ld;
+    __device__ inline u32x4 piece(int c, int col) const { return *reinterpret_cast<const u32x4*>(w + c * ld + col); }
+    __device__ inline Quad<T> quad(int c, int col) const {
+        Quad<T> v;
+        if constexpr (sizeof(T) == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(w + c * ld + col);
+            v.d[0] = x.x, v.d[1] = x.y;
+        } else {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(w + c * ld + col);
+            for (int k = 0; k < 4; ++k) v.d[k] = x[k];
+        }
+        return v;
+    }
+};
+// Columns of the copy: whole pieces of a wave (16 lanes x n columns, and the 8 n of a step over the logits), and 16 bytes so that the 16 rows
+// of a tile begin in different banks.
+template <typename T>
+__host__ __device__ inline int shared_ld(int dim) {
+    constexpr int n = Piece<T>::n;
+    return (dim + 16 * n - 1) / (16 * n) * (16 * n) + n;
+}
+template <typename T, int CT>
+__device__ inline SharedWeight<T> share_weight(const Head& a, T* to) {
+    constexpr int n = Piece<T>::n;
+    const int ld = shared_ld<T>(a.dim), pieces = ld / n;
+    const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
+    for (int at = threadIdx.x; at < 16 * CT * pieces; at += kBlock)
+        *reinterpret_cast<u32x4*>(to + at * n) = w.piece(at / pieces, at % pieces * n);
+    __syncthreads();
+    return SharedWeight<T>{to, ld};
+}
+
+// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.  The next step's part of h is
+// asked for before this step's products.
+template <typename T, int CT, int NT, typename W>
+__device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32x4 (&z)[NT][CT]) {
     constexpr int n = Piece<T>::n;
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const T* w = static_cast<const T*>(a.weight);
     const T* h = static_cast<const T*>(a.h);
-    const T* wr[CT];
     const T* hr[NT];
-    for (int t = 0; t < CT; ++t) wr[t] = w + (int64_t)min(16 * t + r, a.classes - 1) * a.ld_w;
     for (int m = 0; m < NT; ++m) {
         hr[m] = h + min(first + 16 * m + r, a.rows - 1) * a.ld_h;
         for (int t = 0; t < CT; ++t) z[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    u32x4 now[NT][2], next[NT][2];
+    auto ask = [&](int k0) {
+        for (int m = 0; m < NT; ++m)
+            for (int s = 0; s < 2; ++s) next[m][s] = load_columns(hr[m], k0 + q * 2 * n + s * n, a.dim);
+    };
+    ask(0);
+#pragma unroll 1
     for (int k0 = 0; k0 < a.dim; k0 += 8 * n) {
+        for (int m = 0; m < NT; ++m)
+            for (int s = 0; s < 2; ++s) now[m][s] = next[m][s];
+        if (k0 + 8 * n < a.dim) ask(k0 + 8 * n);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int col = k0 + q * 2 * n + s * n;
-            u32x4 wv[CT], hv[NT];
-            for (int m = 0; m < NT; ++m) hv[m] = load_columns(hr[m], col, a.dim);
-            for (int t = 0; t < CT; ++t) wv[t] = load_columns(wr[t], col, a.dim);
-            for (int t = 0; t < CT; ++t)
-                for (int m = 0; m < NT; ++m) z[m][t] = mma(wv[t], hv[m], z[m][t], T());
-        }
+        for (int s = 0; s < 2; ++s)
+            for (int t = 0; t < CT; ++t) {
+                const u32x4 wv = w.piece(16 * t + r, k0 + q * 2 * n + s * n);
+                for (int m = 0; m < NT; ++m) z[m][t] = mma(wv, now[m][s], z[m][t], T());
+            }
     }
     for (int t = 0; t < CT; ++t)
         for (int i = 0; i < 4; ++i) {
@@ -131,41 +223,49 @@ __device__ inline float head_exp(f32x4 (&z)[CT], float* top) {
 constexpr int kHeadTiles = 2;                       // tiles of 16 rows per wave
 constexpr int kHeadRows = kHeadTiles * 16 * (kBlock / kWave);  // rows per workgroup
 
-template <typename T, int CT>
+// One tile of rows per wave from W as it is, or (SHARED) any number of them from a copy of W in shared memory.
+template <typename T, int CT, bool SHARED>
 __global__ __launch_bounds__(kBlock) void k_head_labels(Head a, float* soft, int32_t* hard) {
     constexpr int NT = kHeadTiles;
-    const int64_t first = (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
-    if (first >= a.rows) return;
+    extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    f32x4 z[NT][CT];
-    head_logits<T, CT, NT>(a, first, z);
-    for (int m = 0; m < NT; ++m) {
-        const int64_t row = first + 16 * m + r;
-        if (hard) {
-            float best = -INFINITY;
-            int at = a.classes;
-            for (int t = 0; t < CT; ++t)
-                for (int i = 0; i < 4; ++i)
-                    if (z[m][t][i] > best) best = z[m][t][i], at = 16 * t + 4 * q + i;
-            for (int d = 16; d < kWave; d <<= 1) {
-                const float other = __shfl_xor(best, d, kWave);
-                const int other_at = __shfl_xor(at, d, kWave);
-                if (other > best || (other == best && other_at < at)) best = other, at = other_at;
-            }
-            if (q == 0 && row < a.rows) hard[row] = at < a.classes ? at : 0;
-        }
-        if (soft) {
-            float top;
-            const float sum = head_exp(z[m], &top);
-            if (row < a.rows) {
-                float* out = soft + row * a.classes;
+    auto tile = [&](const auto& w, int64_t first) {
+        f32x4 z[NT][CT];
+        head_logits<T, CT, NT>(a, w, first, z);
+        for (int m = 0; m < NT; ++m) {
+            const int64_t row = first + 16 * m + r;
+            if (hard) {
+                float best = -INFINITY;
+                int at = a.classes;
                 for (int t = 0; t < CT; ++t)
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = 16 * t + 4 * q + i;
-                        if (c < a.classes) out[c] = sum == 0.f ? 1.f / (float)a.classes : z[m][t][i] / sum;
+                    for (int i = 0; i < 4; ++i)
+                        if (z[m][t][i] > best) best = z[m][t][i], at = 16 * t + 4 * q + i;
+                for (int d = 16; d < kWave; d <<= 1) {
+                    const float other = __shfl_xor(best, d, kWave);
+                    const int other_at = __shfl_xor(at, d, kWave);
+                    if (other > best || (other == best && other_at < at)) best = other, at = other_at;
+                }
+                if (q == 0 && row < a.rows) hard[row] = at < a.classes ? at : 0;
+            }
+            if (soft) {
+                float top;
+                const float sum = head_exp(z[m], &top);
+                if (row < a.rows)
+                    for (int t = 0; t < CT; ++t) {
+                        float f[4];
+                        for (int i = 0; i < 4; ++i) f[i] = sum == 0.f ? 1.f / (float)a.classes : z[m][t][i] / sum;
+                        if (16 * t + 4 * q < a.classes) store_columns(soft + row * a.classes, 16 * t + 4 * q, a.classes, f);
                     }
             }
         }
+    };
+    const int64_t first = (threadIdx.x / kWave) * (NT * 16);
+    if constexpr (SHARED) {
+        const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
+        for (int64_t at = (int64_t)blockIdx.x * kHeadRows; at + first < a.rows; at += (int64_t)gridDim.x * kHeadRows) tile(w, at + first);
+    } else {
+        const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
+        if ((int64_t)blockIdx.x * kHeadRows + first < a.rows) tile(w, (int64_t)blockIdx.x * kHeadRows + first);
     }
 }
 
@@ -185,10 +285,25 @@ struct Loss {
 // x = high + low (+ what 16 or more further bits would hold), both bfloat16.
 __device__ inline uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (bf16)x); }
 
-// dh of the tile's rows from their dz.  Pieces of W's rows are the left operand; for two-byte types a lane's 8 x 8 block (8 classes, 8
+// dh of the tile's rows from their dz, 64 columns at a time.  Quads of W's rows are the left operand; in bfloat16 a lane's 8 x 4 block (8 classes, 4
 // columns) is transposed by v_perm.
-template <int CT, int NT>
-__device__ inline void head_dh(const Head& a, int64_t first, const f32x4 (&dz)[NT][CT], const bool (&kept)[NT], bf16* dh, int64_t ld_dh) {
+template <int CT, int NT, typename T>
+__device__ inline void store_dh(const Head& a, int64_t first, int base, const f32x4 (&acc)[NT][4], const bool (&kept)[NT], T* dh, int64_t ld_dh) {
+    const int q = lane_id() >> 4, r = lane_id() & 15;
+    for (int m = 0; m < NT; ++m) {
+        const int64_t row = first + 16 * m + r;
+        if (row >= a.rows) continue;
+        for (int i = 0; i < 4; ++i) {
+            const int to = base + 4 * (4 * q + i);
+            float f[4];
+            for (int t = 0; t < 4; ++t) f[t] = kept[m] ? acc[m][t][i] : 0.f;
+            if (to < a.dim) store_quad(dh + row * ld_dh, to, a.dim, f);
+        }
+    }
+}
+template <int CT, int NT, typename W>
+__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f32x4 (&dz)[NT][CT], const bool (&kept)[NT], bf16* dh,
+                               int64_t ld_dh) {
     constexpr int P = (CT + 1) / 2;
     const int q = lane_id() >> 4, r = lane_id() & 15;
     // dz in two bfloat16 terms, which leave out 2^-17 of it: far below the rounding of dh itself
@@ -207,135 +322,114 @@ __device__ inline void head_dh(const Head& a, int64_t first, const f32x4 (&dz)[N
                 high[m][p][j >> 1] = hi;
                 low[m][p][j >> 1] = lo;
             }
-    const bf16* w = static_cast<const bf16*>(a.weight);
-    for (int base = 0; base < a.dim; base += 128) {
-        f32x4 acc[NT][8];
+#pragma unroll 1
+    for (int base = 0; base < a.dim; base += 64) {
+        f32x4 acc[NT][4];
         for (int m = 0; m < NT; ++m)
-            for (int t = 0; t < 8; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int col = base + 8 * r;
+            for (int t = 0; t < 4; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int p = 0; p < P; ++p) {
-            u32x4 x[8];
+            Quad<bf16> x[8];
             for (int j = 0; j < 8; ++j) {
-                const int c = 16 * (2 * p + (j >> 2)) + 4 * q + (j & 3);
-                x[j] = u32x4{0u, 0u, 0u, 0u};
-                if (c < a.classes && col < a.dim) x[j] = load_columns(w + (int64_t)c * a.ld_w, col, a.dim);
+                const int t = 2 * p + (j >> 2);
+                if (t < CT)
+                    x[j] = w.quad(16 * t + 4 * q + (j & 3), base + 4 * r);
+                else
+                    x[j].zero();
             }
-            for (int t = 0; t < 8; ++t) {
-                u32x4 left;
-                for (int j = 0; j < 4; ++j)
-                    left[j] = __builtin_amdgcn_perm(x[2 * j + 1][t >> 1], x[2 * j][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+            for (int t = 0; t < 4; ++t) {
+                const u32x4 left = column_of(x, t);
                 for (int m = 0; m < NT; ++m) {
                     acc[m][t] = mma(left, low[m][p], acc[m][t], bf16());
                     acc[m][t] = mma(left, high[m][p], acc[m][t], bf16());
                 }
             }
         }
-        for (int m = 0; m < NT; ++m) {
-            const int64_t row = first + 16 * m + r;
-            if (row >= a.rows) continue;
-            for (int i = 0; i < 4; ++i) {
-                const int to = base + 8 * (4 * q + i);
-                float f[8];
-                for (int t = 0; t < 8; ++t) f[t] = kept[m] ? acc[m][t][i] : 0.f;
-                if (to < a.dim) store_columns(dh + row * ld_dh, to, a.dim, f);
-            }
-        }
+        store_dh<CT, NT>(a, first, base, acc, kept, dh, ld_dh);
     }
 }
-template <int CT, int NT, typename T>
-__device__ inline void head_dh(const Head& a, int64_t first, const f32x4 (&dz)[NT][CT], const bool (&kept)[NT], T* dh, int64_t ld_dh) {
-    constexpr int n = Piece<T>::n;
+template <int CT, int NT, typename W, typename T>
+__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f32x4 (&dz)[NT][CT], const bool (&kept)[NT], T* dh, int64_t ld_dh) {
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const T* w = static_cast<const T*>(a.weight);
-    for (int base = 0; base < a.dim; base += 16 * n) {
-        f32x4 acc[NT][n];
+#pragma unroll 1
+    for (int base = 0; base < a.dim; base += 64) {
+        f32x4 acc[NT][4];
         for (int m = 0; m < NT; ++m)
-            for (int t = 0; t < n; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int col = base + n * r;
+            for (int t = 0; t < 4; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int ct = 0; ct < CT; ++ct)
             for (int i = 0; i < 4; ++i) {
-                const int c = 16 * ct + 4 * q + i;
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (c < a.classes && col < a.dim) x = load_columns(w + (int64_t)c * a.ld_w, col, a.dim);
-                float f[n];
-                widen(x, f, T());
-                for (int t = 0; t < n; ++t)
-                    for (int m = 0; m < NT; ++m) acc[m][t] = mma4(f[t], dz[m][ct][i], acc[m][t]);
+                const Quad<T> x = w.quad(16 * ct + 4 * q + i, base + 4 * r);
+                for (int t = 0; t < 4; ++t)
+                    for (int m = 0; m < NT; ++m) acc[m][t] = mma4(x.get(t), dz[m][ct][i], acc[m][t]);
             }
-        for (int m = 0; m < NT; ++m) {
-            const int64_t row = first + 16 * m + r;
-            if (row >= a.rows) continue;
-            for (int i = 0; i < 4; ++i) {
-                const int to = base + n * (4 * q + i);
-                float f[n];
-                for (int t = 0; t < n; ++t) f[t] = kept[m] ? acc[m][t][i] : 0.f;
-                if (to < a.dim) store_columns(dh + row * ld_dh, to, a.dim, f);
-            }
-        }
+        store_dh<CT, NT>(a, first, base, acc, kept, dh, ld_dh);
     }
 }
 
-// Loss, dz and dh of a tile of rows: logits, softmax and the product with W, without leaving the registers.
+// From the logits z of row `row` of a lane (first + 16 m + r): its loss is stored, z becomes dz.  Returns whether the row takes part.
+template <int CT>
+__device__ inline bool head_dz(const Head& a, const Loss& g, int64_t row, f32x4 (&z)[CT]) {
+    const int q = lane_id() >> 4;
+    const bool inside = row < a.rows;
+    const int64_t at = inside ? row : a.rows - 1;
+    const float weight = g.row_weight ? g.row_weight[at] : 1.f;
+    bool use = inside && weight != 0.f;
+    int label = -1;
+    f32x4 target[CT];
+    if (g.hard) {
+        label = g.hard[at];
+        if (inside && q == 0 && label >= a.classes && g.rejected) atomicAdd(g.rejected, 1);
+        use = use && label >= 0 && label < a.classes;
+    }
+    for (int t = 0; t < CT; ++t) {
+        const int c = 16 * t + 4 * q;
+        if (g.hard)
+            for (int i = 0; i < 4; ++i) target[t][i] = c + i == label ? 1.f : 0.f;
+        else
+            target[t] = __builtin_bit_cast(f32x4, c < a.classes ? load_columns(g.soft + at * a.classes, c, a.classes) : u32x4{0u, 0u, 0u, 0u});
+    }
+    f32x4 e[CT];
+    for (int t = 0; t < CT; ++t) e[t] = z[t];
+    float top;
+    const float sum = head_exp(e, &top);
+    use = use && sum != 0.f;
+    const float lse = logf(sum);  // of the shifted logits
+    float total = 0.f, loss = 0.f;
+    for (int t = 0; t < CT; ++t)
+        for (int i = 0; i < 4; ++i) {
+            const float y = target[t][i];
+            total += y;
+            loss += y != 0.f ? y * (lse - (z[t][i] - top)) : 0.f;
+        }
+    total = row_sum(total);
+    loss = row_sum(loss);
+    const float scale = g.grad_scale * weight;
+    for (int t = 0; t < CT; ++t)
+        for (int i = 0; i < 4; ++i) z[t][i] = use ? scale * (total * (e[t][i] / sum) - target[t][i]) : 0.f;
+    if (inside && q == 0 && g.loss) g.loss[row] = use ? weight * loss : 0.f;
+    return use;
+}
+
+// Loss, dz and dh of a tile of rows: logits, softmax and the product with W, without leaving the registers.  For heads whose W and dweight do
+// not fit a workgroup, and where no dweight is asked for.
 template <typename T, int CT>
 __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
     constexpr int NT = kHeadTiles;
     const int64_t first = (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
     if (first >= a.rows) return;
     const int q = lane_id() >> 4, r = lane_id() & 15;
+    const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
     f32x4 z[NT][CT];
     bool kept[NT];
-    head_logits<T, CT, NT>(a, first, z);
+    head_logits<T, CT, NT>(a, w, first, z);
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
-        const bool inside = row < a.rows;
-        const int64_t at = inside ? row : a.rows - 1;
-        const float weight = g.row_weight ? g.row_weight[at] : 1.f;
-        bool use = inside && weight != 0.f;
-        int label = -1;
-        f32x4 target[CT];
-        if (g.hard) {
-            label = g.hard[at];
-            if (inside && q == 0 && label >= a.classes && g.rejected) atomicAdd(g.rejected, 1);
-            use = use && label >= 0 && label < a.classes;
-        }
-        for (int t = 0; t < CT; ++t) {
-            const int c = 16 * t + 4 * q;
-            target[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (g.hard) {
-                for (int i = 0; i < 4; ++i) target[t][i] = c + i == label ? 1.f : 0.f;
-            } else {
-                for (int i = 0; i < 4; ++i)
-                    if (c + i < a.classes) target[t][i] = g.soft[at * a.classes + c + i];
-            }
-        }
-        f32x4 e[CT];
-        for (int t = 0; t < CT; ++t) e[t] = z[m][t];
-        float top;
-        const float sum = head_exp(e, &top);
-        use = use && sum != 0.f;
-        const float lse = logf(sum);  // of the shifted logits
-        float total = 0.f, loss = 0.f;
-        for (int t = 0; t < CT; ++t)
-            for (int i = 0; i < 4; ++i) {
-                const float y = target[t][i];
-                total += y;
-                loss += y != 0.f ? y * (lse - (z[m][t][i] - top)) : 0.f;
-            }
-        total = row_sum(total);
-        loss = row_sum(loss);
-        const float scale = g.grad_scale * weight;
-        for (int t = 0; t < CT; ++t)
-            for (int i = 0; i < 4; ++i) z[m][t][i] = use ? scale * (total * (e[t][i] / sum) - target[t][i]) : 0.f;
-        kept[m] = use;
-        if (inside) {
-            if (q == 0 && g.loss) g.loss[row] = use ? weight * loss : 0.f;
-            if (g.dz) {
-                if (q == 0) g.kept[row] = use ? 1 : 0;
-                for (int t = 0; t < CT; ++t) *reinterpret_cast<f32x4*>(g.dz + row * (16 * CT) + 16 * t + 4 * q) = z[m][t];
-            }
+        kept[m] = head_dz(a, g, row, z[m]);
+        if (row < a.rows && g.dz) {
+            if (q == 0) g.kept[row] = kept[m] ? 1 : 0;
+            for (int t = 0; t < CT; ++t) *reinterpret_cast<f32x4*>(g.dz + row * (16 * CT) + 16 * t + 4 * q) = z[m][t];
         }
     }
-    if (g.dh) head_dh<CT, NT>(a, first, z, kept, static_cast<T*>(g.dh), g.ld_dh);
+    if (g.dh) head_dh<CT, NT>(a, w, first, z, kept, static_cast<T*>(g.dh), g.ld_dh);
 }
 
 // ---- dweight = dz^T h, dbias ------------------------------------------------------------------------------------------
@@ -454,6 +548,168 @@ __global__ __launch_bounds__(kBlock) void k_head_outer(Outer o) {
         if (k < kCols && base + k < o.dim) part[(int64_t)c * (o.dim + 1) + base + k] = joined[c][k];
         if (k == kCols && blockIdx.y == 0) part[(int64_t)c * (o.dim + 1) + o.dim] = joined[c][k];
     }
+}
+
+// ---- everything in one pass over h ------------------------------------------------------------------------------------
+
+// dz of a workgroup's 128 rows in shared memory: [row][class], padded so that the four row groups that a wave reads at once (4 j + q, or 8 q + j
+// for bfloat16) lie in different banks.
+template <typename T, int CT>
+struct SharedDz {
+    static constexpr int ld = 16 * CT + (sizeof(T) == 2 && !__is_same(T, f16) ? 2 : 16), bytes = kHeadRows * ld * 4;
+    float* p;
+    __device__ inline void put(int row, int t, int q, const f32x4& z) {
+        float2* to = reinterpret_cast<float2*>(p + row * ld + 16 * t + 4 * q);
+        to[0] = float2{z[0], z[1]};
+        to[1] = float2{z[2], z[3]};
+    }
+    // Sum of a class over 32 rows.
+    __device__ inline float rows_of(int c, int from) const {
+        float s = 0.f;
+        for (int k = 0; k < 32; ++k) s += p[(from + k) * ld + c];
+        return s;
+    }
+};
+
+// acc[ct][t] += rows from .. to of the tile, columns col + t.  h is read once more here, from the L2: the workgroup has just read it.
+template <int CT>
+__device__ inline void tile_outer(const Head& a, int64_t tile, int from, int to, int col, const SharedDz<bf16, CT>& dz, const uint8_t* kept,
+                                  f32x4 (&acc)[CT][4]) {
+    const int q = lane_id() >> 4, r = lane_id() & 15;
+    const bf16* h = static_cast<const bf16*>(a.h);
+#pragma unroll 1
+    for (int k0 = from; k0 < to; k0 += 32) {
+        Quad<bf16> x[8];
+        for (int j = 0; j < 8; ++j) {
+            const int row = k0 + 8 * q + j;
+            x[j].zero();
+            if (kept[row] && col < a.dim) x[j] = load_quad(h + (tile + row) * a.ld_h, col, a.dim);
+        }
+        u32x4 right[4];
+        for (int t = 0; t < 4; ++t) right[t] = column_of(x, t);
+        for (int ct = 0; ct < CT; ++ct) {
+            // dz in three bfloat16 terms, which hold all 24 bits of it: dweight is a float32 sum over all rows
+            u32x4 term[3];
+            for (int j = 0; j < 8; j += 2) {
+                uint32_t b[3] = {0, 0, 0};
+                for (int e = 0; e < 2; ++e) {
+                    float v = dz.p[(k0 + 8 * q + j + e) * SharedDz<bf16, CT>::ld + 16 * ct + r];
+                    for (int k = 0; k < 3; ++k) {
+                        const uint32_t bits = bf16_bits(v);
+                        b[k] |= bits << (16 * e);
+                        v -= __uint_as_float(bits << 16);
+                    }
+                }
+                for (int k = 0; k < 3; ++k) term[k][j >> 1] = b[k];
+            }
+            for (int k = 2; k >= 0; --k)
+                for (int t = 0; t < 4; ++t) acc[ct][t] = mma(term[k], right[t], acc[ct][t], bf16());
+        }
+    }
+}
+template <int CT, typename T>
+__device__ inline void tile_outer(const Head& a, int64_t tile, int from, int to, int col, const SharedDz<T, CT>& dz, const uint8_t* kept,
+                                  f32x4 (&acc)[CT][4]) {
+    const int q = lane_id() >> 4, r = lane_id() & 15;
+    const T* h = static_cast<const T*>(a.h);
+#pragma unroll 1
+    for (int k0 = from; k0 < to; k0 += 16) {
+        Quad<T> x[4];
+        for (int j = 0; j < 4; ++j) {
+            const int row = k0 + 4 * j + q;
+            x[j].zero();
+            if (kept[row] && col < a.dim) x[j] = load_quad(h + (tile + row) * a.ld_h, col, a.dim);
+        }
+        for (int j = 0; j < 4; ++j)
+            for (int ct = 0; ct < CT; ++ct) {
+                const float left = dz.p[(k0 + 4 * j + q) * SharedDz<T, CT>::ld + 16 * ct + r];
+                for (int t = 0; t < 4; ++t) acc[ct][t] = mma4(left, x[j].get(t), acc[ct][t]);
+            }
+    }
+}
+
+constexpr int kFusedColumns = 64;
+
+// Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight in registers over all tiles of 128 rows.  The columns
+// are cut into groups of 64 (a quad for each of 16 lanes).  One group: the four waves share the tile's rows; two: two waves
+// each; more: each wave has GPW groups and all rows.
+template <typename T, int CT, int GPW>
+__global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a, Loss g, float* part) {
+    constexpr int NT = kHeadTiles, N = 4, kCols = kFusedColumns;
+    extern __shared__ char space[];
+    const int q = lane_id() >> 4, r = lane_id() & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
+    char* behind = space + 16 * CT * w.ld * sizeof(T);
+    SharedDz<T, CT> dz{reinterpret_cast<decltype(SharedDz<T, CT>::p)>(behind)};
+    uint8_t* kept = reinterpret_cast<uint8_t*>(behind + SharedDz<T, CT>::bytes);
+    const int groups = (a.dim + kCols - 1) / kCols;
+    const int my_group = groups == 1 ? 0 : groups == 2 ? wave & 1 : wave;
+    const int from = groups == 1 ? wave * (kHeadRows / 4) : groups == 2 ? (wave >> 1) * (kHeadRows / 2) : 0;
+    const int to = groups == 1 ? from + kHeadRows / 4 : groups == 2 ? from + kHeadRows / 2 : kHeadRows;
+    f32x4 acc[GPW][CT][N];
+    for (int ct = 0; ct < CT; ++ct)
+        for (int p = 0; p < GPW; ++p)
+            for (int t = 0; t < N; ++t) acc[p][ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int my_class = threadIdx.x % (16 * CT), my_rows = threadIdx.x / (16 * CT) * 32;  // of dbias: 32 rows of the tile
+    float sum = 0.f;
+    for (int64_t tile = (int64_t)blockIdx.x * kHeadRows; tile < a.rows; tile += (int64_t)gridDim.x * kHeadRows) {
+        const int mine = wave * (NT * 16);
+        {
+            f32x4 z[NT][CT];
+            bool use[NT];
+            head_logits<T, CT, NT>(a, w, tile + mine, z);
+            for (int m = 0; m < NT; ++m) {
+                const int row = mine + 16 * m + r;
+                use[m] = head_dz(a, g, tile + row, z[m]);
+                if (q == 0) kept[row] = use[m] ? 1 : 0;
+                for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
+            }
+            if (g.dh) head_dh<CT, NT>(a, w, tile + mine, z, use, static_cast<T*>(g.dh), g.ld_dh);
+        }
+        __syncthreads();
+        if (my_rows < kHeadRows) sum += dz.rows_of(my_class, my_rows);
+        for (int p = 0; p < GPW; ++p)
+            if (my_group + 4 * p < groups) tile_outer(a, tile, from, to, (my_group + 4 * p) * kCols + N * r, dz, kept, acc[p]);
+        __syncthreads();
+    }
+    part += (int64_t)blockIdx.x * a.classes * (a.dim + 1);
+    float* bias = reinterpret_cast<float*>(behind);
+    bias[threadIdx.x] = sum;
+    __syncthreads();
+    if ((int)threadIdx.x < a.classes) {
+        float v = 0.f;
+        for (int k = 0; k < kHeadRows / 32; ++k) v += bias[k * 16 * CT + threadIdx.x];
+        part[(int64_t)threadIdx.x * (a.dim + 1) + a.dim] = v;
+    }
+    // dweight: a group of columns after the other, its waves' parts added in order
+    float* joined = reinterpret_cast<float*>(behind);
+    for (int k = 0; k < groups; ++k) {
+        const bool owner = groups <= 2 ? my_group == k : wave == (k & 3);
+        __syncthreads();
+        for (int turn = 0; turn < (groups == 1 ? 4 : groups == 2 ? 2 : 1); ++turn) {
+            if (owner && (groups == 1 ? wave == turn : groups == 2 ? wave >> 1 == turn : true))
+                for (int p = 0; p < GPW; ++p)
+                    if (p == (groups <= 2 ? 0 : k >> 2))
+                        for (int ct = 0; ct < CT; ++ct)
+                            for (int t = 0; t < N; ++t)
+                                for (int i = 0; i < 4; ++i) {
+                                    float& to_sum = joined[(16 * ct + 4 * q + i) * (kCols + 1) + N * r + t];
+                                    to_sum = turn ? to_sum + acc[p][ct][t][i] : acc[p][ct][t][i];
+                                }
+            __syncthreads();
+        }
+        for (int at = threadIdx.x; at < a.classes * kCols; at += kBlock) {
+            const int c = at / kCols, col = at % kCols;
+            if (k * kCols + col < a.dim) part[(int64_t)c * (a.dim + 1) + k * kCols + col] = joined[c * (kCols + 1) + col];
+        }
+    }
+}
+
+// Bytes of shared memory of k_head_fused.
+template <typename T, int CT>
+inline int64_t fused_bytes(int dim) {
+    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kHeadRows;
+    return (int64_t)16 * CT * shared_ld<T>(dim) * (int64_t)sizeof(T) + (joined > dz ? joined : dz);
 }
 
 // Sums the parts: 16 neighbouring elements per workgroup, 16 groups of lanes taking turns on the parts, then joined in order.

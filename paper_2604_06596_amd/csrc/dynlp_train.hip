@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -391,24 +392,50 @@ void by_head(int32_t type, int64_t classes, F f) {
     else tiles(f16());
 }
 
+constexpr int64_t kSharedMemory = 160 * 1024;  // of a CU
+
+// Column groups of dweight that a workgroup keeps in registers: up to eight, two per wave.  0: it does not fit, or W does not fit beside dz.
+int fused_groups(int dim, int classes, int32_t type) {
+    int groups = 0;
+    by_head(type, classes, [&](auto t, auto tiles) {
+        using T = decltype(t);
+        const int64_t n = ceil_div(dim, kFusedColumns);
+        if (n <= 8 && fused_bytes<T, decltype(tiles)::v>(dim) <= kSharedMemory) groups = (int)n;
+    });
+    return groups;
+}
+
 struct LossSpace {
     float* dz;
     uint8_t* kept;
     float* part;
-    int splits;
+    int splits, groups;
     int64_t per_wave;
 };
 
 int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type, LossSpace* s) {
     Carve c{base};
-    const int64_t across = ceil_div(dim, 16 * (16 / type_size(type)));
-    // workgroups of dweight: twice the CUs over all columns, each wave with 64 rows at least
-    s->splits = (int)std::min<int64_t>(std::max<int64_t>(512 / across, 1), std::max<int64_t>(ceil_div(rows, 64 * (kBlock / kWave)), 1));
-    s->per_wave = round_up(ceil_div(rows, (int64_t)s->splits * (kBlock / kWave)), 32);
-    s->dz = c.take<float>(rows * round_up(classes, 16));
-    s->kept = c.take<uint8_t>(rows);
+    s->groups = fused_groups(dim, classes, type);
+    if (s->groups) {
+        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, kHeadRows), 1), s->groups > 4 ? 256 : 512);
+    } else {
+        const int64_t across = ceil_div(dim, 16 * (16 / type_size(type)));
+        // workgroups of dweight: twice the CUs over all columns, each wave with 64 rows at least
+        s->splits = (int)std::min<int64_t>(std::max<int64_t>(512 / across, 1), std::max<int64_t>(ceil_div(rows, 64 * (kBlock / kWave)), 1));
+        s->per_wave = round_up(ceil_div(rows, (int64_t)s->splits * (kBlock / kWave)), 32);
+        s->dz = c.take<float>(rows * round_up(classes, 16));
+        s->kept = c.take<uint8_t>(rows);
+    }
     s->part = c.take<float>((int64_t)s->splits * classes * (dim + 1));
     return c.used;
+}
+
+// Shared memory beyond 64 KB is to be asked for, once per kernel.
+template <typename F>
+void allow_shared(F kernel, std::atomic<bool>& done) {
+    if (done.load(std::memory_order_relaxed)) return;
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedMemory);
+    done.store(true, std::memory_order_relaxed);
 }
 
 }  // namespace
@@ -423,7 +450,18 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const Head a = head_of(h, weight, bias);
     by_head(h->type, weight->rows, [&](auto type, auto tiles) {
-        k_head_labels<decltype(type), decltype(tiles)::v><<<(unsigned)ceil_div(a.rows, kHeadRows), kBlock, 0, stream>>>(a, soft, hard);
+        using T = decltype(type);
+        constexpr int CT = decltype(tiles)::v;
+        const int64_t bytes = (int64_t)16 * CT * shared_ld<T>(a.dim) * (int64_t)sizeof(T), blocks = ceil_div(a.rows, kHeadRows);
+        // a copy of W pays once a workgroup has several tiles of rows
+        const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 8);
+        if (bytes <= kSharedMemory && blocks >= 2 * stay) {
+            static std::atomic<bool> allowed{false};
+            allow_shared(k_head_labels<T, CT, true>, allowed);
+            k_head_labels<T, CT, true><<<(unsigned)stay, kBlock, (size_t)bytes, stream>>>(a, soft, hard);
+        } else {
+            k_head_labels<T, CT, false><<<(unsigned)blocks, kBlock, 0, stream>>>(a, soft, hard);
+        }
     });
     return launched();
 }
@@ -452,13 +490,22 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
     by_head(h->type, weight->rows, [&](auto type, auto tiles) {
         using T = decltype(type);
         constexpr int CT = decltype(tiles)::v;
-        if (a.rows > 0) {
-            const Loss g{targets->soft, targets->hard, targets->row_weight, targets->rejected, targets->grad_scale, loss,
-                         dh ? dh->data : nullptr, dh ? dh->stride : 0, bytes ? s.dz : nullptr, s.kept};
+        const Loss g{targets->soft, targets->hard, targets->row_weight, targets->rejected, targets->grad_scale, loss,
+                     dh ? dh->data : nullptr, dh ? dh->stride : 0, s.dz, s.kept};
+        if (a.rows > 0 && s.groups) {
+            auto fused = [&](auto per_wave) {
+                constexpr int GPW = decltype(per_wave)::v;
+                static std::atomic<bool> allowed{false};
+                allow_shared(k_head_fused<T, CT, GPW>, allowed);
+                k_head_fused<T, CT, GPW><<<(unsigned)s.splits, kBlock, (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, s.part);
+            };
+            if (s.groups <= 4) fused(Tiles<1>());
+            else fused(Tiles<2>());
+        } else if (a.rows > 0) {
             k_head_loss<T, CT><<<(unsigned)ceil_div(a.rows, kHeadRows), kBlock, 0, stream>>>(a, g);
         }
         if (!bytes) return;
-        if (a.rows > 0) {
+        if (a.rows > 0 && !s.groups) {
             const Outer o{a.h, s.dz, s.kept, s.part, a.ld_h, a.rows, s.per_wave, a.dim, a.classes};
             k_head_outer<T, CT><<<dim3((unsigned)s.splits, (unsigned)ceil_div(a.dim, 16 * Piece<T>::n)), kBlock, 0, stream>>>(o);
         }
