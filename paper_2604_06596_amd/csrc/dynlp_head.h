@@ -107,8 +107,15 @@ __device__ inline u32x4 column_of(const Quad<bf16> (&x)[8], int t) {
 template <typename T>
 struct WeightRows {
     const T* w;
+    const float* bias;
     int64_t ld;
     int dim, classes;
+    // Bias of classes c .. c + 3; -infinity, which makes the logit so whatever h holds, for what is not a class.
+    __device__ inline f32x4 bias4(int c) const {
+        f32x4 b;
+        for (int i = 0; i < 4; ++i) b[i] = c + i >= classes ? -INFINITY : bias ? bias[c + i] : 0.f;
+        return b;
+    }
     __device__ inline u32x4 piece(int c, int col) const {
         return c < classes && col < dim ? load_columns(w + (int64_t)c * ld, col, dim) : u32x4{0u, 0u, 0u, 0u};
     }
@@ -122,7 +129,9 @@ struct WeightRows {
 template <typename T>
 struct SharedWeight {
     const T* w;
+    const float* bias;
     int ld;
+    __device__ inline f32x4 bias4(int c) const { return *reinterpret_cast<const f32x4*>(bias + c); }
     __device__ inline u32x4 piece(int c, int col) const { return *reinterpret_cast<const u32x4*>(w + c * ld + col); }
     __device__ inline Quad<T> quad(int c, int col) const {
         Quad<T> v;
@@ -147,49 +156,62 @@ template <typename T, int CT>
 __device__ inline SharedWeight<T> share_weight(const Head& a, T* to) {
     constexpr int n = Piece<T>::n;
     const int ld = shared_ld<T>(a.dim), pieces = ld / n;
-    const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
+    const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
+    float* bias = reinterpret_cast<float*>(to + 16 * CT * ld);
+    if ((int)threadIdx.x < 4 * CT) *reinterpret_cast<f32x4*>(bias + 4 * threadIdx.x) = w.bias4(4 * threadIdx.x);
     for (int at = threadIdx.x; at < 16 * CT * pieces; at += kBlock)
         *reinterpret_cast<u32x4*>(to + at * n) = w.piece(at / pieces, at % pieces * n);
     __syncthreads();
-    return SharedWeight<T>{to, ld};
+    return SharedWeight<T>{to, bias, ld};
+}
+// Bytes of that copy, a multiple of 16.
+template <typename T, int CT>
+__host__ __device__ inline int shared_bytes(int dim) {
+    return 16 * CT * (shared_ld<T>(dim) * (int)sizeof(T) + 4);
 }
 
-// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.  The next step's part of h is
-// asked for before this step's products.
+// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.  Two steps' parts of h are asked for
+// before the first's products.
 template <typename T, int CT, int NT, typename W>
 __device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32x4 (&z)[NT][CT]) {
-    constexpr int n = Piece<T>::n;
+    constexpr int n = Piece<T>::n, S = 2;
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const T* h = static_cast<const T*>(a.h);
-    const T* hr[NT];
+    const T* h[NT];
     for (int m = 0; m < NT; ++m) {
-        hr[m] = h + min(first + 16 * m + r, a.rows - 1) * a.ld_h;
+        h[m] = static_cast<const T*>(a.h) + min(first + 16 * m + r, a.rows - 1) * a.ld_h;
         for (int t = 0; t < CT; ++t) z[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    u32x4 now[NT][2], next[NT][2];
-    auto ask = [&](int k0) {
-        for (int m = 0; m < NT; ++m)
-            for (int s = 0; s < 2; ++s) next[m][s] = load_columns(hr[m], k0 + q * 2 * n + s * n, a.dim);
-    };
-    ask(0);
+    const int mine = q * 2 * n;
 #pragma unroll 1
-    for (int k0 = 0; k0 < a.dim; k0 += 8 * n) {
-        for (int m = 0; m < NT; ++m)
-            for (int s = 0; s < 2; ++s) now[m][s] = next[m][s];
-        if (k0 + 8 * n < a.dim) ask(k0 + 8 * n);
+    for (int k0 = 0; k0 < a.dim; k0 += S * 8 * n) {
+        u32x4 v[S][NT][2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-            for (int t = 0; t < CT; ++t) {
-                const u32x4 wv = w.piece(16 * t + r, k0 + q * 2 * n + s * n);
-                for (int m = 0; m < NT; ++m) z[m][t] = mma(wv, now[m][s], z[m][t], T());
+        for (int s = 0; s < S; ++s) {
+            const int c = k0 + s * 8 * n;
+            if (c + 8 * n <= a.dim) {
+                for (int m = 0; m < NT; ++m)
+                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_piece(h[m] + c + mine + e * n);
+            } else if (c < a.dim) {
+                for (int m = 0; m < NT; ++m)
+                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_columns(h[m], c + mine + e * n, a.dim);
             }
-    }
-    for (int t = 0; t < CT; ++t)
-        for (int i = 0; i < 4; ++i) {
-            const int c = 16 * t + 4 * q + i;
-            const float b = c < a.classes && a.bias ? a.bias[c] : 0.f;
-            for (int m = 0; m < NT; ++m) z[m][t][i] = c < a.classes ? z[m][t][i] + b : -INFINITY;
         }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int c = k0 + s * 8 * n;
+            if (c < a.dim)
+                for (int e = 0; e < 2; ++e)
+                    for (int t = 0; t < CT; ++t) {
+                        const u32x4 wv = w.piece(16 * t + r, c + mine + e * n);
+                        for (int m = 0; m < NT; ++m) z[m][t] = mma(wv, v[s][m][e], z[m][t], T());
+                    }
+        }
+    }
+    for (int t = 0; t < CT; ++t) {
+        const f32x4 b = w.bias4(16 * t + 4 * q);
+        for (int m = 0; m < NT; ++m)
+            for (int i = 0; i < 4; ++i) z[m][t][i] = b[i] == -INFINITY ? b[i] : z[m][t][i] + b[i];
+    }
 }
 
 // Over the four lanes that share a row.
@@ -202,6 +224,15 @@ __device__ inline float row_max(float v) {
     return fmaxf(v, __shfl_xor(v, 32, kWave));
 }
 
+// e^x for x <= 0, or not a number: 2^y for y = x log2(e) as it is rounded, times 1 + ln(2) (what the rounding took).  Values below 2^-126 may be 0.
+__device__ inline float exp_below_0(float x) {
+    x = x < -150.f ? -150.f : x;
+    const float y = x * 1.44269502f;
+    const float rest = __builtin_fmaf(x, 1.44269502f, -y) + x * 1.92596299e-8f;
+    const float p = __builtin_amdgcn_exp2f(y);
+    return __builtin_fmaf(p, rest * 0.693147182f, p);
+}
+
 // z becomes exp(z - max); returns the sum, and the largest logit.  A NaN among the logits makes the sum one.
 template <int CT>
 __device__ inline float head_exp(f32x4 (&z)[CT], float* top) {
@@ -212,8 +243,8 @@ __device__ inline float head_exp(f32x4 (&z)[CT], float* top) {
     float sum = 0.f;
     for (int t = 0; t < CT; ++t)
         for (int i = 0; i < 4; ++i) {
-            // (-infinity)^0: a row of nothing else keeps sum 0; +infinity - +infinity is not a number, as it should be
-            z[t][i] = m == -INFINITY && z[t][i] == -INFINITY ? 0.f : expf(z[t][i] - m);
+            // a row of nothing but -infinity keeps sum 0; +infinity - +infinity is not a number, as it should be
+            z[t][i] = z[t][i] == -INFINITY ? 0.f : exp_below_0(z[t][i] - m);
             sum += z[t][i];
         }
     *top = m;
@@ -249,11 +280,11 @@ __global__ __launch_bounds__(kBlock) void k_head_labels(Head a, float* soft, int
             }
             if (soft) {
                 float top;
-                const float sum = head_exp(z[m], &top);
+                const float sum = head_exp(z[m], &top), inverse = 1.f / sum;
                 if (row < a.rows)
                     for (int t = 0; t < CT; ++t) {
                         float f[4];
-                        for (int i = 0; i < 4; ++i) f[i] = sum == 0.f ? 1.f / (float)a.classes : z[m][t][i] / sum;
+                        for (int i = 0; i < 4; ++i) f[i] = sum == 0.f ? 1.f / (float)a.classes : z[m][t][i] * inverse;
                         if (16 * t + 4 * q < a.classes) store_columns(soft + row * a.classes, 16 * t + 4 * q, a.classes, f);
                     }
             }
@@ -264,7 +295,7 @@ __global__ __launch_bounds__(kBlock) void k_head_labels(Head a, float* soft, int
         const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
         for (int64_t at = (int64_t)blockIdx.x * kHeadRows; at + first < a.rows; at += (int64_t)gridDim.x * kHeadRows) tile(w, at + first);
     } else {
-        const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
+        const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
         if ((int64_t)blockIdx.x * kHeadRows + first < a.rows) tile(w, (int64_t)blockIdx.x * kHeadRows + first);
     }
 }
@@ -282,8 +313,20 @@ struct Loss {
     uint8_t* kept;   // rows: 0 if left out
 };
 
-// x = high + low (+ what 16 or more further bits would hold), both bfloat16.
-__device__ inline uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (bf16)x); }
+// Two values rounded to bfloat16, the first in the low half; TERMS of them hold 8 TERMS bits of the values.
+__device__ inline uint32_t bf16_pair(float x, float y) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+}
+template <int TERMS>
+__device__ inline void bf16_terms(float x, float y, uint32_t (&term)[TERMS]) {
+    for (int k = 0; k < TERMS; ++k) {
+        term[k] = bf16_pair(x, y);
+        x -= __uint_as_float(term[k] << 16);
+        y -= __uint_as_float(term[k] & 0xffff0000u);
+    }
+}
 
 // dh of the tile's rows from their dz, 64 columns at a time.  Quads of W's rows are the left operand; in bfloat16 a lane's 8 x 4 block (8 classes, 4
 // columns) is transposed by v_perm.
@@ -311,16 +354,11 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f
     for (int m = 0; m < NT; ++m)
         for (int p = 0; p < P; ++p)
             for (int j = 0; j < 8; j += 2) {
-                uint32_t hi = 0, lo = 0;
-                for (int e = 0; e < 2; ++e) {
-                    const int t = 2 * p + (j >> 2);
-                    const float x = t < CT ? dz[m][t < CT ? t : 0][(j + e) & 3] : 0.f;
-                    const uint32_t b = bf16_bits(x);
-                    hi |= b << (16 * e);
-                    lo |= bf16_bits(x - __uint_as_float(b << 16)) << (16 * e);
-                }
-                high[m][p][j >> 1] = hi;
-                low[m][p][j >> 1] = lo;
+                const int t = 2 * p + (j >> 2), c = t < CT ? t : 0;
+                uint32_t two[2];
+                bf16_terms(t < CT ? dz[m][c][j & 3] : 0.f, t < CT ? dz[m][c][(j & 3) + 1] : 0.f, two);
+                high[m][p][j >> 1] = two[0];
+                low[m][p][j >> 1] = two[1];
             }
 #pragma unroll 1
     for (int base = 0; base < a.dim; base += 64) {
@@ -365,47 +403,55 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f
     }
 }
 
+// What a lane needs of row `row` beside its logits, asked for before them.
+template <int CT>
+struct RowTarget {
+    f32x4 y[CT];
+    float weight;
+    bool use;
+    __device__ inline void ask(const Head& a, const Loss& g, int64_t row) {
+        const int q = lane_id() >> 4;
+        const bool inside = row < a.rows;
+        const int64_t at = inside ? row : a.rows - 1;
+        weight = g.row_weight ? g.row_weight[at] : 1.f;
+        use = inside;
+        if (g.hard) {
+            const int label = g.hard[at];
+            if (inside && q == 0 && label >= a.classes && g.rejected) atomicAdd(g.rejected, 1);
+            use = use && label >= 0 && label < a.classes;
+            for (int t = 0; t < CT; ++t)
+                for (int i = 0; i < 4; ++i) y[t][i] = 16 * t + 4 * q + i == label ? 1.f : 0.f;
+        } else {
+            for (int t = 0; t < CT; ++t) {
+                const int c = 16 * t + 4 * q;
+                y[t] = __builtin_bit_cast(f32x4, c < a.classes ? load_columns(g.soft + at * a.classes, c, a.classes) : u32x4{0u, 0u, 0u, 0u});
+            }
+        }
+    }
+};
+
 // From the logits z of row `row` of a lane (first + 16 m + r): its loss is stored, z becomes dz.  Returns whether the row takes part.
 template <int CT>
-__device__ inline bool head_dz(const Head& a, const Loss& g, int64_t row, f32x4 (&z)[CT]) {
-    const int q = lane_id() >> 4;
-    const bool inside = row < a.rows;
-    const int64_t at = inside ? row : a.rows - 1;
-    const float weight = g.row_weight ? g.row_weight[at] : 1.f;
-    bool use = inside && weight != 0.f;
-    int label = -1;
-    f32x4 target[CT];
-    if (g.hard) {
-        label = g.hard[at];
-        if (inside && q == 0 && label >= a.classes && g.rejected) atomicAdd(g.rejected, 1);
-        use = use && label >= 0 && label < a.classes;
-    }
-    for (int t = 0; t < CT; ++t) {
-        const int c = 16 * t + 4 * q;
-        if (g.hard)
-            for (int i = 0; i < 4; ++i) target[t][i] = c + i == label ? 1.f : 0.f;
-        else
-            target[t] = __builtin_bit_cast(f32x4, c < a.classes ? load_columns(g.soft + at * a.classes, c, a.classes) : u32x4{0u, 0u, 0u, 0u});
-    }
+__device__ inline bool head_dz(const Loss& g, int64_t row, int64_t rows, const RowTarget<CT>& target, f32x4 (&z)[CT]) {
     f32x4 e[CT];
     for (int t = 0; t < CT; ++t) e[t] = z[t];
     float top;
     const float sum = head_exp(e, &top);
-    use = use && sum != 0.f;
+    const bool use = target.use && target.weight != 0.f && sum != 0.f;
     const float lse = logf(sum);  // of the shifted logits
     float total = 0.f, loss = 0.f;
     for (int t = 0; t < CT; ++t)
         for (int i = 0; i < 4; ++i) {
-            const float y = target[t][i];
+            const float y = target.y[t][i];
             total += y;
             loss += y != 0.f ? y * (lse - (z[t][i] - top)) : 0.f;
         }
     total = row_sum(total);
     loss = row_sum(loss);
-    const float scale = g.grad_scale * weight;
+    const float scale = g.grad_scale * target.weight, part = total / sum;
     for (int t = 0; t < CT; ++t)
-        for (int i = 0; i < 4; ++i) z[t][i] = use ? scale * (total * (e[t][i] / sum) - target[t][i]) : 0.f;
-    if (inside && q == 0 && g.loss) g.loss[row] = use ? weight * loss : 0.f;
+        for (int i = 0; i < 4; ++i) z[t][i] = use ? scale * (part * e[t][i] - target.y[t][i]) : 0.f;
+    if (row < rows && lane_id() < 16 && g.loss) g.loss[row] = use ? target.weight * loss : 0.f;
     return use;
 }
 
@@ -417,13 +463,15 @@ __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
     const int64_t first = (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
     if (first >= a.rows) return;
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const WeightRows<T> w{static_cast<const T*>(a.weight), a.ld_w, a.dim, a.classes};
+    const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
     f32x4 z[NT][CT];
+    RowTarget<CT> target[NT];
     bool kept[NT];
+    for (int m = 0; m < NT; ++m) target[m].ask(a, g, first + 16 * m + r);
     head_logits<T, CT, NT>(a, w, first, z);
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
-        kept[m] = head_dz(a, g, row, z[m]);
+        kept[m] = head_dz(g, row, a.rows, target[m], z[m]);
         if (row < a.rows && g.dz) {
             if (q == 0) g.kept[row] = kept[m] ? 1 : 0;
             for (int t = 0; t < CT; ++t) *reinterpret_cast<f32x4*>(g.dz + row * (16 * CT) + 16 * t + 4 * q) = z[m][t];
@@ -465,17 +513,12 @@ __device__ inline void outer_rows(const Outer& o, int64_t first, int64_t end, in
         u32x4 term[3][CT];
         for (int t = 0; t < CT; ++t)
             for (int j = 0; j < 8; j += 2) {
-                uint32_t b[3] = {0, 0, 0};
-                for (int e = 0; e < 2; ++e) {
-                    float v = a[t][j >> 2][(j + e) & 3];
-                    sum[t] += v;
-                    for (int k = 0; k < 3; ++k) {
-                        const uint32_t bits = bf16_bits(v);
-                        b[k] |= bits << (16 * e);
-                        v -= __uint_as_float(bits << 16);
-                    }
-                }
-                for (int k = 0; k < 3; ++k) term[k][t][j >> 1] = b[k];
+                const float v0 = a[t][j >> 2][j & 3], v1 = a[t][j >> 2][(j & 3) + 1];
+                sum[t] += v0;
+                sum[t] += v1;
+                uint32_t three[3];
+                bf16_terms(v0, v1, three);
+                for (int k = 0; k < 3; ++k) term[k][t][j >> 1] = three[k];
             }
         for (int t = 0; t < 8; ++t) {
             u32x4 right;
@@ -571,61 +614,65 @@ struct SharedDz {
     }
 };
 
-// acc[ct][t] += rows from .. to of the tile, columns col + t.  h is read once more here, from the L2: the workgroup has just read it.
+// dweight's right operand: quads of h's rows, K of them per lane (8 q + j, or 4 j + q), which the workgroup has just read: this time they come from the L2.
+// They are asked for a step ahead, and the rows that are left out are blanked when they are used.
+template <typename T>
+struct OuterRows {
+    static constexpr bool two = __is_same(T, bf16);
+    static constexpr int K = two ? 8 : 4, step = two ? 32 : 16;
+    const char* h;     // of the tile's first row, this lane's columns
+    uint32_t pitch;    // bytes from one row to the next
+    int last;          // row of the tile that is there
+    int room;          // columns from this lane's first one on
+    __device__ inline static int row_of(int j) {
+        const int q = lane_id() >> 4;
+        return two ? 8 * q + j : 4 * j + q;
+    }
+    __device__ inline void ask(int k0, Quad<T> (&x)[K]) const {
+        for (int j = 0; j < K; ++j) {
+            const T* p = reinterpret_cast<const T*>(h + (uint64_t)(uint32_t)min(k0 + row_of(j), last) * pitch);
+            if (room >= 4) __builtin_memcpy(x[j].d, p, sizeof x[j].d);
+            else x[j] = load_quad(p, 0, room);
+        }
+    }
+    // kept: a bit per row of the tile, 32 to a word.
+    __device__ inline static void blank(const uint32_t* kept, int k0, Quad<T> (&x)[K]) {
+        const uint32_t word = kept[k0 >> 5];
+        if (__builtin_amdgcn_readfirstlane(word) == ~0u) return;
+        for (int j = 0; j < K; ++j) {
+            const bool ok = word >> ((k0 & 31) + row_of(j)) & 1;
+            for (int e = 0; e < Quad<T>::words; ++e) x[j].d[e] = ok ? x[j].d[e] : 0u;
+        }
+    }
+};
+
+// acc[ct][t] += dz^T h for the rows k0 .. k0 + step - 1 of the tile.
 template <int CT>
-__device__ inline void tile_outer(const Head& a, int64_t tile, int from, int to, int col, const SharedDz<bf16, CT>& dz, const uint8_t* kept,
-                                  f32x4 (&acc)[CT][4]) {
+__device__ inline void outer_step(const SharedDz<bf16, CT>& dz, int k0, const Quad<bf16> (&x)[8], f32x4 (&acc)[CT][4]) {
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const bf16* h = static_cast<const bf16*>(a.h);
-#pragma unroll 1
-    for (int k0 = from; k0 < to; k0 += 32) {
-        Quad<bf16> x[8];
-        for (int j = 0; j < 8; ++j) {
-            const int row = k0 + 8 * q + j;
-            x[j].zero();
-            if (kept[row] && col < a.dim) x[j] = load_quad(h + (tile + row) * a.ld_h, col, a.dim);
+    u32x4 right[4];
+    for (int t = 0; t < 4; ++t) right[t] = column_of(x, t);
+    for (int ct = 0; ct < CT; ++ct) {
+        // dz in three bfloat16 terms, which hold all 24 bits of it: dweight is a float32 sum over all rows
+        u32x4 term[3];
+        for (int j = 0; j < 8; j += 2) {
+            const float* v = dz.p + (k0 + 8 * q + j) * SharedDz<bf16, CT>::ld + 16 * ct + r;
+            uint32_t three[3];
+            bf16_terms(v[0], v[SharedDz<bf16, CT>::ld], three);
+            for (int k = 0; k < 3; ++k) term[k][j >> 1] = three[k];
         }
-        u32x4 right[4];
-        for (int t = 0; t < 4; ++t) right[t] = column_of(x, t);
-        for (int ct = 0; ct < CT; ++ct) {
-            // dz in three bfloat16 terms, which hold all 24 bits of it: dweight is a float32 sum over all rows
-            u32x4 term[3];
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t b[3] = {0, 0, 0};
-                for (int e = 0; e < 2; ++e) {
-                    float v = dz.p[(k0 + 8 * q + j + e) * SharedDz<bf16, CT>::ld + 16 * ct + r];
-                    for (int k = 0; k < 3; ++k) {
-                        const uint32_t bits = bf16_bits(v);
-                        b[k] |= bits << (16 * e);
-                        v -= __uint_as_float(bits << 16);
-                    }
-                }
-                for (int k = 0; k < 3; ++k) term[k][j >> 1] = b[k];
-            }
-            for (int k = 2; k >= 0; --k)
-                for (int t = 0; t < 4; ++t) acc[ct][t] = mma(term[k], right[t], acc[ct][t], bf16());
-        }
+        for (int k = 2; k >= 0; --k)
+            for (int t = 0; t < 4; ++t) acc[ct][t] = mma(term[k], right[t], acc[ct][t], bf16());
     }
 }
 template <int CT, typename T>
-__device__ inline void tile_outer(const Head& a, int64_t tile, int from, int to, int col, const SharedDz<T, CT>& dz, const uint8_t* kept,
-                                  f32x4 (&acc)[CT][4]) {
+__device__ inline void outer_step(const SharedDz<T, CT>& dz, int k0, const Quad<T> (&x)[4], f32x4 (&acc)[CT][4]) {
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    const T* h = static_cast<const T*>(a.h);
-#pragma unroll 1
-    for (int k0 = from; k0 < to; k0 += 16) {
-        Quad<T> x[4];
-        for (int j = 0; j < 4; ++j) {
-            const int row = k0 + 4 * j + q;
-            x[j].zero();
-            if (kept[row] && col < a.dim) x[j] = load_quad(h + (tile + row) * a.ld_h, col, a.dim);
+    for (int j = 0; j < 4; ++j)
+        for (int ct = 0; ct < CT; ++ct) {
+            const float left = dz.p[(k0 + 4 * j + q) * SharedDz<T, CT>::ld + 16 * ct + r];
+            for (int t = 0; t < 4; ++t) acc[ct][t] = mma4(left, x[j].get(t), acc[ct][t]);
         }
-        for (int j = 0; j < 4; ++j)
-            for (int ct = 0; ct < CT; ++ct) {
-                const float left = dz.p[(k0 + 4 * j + q) * SharedDz<T, CT>::ld + 16 * ct + r];
-                for (int t = 0; t < 4; ++t) acc[ct][t] = mma4(left, x[j].get(t), acc[ct][t]);
-            }
-    }
 }
 
 constexpr int kFusedColumns = 64;
@@ -639,9 +686,9 @@ __global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a,
     extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
-    char* behind = space + 16 * CT * w.ld * sizeof(T);
+    char* behind = space + shared_bytes<T, CT>(a.dim);
     SharedDz<T, CT> dz{reinterpret_cast<decltype(SharedDz<T, CT>::p)>(behind)};
-    uint8_t* kept = reinterpret_cast<uint8_t*>(behind + SharedDz<T, CT>::bytes);
+    uint32_t* kept = reinterpret_cast<uint32_t*>(behind + SharedDz<T, CT>::bytes);  // a bit per row of the tile
     const int groups = (a.dim + kCols - 1) / kCols;
     const int my_group = groups == 1 ? 0 : groups == 2 ? wave & 1 : wave;
     const int from = groups == 1 ? wave * (kHeadRows / 4) : groups == 2 ? (wave >> 1) * (kHeadRows / 2) : 0;
@@ -652,24 +699,47 @@ __global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a,
             for (int t = 0; t < N; ++t) acc[p][ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int my_class = threadIdx.x % (16 * CT), my_rows = threadIdx.x / (16 * CT) * 32;  // of dbias: 32 rows of the tile
     float sum = 0.f;
+    using Right = OuterRows<T>;
+    const int mine = wave * (NT * 16);
+#pragma unroll 1
     for (int64_t tile = (int64_t)blockIdx.x * kHeadRows; tile < a.rows; tile += (int64_t)gridDim.x * kHeadRows) {
-        const int mine = wave * (NT * 16);
         {
             f32x4 z[NT][CT];
+            RowTarget<CT> target[NT];
             bool use[NT];
+            for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r);
             head_logits<T, CT, NT>(a, w, tile + mine, z);
+            uint32_t bits = 0;
             for (int m = 0; m < NT; ++m) {
                 const int row = mine + 16 * m + r;
-                use[m] = head_dz(a, g, tile + row, z[m]);
-                if (q == 0) kept[row] = use[m] ? 1 : 0;
+                use[m] = head_dz(g, tile + row, a.rows, target[m], z[m]);
+                bits |= ((uint32_t)__ballot(use[m]) & 0xffffu) << (16 * m);
                 for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
             }
+            if (lane_id() == 0) kept[wave] = bits;
             if (g.dh) head_dh<CT, NT>(a, w, tile + mine, z, use, static_cast<T*>(g.dh), g.ld_dh);
         }
-        __syncthreads();
-        if (my_rows < kHeadRows) sum += dz.rows_of(my_class, my_rows);
-        for (int p = 0; p < GPW; ++p)
-            if (my_group + 4 * p < groups) tile_outer(a, tile, from, to, (my_group + 4 * p) * kCols + N * r, dz, kept, acc[p]);
+        const int last = (int)min((int64_t)kHeadRows, a.rows - tile) - 1;
+        for (int p = 0; p < GPW; ++p) {
+            const int col = (my_group + 4 * p) * kCols + 4 * r;
+            const bool owner = my_group + 4 * p < groups;
+            const Right right{reinterpret_cast<const char*>(static_cast<const T*>(a.h) + tile * a.ld_h + min(col, a.dim - 1)),
+                              (uint32_t)(a.ld_h * sizeof(T)), last, a.dim - col};
+            Quad<T> x[Right::K], next[Right::K];
+            if (owner) right.ask(from, next);
+            if (p == 0) {
+                __syncthreads();
+                if (my_rows < kHeadRows) sum += dz.rows_of(my_class, my_rows);
+            }
+            if (owner)
+#pragma unroll 1
+                for (int k0 = from; k0 < to; k0 += Right::step) {
+                    for (int j = 0; j < Right::K; ++j) x[j] = next[j];
+                    if (k0 + Right::step < to) right.ask(k0 + Right::step, next);
+                    Right::blank(kept, k0, x);
+                    outer_step(dz, k0, x, acc[p]);
+                }
+        }
         __syncthreads();
     }
     part += (int64_t)blockIdx.x * a.classes * (a.dim + 1);
@@ -708,8 +778,8 @@ __global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a,
 // Bytes of shared memory of k_head_fused.
 template <typename T, int CT>
 inline int64_t fused_bytes(int dim) {
-    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kHeadRows;
-    return (int64_t)16 * CT * shared_ld<T>(dim) * (int64_t)sizeof(T) + (joined > dz ? joined : dz);
+    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kHeadRows / 8;
+    return shared_bytes<T, CT>(dim) + (joined > dz ? joined : dz);
 }
 
 // Sums the parts: 16 neighbouring elements per workgroup, 16 groups of lanes taking turns on the parts, then joined in order.

@@ -393,14 +393,17 @@ void by_head(int32_t type, int64_t classes, F f) {
 }
 
 constexpr int64_t kSharedMemory = 160 * 1024;  // of a CU
+constexpr int kMostSharedDim = 1 << 14;        // rows of W that may fit it at all
+constexpr int64_t kMostFusedStride = 1 << 28;  // elements: 32 bits hold the bytes from one row to the next
 
 // Column groups of dweight that a workgroup keeps in registers: up to eight, two per wave.  0: it does not fit, or W does not fit beside dz.
 int fused_groups(int dim, int classes, int32_t type) {
     int groups = 0;
+    if (dim > 8 * kFusedColumns) return 0;
     by_head(type, classes, [&](auto t, auto tiles) {
         using T = decltype(t);
         const int64_t n = ceil_div(dim, kFusedColumns);
-        if (n <= 8 && fused_bytes<T, decltype(tiles)::v>(dim) <= kSharedMemory) groups = (int)n;
+        if (fused_bytes<T, decltype(tiles)::v>(dim) <= kSharedMemory) groups = (int)n;
     });
     return groups;
 }
@@ -413,9 +416,9 @@ struct LossSpace {
     int64_t per_wave;
 };
 
-int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type, LossSpace* s) {
+int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type, bool fused, LossSpace* s) {
     Carve c{base};
-    s->groups = fused_groups(dim, classes, type);
+    s->groups = fused ? fused_groups(dim, classes, type) : 0;
     if (s->groups) {
         s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, kHeadRows), 1), s->groups > 4 ? 256 : 512);
     } else {
@@ -452,7 +455,7 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
     by_head(h->type, weight->rows, [&](auto type, auto tiles) {
         using T = decltype(type);
         constexpr int CT = decltype(tiles)::v;
-        const int64_t bytes = (int64_t)16 * CT * shared_ld<T>(a.dim) * (int64_t)sizeof(T), blocks = ceil_div(a.rows, kHeadRows);
+        const int64_t bytes = a.dim <= kMostSharedDim ? shared_bytes<T, CT>(a.dim) : kSharedMemory + 1, blocks = ceil_div(a.rows, kHeadRows);
         // a copy of W pays once a workgroup has several tiles of rows
         const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 8);
         if (bytes <= kSharedMemory && blocks >= 2 * stay) {
@@ -469,7 +472,7 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
 int64_t dynlp_head_loss_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type) {
     if (rows < 0 || rows > kMostRows || dim < 1 || classes < 1 || classes > DYNLP_MAX_CLASSES) return 0;
     LossSpace s;
-    return loss_space(nullptr, rows, dim, classes, type, &s);
+    return std::max(loss_space(nullptr, rows, dim, classes, type, true, &s), loss_space(nullptr, rows, dim, classes, type, false, &s));
 }
 
 dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_targets* targets,
@@ -486,7 +489,7 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const Head a = head_of(h, weight, bias);
     LossSpace s{};
-    if (bytes) loss_space(static_cast<char*>(call->workspace), a.rows, a.dim, a.classes, h->type, &s);
+    if (bytes) loss_space(static_cast<char*>(call->workspace), a.rows, a.dim, a.classes, h->type, a.ld_h < kMostFusedStride, &s);
     by_head(h->type, weight->rows, [&](auto type, auto tiles) {
         using T = decltype(type);
         constexpr int CT = decltype(tiles)::v;
