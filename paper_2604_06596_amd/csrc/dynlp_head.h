@@ -159,7 +159,7 @@ __device__ inline SharedWeight<T> share_weight(const Head& a, T* to) {
     const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
     float* bias = reinterpret_cast<float*>(to + 16 * CT * ld);
     if ((int)threadIdx.x < 4 * CT) *reinterpret_cast<f32x4*>(bias + 4 * threadIdx.x) = w.bias4(4 * threadIdx.x);
-    for (int at = threadIdx.x; at < 16 * CT * pieces; at += kBlock)
+    for (int at = threadIdx.x; at < 16 * CT * pieces; at += blockDim.x)
         *reinterpret_cast<u32x4*>(to + at * n) = w.piece(at / pieces, at % pieces * n);
     __syncthreads();
     return SharedWeight<T>{to, bias, ld};
@@ -595,21 +595,30 @@ __global__ __launch_bounds__(kBlock) void k_head_outer(Outer o) {
 
 // ---- everything in one pass over h ------------------------------------------------------------------------------------
 
+constexpr int kFusedRows = 128;    // of a tile
+constexpr int kFusedColumns = 64;  // of a group: a wave's part of dweight
+constexpr int kFusedMost = kFusedColumns * 8;
+
+// Up to 32 classes a wave needs few enough registers for four waves on a SIMD: eight waves with 16 rows each.  Beyond that: four waves with 32 rows
+// each, two on a SIMD (in bfloat16 with 50 classes of 256 columns, 1M rows: 423 us; eight waves 467 us, and 656 us when held to 128 registers.  In
+// float32 with 10 classes of 64 columns, 100,000 rows: 25.7 us with eight waves, 28.2 us with four).
+__host__ __device__ constexpr int fused_waves(int class_tiles) { return class_tiles <= 2 ? 8 : 4; }
+
 // dz of a workgroup's 128 rows in shared memory: [row][class], padded so that the four row groups that a wave reads at once (4 j + q, or 8 q + j
 // for bfloat16) lie in different banks.
 template <typename T, int CT>
 struct SharedDz {
-    static constexpr int ld = 16 * CT + (sizeof(T) == 2 && !__is_same(T, f16) ? 2 : 16), bytes = kHeadRows * ld * 4;
+    static constexpr int ld = 16 * CT + (sizeof(T) == 2 && !__is_same(T, f16) ? 2 : 16), bytes = kFusedRows * ld * 4;
     float* p;
     __device__ inline void put(int row, int t, int q, const f32x4& z) {
         float2* to = reinterpret_cast<float2*>(p + row * ld + 16 * t + 4 * q);
         to[0] = float2{z[0], z[1]};
         to[1] = float2{z[2], z[3]};
     }
-    // Sum of a class over 32 rows.
+    // Sum of a class over 16 rows.
     __device__ inline float rows_of(int c, int from) const {
         float s = 0.f;
-        for (int k = 0; k < 32; ++k) s += p[(from + k) * ld + c];
+        for (int k = 0; k < 16; ++k) s += p[(from + k) * ld + c];
         return s;
     }
 };
@@ -675,61 +684,67 @@ __device__ inline void outer_step(const SharedDz<T, CT>& dz, int k0, const Quad<
         }
 }
 
-constexpr int kFusedColumns = 64;
+// How many waves share the rows of a tile for one group of columns of dweight: those that the groups leave, but a wave has whole steps.
+template <typename T>
+__host__ __device__ inline int fused_splits(int groups, int waves) {
+    const int most = kFusedRows / (__is_same(T, bf16) ? 32 : 16);
+    int splits = waves;
+    while (splits > 1 && (splits > most || splits * groups > waves)) splits >>= 1;
+    return splits;
+}
 
-// Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight in registers over all tiles of 128 rows.  The columns
-// are cut into groups of 64 (a quad for each of 16 lanes).  One group: the four waves share the tile's rows; two: two waves
-// each; more: each wave has GPW groups and all rows.
+// Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight (GPW groups of 64, a quad for each of 16 lanes) in registers
+// over all tiles of 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
 template <typename T, int CT, int GPW>
-__global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a, Loss g, float* part) {
-    constexpr int NT = kHeadTiles, N = 4, kCols = kFusedColumns;
+__global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) void k_head_fused(Head a, Loss g, float* part) {
+    constexpr int kCols = kFusedColumns, kWaves = fused_waves(CT), NT = 8 / kWaves;
     extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
     char* behind = space + shared_bytes<T, CT>(a.dim);
-    SharedDz<T, CT> dz{reinterpret_cast<decltype(SharedDz<T, CT>::p)>(behind)};
+    SharedDz<T, CT> dz{reinterpret_cast<float*>(behind)};
     uint32_t* kept = reinterpret_cast<uint32_t*>(behind + SharedDz<T, CT>::bytes);  // a bit per row of the tile
-    const int groups = (a.dim + kCols - 1) / kCols;
-    const int my_group = groups == 1 ? 0 : groups == 2 ? wave & 1 : wave;
-    const int from = groups == 1 ? wave * (kHeadRows / 4) : groups == 2 ? (wave >> 1) * (kHeadRows / 2) : 0;
-    const int to = groups == 1 ? from + kHeadRows / 4 : groups == 2 ? from + kHeadRows / 2 : kHeadRows;
-    f32x4 acc[GPW][CT][N];
-    for (int ct = 0; ct < CT; ++ct)
-        for (int p = 0; p < GPW; ++p)
-            for (int t = 0; t < N; ++t) acc[p][ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int my_class = threadIdx.x % (16 * CT), my_rows = threadIdx.x / (16 * CT) * 32;  // of dbias: 32 rows of the tile
+    uint16_t* kept16 = reinterpret_cast<uint16_t*>(kept);
+    const int groups = (a.dim + kCols - 1) / kCols, splits = fused_splits<T>(groups, kWaves);
+    const int my_group = wave / splits, my_split = wave % splits;
+    const int from = my_split * (kFusedRows / splits), to = from + kFusedRows / splits;
+    f32x4 acc[GPW][CT][4];
+    for (int p = 0; p < GPW; ++p)
+        for (int ct = 0; ct < CT; ++ct)
+            for (int t = 0; t < 4; ++t) acc[p][ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int my_class = threadIdx.x % (16 * CT), my_rows = threadIdx.x / (16 * CT) * 16;  // of dbias: 16 rows of the tile
     float sum = 0.f;
     using Right = OuterRows<T>;
-    const int mine = wave * (NT * 16);
+    const int mine = wave * (16 * NT);
 #pragma unroll 1
-    for (int64_t tile = (int64_t)blockIdx.x * kHeadRows; tile < a.rows; tile += (int64_t)gridDim.x * kHeadRows) {
+    for (int64_t tile = (int64_t)blockIdx.x * kFusedRows; tile < a.rows; tile += (int64_t)gridDim.x * kFusedRows) {
         {
             f32x4 z[NT][CT];
             RowTarget<CT> target[NT];
             bool use[NT];
             for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r);
             head_logits<T, CT, NT>(a, w, tile + mine, z);
-            uint32_t bits = 0;
             for (int m = 0; m < NT; ++m) {
                 const int row = mine + 16 * m + r;
                 use[m] = head_dz(g, tile + row, a.rows, target[m], z[m]);
-                bits |= ((uint32_t)__ballot(use[m]) & 0xffffu) << (16 * m);
+                const uint16_t bits = (uint16_t)__ballot(use[m]);
+                if (lane_id() == 0) kept16[wave * NT + m] = bits;
                 for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
             }
-            if (lane_id() == 0) kept[wave] = bits;
             if (g.dh) head_dh<CT, NT>(a, w, tile + mine, z, use, static_cast<T*>(g.dh), g.ld_dh);
         }
-        const int last = (int)min((int64_t)kHeadRows, a.rows - tile) - 1;
+        const int last = (int)min((int64_t)kFusedRows, a.rows - tile) - 1;
+#pragma unroll
         for (int p = 0; p < GPW; ++p) {
-            const int col = (my_group + 4 * p) * kCols + 4 * r;
-            const bool owner = my_group + 4 * p < groups;
+            const int col = (my_group + kWaves * p) * kCols + 4 * r;
+            const bool owner = my_group + kWaves * p < groups;
             const Right right{reinterpret_cast<const char*>(static_cast<const T*>(a.h) + tile * a.ld_h + min(col, a.dim - 1)),
                               (uint32_t)(a.ld_h * sizeof(T)), last, a.dim - col};
             Quad<T> x[Right::K], next[Right::K];
             if (owner) right.ask(from, next);
             if (p == 0) {
                 __syncthreads();
-                if (my_rows < kHeadRows) sum += dz.rows_of(my_class, my_rows);
+                for (int at = my_rows; at < kFusedRows; at += kWave * kWaves / (16 * CT) * 16) sum += dz.rows_of(my_class, at);
             }
             if (owner)
 #pragma unroll 1
@@ -748,29 +763,28 @@ __global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a,
     __syncthreads();
     if ((int)threadIdx.x < a.classes) {
         float v = 0.f;
-        for (int k = 0; k < kHeadRows / 32; ++k) v += bias[k * 16 * CT + threadIdx.x];
+        for (int k = threadIdx.x; k < kWave * kWaves / (16 * CT) * (16 * CT); k += 16 * CT) v += bias[k];
         part[(int64_t)threadIdx.x * (a.dim + 1) + a.dim] = v;
     }
     // dweight: a group of columns after the other, its waves' parts added in order
     float* joined = reinterpret_cast<float*>(behind);
     for (int k = 0; k < groups; ++k) {
-        const bool owner = groups <= 2 ? my_group == k : wave == (k & 3);
         __syncthreads();
-        for (int turn = 0; turn < (groups == 1 ? 4 : groups == 2 ? 2 : 1); ++turn) {
-            if (owner && (groups == 1 ? wave == turn : groups == 2 ? wave >> 1 == turn : true))
-                for (int p = 0; p < GPW; ++p)
-                    if (p == (groups <= 2 ? 0 : k >> 2))
-                        for (int ct = 0; ct < CT; ++ct)
-                            for (int t = 0; t < N; ++t)
-                                for (int i = 0; i < 4; ++i) {
-                                    float& to_sum = joined[(16 * ct + 4 * q + i) * (kCols + 1) + N * r + t];
-                                    to_sum = turn ? to_sum + acc[p][ct][t][i] : acc[p][ct][t][i];
-                                }
+        for (int turn = 0; turn < splits; ++turn) {
+#pragma unroll
+            for (int p = 0; p < GPW; ++p)
+                if (my_group + kWaves * p == k && my_split == turn)
+                    for (int ct = 0; ct < CT; ++ct)
+                        for (int t = 0; t < 4; ++t)
+                            for (int i = 0; i < 4; ++i) {
+                                float& to_sum = joined[(16 * ct + 4 * q + i) * (kCols + 1) + 4 * r + t];
+                                to_sum = turn ? to_sum + acc[p][ct][t][i] : acc[p][ct][t][i];
+                            }
             __syncthreads();
         }
-        for (int at = threadIdx.x; at < a.classes * kCols; at += kBlock) {
-            const int c = at / kCols, col = at % kCols;
-            if (k * kCols + col < a.dim) part[(int64_t)c * (a.dim + 1) + k * kCols + col] = joined[c * (kCols + 1) + col];
+        for (int at = threadIdx.x; at < a.classes * kCols; at += kWave * kWaves) {
+            const int c = at / kCols, x = at % kCols;
+            if (k * kCols + x < a.dim) part[(int64_t)c * (a.dim + 1) + k * kCols + x] = joined[c * (kCols + 1) + x];
         }
     }
 }
@@ -778,7 +792,7 @@ __global__ __launch_bounds__(kBlock, GPW == 1 ? 2 : 1) void k_head_fused(Head a,
 // Bytes of shared memory of k_head_fused.
 template <typename T, int CT>
 inline int64_t fused_bytes(int dim) {
-    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kHeadRows / 8;
+    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kFusedRows / 8;
     return shared_bytes<T, CT>(dim) + (joined > dz ? joined : dz);
 }
 

@@ -396,31 +396,28 @@ constexpr int64_t kSharedMemory = 160 * 1024;  // of a CU
 constexpr int kMostSharedDim = 1 << 14;        // rows of W that may fit it at all
 constexpr int64_t kMostFusedStride = 1 << 28;  // elements: 32 bits hold the bytes from one row to the next
 
-// Column groups of dweight that a workgroup keeps in registers: up to eight, two per wave.  0: it does not fit, or W does not fit beside dz.
-int fused_groups(int dim, int classes, int32_t type) {
-    int groups = 0;
-    if (dim > 8 * kFusedColumns) return 0;
-    by_head(type, classes, [&](auto t, auto tiles) {
-        using T = decltype(t);
-        const int64_t n = ceil_div(dim, kFusedColumns);
-        if (fused_bytes<T, decltype(tiles)::v>(dim) <= kSharedMemory) groups = (int)n;
-    });
-    return groups;
+// Whether one pass over h does all: dweight's columns have a wave each, and W fits a workgroup's shared memory beside dz.
+bool fits_fused(int dim, int classes, int32_t type) {
+    if (dim > kFusedMost) return false;
+    bool fits = false;
+    by_head(type, classes, [&](auto t, auto tiles) { fits = fused_bytes<decltype(t), decltype(tiles)::v>(dim) <= kSharedMemory; });
+    return fits;
 }
 
 struct LossSpace {
     float* dz;
     uint8_t* kept;
     float* part;
-    int splits, groups;
+    int splits;
+    bool fused;
     int64_t per_wave;
 };
 
 int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type, bool fused, LossSpace* s) {
     Carve c{base};
-    s->groups = fused ? fused_groups(dim, classes, type) : 0;
-    if (s->groups) {
-        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, kHeadRows), 1), s->groups > 4 ? 256 : 512);
+    s->fused = fused && fits_fused(dim, classes, type);
+    if (s->fused) {
+        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, kFusedRows), 1), 512);
     } else {
         const int64_t across = ceil_div(dim, 16 * (16 / type_size(type)));
         // workgroups of dweight: twice the CUs over all columns, each wave with 64 rows at least
@@ -495,20 +492,24 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
         constexpr int CT = decltype(tiles)::v;
         const Loss g{targets->soft, targets->hard, targets->row_weight, targets->rejected, targets->grad_scale, loss,
                      dh ? dh->data : nullptr, dh ? dh->stride : 0, s.dz, s.kept};
-        if (a.rows > 0 && s.groups) {
+        if (a.rows > 0 && s.fused) {
             auto fused = [&](auto per_wave) {
                 constexpr int GPW = decltype(per_wave)::v;
                 static std::atomic<bool> allowed{false};
                 allow_shared(k_head_fused<T, CT, GPW>, allowed);
-                k_head_fused<T, CT, GPW><<<(unsigned)s.splits, kBlock, (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, s.part);
+                k_head_fused<T, CT, GPW><<<(unsigned)s.splits, kWave * fused_waves(CT), (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, s.part);
             };
-            if (s.groups <= 4) fused(Tiles<1>());
-            else fused(Tiles<2>());
+            if constexpr (fused_waves(CT) < 8) {
+                if (a.dim > kFusedColumns * fused_waves(CT)) fused(Tiles<2>());
+                else fused(Tiles<1>());
+            } else {
+                fused(Tiles<1>());
+            }
         } else if (a.rows > 0) {
             k_head_loss<T, CT><<<(unsigned)ceil_div(a.rows, kHeadRows), kBlock, 0, stream>>>(a, g);
         }
         if (!bytes) return;
-        if (a.rows > 0 && !s.groups) {
+        if (a.rows > 0 && !s.fused) {
             const Outer o{a.h, s.dz, s.kept, s.part, a.ld_h, a.rows, s.per_wave, a.dim, a.classes};
             k_head_outer<T, CT><<<dim3((unsigned)s.splits, (unsigned)ceil_div(a.dim, 16 * Piece<T>::n)), kBlock, 0, stream>>>(o);
         }
