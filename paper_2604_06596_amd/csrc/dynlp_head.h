@@ -5,8 +5,8 @@
 // long as both operands agree, and so is which columns of a matrix stand behind the 16 rows or columns of a tile; both are chosen
 // here so that every lane reads 16 consecutive bytes and the result of one product is, as it lies in the registers, an operand of the
 // next:
-//   logits   z^T = W h^T.   Lane (q, r): W of class r, h of row r, columns k0 + 2 n q ... of a piece of n elements (a lane's two pieces
-//            fill its part of a 128-byte line).  Result: row r's logits of classes 16 t + 4 q + i.
+//   logits   z^T = W h^T.   Lane (q, r): W of class r, h of row r, a piece of n columns from k0 + n q on (64 bytes of a row per access).
+//            Result: row r's logits of classes 16 t + 4 q + i.
 //   dh       dh^T = W^T dz^T.  The right operand (k = class, column = row r) is what the lane holds after the softmax.  The left one
 //            needs W by columns: pieces of W's rows, for two-byte types transposed between registers.  Result: row r, n consecutive columns.
 //   dweight  dz^T h.  Both operands are read row by row of h and dz, h in pieces, transposed between registers where needed.
@@ -87,15 +87,6 @@ __device__ inline Quad<T> load_quad(const T* row, int col, int dim) {
         }
     return v;
 }
-template <typename T>
-__device__ inline void store_quad(T* row, int col, int dim, const float (&f)[4]) {
-    if (col + 4 <= dim) {
-        store_values<4>(row + col, f);
-    } else {
-        for (int k = 0; k < 4; ++k)
-            if (col + k < dim) row[col + k] = (T)f[k];
-    }
-}
 // Column t of eight rows' quads, as an operand with these rows for k.
 __device__ inline u32x4 column_of(const Quad<bf16> (&x)[8], int t) {
     u32x4 v;
@@ -145,6 +136,16 @@ struct SharedWeight {
         return v;
     }
 };
+// The same rows, but addresses made from them are not kept in registers from one step of a loop to the next.
+template <typename T>
+__device__ inline WeightRows<T> anew(const WeightRows<T>& w) {
+    return w;
+}
+template <typename T>
+__device__ inline SharedWeight<T> anew(SharedWeight<T> w) {
+    asm volatile("" : "+s"(w.ld));
+    return w;
+}
 // Columns of the copy: whole pieces of a wave (16 lanes x n columns, and the 8 n of a step over the logits), and 16 bytes so that the 16 rows
 // of a tile begin in different banks.
 template <typename T>
@@ -181,19 +182,20 @@ __device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32
         h[m] = static_cast<const T*>(a.h) + min(first + 16 * m + r, a.rows - 1) * a.ld_h;
         for (int t = 0; t < CT; ++t) z[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int mine = q * 2 * n;
+    const int mine = q * n;
 #pragma unroll 1
     for (int k0 = 0; k0 < a.dim; k0 += S * 8 * n) {
+        const W rows = anew(w);
         u32x4 v[S][NT][2];
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const int c = k0 + s * 8 * n;
             if (c + 8 * n <= a.dim) {
                 for (int m = 0; m < NT; ++m)
-                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_piece(h[m] + c + mine + e * n);
+                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_piece(h[m] + c + mine + e * 4 * n);
             } else if (c < a.dim) {
                 for (int m = 0; m < NT; ++m)
-                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_columns(h[m], c + mine + e * n, a.dim);
+                    for (int e = 0; e < 2; ++e) v[s][m][e] = load_columns(h[m], c + mine + e * 4 * n, a.dim);
             }
         }
 #pragma unroll
@@ -202,7 +204,7 @@ __device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32
             if (c < a.dim)
                 for (int e = 0; e < 2; ++e)
                     for (int t = 0; t < CT; ++t) {
-                        const u32x4 wv = w.piece(16 * t + r, c + mine + e * n);
+                        const u32x4 wv = rows.piece(16 * t + r, c + mine + e * 4 * n);
                         for (int m = 0; m < NT; ++m) z[m][t] = mma(wv, v[s][m][e], z[m][t], T());
                     }
         }
@@ -336,32 +338,40 @@ __device__ inline void store_dh(const Head& a, int64_t first, int base, const f3
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
         if (row >= a.rows) continue;
-        for (int i = 0; i < 4; ++i) {
-            const int to = base + 4 * (4 * q + i);
-            float f[4];
-            for (int t = 0; t < 4; ++t) f[t] = kept[m] ? acc[m][t][i] : 0.f;
-            if (to < a.dim) store_quad(dh + row * ld_dh, to, a.dim, f);
+        // a lane holds 16 consecutive columns
+        constexpr int n = Piece<T>::n;
+        for (int k = 0; k < 16; k += n) {
+            const int to = base + 16 * q + k;
+            float f[n];
+            for (int e = 0; e < n; ++e) f[e] = kept[m] ? acc[m][(k + e) & 3][(k + e) >> 2] : 0.f;
+            if (to < a.dim) store_columns(dh + row * ld_dh, to, a.dim, f);
         }
     }
 }
-template <int CT, int NT, typename W>
-__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f32x4 (&dz)[NT][CT], const bool (&kept)[NT], bf16* dh,
+// dz of a lane's row and classes 16 t + 4 q + i in bfloat16 terms: pairs (i = 0, 1) and (2, 3).
+template <int CT, int TERMS>
+struct DzTerms {
+    uint32_t v[CT][2][TERMS];
+    __device__ inline void make(const f32x4 (&dz)[CT]) {
+        for (int t = 0; t < CT; ++t)
+            for (int k = 0; k < 2; ++k) bf16_terms(dz[t][2 * k], dz[t][2 * k + 1], v[t][k]);
+    }
+    // Operand whose k = 8 q + j stands for class 16 (2 p + j / 4) + 4 q + j % 4.
+    __device__ inline u32x4 operand(int p, int term) const {
+        const bool two = 2 * p + 1 < CT;
+        const int o = two ? 2 * p + 1 : 0;
+        return u32x4{v[2 * p][0][term], v[2 * p][1][term], two ? v[o][0][term] : 0u, two ? v[o][1][term] : 0u};
+    }
+};
+// In bfloat16 dh takes two terms of dz, which leave out 2^-17 of it: far below the rounding of dh itself.
+template <int CT, int NT, int TERMS, typename W>
+__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const DzTerms<CT, TERMS> (&dz)[NT], const bool (&kept)[NT], bf16* dh,
                                int64_t ld_dh) {
     constexpr int P = (CT + 1) / 2;
     const int q = lane_id() >> 4, r = lane_id() & 15;
-    // dz in two bfloat16 terms, which leave out 2^-17 of it: far below the rounding of dh itself
-    u32x4 high[NT][P], low[NT][P];
-    for (int m = 0; m < NT; ++m)
-        for (int p = 0; p < P; ++p)
-            for (int j = 0; j < 8; j += 2) {
-                const int t = 2 * p + (j >> 2), c = t < CT ? t : 0;
-                uint32_t two[2];
-                bf16_terms(t < CT ? dz[m][c][j & 3] : 0.f, t < CT ? dz[m][c][(j & 3) + 1] : 0.f, two);
-                high[m][p][j >> 1] = two[0];
-                low[m][p][j >> 1] = two[1];
-            }
 #pragma unroll 1
     for (int base = 0; base < a.dim; base += 64) {
+        const W rows = anew(w);
         f32x4 acc[NT][4];
         for (int m = 0; m < NT; ++m)
             for (int t = 0; t < 4; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -370,15 +380,15 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f
             for (int j = 0; j < 8; ++j) {
                 const int t = 2 * p + (j >> 2);
                 if (t < CT)
-                    x[j] = w.quad(16 * t + 4 * q + (j & 3), base + 4 * r);
+                    x[j] = rows.quad(16 * t + 4 * q + (j & 3), base + 4 * r);
                 else
                     x[j].zero();
             }
             for (int t = 0; t < 4; ++t) {
                 const u32x4 left = column_of(x, t);
                 for (int m = 0; m < NT; ++m) {
-                    acc[m][t] = mma(left, low[m][p], acc[m][t], bf16());
-                    acc[m][t] = mma(left, high[m][p], acc[m][t], bf16());
+                    acc[m][t] = mma(left, dz[m].operand(p, 1), acc[m][t], bf16());
+                    acc[m][t] = mma(left, dz[m].operand(p, 0), acc[m][t], bf16());
                 }
             }
         }
@@ -390,12 +400,13 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f
     const int q = lane_id() >> 4, r = lane_id() & 15;
 #pragma unroll 1
     for (int base = 0; base < a.dim; base += 64) {
+        const W rows = anew(w);
         f32x4 acc[NT][4];
         for (int m = 0; m < NT; ++m)
             for (int t = 0; t < 4; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int ct = 0; ct < CT; ++ct)
             for (int i = 0; i < 4; ++i) {
-                const Quad<T> x = w.quad(16 * ct + 4 * q + i, base + 4 * r);
+                const Quad<T> x = rows.quad(16 * ct + 4 * q + i, base + 4 * r);
                 for (int t = 0; t < 4; ++t)
                     for (int m = 0; m < NT; ++m) acc[m][t] = mma4(x.get(t), dz[m][ct][i], acc[m][t]);
             }
@@ -477,7 +488,14 @@ __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
             for (int t = 0; t < CT; ++t) *reinterpret_cast<f32x4*>(g.dz + row * (16 * CT) + 16 * t + 4 * q) = z[m][t];
         }
     }
-    if (g.dh) head_dh<CT, NT>(a, w, first, z, kept, static_cast<T*>(g.dh), g.ld_dh);
+    if (!g.dh) return;
+    if constexpr (__is_same(T, bf16)) {
+        DzTerms<CT, 2> terms[NT];
+        for (int m = 0; m < NT; ++m) terms[m].make(z[m]);
+        head_dh<CT, NT>(a, w, first, terms, kept, static_cast<T*>(g.dh), g.ld_dh);
+    } else {
+        head_dh<CT, NT>(a, w, first, z, kept, static_cast<T*>(g.dh), g.ld_dh);
+    }
 }
 
 // ---- dweight = dz^T h, dbias ------------------------------------------------------------------------------------------
@@ -595,7 +613,6 @@ __global__ __launch_bounds__(kBlock) void k_head_outer(Outer o) {
 
 // ---- everything in one pass over h ------------------------------------------------------------------------------------
 
-constexpr int kFusedRows = 128;    // of a tile
 constexpr int kFusedColumns = 64;  // of a group: a wave's part of dweight
 constexpr int kFusedMost = kFusedColumns * 8;
 
@@ -603,22 +620,44 @@ constexpr int kFusedMost = kFusedColumns * 8;
 // each, two on a SIMD (in bfloat16 with 50 classes of 256 columns, 1M rows: 423 us; eight waves 467 us, and 656 us when held to 128 registers.  In
 // float32 with 10 classes of 64 columns, 100,000 rows: 25.7 us with eight waves, 28.2 us with four).
 __host__ __device__ constexpr int fused_waves(int class_tiles) { return class_tiles <= 2 ? 8 : 4; }
+__host__ __device__ constexpr int fused_rows(int class_tiles) { return 16 * fused_waves(class_tiles); }  // of a tile
 
-// dz of a workgroup's 128 rows in shared memory: [row][class], padded so that the four row groups that a wave reads at once (4 j + q, or 8 q + j
-// for bfloat16) lie in different banks.
+// dz of a tile in shared memory: [row][class], padded so that the four rows that a wave reads at once lie in different banks.
 template <typename T, int CT>
 struct SharedDz {
-    static constexpr int ld = 16 * CT + (sizeof(T) == 2 && !__is_same(T, f16) ? 2 : 16), bytes = kFusedRows * ld * 4;
+    static constexpr int ld = 16 * CT + 16, bytes = fused_rows(CT) * ld * 4;
     float* p;
-    __device__ inline void put(int row, int t, int q, const f32x4& z) {
-        float2* to = reinterpret_cast<float2*>(p + row * ld + 16 * t + 4 * q);
-        to[0] = float2{z[0], z[1]};
-        to[1] = float2{z[2], z[3]};
-    }
+    __device__ inline void put(int row, int t, int q, const f32x4& z) { *reinterpret_cast<f32x4*>(p + row * ld + 16 * t + 4 * q) = z; }
     // Sum of a class over 16 rows.
     __device__ inline float rows_of(int c, int from) const {
         float s = 0.f;
         for (int k = 0; k < 16; ++k) s += p[(from + k) * ld + c];
+        return s;
+    }
+};
+// For bfloat16 in three terms, which hold all 24 bits (dweight is a float32 sum over all rows): [term][class][row].
+template <int CT>
+struct SharedDz<bf16, CT> {
+    static constexpr int ld = fused_rows(CT) + 8, bytes = 3 * 16 * CT * ld * 2;
+    float* p;
+    __device__ inline bf16* at(int term, int c, int row) const { return reinterpret_cast<bf16*>(p) + (term * 16 * CT + c) * ld + row; }
+    __device__ inline void put(int row, int q, const DzTerms<CT, 3>& z) {
+        for (int t = 0; t < CT; ++t)
+            for (int k = 0; k < 2; ++k)
+                for (int term = 0; term < 3; ++term) {
+                    const uint32_t v = z.v[t][k][term];
+                    *at(term, 16 * t + 4 * q + 2 * k, row) = __builtin_bit_cast(bf16, (uint16_t)v);
+                    *at(term, 16 * t + 4 * q + 2 * k + 1, row) = __builtin_bit_cast(bf16, (uint16_t)(v >> 16));
+                }
+    }
+    __device__ inline float rows_of(int c, int from) const {
+        float s = 0.f;
+        for (int term = 2; term >= 0; --term)
+            for (int k = 0; k < 16; k += 8) {
+                float f[8];
+                widen(*reinterpret_cast<const u32x4*>(at(term, c, from + k)), f, bf16());
+                for (int e = 0; e < 8; ++e) s += f[e];
+            }
         return s;
     }
 };
@@ -629,9 +668,10 @@ template <typename T>
 struct OuterRows {
     static constexpr bool two = __is_same(T, bf16);
     static constexpr int K = two ? 8 : 4, step = two ? 32 : 16;
-    const char* h;     // of the tile's first row, this lane's columns
+    uint64_t h;        // the tile's first row, the same for all lanes
     uint32_t pitch;    // bytes from one row to the next
-    int last;          // row of the tile that is there
+    uint32_t column;   // bytes of this lane's first column
+    uint32_t last;     // bytes of the last row of the tile that is there
     int room;          // columns from this lane's first one on
     __device__ inline static int row_of(int j) {
         const int q = lane_id() >> 4;
@@ -639,18 +679,17 @@ struct OuterRows {
     }
     __device__ inline void ask(int k0, Quad<T> (&x)[K]) const {
         for (int j = 0; j < K; ++j) {
-            const T* p = reinterpret_cast<const T*>(h + (uint64_t)(uint32_t)min(k0 + row_of(j), last) * pitch);
-            if (room >= 4) __builtin_memcpy(x[j].d, p, sizeof x[j].d);
-            else x[j] = load_quad(p, 0, room);
+            const uint32_t at = min((uint32_t)(k0 + row_of(j)) * pitch, last) + column;
+            if (room >= 4) x[j].load(h, at);
+            else x[j] = load_quad(reinterpret_cast<const T*>(h + at), 0, room);
         }
     }
     // kept: a bit per row of the tile, 32 to a word.
     __device__ inline static void blank(const uint32_t* kept, int k0, Quad<T> (&x)[K]) {
-        const uint32_t word = kept[k0 >> 5];
-        if (__builtin_amdgcn_readfirstlane(word) == ~0u) return;
+        const int word = (int)kept[k0 >> 5] >> (k0 & 31);
         for (int j = 0; j < K; ++j) {
-            const bool ok = word >> ((k0 & 31) + row_of(j)) & 1;
-            for (int e = 0; e < Quad<T>::words; ++e) x[j].d[e] = ok ? x[j].d[e] : 0u;
+            const uint32_t mask = (uint32_t)__builtin_amdgcn_sbfe(word, row_of(j), 1);
+            for (int e = 0; e < Quad<T>::words; ++e) x[j].d[e] &= mask;
         }
     }
 };
@@ -661,18 +700,11 @@ __device__ inline void outer_step(const SharedDz<bf16, CT>& dz, int k0, const Qu
     const int q = lane_id() >> 4, r = lane_id() & 15;
     u32x4 right[4];
     for (int t = 0; t < 4; ++t) right[t] = column_of(x, t);
-    for (int ct = 0; ct < CT; ++ct) {
-        // dz in three bfloat16 terms, which hold all 24 bits of it: dweight is a float32 sum over all rows
-        u32x4 term[3];
-        for (int j = 0; j < 8; j += 2) {
-            const float* v = dz.p + (k0 + 8 * q + j) * SharedDz<bf16, CT>::ld + 16 * ct + r;
-            uint32_t three[3];
-            bf16_terms(v[0], v[SharedDz<bf16, CT>::ld], three);
-            for (int k = 0; k < 3; ++k) term[k][j >> 1] = three[k];
+    for (int ct = 0; ct < CT; ++ct)
+        for (int k = 2; k >= 0; --k) {
+            const u32x4 term = *reinterpret_cast<const u32x4*>(dz.at(k, 16 * ct + r, k0 + 8 * q));
+            for (int t = 0; t < 4; ++t) acc[ct][t] = mma(term, right[t], acc[ct][t], bf16());
         }
-        for (int k = 2; k >= 0; --k)
-            for (int t = 0; t < 4; ++t) acc[ct][t] = mma(term[k], right[t], acc[ct][t], bf16());
-    }
 }
 template <int CT, typename T>
 __device__ inline void outer_step(const SharedDz<T, CT>& dz, int k0, const Quad<T> (&x)[4], f32x4 (&acc)[CT][4]) {
@@ -687,7 +719,7 @@ __device__ inline void outer_step(const SharedDz<T, CT>& dz, int k0, const Quad<
 // How many waves share the rows of a tile for one group of columns of dweight: those that the groups leave, but a wave has whole steps.
 template <typename T>
 __host__ __device__ inline int fused_splits(int groups, int waves) {
-    const int most = kFusedRows / (__is_same(T, bf16) ? 32 : 16);
+    const int most = 16 * waves / (__is_same(T, bf16) ? 32 : 16);
     int splits = waves;
     while (splits > 1 && (splits > most || splits * groups > waves)) splits >>= 1;
     return splits;
@@ -697,7 +729,7 @@ __host__ __device__ inline int fused_splits(int groups, int waves) {
 // over all tiles of 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
 template <typename T, int CT, int GPW>
 __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) void k_head_fused(Head a, Loss g, float* part) {
-    constexpr int kCols = kFusedColumns, kWaves = fused_waves(CT), NT = 8 / kWaves;
+    constexpr int kCols = kFusedColumns, kWaves = fused_waves(CT), NT = 1, kFusedRows = fused_rows(CT);
     extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
@@ -729,17 +761,28 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
                 use[m] = head_dz(g, tile + row, a.rows, target[m], z[m]);
                 const uint16_t bits = (uint16_t)__ballot(use[m]);
                 if (lane_id() == 0) kept16[wave * NT + m] = bits;
-                for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
+                if constexpr (!__is_same(T, bf16))
+                    for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
             }
-            if (g.dh) head_dh<CT, NT>(a, w, tile + mine, z, use, static_cast<T*>(g.dh), g.ld_dh);
+            if constexpr (__is_same(T, bf16)) {
+                DzTerms<CT, 3> terms[NT];
+                for (int m = 0; m < NT; ++m) {
+                    terms[m].make(z[m]);
+                    dz.put(mine + 16 * m + r, q, terms[m]);
+                }
+                if (g.dh) head_dh<CT, NT>(a, w, tile + mine, terms, use, static_cast<T*>(g.dh), g.ld_dh);
+            } else if (g.dh) {
+                head_dh<CT, NT>(a, w, tile + mine, z, use, static_cast<T*>(g.dh), g.ld_dh);
+            }
         }
         const int last = (int)min((int64_t)kFusedRows, a.rows - tile) - 1;
 #pragma unroll
         for (int p = 0; p < GPW; ++p) {
             const int col = (my_group + kWaves * p) * kCols + 4 * r;
             const bool owner = my_group + kWaves * p < groups;
-            const Right right{reinterpret_cast<const char*>(static_cast<const T*>(a.h) + tile * a.ld_h + min(col, a.dim - 1)),
-                              (uint32_t)(a.ld_h * sizeof(T)), last, a.dim - col};
+            const uint32_t pitch = (uint32_t)(a.ld_h * sizeof(T));
+            const Right right{reinterpret_cast<uint64_t>(static_cast<const T*>(a.h) + tile * a.ld_h), pitch,
+                              (uint32_t)min(col, a.dim - 1) * (uint32_t)sizeof(T), (uint32_t)last * pitch, a.dim - col};
             Quad<T> x[Right::K], next[Right::K];
             if (owner) right.ask(from, next);
             if (p == 0) {
@@ -792,7 +835,7 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
 // Bytes of shared memory of k_head_fused.
 template <typename T, int CT>
 inline int64_t fused_bytes(int dim) {
-    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + kFusedRows / 8;
+    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + fused_rows(CT) / 8;
     return shared_bytes<T, CT>(dim) + (joined > dz ? joined : dz);
 }
 

@@ -394,7 +394,7 @@ void by_head(int32_t type, int64_t classes, F f) {
 
 constexpr int64_t kSharedMemory = 160 * 1024;  // of a CU
 constexpr int kMostSharedDim = 1 << 14;        // rows of W that may fit it at all
-constexpr int64_t kMostFusedStride = 1 << 28;  // elements: 32 bits hold the bytes from one row to the next
+constexpr int64_t kMostFusedStride = 1 << 22;  // elements: 32 bits hold the bytes of a tile of 128 rows
 
 // Whether one pass over h does all: dweight's columns have a wave each, and W fits a workgroup's shared memory beside dz.
 bool fits_fused(int dim, int classes, int32_t type) {
@@ -417,7 +417,7 @@ int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type,
     Carve c{base};
     s->fused = fused && fits_fused(dim, classes, type);
     if (s->fused) {
-        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, kFusedRows), 1), 512);
+        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, fused_rows((classes + 15) / 16)), 1), 512);
     } else {
         const int64_t across = ceil_div(dim, 16 * (16 / type_size(type)));
         // workgroups of dweight: twice the CUs over all columns, each wave with 64 rows at least
