@@ -335,16 +335,19 @@ __device__ inline void bf16_terms(float x, float y, uint32_t (&term)[TERMS]) {
 template <int CT, int NT, typename T>
 __device__ inline void store_dh(const Head& a, int64_t first, int base, const f32x4 (&acc)[NT][4], const bool (&kept)[NT], T* dh, int64_t ld_dh) {
     const int q = lane_id() >> 4, r = lane_id() & 15;
+    constexpr int n = Piece<T>::n;
+    const bool whole = first + 16 * NT <= a.rows && base + 64 <= a.dim;  // nothing to look at lane by lane
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
-        if (row >= a.rows) continue;
         // a lane holds 16 consecutive columns
-        constexpr int n = Piece<T>::n;
         for (int k = 0; k < 16; k += n) {
             const int to = base + 16 * q + k;
             float f[n];
             for (int e = 0; e < n; ++e) f[e] = kept[m] ? acc[m][(k + e) & 3][(k + e) >> 2] : 0.f;
-            if (to < a.dim) store_columns(dh + row * ld_dh, to, a.dim, f);
+            if (whole)
+                store_values<n>(dh + row * ld_dh + to, f);
+            else if (row < a.rows && to < a.dim)
+                store_columns(dh + row * ld_dh, to, a.dim, f);
         }
     }
 }
@@ -420,7 +423,8 @@ struct RowTarget {
     f32x4 y[CT];
     float weight;
     bool use;
-    __device__ inline void ask(const Head& a, const Loss& g, int64_t row) {
+    // inner (the same for all lanes): 64 rows follow, so that a whole tile of classes may be read from every row.
+    __device__ inline void ask(const Head& a, const Loss& g, int64_t row, bool inner) {
         const int q = lane_id() >> 4;
         const bool inside = row < a.rows;
         const int64_t at = inside ? row : a.rows - 1;
@@ -432,6 +436,9 @@ struct RowTarget {
             use = use && label >= 0 && label < a.classes;
             for (int t = 0; t < CT; ++t)
                 for (int i = 0; i < 4; ++i) y[t][i] = 16 * t + 4 * q + i == label ? 1.f : 0.f;
+        } else if (inner) {
+            for (int t = 0; t < CT; ++t) y[t] = __builtin_bit_cast(f32x4, load_piece(g.soft + at * a.classes + 16 * t + 4 * q));
+            for (int i = 0; i < 4; ++i) y[CT - 1][i] = 16 * (CT - 1) + 4 * q + i < a.classes ? y[CT - 1][i] : 0.f;
         } else {
             for (int t = 0; t < CT; ++t) {
                 const int c = 16 * t + 4 * q;
@@ -478,7 +485,7 @@ __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
     f32x4 z[NT][CT];
     RowTarget<CT> target[NT];
     bool kept[NT];
-    for (int m = 0; m < NT; ++m) target[m].ask(a, g, first + 16 * m + r);
+    for (int m = 0; m < NT; ++m) target[m].ask(a, g, first + 16 * m + r, first + 16 * NT + 64 <= a.rows);
     head_logits<T, CT, NT>(a, w, first, z);
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
@@ -673,15 +680,17 @@ struct OuterRows {
     uint32_t column;   // bytes of this lane's first column
     uint32_t last;     // bytes of the last row of the tile that is there
     int room;          // columns from this lane's first one on
+    bool whole;        // every lane has four (the same for all lanes)
     __device__ inline static int row_of(int j) {
         const int q = lane_id() >> 4;
         return two ? 8 * q + j : 4 * j + q;
     }
     __device__ inline void ask(int k0, Quad<T> (&x)[K]) const {
-        for (int j = 0; j < K; ++j) {
-            const uint32_t at = min((uint32_t)(k0 + row_of(j)) * pitch, last) + column;
-            if (room >= 4) x[j].load(h, at);
-            else x[j] = load_quad(reinterpret_cast<const T*>(h + at), 0, room);
+        if (whole) {
+            for (int j = 0; j < K; ++j) x[j].load(h, min((uint32_t)(k0 + row_of(j)) * pitch, last) + column);
+        } else {
+            for (int j = 0; j < K; ++j)
+                x[j] = load_quad(reinterpret_cast<const T*>(h + min((uint32_t)(k0 + row_of(j)) * pitch, last) + column), 0, room);
         }
     }
     // kept: a bit per row of the tile, 32 to a word.
@@ -754,7 +763,7 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
             f32x4 z[NT][CT];
             RowTarget<CT> target[NT];
             bool use[NT];
-            for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r);
+            for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r, tile + kFusedRows + 64 <= a.rows);
             head_logits<T, CT, NT>(a, w, tile + mine, z);
             for (int m = 0; m < NT; ++m) {
                 const int row = mine + 16 * m + r;
@@ -782,7 +791,7 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
             const bool owner = my_group + kWaves * p < groups;
             const uint32_t pitch = (uint32_t)(a.ld_h * sizeof(T));
             const Right right{reinterpret_cast<uint64_t>(static_cast<const T*>(a.h) + tile * a.ld_h), pitch,
-                              (uint32_t)min(col, a.dim - 1) * (uint32_t)sizeof(T), (uint32_t)last * pitch, a.dim - col};
+                              (uint32_t)min(col, a.dim - 1) * (uint32_t)sizeof(T), (uint32_t)last * pitch, a.dim - col, (my_group + kWaves * p + 1) * kCols <= a.dim};
             Quad<T> x[Right::K], next[Right::K];
             if (owner) right.ask(from, next);
             if (p == 0) {
