@@ -302,15 +302,15 @@ __device__ inline void zero_empty_items(const TokenList& t, int64_t block, T* ou
 
 // mark[i] = the item of token first + i, for a tile of TILE tokens of which n are there: -1 before the first item, t.items behind the last.  Each
 // item that begins in the tile is noted at its first token, and a running maximum carries it on.  From all threads of the workgroup.
-template <int TILE>
+template <int TILE, int NT>
 __device__ inline void tile_items(const TokenList& t, int64_t first, int n, int32_t* mark, int32_t* range) {
-    constexpr int per = TILE / kBlock;
+    constexpr int per = TILE / NT;
     if (threadIdx.x < 2) range[threadIdx.x] = (int32_t)t.item_from(threadIdx.x ? first + n - 1 : first, -1, t.items);
     __syncthreads();
     const int32_t lo = range[0], hi = range[1];
-    for (int i = threadIdx.x; i < TILE; i += kBlock) mark[i] = lo;
+    for (int i = threadIdx.x; i < TILE; i += NT) mark[i] = lo;
     __syncthreads();
-    for (int64_t b = (int64_t)lo + 1 + threadIdx.x; b <= hi; b += kBlock) {
+    for (int64_t b = (int64_t)lo + 1 + threadIdx.x; b <= hi; b += NT) {
         const int64_t at = t.offsets[b] - first;
         if (at >= 0 && at < n) atomicMax(&mark[at], (int32_t)b);
     }
@@ -334,7 +334,7 @@ __device__ inline void tile_items(const TokenList& t, int64_t first, int n, int3
     for (int k = 0; k < per; ++k) mark[threadIdx.x * per + k] = max(v[k], before);
     __syncthreads();
 }
-constexpr int kTileRange = 2 + kBlock / kWave;  // words of tile_items' `range`
+constexpr int kTileRange = 2 + 1024 / kWave;  // words of tile_items' `range`, of the largest workgroup
 
 // For rows that are narrower than a wave: key[i] = the item of token i (-1: none), src[i] = its id (-1: contributes nothing); the blocks
 // behind those of the tokens zero the rows of items without tokens.
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kBlock) void k_item_keys(TokenList t, int32_t* key,
     __shared__ int32_t mark[kKeyTile], range[kTileRange];
     const int64_t first = (int64_t)blockIdx.x * kKeyTile;
     const int n = (int)min((int64_t)kKeyTile, t.count - first);
-    tile_items<kKeyTile>(t, first, n, mark, range);
+    tile_items<kKeyTile, kBlock>(t, first, n, mark, range);
     for (int i = threadIdx.x; i < n; i += kBlock) {
         key[first + i] = mark[i] < t.items ? mark[i] : -1;
         bool bad;
@@ -651,11 +651,17 @@ __global__ __launch_bounds__(kBlock) void k_zero_absent(const uint8_t* present, 
 }
 
 // ---- stable radix sort of (id, item, weight) by id -------------------------------------------------------------------
+//
+// Digits of up to ten bits: two passes for tables of up to a million rows.  A pass reads and writes the list once (12 bytes an entry with
+// weights); it is bound by that, a copy of as many bytes.
 
-constexpr int kSortTile = 4096;                       // entries per workgroup
-constexpr int kSortItems = kSortTile / kBlock;        // per thread
-constexpr int kDigits = 256;
-constexpr int kClear = kBlock * 16;                   // bytes a workgroup clears
+constexpr int kSortBlock = 512;
+constexpr int kSortTile = 8192;                       // entries per workgroup: eight of each digit on average
+constexpr int kSortItems = kSortTile / kSortBlock;    // per thread
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kDigitBits = 10;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kClear = kSortBlock * 16;               // bytes a workgroup clears
 
 struct SortPass {
     const int32_t* key;  // NULL in the first pass: ids are read from the list
@@ -664,10 +670,11 @@ struct SortPass {
     int32_t* key_out;
     int32_t* src_out;
     float* factor_out;   // NULL without weights
-    uint32_t* hist;      // [digit][tile]
+    uint32_t* hist;      // [tile][digit]
     uint32_t* totals;    // [digit]
     int tiles;
     int shift, bits;
+    __device__ inline uint32_t digit(int32_t k) const { return ((uint32_t)k >> shift) & ((1u << bits) - 1); }
 };
 
 // Ids that contribute nothing sort behind all others.
@@ -678,64 +685,77 @@ __device__ inline int32_t sort_key(const TokenList& t, const SortPass& p, int64_
 }
 
 // The blocks behind those of the tiles (first pass) clear the notes of which ids occur.
-__global__ __launch_bounds__(kBlock) void k_sort_count(TokenList t, SortPass p, uint8_t* present) {
+__global__ __launch_bounds__(kSortBlock) void k_sort_count(TokenList t, SortPass p, uint8_t* present) {
     if ((int)blockIdx.x >= p.tiles) {
         const int64_t at = ((int64_t)blockIdx.x - p.tiles) * kClear + threadIdx.x * 16;
         if (at < t.limit) *reinterpret_cast<u32x4*>(present + at) = u32x4{0u, 0u, 0u, 0u};  // its end is padded to 256 bytes
         return;
     }
     __shared__ uint32_t count[kDigits];
-    count[threadIdx.x] = 0;
+    for (int d = threadIdx.x; d < kDigits; d += kSortBlock) count[d] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kSortTile;
-    const uint32_t mask = (1u << p.bits) - 1;
+    int32_t key[kSortItems];
+#pragma unroll
     for (int k = 0; k < kSortItems; ++k) {
-        const int64_t i = first + k * kBlock + threadIdx.x;
+        const int64_t i = first + k * kSortBlock + threadIdx.x;
+        key[k] = -1;
         if (i < t.count) {
-            if (!p.key) {
+            if (p.key) {
+                key[k] = p.key[i];
+            } else {
                 bool bad;
-                t.id(i, &bad);
+                key[k] = t.id(i, &bad);
                 count_rejected(t.rejected, bad);
+                if (key[k] < 0) key[k] = (int32_t)t.limit;
             }
-            atomicAdd(&count[((uint32_t)sort_key(t, p, i) >> p.shift) & mask], 1u);
         }
     }
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k)
+        if (key[k] >= 0) atomicAdd(&count[p.digit(key[k])], 1u);
     __syncthreads();
-    if (threadIdx.x <= mask) p.hist[(int64_t)threadIdx.x * p.tiles + blockIdx.x] = count[threadIdx.x];
+    for (int d = threadIdx.x; d < 1 << p.bits; d += kSortBlock) p.hist[(int64_t)blockIdx.x * kDigits + d] = count[d];
 }
 
-// One workgroup per digit: where each tile's entries of it begin among all of that digit, and how many there are.
-__global__ __launch_bounds__(kBlock) void k_sort_offsets(SortPass p) {
-    __shared__ uint32_t smem[kBlock / kWave + 1];
-    uint32_t* h = p.hist + (int64_t)blockIdx.x * p.tiles;
+// One workgroup for 32 digits: where each tile's entries of a digit begin among all of that digit, and how many there are.  32 threads share a digit's tiles.
+constexpr int kOffsetDigits = 32, kOffsetParts = 32;
+__global__ __launch_bounds__(kOffsetDigits * kOffsetParts) void k_sort_offsets(SortPass p) {
+    __shared__ uint32_t sums[kOffsetParts][kOffsetDigits + 1];
+    const int d = threadIdx.x % kOffsetDigits, part = threadIdx.x / kOffsetDigits;
+    uint32_t* h = p.hist + blockIdx.x * kOffsetDigits + d;
+    const int per = (p.tiles + kOffsetParts - 1) / kOffsetParts;
+    const int from = min(part * per, p.tiles), to = min(from + per, p.tiles);
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (int t = from; t < to; ++t) sum += h[(int64_t)t * kDigits];
+    sums[part][d] = sum;
+    __syncthreads();
     uint32_t run = 0;
-    for (int at = 0; at < p.tiles; at += kBlock) {
-        const int i = at + (int)threadIdx.x;
-        const uint32_t v = i < p.tiles ? h[i] : 0u;
-        uint32_t total;
-        const uint32_t ex = block_exclusive_scan<uint32_t>(v, smem, &total);
-        if (i < p.tiles) h[i] = run + ex;
-        run += total;
+    for (int k = 0; k < part; ++k) run += sums[k][d];
+    if (part == kOffsetParts - 1) p.totals[blockIdx.x * kOffsetDigits + d] = run + sum;
+#pragma unroll 8
+    for (int t = from; t < to; ++t) {
+        const uint32_t v = h[(int64_t)t * kDigits];
+        h[(int64_t)t * kDigits] = run;
+        run += v;
     }
-    if (threadIdx.x == 0) p.totals[blockIdx.x] = run;
 }
 
 // Each wave ranks its 1,024 consecutive entries 64 at a time among those of the same digit (lanes of one digit are found by a ballot
-// per bit), the ranks are made the tile's, and keys, sources and factors are put in order in shared memory, one after the other in the same 16 KB, and
+// per bit), the ranks are made the tile's, and keys, sources and factors are put in order in shared memory, one after the other in the same 32 KB, and
 // written out as runs.
-__global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p) {
-    constexpr int kWaves = kBlock / kWave;
-    __shared__ uint32_t count[kWaves][kDigits];
+__global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPass p) {
+    __shared__ uint16_t count[kSortWaves][kDigits];
     __shared__ uint32_t to[kDigits];  // place of a digit's entries of this tile in the output, less their place in the tile
-    __shared__ uint32_t smem[kWaves + 1];
+    __shared__ uint32_t smem[kSortWaves + 1];
     __shared__ int32_t range[kTileRange];
     __shared__ int32_t order[kSortTile];
     const int wave = threadIdx.x / kWave, lane = lane_id();
-    const uint32_t mask = (1u << p.bits) - 1;
     const int64_t first = (int64_t)blockIdx.x * kSortTile;
     const int n = (int)min((int64_t)kSortTile, t.count - first);
-    for (int k = 0; k < kWaves; ++k) count[k][threadIdx.x] = 0;
-    const int mine = wave * (kSortTile / kWaves) + lane;  // entry mine + 64 r of the tile
+    for (int k = threadIdx.x; k < kSortWaves * kDigits / 2; k += kSortBlock) reinterpret_cast<uint32_t*>(count)[k] = 0;
+    const int mine = wave * (kSortTile / kSortWaves) + lane;  // entry mine + 64 r of the tile
     int32_t key[kSortItems], src[kSortItems];
     uint32_t rank[kSortItems];
 #pragma unroll
@@ -745,7 +765,7 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p
         if (p.key) src[r] = at < n ? p.src[first + at] : 0;
     }
     if (!p.key) {
-        if (t.offsets) tile_items<kSortTile>(t, first, n, order, range);
+        if (t.offsets) tile_items<kSortTile, kSortBlock>(t, first, n, order, range);
 #pragma unroll
         for (int r = 0; r < kSortItems; ++r) {
             const int at = mine + r * kWave;
@@ -757,46 +777,54 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
         const bool in = mine + r * kWave < n;
-        const uint32_t d = ((uint32_t)key[r] >> p.shift) & mask;
+        const uint32_t d = p.digit(key[r]);
         unsigned long long same = __ballot(in);
         for (int b = 0; b < p.bits; ++b) {
             const unsigned long long one = __ballot(d >> b & 1);
             same &= (d >> b & 1) ? one : ~one;
         }
-        const int leader = in ? __ffsll(same) - 1 : lane;
-        uint32_t base = 0;
-        if (in && lane == leader) base = atomicAdd(&count[wave][d], (uint32_t)__popcll(same));
-        base = __shfl(base, leader, kWave);
+        // every lane of a digit reads its count, then the first writes it back: a wave's accesses to shared memory are in order
+        const uint32_t base = count[wave][d];
         rank[r] = base + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        __builtin_amdgcn_wave_barrier();
+        if (in && lane == __ffsll(same) - 1) count[wave][d] = (uint16_t)(base + (uint32_t)__popcll(same));
+        __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
     {
-        const uint32_t d = threadIdx.x;
-        uint32_t sum = 0;
-        for (int k = 0; k < kWaves; ++k) sum += count[k][d];
+        // two neighbouring digits per thread
+        static_assert(kDigits == 2 * kSortBlock, "two digits per thread");
+        const uint32_t d = 2 * threadIdx.x;
+        uint32_t sum[2] = {0, 0}, all[2];
+        for (int k = 0; k < kSortWaves; ++k)
+            for (int e = 0; e < 2; ++e) sum[e] += count[k][d + e];
+        for (int e = 0; e < 2; ++e) all[e] = d + e < 1u << p.bits ? p.totals[d + e] : 0u;
         uint32_t ignored;
-        uint32_t begin = block_exclusive_scan<uint32_t>(sum, smem, &ignored);
-        const uint32_t all = block_exclusive_scan<uint32_t>(d <= mask ? p.totals[d] : 0u, smem, &ignored);
-        to[d] = all + (d <= mask ? p.hist[(int64_t)d * p.tiles + blockIdx.x] : 0u) - begin;
-        for (int k = 0; k < kWaves; ++k) {
-            const uint32_t v = count[k][d];
-            count[k][d] = begin;
-            begin += v;
+        uint32_t begin = block_exclusive_scan<uint32_t, kSortBlock>(sum[0] + sum[1], smem, &ignored);
+        uint32_t at = block_exclusive_scan<uint32_t, kSortBlock>(all[0] + all[1], smem, &ignored);
+        for (int e = 0; e < 2; ++e) {
+            to[d + e] = at + (d + e < 1u << p.bits ? p.hist[(int64_t)blockIdx.x * kDigits + d + e] : 0u) - begin;
+            for (int k = 0; k < kSortWaves; ++k) {
+                const uint32_t v = count[k][d + e];
+                count[k][d + e] = (uint16_t)begin;
+                begin += v;
+            }
+            at += all[e];
         }
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        rank[r] += count[wave][((uint32_t)key[r] >> p.shift) & mask];
+        rank[r] += count[wave][p.digit(key[r])];
         if (mine + r * kWave < n) order[rank[r]] = key[r];
     }
     __syncthreads();
     uint32_t place[kSortItems];
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int at = (int)threadIdx.x + r * kBlock;
+        const int at = (int)threadIdx.x + r * kSortBlock;
         const int32_t k = at < n ? order[at] : 0;
-        place[r] = to[((uint32_t)k >> p.shift) & mask] + (uint32_t)at;
+        place[r] = to[p.digit(k)] + (uint32_t)at;
         if (at < n) p.key_out[place[r]] = k;
     }
     __syncthreads();
@@ -806,7 +834,7 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int at = (int)threadIdx.x + r * kBlock;
+        const int at = (int)threadIdx.x + r * kSortBlock;
         if (at < n) p.src_out[place[r]] = order[at];
     }
     if (!p.factor_out) return;
@@ -818,7 +846,7 @@ __global__ __launch_bounds__(kBlock) void k_sort_scatter(TokenList t, SortPass p
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int at = (int)threadIdx.x + r * kBlock;
+        const int at = (int)threadIdx.x + r * kSortBlock;
         if (at < n) p.factor_out[place[r]] = __int_as_float(order[at]);
     }
 }

@@ -315,7 +315,7 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
             sum_space(static_cast<char*>(call->workspace), count, dim, wide, out->rows, &s);
             int bits = 1;
             while (bits < 31 && (out->rows >> bits) != 0) ++bits;
-            const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes;
+            const int passes = (bits + kDigitBits - 1) / kDigitBits, per = (bits + passes - 1) / passes;
             SortPass p{};
             for (int k = 0; k < passes; ++k) {
                 const bool even = (k & 1) == 0;
@@ -330,9 +330,9 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
                 p.tiles = (int)s.tiles;
                 p.shift = k * per;
                 p.bits = std::min(per, bits - k * per);
-                k_sort_count<<<(unsigned)(s.tiles + (k == 0 ? ceil_div(out->rows, kClear) : 0)), kBlock, 0, stream>>>(t, p, s.present);
-                k_sort_offsets<<<1u << p.bits, kBlock, 0, stream>>>(p);
-                k_sort_scatter<<<(unsigned)s.tiles, kBlock, 0, stream>>>(t, p);
+                k_sort_count<<<(unsigned)(s.tiles + (k == 0 ? ceil_div(out->rows, kClear) : 0)), kSortBlock, 0, stream>>>(t, p, s.present);
+                k_sort_offsets<<<(unsigned)ceil_div(1 << p.bits, kOffsetDigits), kOffsetDigits * kOffsetParts, 0, stream>>>(p);
+                k_sort_scatter<<<(unsigned)s.tiles, kSortBlock, 0, stream>>>(t, p);
             }
             const SumList list{p.key_out, p.src_out, p.factor_out, s.part, s.flags, s.open, s.present, count, t.items, out->rows, s.piece, t.scale};
             if (wide)
