@@ -74,6 +74,19 @@ struct TokenList {
         }
         return lo;
     }
+    // The same over all items by a whole wave, 64 offsets at a time: as many reads one after the other as 64 has to be multiplied by itself.
+    __device__ inline int64_t item_by_wave(int64_t i) const {
+        int64_t lo = -1, hi = items;  // the answer is in [lo, hi]
+        while (lo < hi) {
+            const int64_t step = (hi - lo + kWave - 1) / kWave;
+            const int64_t at = lo + step * (lane_id() + 1);
+            const unsigned long long m = __ballot(at <= hi && offsets[min(at, hi)] <= i);
+            const int n = (int)__popcll(m);  // offsets do not decrease: these are the first n lanes
+            hi = min(lo + step * (n + 1) - 1, hi);
+            lo = lo + step * n;
+        }
+        return lo;
+    }
     // The item of token i, -1 if it is in none.
     __device__ inline int32_t item(int64_t i) const {
         if (!offsets) return (int32_t)i;
@@ -483,7 +496,7 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
     int32_t cur;
     bool before;
     if (ITEMS) {
-        item = t.item_from(first, -1, t.items);
+        item = t.item_by_wave(first);
         next = item < t.items ? t.offsets[item + 1] : INT64_MAX;
         cur = item >= 0 && item < t.items ? (int32_t)item : -1;
         before = cur >= 0 && t.offsets[item] < first;
@@ -506,7 +519,8 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
         before = false;
         for (int k = 0; k < E; ++k) acc[k] = 0.f;
     };
-    constexpr int U = 8;
+    constexpr int U = Columns<T, E>::words <= 2 ? 16 : 8;
+    constexpr unsigned kAll = (1u << U) - 1;
     for (int64_t base = first; base < end; base += kWave) {
         const int64_t at = base + lane;
         const int n = (int)min((int64_t)kWave, end - base);
@@ -540,7 +554,7 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
             auto ask = [&](int u) {
                 x[u].load((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, u) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, u), off);
             };
-            if ((real >> j & 255) == 255) {
+            if ((real >> j & kAll) == kAll) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) ask(u);
             } else {
@@ -554,12 +568,12 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) f[u] = __uint_as_float(__builtin_amdgcn_readlane(factor, u));
-            // the next eight entries to the first lanes
+            // the next U entries to the first lanes
             low = __shfl_down(low, U, kWave);
             high = __shfl_down(high, U, kWave);
             factor = __shfl_down(factor, U, kWave);
             const int64_t pos = base + j;
-            if (ITEMS ? next >= end || next >= pos + U : (ends >> j & 255) == 0) {
+            if (ITEMS ? next >= end || next >= pos + U : (ends >> j & kAll) == 0) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     for (int e = 0; e < E; ++e) acc[e] += f[u] * x[u].get(e);
