@@ -19,5 +19,6 @@ def __getattr__(name):
     if name in _TRAIN:
         from . import train
 
-        return getattr(train, name)
+        globals().update((n, getattr(train, n)) for n in _TRAIN)
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -93,17 +93,17 @@ def _matrix(t, name, device):
     if t.device != device:
         _refuse(f"{name} is on {t.device}, not on {device}")
     rows, dim = t.shape
-    stride = t.stride(0) if rows > 1 else max(dim, 1)
-    if dim > 1 and t.stride(1) != 1:
+    stride, step = t.stride()
+    if dim > 1 and step != 1:
         _refuse(f"{name}: the elements of a row have to be contiguous")
-    return _Matrix(t.data_ptr(), rows, stride, dim, _TYPES[t.dtype])
+    return _Matrix(t.data_ptr(), rows, stride if rows > 1 else max(dim, 1), dim, _TYPES[t.dtype])
 
 
 def _vector(t, name, dtype, count, device):
     """Address of a contiguous tensor of `count` elements (None: 0)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
         _refuse(f"{name}: a contiguous tensor of {count} elements of {dtype} is wanted")
     if t.device != device:
         _refuse(f"{name} is on {t.device}, not on {device}")
@@ -116,26 +116,24 @@ def _device(t, name):
     return t.device
 
 
-class _On:
-    """Makes a tensor's GPU the current one for the call, where it is not."""
+# The handle of the current stream without making a Stream object of it (1.8 us less per call), where torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __init__(self, device):
-        self.device, self.before = device, torch.cuda.current_device()
 
-    def __enter__(self):
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-
-    def __exit__(self, *exc):
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.before)
+def _run(device, function, *args):
+    """function(*args) with the tensors' GPU as the current one."""
+    if torch.cuda.current_device() == device.index:
+        return function(*args)
+    with torch.cuda.device(device):
+        return function(*args)
 
 
 def _call(device, nbytes=0):
     """(dynlp_call on the current stream, what has to live until the call has been made)."""
-    space = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    stream = torch.cuda.current_stream(device).cuda_stream
-    return _Call(stream, space.data_ptr() if nbytes else None, nbytes), space
+    if not nbytes:
+        return _Call(_raw_stream(device.index), None, 0), None
+    space = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _Call(_raw_stream(device.index), space.data_ptr(), nbytes), space
 
 
 def _tokens(ids, offsets, weights, scale, rejected, device):
@@ -161,11 +159,10 @@ def embed(table, ids, offsets=None, weights=None, scale=1.0, *, rejected=None):
     L = _library()
     t = _tokens(ids, offsets, weights, scale, rejected, device)
     m = _matrix(table, "table", device)
-    with _On(device):
-        out = torch.empty(t.items, m.dim, dtype=table.dtype, device=device)
-        call, space = _call(device, L.dynlp_embed_workspace(t.count, t.items, m.dim) if offsets is not None else 0)
-        to = _Matrix(out.data_ptr(), t.items, max(m.dim, 1), m.dim, m.type)
-        _check(L.dynlp_embed(m, t, to, call))
+    out = table.new_empty((t.items, m.dim))
+    call, space = _call(device, L.dynlp_embed_workspace(t.count, t.items, m.dim) if offsets is not None else 0)
+    to = _Matrix(out.data_ptr(), t.items, max(m.dim, 1), m.dim, m.type)
+    _check(_run(device, L.dynlp_embed, m, t, to, call))
     return out
 
 
@@ -180,11 +177,10 @@ def embed_grad(grad, ids, num_rows, offsets=None, weights=None, scale=1.0, *, dt
         _refuse("dtype: float32, bfloat16 or float16 is wanted")
     if num_rows < 0:
         _refuse(f"{num_rows} rows")
-    with _On(device):
-        out = torch.empty(num_rows, m.dim, dtype=dtype, device=device)
-        call, space = _call(device, L.dynlp_embed_grad_workspace(t.count, t.items, m.dim, num_rows))
-        to = _Matrix(out.data_ptr(), num_rows, max(m.dim, 1), m.dim, _TYPES[dtype])
-        _check(L.dynlp_embed_grad(m, t, to, call))
+    out = grad.new_empty((num_rows, m.dim), dtype=dtype)
+    call, space = _call(device, L.dynlp_embed_grad_workspace(t.count, t.items, m.dim, num_rows))
+    to = _Matrix(out.data_ptr(), num_rows, max(m.dim, 1), m.dim, _TYPES[dtype])
+    _check(_run(device, L.dynlp_embed_grad, m, t, to, call))
     return out
 
 
@@ -195,11 +191,10 @@ def head_labels(h, weight, bias=None, soft=True, hard=True):
     L = _library()
     m, w = _matrix(h, "h", device), _matrix(weight, "weight", device)
     b = _vector(bias, "bias", torch.float32, w.rows, device)
-    with _On(device):
-        so = torch.empty(m.rows, w.rows, dtype=torch.float32, device=device) if soft else None
-        ho = torch.empty(m.rows, dtype=torch.int32, device=device) if hard else None
-        call, _ = _call(device)
-        _check(L.dynlp_head_labels(m, w, b, so.data_ptr() if soft else None, ho.data_ptr() if hard else None, call))
+    so = h.new_empty((m.rows, w.rows), dtype=torch.float32) if soft else None
+    ho = h.new_empty(m.rows, dtype=torch.int32) if hard else None
+    call, _ = _call(device)
+    _check(_run(device, L.dynlp_head_labels, m, w, b, so.data_ptr() if soft else None, ho.data_ptr() if hard else None, call))
     return so, ho
 
 
@@ -217,18 +212,17 @@ def head_loss(h, weight, bias, target, *, row_weight=None, grad_scale=1.0, grads
     y = _vector(target, "target", torch.float32 if soft else torch.int32, m.rows * w.rows if soft else m.rows, device)
     t = _Targets(y if soft else None, None if soft else y, _vector(row_weight, "row_weight", torch.float32, m.rows, device),
                  _vector(rejected, "rejected", torch.int32, 1, device), float(grad_scale))
-    with _On(device):
-        loss = torch.empty(m.rows, dtype=torch.float32, device=device)
-        if not grads:
-            call, _ = _call(device)
-            _check(L.dynlp_head_loss(m, w, b, t, loss.data_ptr(), None, None, None, call))
-            return loss, None, None, None
-        dh = torch.empty(m.rows, m.dim, dtype=h.dtype, device=device)
-        dweight = torch.empty(w.rows, m.dim, dtype=torch.float32, device=device)
-        dbias = torch.empty(w.rows, dtype=torch.float32, device=device)
-        call, space = _call(device, L.dynlp_head_loss_workspace(m.rows, m.dim, w.rows, m.type))
-        to = _Matrix(dh.data_ptr(), m.rows, max(m.dim, 1), m.dim, m.type)
-        _check(L.dynlp_head_loss(m, w, b, t, loss.data_ptr(), to, dweight.data_ptr(), dbias.data_ptr(), call))
+    loss = h.new_empty(m.rows, dtype=torch.float32)
+    if not grads:
+        call, _ = _call(device)
+        _check(_run(device, L.dynlp_head_loss, m, w, b, t, loss.data_ptr(), None, None, None, call))
+        return loss, None, None, None
+    dh = h.new_empty((m.rows, m.dim))
+    dweight = h.new_empty((w.rows, m.dim), dtype=torch.float32)
+    dbias = h.new_empty(w.rows, dtype=torch.float32)
+    call, space = _call(device, L.dynlp_head_loss_workspace(m.rows, m.dim, w.rows, m.type))
+    to = _Matrix(dh.data_ptr(), m.rows, max(m.dim, 1), m.dim, m.type)
+    _check(_run(device, L.dynlp_head_loss, m, w, b, t, loss.data_ptr(), to, dweight.data_ptr(), dbias.data_ptr(), call))
     return loss, dh, dweight, dbias
 
 
@@ -287,6 +281,5 @@ def adamw_step(params, grads, states, *, step, lr, betas=(0.9, 0.999), eps=1e-8,
     o = _AdamwOptions(lr, betas[0], betas[1], eps, step, _vector(grad_scale, "grad_scale", torch.float32, 1, device),
                       seed & 0xFFFFFFFF, 8 if bits8 else 32)
     L = _library()
-    with _On(device):
-        call, _ = _call(device)
-        _check(L.dynlp_adamw_step(count, table.ctypes.data, o, call))
+    call, _ = _call(device)
+    _check(_run(device, L.dynlp_adamw_step, count, table.ctypes.data, o, call))
