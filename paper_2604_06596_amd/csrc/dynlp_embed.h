@@ -58,6 +58,17 @@ struct TokenList {
         bool ignored;
         return id(i, &ignored);
     }
+    // The ids of tokens i, i + 64, ... below `end`, all asked for at once; -1 for what id() says so of, and beyond the end.
+    template <int N>
+    __device__ inline void ids_from(int64_t i, int64_t end, int32_t (&to)[N]) const {
+        int64_t v[N];
+        if (wide) {
+            for (int u = 0; u < N; ++u) v[u] = i + u * kWave < end ? static_cast<const int64_t*>(ids)[i + u * kWave] : -1;
+        } else {
+            for (int u = 0; u < N; ++u) v[u] = i + u * kWave < end ? static_cast<const int32_t*>(ids)[i + u * kWave] : -1;
+        }
+        for (int u = 0; u < N; ++u) to[u] = v[u] < 0 || v[u] >= limit ? -1 : (int32_t)v[u];
+    }
     // Bounds of item b within the list.
     __device__ inline void bounds(int64_t b, int64_t* begin, int64_t* end) const {
         *begin = min(max(offsets[b], (int64_t)0), count);
@@ -196,20 +207,21 @@ __global__ __launch_bounds__(kBlock) void k_embed_items(TokenList t, const T* ta
 constexpr int kFewTokens = 8192;     // 32 for each thread of a workgroup
 constexpr int kZeroRows = 8192;      // rows whose presence one workgroup notes at most
 
-// The gradient for few tokens, without a sort: workgroup i looks through all ids, each wave through a quarter of them.  If token i is the first
-// with its id, every wave adds up the rows of those it found, four at a time, and the waves' sums are joined in order.  The workgroups behind those zero the rows of
+// The gradient for few tokens, without a sort: a workgroup per token looks through all ids, each wave through a quarter of them.  If token i is the first
+// with its id, every wave adds up the rows of those it found, four at a time, and the waves' sums are joined in order.  The workgroups before those zero the rows of
 // ids that do not occur.  One launch instead of the sort's ten; the ids are read count^2 times, from the L2.
 template <typename T, typename O, int V>
-__global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T* grad, int64_t ld, O* out, int64_t out_ld, int dim, int zero_rows) {
-    constexpr int kWaves = kBlock / kWave;
+__global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T* grad, int64_t ld, O* out, int64_t out_ld, int dim, int zero_rows,
+                                                           int zero_blocks) {
+    constexpr int kWaves = kBlock / kWave, kAhead = 8;
     __shared__ float part[kWaves][kWave * V];
     __shared__ uint16_t list[kWaves][kFewTokens / kWaves];
     __shared__ int found[kWaves];
     __shared__ uint32_t present[kZeroRows / 32];
     const int n = (int)t.count, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
     const int pieces = (dim + V - 1) / V;
-    if ((int64_t)blockIdx.x < t.count) {
-        const int me = (int)blockIdx.x;
+    if ((int)blockIdx.x >= zero_blocks) {
+        const int me = (int)blockIdx.x - zero_blocks;
         bool bad;
         const int32_t id = t.id(me, &bad);
         if (bad && threadIdx.x == 0 && t.rejected) atomicAdd(t.rejected, 1);
@@ -217,13 +229,19 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T*
         const int from = (int)((int64_t)n * wave / kWaves), to = (int)((int64_t)n * (wave + 1) / kWaves);
         bool earlier = false;
         int mine = 0;
-        for (int i0 = from; i0 < to; i0 += kWave) {
-            const int i = i0 + lane;
-            const bool hit = i < to && t.id(i) == id;
-            earlier |= hit && i < me;
-            const unsigned long long m = __ballot(hit);
-            if (hit) list[wave][mine + (int)__popcll(m & ((1ull << lane) - 1))] = (uint16_t)i;
-            mine += (int)__popcll(m);
+        for (int i0 = from; i0 < to; i0 += kAhead * kWave) {
+            int32_t ids[kAhead];
+            t.ids_from<kAhead>(i0 + lane, to, ids);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = i0 + u * kWave + lane;
+                const bool hit = ids[u] == id;
+                const unsigned long long m = __ballot(hit);
+                if (!m) continue;
+                earlier |= hit && i < me;
+                if (hit) list[wave][mine + (int)__popcll(m & ((1ull << lane) - 1))] = (uint16_t)i;
+                mine += (int)__popcll(m);
+            }
         }
         if (lane == 0) found[wave] = mine;
         if (__syncthreads_or(earlier)) return;
@@ -271,13 +289,18 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T*
         }
         return;
     }
-    const int64_t first = ((int64_t)blockIdx.x - t.count) * zero_rows;
+    const int64_t first = (int64_t)blockIdx.x * zero_rows;
     const int rows = (int)min((int64_t)zero_rows, t.limit - first);
     for (int k = threadIdx.x; k < (zero_rows + 31) / 32; k += kBlock) present[k] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kBlock) {
-        const int64_t r = (int64_t)t.id(i) - first;
-        if (r >= 0 && r < rows) atomicOr(&present[r >> 5], 1u << (r & 31));
+    for (int i0 = wave * kAhead * kWave; i0 < n; i0 += kWaves * kAhead * kWave) {
+        int32_t ids[kAhead];
+        t.ids_from<kAhead>(i0 + lane, n, ids);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t r = (int64_t)ids[u] - first;
+            if (r >= 0 && r < rows) atomicOr(&present[r >> 5], 1u << (r & 31));
+        }
     }
     __syncthreads();
     float zero[V] = {};

@@ -307,8 +307,9 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
         } else if (count <= kFewTokens) {
             // zero rows: workgroups enough for the chip, 64 rows at least for the look through the ids
             const int zero_rows = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(out->rows, 1024), 64), kZeroRows);
-            k_embed_grad_few<T, O, V><<<(unsigned)(count + ceil_div(out->rows, zero_rows)), kBlock, 0, stream>>>(
-                t, rows, grad->stride, to, out->stride, dim, zero_rows);
+            const int zero_blocks = (int)ceil_div(out->rows, zero_rows);
+            k_embed_grad_few<T, O, V><<<(unsigned)(zero_blocks + count), kBlock, 0, stream>>>(t, rows, grad->stride, to, out->stride, dim, zero_rows,
+                                                                                             zero_blocks);
         } else {
             SumSpace s{};
             const bool wide = wide_rows(grad->type, dim);
