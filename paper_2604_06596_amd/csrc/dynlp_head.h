@@ -171,11 +171,11 @@ __host__ __device__ inline int shared_bytes(int dim) {
     return 16 * CT * (shared_ld<T>(dim) * (int)sizeof(T) + 4);
 }
 
-// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.  Two steps' parts of h are asked for
+// z[m][t] = logits of rows first + 16 m + r, classes 16 t + 4 q + i, bias added; -infinity beyond the classes.  S steps' parts of h are asked for
 // before the first's products.
-template <typename T, int CT, int NT, typename W>
+template <typename T, int CT, int NT, int S, typename W>
 __device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32x4 (&z)[NT][CT]) {
-    constexpr int n = Piece<T>::n, S = 2;
+    constexpr int n = Piece<T>::n;
     const int q = lane_id() >> 4, r = lane_id() & 15;
     const T* h[NT];
     for (int m = 0; m < NT; ++m) {
@@ -253,18 +253,20 @@ __device__ inline float head_exp(f32x4 (&z)[CT], float* top) {
     return row_sum(sum);
 }
 
-constexpr int kHeadTiles = 2;                       // tiles of 16 rows per wave
+constexpr int kLabelRows = 16 * (kBlock / kWave);   // rows of a workgroup's tile for labels
+constexpr int kHeadTiles = 2;                       // tiles of 16 rows per wave where loss and gradients are not made in one pass
 constexpr int kHeadRows = kHeadTiles * 16 * (kBlock / kWave);  // rows per workgroup
 
-// One tile of rows per wave from W as it is, or (SHARED) any number of them from a copy of W in shared memory.
+// One tile of 16 rows per wave from W as it is, or (SHARED) any number of them from a copy of W in shared memory.  Bound by reading h, with enough of it
+// under way: 300,007 x 200 float16, 29 classes: 37 us (4.2 TB/s), where tiles of 32 rows and half as many steps ahead took 53 us.
 template <typename T, int CT, bool SHARED>
 __global__ __launch_bounds__(kBlock) void k_head_labels(Head a, float* soft, int32_t* hard) {
-    constexpr int NT = kHeadTiles;
+    constexpr int NT = 1;
     extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15;
     auto tile = [&](const auto& w, int64_t first) {
         f32x4 z[NT][CT];
-        head_logits<T, CT, NT>(a, w, first, z);
+        head_logits<T, CT, NT, 4>(a, w, first, z);
         for (int m = 0; m < NT; ++m) {
             const int64_t row = first + 16 * m + r;
             if (hard) {
@@ -295,10 +297,10 @@ __global__ __launch_bounds__(kBlock) void k_head_labels(Head a, float* soft, int
     const int64_t first = (threadIdx.x / kWave) * (NT * 16);
     if constexpr (SHARED) {
         const SharedWeight<T> w = share_weight<T, CT>(a, reinterpret_cast<T*>(space));
-        for (int64_t at = (int64_t)blockIdx.x * kHeadRows; at + first < a.rows; at += (int64_t)gridDim.x * kHeadRows) tile(w, at + first);
+        for (int64_t at = (int64_t)blockIdx.x * kLabelRows; at + first < a.rows; at += (int64_t)gridDim.x * kLabelRows) tile(w, at + first);
     } else {
         const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
-        if ((int64_t)blockIdx.x * kHeadRows + first < a.rows) tile(w, (int64_t)blockIdx.x * kHeadRows + first);
+        if ((int64_t)blockIdx.x * kLabelRows + first < a.rows) tile(w, (int64_t)blockIdx.x * kLabelRows + first);
     }
 }
 
@@ -486,7 +488,7 @@ __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
     RowTarget<CT> target[NT];
     bool kept[NT];
     for (int m = 0; m < NT; ++m) target[m].ask(a, g, first + 16 * m + r, first + 16 * NT + 64 <= a.rows);
-    head_logits<T, CT, NT>(a, w, first, z);
+    head_logits<T, CT, NT, 2>(a, w, first, z);
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
         kept[m] = head_dz(g, row, a.rows, target[m], z[m]);
@@ -764,7 +766,7 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
             RowTarget<CT> target[NT];
             bool use[NT];
             for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r, tile + kFusedRows + 64 <= a.rows);
-            head_logits<T, CT, NT>(a, w, tile + mine, z);
+            head_logits<T, CT, NT, 2>(a, w, tile + mine, z);
             for (int m = 0; m < NT; ++m) {
                 const int row = mine + 16 * m + r;
                 use[m] = head_dz(g, tile + row, a.rows, target[m], z[m]);

@@ -453,9 +453,9 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
     by_head(h->type, weight->rows, [&](auto type, auto tiles) {
         using T = decltype(type);
         constexpr int CT = decltype(tiles)::v;
-        const int64_t bytes = a.dim <= kMostSharedDim ? shared_bytes<T, CT>(a.dim) : kSharedMemory + 1, blocks = ceil_div(a.rows, kHeadRows);
+        const int64_t bytes = a.dim <= kMostSharedDim ? shared_bytes<T, CT>(a.dim) : kSharedMemory + 1, blocks = ceil_div(a.rows, kLabelRows);
         // a copy of W pays once a workgroup has several tiles of rows
-        const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 8);
+        const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 4);
         if (bytes <= kSharedMemory && blocks >= 2 * stay) {
             static std::atomic<bool> allowed{false};
             allow_shared(k_head_labels<T, CT, true>, allowed);
