@@ -820,34 +820,37 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
         for (int k = threadIdx.x; k < kWave * kWaves / (16 * CT) * (16 * CT); k += 16 * CT) v += bias[k];
         part[(int64_t)threadIdx.x * (a.dim + 1) + a.dim] = v;
     }
-    // dweight: a group of columns after the other, its waves' parts added in order
-    float* joined = reinterpret_cast<float*>(behind);
-    for (int k = 0; k < groups; ++k) {
+    // dweight: the parts of waves that shared a group's rows, halves of them at a time; in place of everything else in shared memory
+    f32x4* slots = reinterpret_cast<f32x4*>(space);
+    for (int half = splits >> 1; half > 0; half >>= 1) {
         __syncthreads();
-        for (int turn = 0; turn < splits; ++turn) {
+        if (my_group < groups && my_split >= half && my_split < 2 * half)
+            for (int ct = 0; ct < CT; ++ct)
+                for (int t = 0; t < 4; ++t) slots[((my_group * half + my_split - half) * CT * 4 + ct * 4 + t) * kWave + lane_id()] = acc[0][ct][t];
+        __syncthreads();
+        if (my_group < groups && my_split < half)
+            for (int ct = 0; ct < CT; ++ct)
+                for (int t = 0; t < 4; ++t) acc[0][ct][t] += slots[((my_group * half + my_split) * CT * 4 + ct * 4 + t) * kWave + lane_id()];
+    }
+    if (my_split != 0) return;
 #pragma unroll
-            for (int p = 0; p < GPW; ++p)
-                if (my_group + kWaves * p == k && my_split == turn)
-                    for (int ct = 0; ct < CT; ++ct)
-                        for (int t = 0; t < 4; ++t)
-                            for (int i = 0; i < 4; ++i) {
-                                float& to_sum = joined[(16 * ct + 4 * q + i) * (kCols + 1) + 4 * r + t];
-                                to_sum = turn ? to_sum + acc[p][ct][t][i] : acc[p][ct][t][i];
-                            }
-            __syncthreads();
-        }
-        for (int at = threadIdx.x; at < a.classes * kCols; at += kWave * kWaves) {
-            const int c = at / kCols, x = at % kCols;
-            if (k * kCols + x < a.dim) part[(int64_t)c * (a.dim + 1) + k * kCols + x] = joined[c * (kCols + 1) + x];
-        }
+    for (int p = 0; p < GPW; ++p) {
+        const int col = (my_group + kWaves * p) * kCols + 4 * r;
+        for (int ct = 0; ct < CT; ++ct)
+            for (int i = 0; i < 4; ++i) {
+                const int c = 16 * ct + 4 * q + i;
+                const float f[4] = {acc[p][ct][0][i], acc[p][ct][1][i], acc[p][ct][2][i], acc[p][ct][3][i]};
+                if (c < a.classes && col < a.dim) store_columns(part + (int64_t)c * (a.dim + 1), col, a.dim, f);
+            }
     }
 }
 
 // Bytes of shared memory of k_head_fused.
 template <typename T, int CT>
 inline int64_t fused_bytes(int dim) {
-    const int64_t joined = 16 * CT * (kFusedColumns + 1) * 4, dz = SharedDz<T, CT>::bytes + fused_rows(CT) / 8;
-    return shared_bytes<T, CT>(dim) + (joined > dz ? joined : dz);
+    // in the end, the parts of half the waves: with one group of columns, all of them share its rows
+    const int64_t slots = (fused_waves(CT) / 2) * 16 * CT * kFusedColumns * 4, all = shared_bytes<T, CT>(dim) + SharedDz<T, CT>::bytes + fused_rows(CT) / 8;
+    return all > slots ? all : slots;
 }
 
 // Sums the parts: 16 neighbouring elements per workgroup, 16 groups of lanes taking turns on the parts, then joined in order.

@@ -418,7 +418,9 @@ int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type,
     Carve c{base};
     s->fused = fused && fits_fused(dim, classes, type);
     if (s->fused) {
-        s->splits = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(rows, fused_rows((classes + 15) / 16)), 1), 512);
+        // at most two workgroups for each CU, all with as many tiles but for the last
+        const int64_t tiles = std::max<int64_t>(ceil_div(rows, fused_rows((classes + 15) / 16)), 1);
+        s->splits = (int)ceil_div(tiles, ceil_div(tiles, 512));
     } else {
         const int64_t across = ceil_div(dim, 16 * (16 / type_size(type)));
         // workgroups of dweight: twice the CUs over all columns, each wave with 64 rows at least
