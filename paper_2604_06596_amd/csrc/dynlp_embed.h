@@ -113,27 +113,43 @@ __device__ inline void count_rejected(int32_t* rejected, bool bad) {
 
 // ---- one row per token -----------------------------------------------------------------------------------------------
 
-// out[i] = scale * weight * table[id]: a copy with a factor.  One 16-byte piece per thread; `pieces` of them make a row.
+// out[i] = scale * weight * table[id]: a copy with a factor.  Four 16-byte pieces per thread, asked for at once; `pieces` of them make a row.
+constexpr int kRowsAhead = 4;
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void k_embed_rows(TokenList t, const T* table, int64_t ld, T* out, int64_t out_ld, int dim,
                                                        int pieces) {
-    const int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    const int64_t i = at / pieces;
-    if (i >= t.count) return;
-    const int c = (int)(at - i * pieces);
-    const int col = piece_column<V>(c, dim);
-    bool bad;
-    const int32_t id = t.id(i, &bad);
-    if (bad && c == 0 && t.rejected) atomicAdd(t.rejected, 1);
-    float f[V] = {};
-    if (id >= 0) {
-        Lane<T, V> x;
-        x.load(table + (int64_t)id * ld + col);
-        x.get(f);
-        const float s = t.weights ? t.scale * t.weights[i] : t.scale;
-        for (int k = 0; k < V; ++k) f[k] *= s;
+    const int64_t first = (int64_t)blockIdx.x * (kBlock * kRowsAhead);
+    const int64_t row0 = first / pieces;             // the same for all threads
+    const uint32_t rest = (uint32_t)(first - row0 * pieces);
+    Lane<T, V> x[kRowsAhead];
+    float s[kRowsAhead];
+    int64_t row[kRowsAhead];
+    int col[kRowsAhead];
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) {
+        const uint32_t at = rest + (uint32_t)(k * kBlock) + threadIdx.x, r = at / (uint32_t)pieces, c = at - r * (uint32_t)pieces;
+        row[k] = row0 + r;
+        col[k] = piece_column<V>((int)c, dim);
+        s[k] = 0.f;
+        if (row[k] < t.count) {
+            bool bad;
+            const int32_t id = t.id(row[k], &bad);
+            if (bad && c == 0 && t.rejected) atomicAdd(t.rejected, 1);
+            if (id >= 0) {
+                s[k] = t.weights ? t.scale * t.weights[row[k]] : t.scale;
+                x[k].load(table + (int64_t)id * ld + col[k]);
+            }
+            x[k].keep(id >= 0);
+        }
     }
-    store_values<V>(out + i * out_ld + col, f);
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k)
+        if (row[k] < t.count) {
+            float f[V];
+            x[k].get(f);
+            for (int e = 0; e < V; ++e) f[e] *= s[k];
+            store_values<V>(out + row[k] * out_ld + col[k], f);
+        }
 }
 
 // ---- few tokens: one workgroup per item, or per distinct id ----------------------------------------------------------

@@ -257,7 +257,7 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
         T* to = static_cast<T*>(out->data);
         const int64_t n = ceil_div(dim, V);
         if (!t.offsets) {
-            k_embed_rows<T, V><<<(unsigned)ceil_div(t.count * n, kBlock), kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, (int)n);
+            k_embed_rows<T, V><<<(unsigned)ceil_div(t.count * n, kBlock * kRowsAhead), kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, (int)n);
         } else if (!pieces) {
             k_embed_items<T, V><<<(unsigned)t.items, kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, lanes_log2((int)n));
         } else {
