@@ -512,8 +512,8 @@ __global__ __launch_bounds__(kBlock) void k_segment_sum(SumList s, const T* rows
 // read at once, one per lane; each is then handed to all lanes through scalar registers, so that a row's address, the end of a run and
 // the branch over what contributes nothing cost the vector units nothing: per entry they unpack and add E columns.  Eight rows are
 // asked for at a time.  With ITEMS the keys are the items, whose bounds are read from the offsets as they come; the blocks behind those of the list
-// zero the rows of items without tokens.
-template <typename T, typename O, int E, bool ITEMS>
+// zero the rows of items without tokens.  PAST: `out` is not to take the caches from `rows`.
+template <typename T, typename O, int E, bool ITEMS, bool PAST>
 __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim,
                                                      int sum_blocks) {
     if (ITEMS && (int)blockIdx.x >= sum_blocks) {
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
         } else if (s.real(cur)) {
             float f[E];
             for (int k = 0; k < E; ++k) f[k] = acc[k] * s.scale;
-            if (inside) store_values<E>(out + (int64_t)cur * out_ld, f);
+            if (inside) store_values<E, PAST>(out + (int64_t)cur * out_ld, f);
             if (!ITEMS && s.present && c == 0) s.present[cur] = 1;
         }
         before = false;

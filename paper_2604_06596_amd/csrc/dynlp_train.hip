@@ -126,6 +126,10 @@ int lanes_log2(int pieces) {
 
 // ---- embedding --------------------------------------------------------------------------------------------------------
 
+// Half the 256 MB cache before the memory: a gradient larger than that is written past the caches, which then keep the rows that are read (a million rows
+// of 256 float32: 1,004 us, 1,072 us through the caches).
+constexpr int64_t kHalfCache = int64_t(128) << 20;
+
 constexpr int64_t kFewPerItem = 2048;  // tokens up to which each item has a workgroup
 
 // Rows of 256 bytes and more have waves of their own (k_wave_sum).
@@ -199,14 +203,14 @@ void launch_narrow(const SumList& s, const T* rows, int64_t ld, O* out, int64_t 
 }
 
 // A lane takes as many columns as a row needs for 64 lanes, 4 to 16 bytes of them.
-template <typename T, typename O, bool ITEMS>
+template <typename T, typename O, bool ITEMS, bool PAST>
 void launch_wide(const SumList& s, const TokenList& t, const T* rows, int64_t ld, O* out, int64_t out_ld, int dim, hipStream_t stream) {
     const int64_t n = ceil_div(s.count, s.piece), blocks = ceil_div(n, kBlock / kWave);
     const unsigned grid = (unsigned)(blocks + (ITEMS ? ceil_div(t.items, kBlock) : 0));
     constexpr int e = 4 / (int)sizeof(T);
     auto sum = [&](auto width) {
         constexpr int E = decltype(width)::v;
-        k_wave_sum<T, O, E, ITEMS><<<dim3(grid, (unsigned)ceil_div(dim, kWave * E)), kBlock, 0, stream>>>(s, t, rows, ld, out, out_ld, dim, (int)blocks);
+        k_wave_sum<T, O, E, ITEMS, PAST><<<dim3(grid, (unsigned)ceil_div(dim, kWave * E)), kBlock, 0, stream>>>(s, t, rows, ld, out, out_ld, dim, (int)blocks);
     };
     if (dim <= kWave * e) sum(Width<e>());
     else if (dim <= kWave * 2 * e) sum(Width<2 * e>());
@@ -266,7 +270,7 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
             sum_space(static_cast<char*>(call->workspace), t.count, dim, wide, -1, &s);
             const SumList list{s.key, s.src, t.weights, s.part, s.flags, s.open, nullptr, t.count, table->rows, t.items, s.piece, t.scale};
             if (wide) {
-                launch_wide<T, T, true>(list, t, rows, table->stride, to, out->stride, dim, stream);
+                launch_wide<T, T, true, false>(list, t, rows, table->stride, to, out->stride, dim, stream);
             } else {
                 const int64_t tiles = ceil_div(t.count, kKeyTile);
                 k_item_keys<T, V><<<(unsigned)(tiles + ceil_div(t.items, kBlock)), kBlock, 0, stream>>>(t, s.key, s.src, (int)tiles, to, out->stride, dim);
@@ -336,8 +340,10 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
                 k_sort_scatter<<<(unsigned)s.tiles, kSortBlock, 0, stream>>>(t, p);
             }
             const SumList list{p.key_out, p.src_out, p.factor_out, s.part, s.flags, s.open, s.present, count, t.items, out->rows, s.piece, t.scale};
-            if (wide)
-                launch_wide<T, O, false>(list, t, rows, grad->stride, to, out->stride, dim, stream);
+            if (wide && out->rows * dim * (int64_t)sizeof(O) > kHalfCache)
+                launch_wide<T, O, false, true>(list, t, rows, grad->stride, to, out->stride, dim, stream);
+            else if (wide)
+                launch_wide<T, O, false, false>(list, t, rows, grad->stride, to, out->stride, dim, stream);
             else
                 launch_narrow<T, O, V>(list, rows, grad->stride, to, out->stride, dim, stream);
             constexpr int Z = V == 1 ? 1 : Piece<O>::n;

@@ -57,8 +57,9 @@ __device__ inline void widen(u32x4 p, float (&f)[8], f16) {
     for (int k = 0; k < 8; ++k) f[k] = (float)h[k];
 }
 
-// V float32 values (1, 2 or a multiple of 4) rounded to the type of the array and stored at p (any element alignment).
-template <int V, typename T>
+// V float32 values (1, 2 or a multiple of 4) rounded to the type of the array and stored at p (any element alignment); PAST: past the caches, for
+// what is not read again while it would be in them.
+template <int V, bool PAST = false, typename T>
 __device__ inline void store_values(T* p, const float (&f)[V]) {
     constexpr int n = V < 4 ? V : 4;
     static_assert(V % n == 0 && n != 3, "one value, two, or fours");
@@ -70,7 +71,10 @@ __device__ inline void store_values(T* p, const float (&f)[V]) {
         for (int k = 0; k < V; k += n) {
             vec v;
             for (int j = 0; j < n; ++j) v[j] = (T)f[k + j];
-            *reinterpret_cast<vec_any*>(p + k) = v;
+            if constexpr (PAST)
+                __builtin_nontemporal_store((vec_any)v, reinterpret_cast<vec_any*>(p + k));
+            else
+                *reinterpret_cast<vec_any*>(p + k) = v;
         }
     }
 }
