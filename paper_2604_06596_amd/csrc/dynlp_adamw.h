@@ -43,12 +43,16 @@ __host__ __device__ inline uint32_t dither_mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// Four elements from i on, of which the first `have` exist; the rest are zeros.
+// Four elements from i on, of which the first `have` exist; the rest are zeros.  PAST: past the caches.
+template <bool PAST>
 __device__ inline void load4(const void* p, int type, int64_t i, int have, float (&f)[4]) {
     if (type == 0) {
         const float* x = static_cast<const float*>(p) + i;
         if (have == 4) {
-            const u32x4 v = load_piece(x);
+            const u32x4_any4* from = reinterpret_cast<const u32x4_any4*>(x);
+            u32x4 v;
+            if constexpr (PAST) v = __builtin_nontemporal_load(from);
+            else v = *from;
             for (int k = 0; k < 4; ++k) f[k] = __uint_as_float(v[k]);
         } else {
             for (int k = 0; k < 4; ++k) f[k] = k < have ? x[k] : 0.f;
@@ -59,7 +63,10 @@ __device__ inline void load4(const void* p, int type, int64_t i, int have, float
     const uint16_t* x = static_cast<const uint16_t*>(p) + i;
     uint16_t b[4] = {0, 0, 0, 0};
     if (have == 4) {
-        const u16x4 v = *reinterpret_cast<const u16x4*>(x);
+        const u16x4* from = reinterpret_cast<const u16x4*>(x);
+        u16x4 v;
+        if constexpr (PAST) v = __builtin_nontemporal_load(from);
+        else v = *from;
         for (int k = 0; k < 4; ++k) b[k] = v[k];
     } else {
         for (int k = 0; k < 4; ++k)
@@ -67,46 +74,55 @@ __device__ inline void load4(const void* p, int type, int64_t i, int have, float
     }
     for (int k = 0; k < 4; ++k) f[k] = type == 1 ? to_float(__builtin_bit_cast(bf16, b[k])) : to_float(__builtin_bit_cast(f16, b[k]));
 }
+template <bool PAST>
 __device__ inline void store4(void* p, int type, int64_t i, int have, const float (&f)[4]) {
     if (type == 0) {
         float* x = static_cast<float*>(p) + i;
         if (have == 4)
-            store_values<4>(x, f);
+            store_values<4, PAST>(x, f);
         else
             for (int k = 0; k < 4; ++k)
                 if (k < have) x[k] = f[k];
     } else if (type == 1) {
         bf16* x = static_cast<bf16*>(p) + i;
         if (have == 4)
-            store_values<4>(x, f);
+            store_values<4, PAST>(x, f);
         else
             for (int k = 0; k < 4; ++k)
                 if (k < have) x[k] = (bf16)f[k];
     } else {
         f16* x = static_cast<f16*>(p) + i;
         if (have == 4)
-            store_values<4>(x, f);
+            store_values<4, PAST>(x, f);
         else
             for (int k = 0; k < 4; ++k)
                 if (k < have) x[k] = (f16)f[k];
     }
 }
 typedef uint8_t u8x4 __attribute__((ext_vector_type(4), aligned(1)));
+template <bool PAST>
 __device__ inline void load_codes(const void* p, int64_t i, int have, uint32_t (&c)[4]) {
     const uint8_t* x = static_cast<const uint8_t*>(p) + i;
     if (have == 4) {
-        const u8x4 v = *reinterpret_cast<const u8x4*>(x);
+        const u8x4* from = reinterpret_cast<const u8x4*>(x);
+        u8x4 v;
+        if constexpr (PAST) v = __builtin_nontemporal_load(from);
+        else v = *from;
         for (int k = 0; k < 4; ++k) c[k] = v[k];
     } else {
         for (int k = 0; k < 4; ++k) c[k] = k < have ? x[k] : 0u;
     }
 }
+template <bool PAST>
 __device__ inline void store_codes(void* p, int64_t i, int have, const uint32_t (&c)[4]) {
     uint8_t* x = static_cast<uint8_t*>(p) + i;
     if (have == 4) {
         u8x4 v;
         for (int k = 0; k < 4; ++k) v[k] = (uint8_t)c[k];
-        *reinterpret_cast<u8x4*>(x) = v;
+        if constexpr (PAST)
+            __builtin_nontemporal_store(v, reinterpret_cast<u8x4*>(x));
+        else
+            *reinterpret_cast<u8x4*>(x) = v;
     } else {
         for (int k = 0; k < 4; ++k)
             if (k < have) x[k] = (uint8_t)c[k];
@@ -138,8 +154,8 @@ __device__ inline float block_scale(uint32_t bits, float* inverse) {
 }
 
 // One wave per block of 256 elements, four per lane.  Products and sums are rounded one by one (no fused multiply-add), so that an 8-bit state
-// is a function of its inputs that does not depend on how the compiler joins them.
-template <bool BITS8>
+// is a function of its inputs that does not depend on how the compiler joins them.  PAST: the step's arrays are larger than the caches.
+template <bool BITS8, bool PAST>
 __global__ __launch_bounds__(kBlock) void k_adamw(AdamwBatch b) {
 #pragma clang fp contract(off)
     int k = 0;
@@ -161,21 +177,21 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamwBatch b) {
     const int have = (int)min(max(t.n - i, (int64_t)0), (int64_t)4);
     const float gs = b.grad_scale ? *b.grad_scale : 1.f;
     float p[4], g[4], m[4], v[4];
-    load4(t.param, t.types & 15, i, have, p);
-    load4(t.grad, t.types >> 4 & 15, i, have, g);
+    load4<PAST>(t.param, t.types & 15, i, have, p);
+    load4<PAST>(t.grad, t.types >> 4 & 15, i, have, g);
     if (BITS8) {
         const float ms = t.m_scale[block], vs = t.v_scale[block];
         uint32_t c[4];
-        load_codes(t.m, i, have, c);
+        load_codes<PAST>(t.m, i, have, c);
         for (int e = 0; e < 4; ++e) m[e] = from_code(c[e]) * ms;
-        load_codes(t.v, i, have, c);
+        load_codes<PAST>(t.v, i, have, c);
         for (int e = 0; e < 4; ++e) {
             const float r = from_code(c[e]) * vs;
             v[e] = r * r;
         }
     } else {
-        load4(t.m, 0, i, have, m);
-        load4(t.v, 0, i, have, v);
+        load4<PAST>(t.m, 0, i, have, m);
+        load4<PAST>(t.v, 0, i, have, v);
     }
     float r[4];
     uint32_t m_top = 0, r_top = 0;
@@ -190,11 +206,11 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamwBatch b) {
             r_top = max(r_top, __float_as_uint(r[e]) & 0x7fffffffu);
         }
     }
-    store4(t.param, t.types & 15, i, have, p);
-    if (t.copy) store4(t.copy, t.types >> 8 & 15, i, have, p);
+    store4<PAST>(t.param, t.types & 15, i, have, p);
+    if (t.copy) store4<PAST>(t.copy, t.types >> 8 & 15, i, have, p);
     if (!BITS8) {
-        store4(t.m, 0, i, have, m);
-        store4(t.v, 0, i, have, v);
+        store4<PAST>(t.m, 0, i, have, m);
+        store4<PAST>(t.v, 0, i, have, v);
         return;
     }
     float m_inverse, r_inverse;
@@ -209,8 +225,8 @@ __global__ __launch_bounds__(kBlock) void k_adamw(AdamwBatch b) {
         rc[e] = to_code(ry, h >> 16);
         if (r[e] > 0.f && r_inverse != 0.f) rc[e] = max(rc[e], 1u);
     }
-    store_codes(t.m, i, have, mc);
-    store_codes(t.v, i, have, rc);
+    store_codes<PAST>(t.m, i, have, mc);
+    store_codes<PAST>(t.v, i, have, rc);
     if (lane_id() == 0) {
         t.m_scale[block] = ms;
         t.v_scale[block] = rs;

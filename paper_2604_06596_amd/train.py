@@ -257,20 +257,20 @@ def adamw_step(params, grads, states, *, step, lr, betas=(0.9, 0.999), eps=1e-8,
         _refuse("states: all in 32 bits (two tensors each) or all in 8 (four)")
     if copies is not None:
         columns["copy"] = copies
+    here = [device.index] * count
     for name, tensors in columns.items():
-        for k, t in enumerate(tensors):
-            if t.numel() != n[k] or not t.is_contiguous() or t.device != device:
-                _refuse(f"{name} of tensor {k}: a contiguous tensor of {n[k]} elements on {device} is wanted")
+        if ([t.numel() for t in tensors] != n or [t.get_device() for t in tensors] != here
+                or not all([t.is_contiguous() for t in tensors])):
+            _refuse(f"{name}: a contiguous tensor on {device}, of as many elements as its parameter, is wanted for each")
         table[name] = [t.data_ptr() for t in tensors]
+        types = [t.dtype for t in tensors]
         if name in ("param", "grad", "copy"):
-            kinds = [_TYPES.get(t.dtype, -1) for t in tensors]
+            kinds = [_TYPES.get(t, -1) for t in types]
             if min(kinds) < 0:
                 _refuse(f"{name}: tensors of float32, bfloat16 or float16 are wanted")
             table[name + "_type"] = kinds
-        else:
-            want = torch.float8_e4m3fn if bits8 else torch.float32
-            if any(t.dtype != want for t in tensors):
-                _refuse(f"states: tensors of {want} are wanted")
+        elif types != [torch.float8_e4m3fn if bits8 else torch.float32] * count:
+            _refuse("states: tensors of float8_e4m3fn and their scales, or of float32, are wanted")
     if bits8:
         for name, at in (("m_scale", 2), ("v_scale", 3)):
             table[name] = [_vector(s[at], name, torch.float32, -(-n[k] // STATE_BLOCK), device) for k, s in enumerate(states)]
