@@ -152,6 +152,17 @@ __global__ __launch_bounds__(kBlock) void k_embed_rows(TokenList t, const T* tab
         }
 }
 
+// Zeros in the rows of `out` from `first` on that the lanes ask for, 64 at most: lane l for row first + l.  From whole waves.
+template <typename T, int V>
+__device__ inline void zero_rows_of_wave(bool mine, int64_t first, T* out, int64_t out_ld, int dim) {
+    const float zero[V] = {};
+    const int pieces = (dim + V - 1) / V;
+    for (unsigned long long m = __ballot(mine); m; m &= m - 1) {
+        T* row = out + (first + __ffsll(m) - 1) * out_ld;
+        for (int c = lane_id(); c < pieces; c += kWave) store_values<V>(row + piece_column<V>(c, dim), zero);
+    }
+}
+
 // ---- few tokens: one workgroup per item, or per distinct id ----------------------------------------------------------
 
 // Sum of factor * rows[source] over a workgroup's list, lanes of a group across the columns, groups taking turns on the list;
@@ -319,25 +330,13 @@ __global__ __launch_bounds__(kBlock) void k_embed_grad_few(TokenList t, const T*
         }
     }
     __syncthreads();
-    float zero[V] = {};
-    for (int64_t at = threadIdx.x; at < (int64_t)rows * pieces; at += kBlock) {
-        const int r = (int)(at / pieces), c = (int)(at - (int64_t)r * pieces);
-        if (!(present[r >> 5] >> (r & 31) & 1)) store_values<V>(out + (first + r) * out_ld + piece_column<V>(c, dim), zero);
+    for (int r0 = wave * kWave; r0 < rows; r0 += kBlock) {
+        const int r = r0 + lane;
+        zero_rows_of_wave<O, V>(r < rows && !(present[r >> 5] >> (r & 31) & 1), first + r0, out, out_ld, dim);
     }
 }
 
 // ---- long lists: sums over pieces of the list, joined ----------------------------------------------------------------
-
-// Zeros in the rows of `out` from `first` on that the lanes ask for, 64 at most: lane l for row first + l.  From whole waves.
-template <typename T, int V>
-__device__ inline void zero_rows_of_wave(bool mine, int64_t first, T* out, int64_t out_ld, int dim) {
-    const float zero[V] = {};
-    const int pieces = (dim + V - 1) / V;
-    for (unsigned long long m = __ballot(mine); m; m &= m - 1) {
-        T* row = out + (first + __ffsll(m) - 1) * out_ld;
-        for (int c = lane_id(); c < pieces; c += kWave) store_values<V>(row + piece_column<V>(c, dim), zero);
-    }
-}
 
 // Zeros in the rows of items without tokens: block `block` looks at kBlock items.
 template <typename T, int V>
@@ -709,8 +708,9 @@ __global__ __launch_bounds__(kBlock) void k_zero_absent(const uint8_t* present, 
 // weights); it is bound by that, a copy of as many bytes.
 
 constexpr int kSortBlock = 512;
-constexpr int kSortTile = 8192;                       // entries per workgroup: eight of each digit on average
-constexpr int kSortItems = kSortTile / kSortBlock;    // per thread
+// Entries per thread.  A long list in tiles of 8,192 has eight of each digit to a tile on average, which are written side by side; a short one in tiles
+// of 2,048 has four times the workgroups.
+constexpr int kLongItems = 16, kShortItems = 4;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
@@ -738,7 +738,9 @@ __device__ inline int32_t sort_key(const TokenList& t, const SortPass& p, int64_
 }
 
 // The blocks behind those of the tiles (first pass) clear the notes of which ids occur.
+template <int N>
 __global__ __launch_bounds__(kSortBlock) void k_sort_count(TokenList t, SortPass p, uint8_t* present) {
+    constexpr int kTile = N * kSortBlock;
     if ((int)blockIdx.x >= p.tiles) {
         const int64_t at = ((int64_t)blockIdx.x - p.tiles) * kClear + threadIdx.x * 16;
         if (at < t.limit) *reinterpret_cast<u32x4*>(present + at) = u32x4{0u, 0u, 0u, 0u};  // its end is padded to 256 bytes
@@ -747,10 +749,10 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_count(TokenList t, SortPass
     __shared__ uint32_t count[kDigits];
     for (int d = threadIdx.x; d < kDigits; d += kSortBlock) count[d] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kSortTile;
-    int32_t key[kSortItems];
+    const int64_t first = (int64_t)blockIdx.x * kTile;
+    int32_t key[N];
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
+    for (int k = 0; k < N; ++k) {
         const int64_t i = first + k * kSortBlock + threadIdx.x;
         key[k] = -1;
         if (i < t.count) {
@@ -765,7 +767,7 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_count(TokenList t, SortPass
         }
     }
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k)
+    for (int k = 0; k < N; ++k)
         if (key[k] >= 0) atomicAdd(&count[p.digit(key[k])], 1u);
     __syncthreads();
     for (int d = threadIdx.x; d < 1 << p.bits; d += kSortBlock) p.hist[(int64_t)blockIdx.x * kDigits + d] = count[d];
@@ -795,32 +797,34 @@ __global__ __launch_bounds__(kOffsetDigits * kOffsetParts) void k_sort_offsets(S
     }
 }
 
-// Each wave ranks its 1,024 consecutive entries 64 at a time among those of the same digit (lanes of one digit are found by a ballot
-// per bit), the ranks are made the tile's, and keys, sources and factors are put in order in shared memory, one after the other in the same 32 KB, and
+// Each wave ranks its 64 N consecutive entries 64 at a time among those of the same digit (lanes of one digit are found by a ballot
+// per bit), the ranks are made the tile's, and keys, sources and factors are put in order in shared memory, one after the other in the same space, and
 // written out as runs.
+template <int N>
 __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPass p) {
+    constexpr int kTile = N * kSortBlock;
     __shared__ uint16_t count[kSortWaves][kDigits];
     __shared__ uint32_t to[kDigits];  // place of a digit's entries of this tile in the output, less their place in the tile
     __shared__ uint32_t smem[kSortWaves + 1];
     __shared__ int32_t range[kTileRange];
-    __shared__ int32_t order[kSortTile];
+    __shared__ int32_t order[kTile];
     const int wave = threadIdx.x / kWave, lane = lane_id();
-    const int64_t first = (int64_t)blockIdx.x * kSortTile;
-    const int n = (int)min((int64_t)kSortTile, t.count - first);
+    const int64_t first = (int64_t)blockIdx.x * kTile;
+    const int n = (int)min((int64_t)kTile, t.count - first);
     for (int k = threadIdx.x; k < kSortWaves * kDigits / 2; k += kSortBlock) reinterpret_cast<uint32_t*>(count)[k] = 0;
-    const int mine = wave * (kSortTile / kSortWaves) + lane;  // entry mine + 64 r of the tile
-    int32_t key[kSortItems], src[kSortItems];
-    uint32_t rank[kSortItems];
+    const int mine = wave * (kTile / kSortWaves) + lane;  // entry mine + 64 r of the tile
+    int32_t key[N], src[N];
+    uint32_t rank[N];
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         const int at = mine + r * kWave;
         key[r] = at < n ? sort_key(t, p, first + at) : 0;
         if (p.key) src[r] = at < n ? p.src[first + at] : 0;
     }
     if (!p.key) {
-        if (t.offsets) tile_items<kSortTile, kSortBlock>(t, first, n, order, range);
+        if (t.offsets) tile_items<kTile, kSortBlock>(t, first, n, order, range);
 #pragma unroll
-        for (int r = 0; r < kSortItems; ++r) {
+        for (int r = 0; r < N; ++r) {
             const int at = mine + r * kWave;
             src[r] = t.offsets ? order[at] : (int32_t)(first + at);
             if (src[r] >= t.items) src[r] = -1;
@@ -828,7 +832,7 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPa
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         const bool in = mine + r * kWave < n;
         const uint32_t d = p.digit(key[r]);
         unsigned long long same = __ballot(in);
@@ -867,14 +871,14 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPa
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         rank[r] += count[wave][p.digit(key[r])];
         if (mine + r * kWave < n) order[rank[r]] = key[r];
     }
     __syncthreads();
-    uint32_t place[kSortItems];
+    uint32_t place[N];
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         const int at = (int)threadIdx.x + r * kSortBlock;
         const int32_t k = at < n ? order[at] : 0;
         place[r] = to[p.digit(k)] + (uint32_t)at;
@@ -882,11 +886,11 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPa
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r)
+    for (int r = 0; r < N; ++r)
         if (mine + r * kWave < n) order[rank[r]] = src[r];
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         const int at = (int)threadIdx.x + r * kSortBlock;
         if (at < n) p.src_out[place[r]] = order[at];
     }
@@ -894,11 +898,11 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(TokenList t, SortPa
     __syncthreads();
     const float* factor = p.key ? p.factor : t.weights;
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r)
+    for (int r = 0; r < N; ++r)
         if (mine + r * kWave < n) order[rank[r]] = __float_as_int(factor[first + mine + r * kWave]);
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r) {
+    for (int r = 0; r < N; ++r) {
         const int at = (int)threadIdx.x + r * kSortBlock;
         if (at < n) p.factor_out[place[r]] = __int_as_float(order[at]);
     }

@@ -138,7 +138,10 @@ bool wide_rows(int32_t type, int dim) { return (int64_t)dim * type_size(type) >=
 // over many pieces is joined soon.
 int piece_length(int64_t count, int dim, bool wide) {
     const int64_t lanes = std::min<int64_t>(ceil_div(dim, 8), 64);
-    if (wide) return (int)std::min<int64_t>(std::max<int64_t>(round_up(ceil_div(count, 16384), 64), 64), 512);
+    if (wide) {
+        const int64_t n = ceil_div(count, 16384);
+        return n <= 16 ? 16 : n <= 32 ? 32 : (int)std::min<int64_t>(round_up(n, 64), 512);
+    }
     return (int)std::min<int64_t>(std::max<int64_t>(round_up(ceil_div(count * lanes, 8192 * 64), 8), 16), 512);
 }
 
@@ -151,7 +154,7 @@ struct SumSpace {
     float* part;
     uint8_t *flags, *present;
     int32_t* open;
-    int piece;
+    int piece, items;  // of a piece of the list; of a thread in a sort
     int64_t pieces, tiles;
 };
 
@@ -160,7 +163,8 @@ int64_t sum_space(char* base, int64_t count, int dim, bool wide, int64_t sorted,
     Carve c{base};
     s->piece = piece_length(count, dim, wide);
     s->pieces = ceil_div(count, s->piece);
-    s->tiles = ceil_div(count, kSortTile);
+    s->items = count < (int64_t(1) << 18) ? kShortItems : kLongItems;
+    s->tiles = ceil_div(count, s->items * kSortBlock);
     if (sorted >= 0 || !wide) {
         s->key = c.take<int32_t>(count);
         s->src = c.take<int32_t>(count);
@@ -333,9 +337,14 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
                 p.tiles = (int)s.tiles;
                 p.shift = k * per;
                 p.bits = std::min(per, bits - k * per);
-                k_sort_count<<<(unsigned)(s.tiles + (k == 0 ? ceil_div(out->rows, kClear) : 0)), kSortBlock, 0, stream>>>(t, p, s.present);
-                k_sort_offsets<<<(unsigned)ceil_div(1 << p.bits, kOffsetDigits), kOffsetDigits * kOffsetParts, 0, stream>>>(p);
-                k_sort_scatter<<<(unsigned)s.tiles, kSortBlock, 0, stream>>>(t, p);
+                auto pass = [&](auto items) {
+                    constexpr int N = decltype(items)::v;
+                    k_sort_count<N><<<(unsigned)(s.tiles + (k == 0 ? ceil_div(out->rows, kClear) : 0)), kSortBlock, 0, stream>>>(t, p, s.present);
+                    k_sort_offsets<<<(unsigned)ceil_div(1 << p.bits, kOffsetDigits), kOffsetDigits * kOffsetParts, 0, stream>>>(p);
+                    k_sort_scatter<N><<<(unsigned)s.tiles, kSortBlock, 0, stream>>>(t, p);
+                };
+                if (s.items == kShortItems) pass(Width<kShortItems>());
+                else pass(Width<kLongItems>());
             }
             const SumList list{p.key_out, p.src_out, p.factor_out, s.part, s.flags, s.open, s.present, count, t.items, out->rows, s.piece, t.scale};
             // a gradient larger than half the cache is written past it, which then keeps the rows that are read (a million rows of 256 float32: 992 us,
