@@ -10,6 +10,11 @@
 //   dh       dh^T = W^T dz^T.  The right operand (k = class, column = row r) is what the lane holds after the softmax.  The left one
 //            needs W by columns: pieces of W's rows, for two-byte types transposed between registers.  Result: row r, n consecutive columns.
 //   dweight  dz^T h.  Both operands are read row by row of h and dz, h in pieces, transposed between registers where needed.
+// Precision: products of bfloat16 and float16 values are exact in the matrix cores, sums are float32; dz, which is float32, is taken in bfloat16 terms
+// (two for dh, three for dweight), or the product is made in float32 (float32 and float16 heads).
+// What bounds it: h is read once (from memory; for dweight again, from the L2) and dh written once.  1M rows x 256 bfloat16, 50 classes, with soft
+// targets: 378 us (3.3 TB/s of what has to move; the first kernels, with dz through memory and h read twice, 905 us).  100,000 x 64 float32, 10
+// classes: 24 us, of which each workgroup spends half on its start and end.
 #pragma once
 
 #include "dynlp_device.h"
@@ -736,6 +741,8 @@ __host__ __device__ inline int fused_splits(int groups, int waves) {
     return splits;
 }
 
+// Logits, loss, dz, dh and dweight of a tile of rows, one after the other: switched off one at a time (1M x 256, 50 classes, 379 us), dweight is worth 83 us, dh
+// 103, the logits 63: with two waves to a SIMD they hardly overlap, and registers (233) and shared memory (62 KB) leave room for no third.
 // Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight (GPW groups of 64, a quad for each of 16 lanes) in registers
 // over all tiles of 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
 template <typename T, int CT, int GPW>

@@ -191,6 +191,26 @@ def test_the_same_bits_every_time_and_in_any_list():
             assert all(torch.equal(a, b) for a, b in zip(results[0], other))
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_arrays_larger_than_the_caches(bits):
+    """What is done past them is what is done through them: the first elements of a long tensor, and a tensor of these alone."""
+    P = _api()
+    rng = np.random.default_rng(6)
+    n, few = 20_000_003, 1_000_003
+    p, g = (torch.randn(n, device="cuda") for _ in range(2))
+    state = P.adamw_state(p, bits)
+    short = p[:few].clone()
+    short_state = P.adamw_state(short, bits)
+    for step in (1, 2):
+        g.mul_(1.1)
+        P.adamw_step([p], [g], [state], step=step, lr=0.1, seed=5)
+        P.adamw_step([short], [g[:few]], [short_state], step=step, lr=0.1, seed=5)
+    whole = few // 256 * 256  # the short tensor's last block has another scale
+    assert torch.equal(p[:few], short)
+    for a, b in zip(state[:2], short_state[:2]):
+        assert torch.equal(a.view(torch.uint8)[:whole * a.element_size()], b.view(torch.uint8)[:whole * a.element_size()])
+
+
 def test_replays_of_a_graph():
     P = _api()
     rng = np.random.default_rng(5)

@@ -273,6 +273,32 @@ def test_a_table_beyond_32_bit_offsets():
         del g
 
 
+@pytest.mark.parametrize("count, items, rows, dim, kind", [(300007, 21000, 70003, 8, "float32"), (300007, 900, 1500000, 130, "bfloat16")])
+def test_long_lists(count, items, rows, dim, kind):
+    """Lists long enough for the sort's long tiles, rows narrower and wider than a wave."""
+    P = _api()
+    rng = np.random.default_rng(count + dim)
+    ids, offsets, w = _list(rng, count, items, min(rows, 70003), True, True, "skew")
+    table, exact_table = _matrix(rng, 70003, dim, TYPES[kind])
+    args = _gpu(ids, torch.int32), _gpu(offsets), _gpu(w)
+    _hold(P.embed(table, *args, 0.75), *S.embed(exact_table, ids, offsets, w, 0.75))
+    grad, exact_grad = _matrix(rng, items, dim, TYPES[kind])
+    out = P.embed_grad(grad, args[0], rows, *args[1:], 0.75)
+    assert not out[70003:].any()
+    _hold(out[:70003], *S.embed_grad(exact_grad, ids, 70003, offsets, w, 0.75))
+
+
+def test_a_gradient_larger_than_the_caches():
+    """What is written past them is what is written through them (a table of fewer rows)."""
+    P = _api()
+    rng = np.random.default_rng(21)
+    ids, offsets, w = _list(rng, 12000, 700, 5000, True, True, "skew")
+    grad, _ = _matrix(rng, 700, 256, torch.float32)
+    args = _gpu(ids, torch.int32), _gpu(offsets), _gpu(w)
+    small, large = (P.embed_grad(grad, args[0], rows, *args[1:]) for rows in (5000, 150000))
+    assert torch.equal(large[:5000], small) and not large[5000:].any()
+
+
 def test_the_binding_refuses():
     P = _api()
     table = torch.zeros(5, 8, device="cuda")

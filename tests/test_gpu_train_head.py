@@ -184,6 +184,38 @@ def test_many_rows_and_their_splits():
             _hold(name, x, ref[name], bars[name])
 
 
+@pytest.mark.parametrize("kind, rows, dim, classes", [("float32", 140001, 20, 17), ("bfloat16", 33001, 1000, 64), ("float16", 140001, 33, 29)])
+def test_many_answers(kind, rows, dim, classes):
+    """Rows enough for workgroups that keep a copy of W, of more than 64 KB too: the same as of a few rows at a time, which are held to the bars."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    h, _ = _matrix(rng, rows, dim, TYPES[kind])
+    W, _ = _matrix(rng, classes, dim, TYPES[kind], 2.0 / np.sqrt(dim))
+    b = torch.from_numpy(rng.standard_normal(classes).astype(np.float32)).cuda()
+    soft, hard = P.head_labels(h, W, b)
+    for at in (0, 4097, rows // 2, rows - 300):
+        few = P.head_labels(h[at:at + 300], W, b)
+        assert torch.equal(few[0], soft[at:at + 300]) and torch.equal(few[1], hard[at:at + 300])
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows, dim, classes, stride", [(300, 520, 50, 520), (200, 700, 64, 701), (70, 512, 64, 512), (5, 40, 20, 1 << 22), (3, 24, 3, 1 << 23)])
+def test_heads_that_do_not_fit_a_workgroup(rows, dim, classes, stride, kind):
+    """More columns than one pass keeps, W larger than shared memory (64 x 512 float32), rows further apart than 32 bits hold a tile of."""
+    P = _api()
+    rng = np.random.default_rng(rows + dim)
+    h, eh = _matrix(rng, rows, dim, TYPES[kind], stride=stride)
+    W, eW = _matrix(rng, classes, dim, TYPES[kind], 2.0 / np.sqrt(dim))
+    b = rng.standard_normal(classes).astype(np.float32)
+    soft = rng.random((rows, classes)).astype(np.float32)
+    r = np.where(rng.random(rows) < 0.3, 0.0, rng.random(rows)).astype(np.float32)
+    ref = S.head_loss(eh, eW, b, soft, None, r, 0.5)
+    bars = _bars(eh, eW, b, ref, r.astype(np.float64), 0.5)
+    got = P.head_loss(h, W, torch.from_numpy(b).cuda(), torch.from_numpy(soft).cuda(), row_weight=torch.from_numpy(r).cuda(), grad_scale=0.5)
+    for name, x in zip(("loss", "dh", "dweight", "dbias"), got):
+        _hold(name, x, ref[name], bars[name])
+
+
 def test_classes_out_of_range_leave_rows_out_and_are_counted():
     P = _api()
     rng = np.random.default_rng(12)
