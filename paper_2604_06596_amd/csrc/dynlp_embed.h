@@ -116,8 +116,8 @@ __device__ inline void count_rejected(int32_t* rejected, bool bad) {
 
 // ---- one row per token -----------------------------------------------------------------------------------------------
 
-// out[i] = scale * weight * table[id]: a copy with a factor, bound by the memory: 65,536 rows of 1,000 float16 from a table of 250,007: 46 us
-// (4.0 TB/s of what has to move, with one piece per thread 50 us).  Four 16-byte pieces per thread, asked for at once; `pieces` of them make a row.
+// out[i] = scale * weight * table[id]: a copy with a factor, bound by the memory: 65,536 rows of 1,000 float16 from a table of 250,007: 46 to 48 us
+// (3.9 TB/s of what has to move, with one piece per thread 50 us).  Four 16-byte pieces per thread, asked for at once; `pieces` of them make a row.
 constexpr int kRowsAhead = 4;
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void k_embed_rows(TokenList t, const T* table, int64_t ld, T* out, int64_t out_ld, int dim,
@@ -214,7 +214,7 @@ __device__ inline void block_sum(const T* rows, int64_t ld, int dim, int lanes_l
     }
 }
 
-// An item per workgroup: latency is all there is (one item of 37 tokens: 3.7 us on the GPU, 9 us with the call).
+// An item per workgroup: latency is all there is (one item of 37 tokens: 3.6 us on the GPU, 9 us with the call).
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void k_embed_items(TokenList t, const T* table, int64_t ld, T* out, int64_t out_ld, int dim,
                                                         int lanes_log2) {
