@@ -417,8 +417,8 @@ typedef struct dynlp_round_info {
  */
 int64_t dynlp_round_log(const dynlp_ctx* ctx, int64_t cap, dynlp_round_info* out);
 
-/* Message for the last failed call on ctx (or, with ctx NULL, the last failed dynlp_create on this
- * thread).  Valid until the next call on the same context / thread.  Never NULL. */
+/* Message for the last failed call on ctx (or, with ctx NULL, the last failed dynlp_create, or call of
+ * dynlp_train.h, on this thread).  Valid until the next call on the same context / thread.  Never NULL. */
 const char* dynlp_last_error(const dynlp_ctx* ctx);
 
 /* Release the context and all device memory it owns (see dynlp_options.alloc: some of it may wait for the next context).  NULL is

@@ -37,7 +37,7 @@ extern "C" {
 typedef enum dynlp_type { DYNLP_FLOAT32 = 0, DYNLP_BFLOAT16 = 1, DYNLP_FLOAT16 = 2 } dynlp_type;
 
 /* A matrix in row-major order: element (i, j) is data[i * stride + j].  stride >= dim, and any (no alignment beyond the
- * element's own is needed; 16 bytes are faster). */
+ * element's own is needed; 16 bytes are faster).  rows < 2^31 - 1, 1 <= dim <= 2^28. */
 typedef struct dynlp_matrix {
     void* data;
     int64_t rows;

@@ -48,6 +48,7 @@ dynlp_status launched() {
 }
 
 constexpr int64_t kMostRows = 0x7ffffffe;
+constexpr int32_t kMostDim = 1 << 28;  // 32 bits hold the bytes of a row
 
 int type_size(int32_t type) { return type == DYNLP_FLOAT32 ? 4 : 2; }
 
@@ -55,7 +56,7 @@ dynlp_status check_matrix(const dynlp_matrix* m, const char* name) {
     if (!m) REFUSE("%s is NULL", name);
     if (m->type < DYNLP_FLOAT32 || m->type > DYNLP_FLOAT16) REFUSE("%s: type %d is not a dynlp_type", name, m->type);
     if (m->rows < 0 || m->rows > kMostRows) REFUSE("%s: %lld rows", name, (long long)m->rows);
-    if (m->dim < 1) REFUSE("%s: rows of %d elements", name, m->dim);
+    if (m->dim < 1 || m->dim > kMostDim) REFUSE("%s: rows of %d elements", name, m->dim);
     if (m->stride < m->dim) REFUSE("%s: stride %lld is less than the %d elements of a row", name, (long long)m->stride, m->dim);
     if (m->stride > (int64_t(1) << 40)) REFUSE("%s: stride %lld", name, (long long)m->stride);
     if (m->rows > 0 && !m->data) REFUSE("%s: data is NULL", name);
@@ -448,12 +449,17 @@ int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type,
     return c.used;
 }
 
-// Shared memory beyond 64 KB is to be asked for, once per kernel.
+// Shared memory beyond 64 KB is to be asked for, once per kernel and device; `done` has a bit per device (those from the 64th on are asked each time).
 template <typename F>
-void allow_shared(F kernel, std::atomic<bool>& done) {
-    if (done.load(std::memory_order_relaxed)) return;
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedMemory);
-    done.store(true, std::memory_order_relaxed);
+void allow_shared(F kernel, std::atomic<uint64_t>& done) {
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return;  // the launch will say so
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return;
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedMemory) == hipSuccess)
+        done.fetch_or(bit, std::memory_order_relaxed);
+    else
+        (void)hipGetLastError();  // the launch will say so
 }
 
 }  // namespace
@@ -474,7 +480,7 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
         // a copy of W pays once a workgroup has several tiles of rows
         const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 4);
         if (bytes <= kSharedMemory && blocks >= 2 * stay) {
-            static std::atomic<bool> allowed{false};
+            static std::atomic<uint64_t> allowed{0};
             allow_shared(k_head_labels<T, CT, true>, allowed);
             k_head_labels<T, CT, true><<<(unsigned)stay, kBlock, (size_t)bytes, stream>>>(a, soft, hard);
         } else {
@@ -513,7 +519,7 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
         if (a.rows > 0 && s.fused) {
             auto fused = [&](auto per_wave) {
                 constexpr int GPW = decltype(per_wave)::v;
-                static std::atomic<bool> allowed{false};
+                static std::atomic<uint64_t> allowed{0};
                 allow_shared(k_head_fused<T, CT, GPW>, allowed);
                 k_head_fused<T, CT, GPW><<<(unsigned)s.splits, kWave * fused_waves(CT), (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, s.part);
             };

@@ -82,6 +82,7 @@ def _refused(status, word):
     (dict(rows=-1), {}, {}, "rows"),
     (dict(rows=2 ** 31), {}, {}, "rows"),
     (dict(dim=0), {}, {}, "elements"),
+    (dict(dim=2 ** 28 + 1, stride=2 ** 29), {}, {}, "elements"),
     (dict(stride=15), {}, {}, "stride"),
     (dict(data=None), {}, {}, "NULL"),
     (dict(data=A + 2), {}, {}, "aligned"),
