@@ -544,7 +544,7 @@ __global__ __launch_bounds__(kBlock) void k_wave_sum(SumList s, TokenList t, con
         item = t.item_by_wave(first);
         next = item < t.items ? t.offsets[item + 1] : INT64_MAX;
         cur = item >= 0 && item < t.items ? (int32_t)item : -1;
-        before = cur >= 0 && t.offsets[item] < first;
+        before = cur >= 0 && max(t.offsets[item], (int64_t)0) < first;  // what an item has before the list is no token
     } else {
         cur = s.key[first];
         before = first > 0 && s.key[first - 1] == cur;
