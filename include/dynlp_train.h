@@ -17,6 +17,8 @@
  *     captured in a HIP graph (host scalars such as lr and step are captured as they stand).
  *   - Scratch memory is the caller's: dynlp_call.workspace, of the size that the *_workspace function of the call gives for the same
  *     sizes, aligned to 256 bytes, not shared with calls that may run at the same time.
+ *   - Outputs overlap neither inputs, workspace nor each other, but for what a call says that it updates in place.  Rows of two matrices may
+ *     take turns in one array.  (Checked: the matrices of a call.)
  *   - A call refuses what it can see (DYNLP_ERR_INVALID_ARG, nothing enqueued; dynlp_last_error(NULL) says what, on the same
  *     thread).  Values on the device are not waited for: every id and offset is checked where it is used, and what is out
  *     of range is left out as described below; nothing outside the arrays is read or written.
@@ -78,7 +80,7 @@ typedef struct dynlp_tokens {
 
 /*
  * out[b] = scale * sum over the tokens i of item b of weights[i] * table[ids[i]]; nothing but zeros for an item without tokens.
- * table and out have the same type and dim; out->rows == tokens->items.  out must not overlap the table.
+ * table and out have the same type and dim; out->rows == tokens->items.
  */
 dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, const dynlp_matrix* out, const dynlp_call* call);
 int64_t dynlp_embed_workspace(int64_t count, int64_t items, int32_t dim);
@@ -112,7 +114,7 @@ dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight
  *   row_weight  r, float32, or NULL for 1.  A row with weight 0 is left out: loss 0, dh 0, nothing in the other gradients, whatever
  *               its h and target hold
  *   loss        rows float32; dh: rows x dim, of h's type; dweight: classes x dim float32, no padding; dbias: classes float32.
- *               Each of the four may be NULL (a matrix with data NULL, for dh).
+ *               Each of the four may be NULL (a matrix with data NULL, for dh).  Where dweight is, dh may be h itself: same data and stride.
  * A row whose logits are all -infinity is left out.
  */
 typedef struct dynlp_targets {

@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <numeric>
 #include <string>
 
 #include "dynlp_train.h"
@@ -85,6 +86,27 @@ dynlp_status check_workspace(const dynlp_call* call, int64_t bytes) {
         REFUSE("workspace of %lld bytes: %lld are needed", (long long)(call->workspace ? call->workspace_bytes : 0), (long long)bytes);
     if (bytes > 0 && reinterpret_cast<uintptr_t>(call->workspace) % 256) REFUSE("workspace is not aligned to 256 bytes");
     return DYNLP_OK;
+}
+
+// Whether rows of a and rows of b share memory.  Rows of two matrices may take turns in one array; where their strides differ, matrices whose rows
+// would meet if there were enough of them count as overlapping.
+bool overlap(const dynlp_matrix& a, const dynlp_matrix& b) {
+    using wide = __int128;  // rows times stride
+    if (a.rows == 0 || b.rows == 0) return false;
+    const wide width_a = (wide)a.dim * type_size(a.type), width_b = (wide)b.dim * type_size(b.type);
+    wide step_a = (wide)a.stride * type_size(a.type), step_b = (wide)b.stride * type_size(b.type);
+    const wide behind = (wide) reinterpret_cast<uintptr_t>(b.data) - (wide) reinterpret_cast<uintptr_t>(a.data);
+    if (behind >= (a.rows - 1) * step_a + width_a || -behind >= (b.rows - 1) * step_b + width_b) return false;
+    if (a.rows == 1) step_a = step_b;
+    if (b.rows == 1) step_b = step_a;
+    if (step_a != step_b) {
+        const wide step = std::gcd((int64_t)step_a, (int64_t)step_b), at = (behind % step + step) % step;
+        return at < width_a || at + width_b > step;
+    }
+    // row i of a and row i + k of b meet where -width_b < behind + k step < width_a
+    auto down = [&](wide x) { return (x >= 0 ? x : x - step_a + 1) / step_a; };
+    const wide least = -down(width_b - 1 + behind), most = down(width_a - 1 - behind);
+    return std::max(least, (wide)(1 - a.rows)) <= std::min(most, (wide)(b.rows - 1));
 }
 
 // Hands out the parts of a workspace, or only measures them (base NULL).
@@ -253,6 +275,7 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
     if (tokens->count > 0 && table->rows == 0) REFUSE("%lld tokens and a table without rows", (long long)tokens->count);
     const bool pieces = tokens->offsets && tokens->count > kFewPerItem;
     CHECK(check_workspace(call, pieces ? dynlp_embed_workspace(tokens->count, tokens->items, table->dim) : 0));
+    if (overlap(*table, *out)) REFUSE("out overlaps the table");
     if (tokens->items == 0) return DYNLP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const TokenList t = token_list(tokens, table->rows);
@@ -299,6 +322,7 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
     if (grad->rows != tokens->items) REFUSE("grad has %lld rows for %lld items", (long long)grad->rows, (long long)tokens->items);
     const int64_t count = tokens->items == 0 ? 0 : tokens->count;
     CHECK(check_workspace(call, dynlp_embed_grad_workspace(count, tokens->items, grad->dim, out->rows)));
+    if (overlap(*grad, *out)) REFUSE("out overlaps grad");
     if (out->rows == 0) return DYNLP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const TokenList t = token_list(tokens, out->rows);
@@ -504,6 +528,10 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
     if (dh && dh->data) {
         CHECK(check_matrix(dh, "dh"));
         if (dh->type != h->type || dh->dim != h->dim || dh->rows != h->rows) REFUSE("dh has another shape or type than h");
+        // a row's logits are made before its dh is stored, but dweight reads h again
+        const bool in_place = dh->data == h->data && (dh->stride == h->stride || h->rows == 1);
+        if (overlap(*h, *dh) && (dweight || !in_place)) REFUSE("dh overlaps h%s", in_place ? ", which dweight needs" : "");
+        if (overlap(*weight, *dh)) REFUSE("dh overlaps weight");
     }
     const int64_t bytes = dweight || dbias ? dynlp_head_loss_workspace(h->rows, h->dim, (int32_t)weight->rows, h->type) : 0;
     CHECK(check_workspace(call, bytes));

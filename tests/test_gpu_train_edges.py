@@ -66,3 +66,45 @@ def test_items_that_begin_before_the_list_or_end_behind_it(count, kind, dim):
         _hold_sum(out, *S.embed(exact, ids, offsets, w, 0.5))
         grad, exact_grad = _random(rng, len(offsets) - 1, dim, TYPES[kind])
         _hold_sum(P.embed_grad(grad, _gpu(ids), 50, _gpu(np.array(offsets)), _gpu(w), 0.5), *S.embed_grad(exact_grad, ids, 50, offsets, w, 0.5))
+
+
+def _loss_into(dh, h, weight, target, dweight=None):
+    """dynlp_head_loss with a dh of the caller's; returns (status, loss)."""
+    from paper_2604_06596_amd import train as T
+
+    L = T._library()
+    m, w = T._matrix(h, "h", h.device), T._matrix(weight, "weight", h.device)
+    loss = torch.empty(len(h), device="cuda")
+    call, space = T._call(h.device, L.dynlp_head_loss_workspace(m.rows, m.dim, w.rows, m.type))
+    t = T._Targets(target.data_ptr(), None, None, None, 1.0)
+    status = L.dynlp_head_loss(m, w, None, t, loss.data_ptr(), T._matrix(dh, "dh", h.device), None if dweight is None else dweight.data_ptr(), None, call)
+    return status, loss
+
+
+@pytest.mark.parametrize("kind, rows, dim, classes", [("float32", 700, 64, 10), ("bfloat16", 700, 200, 50), ("float16", 300, 520, 20)])
+def test_a_gradient_of_h_beside_it_or_in_its_place(kind, rows, dim, classes):
+    """Rows of h and dh may take turns in one array, by columns or by rows.  Where no dweight is asked for, dh may take h's place; where it is,
+    that is refused, and so is an overlap that is not the same place."""
+    rng = np.random.default_rng(3)
+    h, _ = _random(rng, rows, dim, TYPES[kind])
+    W, _ = _random(rng, classes, dim, TYPES[kind], 2.0 / np.sqrt(dim))
+    q = torch.softmax(_random(rng, rows, classes, torch.float32)[0], 1)
+    want, dweight, other = torch.empty_like(h), torch.empty(classes, dim, device="cuda"), torch.empty(classes, dim, device="cuda")
+    status, loss = _loss_into(want, h, W, q, dweight)
+    assert status == 0
+    both = torch.zeros(rows, 2 * dim, dtype=h.dtype, device="cuda")
+    for a, b in ((both[:, :dim], both[:, dim:]), (both.view(2 * rows, dim)[::2], both.view(2 * rows, dim)[1::2]), (both[:, dim:], both[:, :dim])):
+        a.copy_(h)
+        status, again = _loss_into(b, a, W, q, other)
+        assert status == 0 and torch.equal(again, loss) and torch.equal(b, want) and torch.equal(other, dweight)
+    alone = torch.empty_like(h)
+    assert _loss_into(alone, h, W, q)[0] == 0
+    same = h.clone()
+    status, again = _loss_into(same, same, W, q)
+    assert status == 0 and torch.equal(again, loss) and torch.equal(same, alone)
+    same = torch.cat([h, h[:1]])
+    before = same.clone()
+    assert _loss_into(same[:rows], same[:rows], W, q, other)[0] == -1
+    assert _loss_into(same[1:], same[:rows], W, q, other)[0] == -1 and _loss_into(same[1:], same[:rows], W, q)[0] == -1
+    torch.cuda.synchronize()
+    assert torch.equal(same, before)
