@@ -64,7 +64,7 @@ typedef struct dynlp_call {
  *            item; offsets that decrease give no defined result, but nothing outside the arrays is touched)
  *   weights  count weights, or NULL for 1.  The weight of a token that contributes nothing is not looked at.
  *   scale    factor of every item
- *   rejected one int32 that grows by the number of rejected ids, or NULL
+ *   rejected one int32 that grows by the number of rejected ids of the whole list, those that are in no item among them, or NULL
  * count and items are below 2^31.
  */
 typedef struct dynlp_tokens {

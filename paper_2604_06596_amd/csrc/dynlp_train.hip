@@ -245,6 +245,13 @@ void launch_wide(const SumList& s, const TokenList& t, const T* rows, int64_t ld
     k_segment_join<O, V><<<dim3((unsigned)ceil_div(n * kWave, kBlock), (unsigned)ceil_div(pieces, 1 << l)), kBlock, 0, stream>>>(s, n, out, out_ld, dim, l);
 }
 
+// Of a list that nothing else looks at.
+dynlp_status launch_count_rejected(const TokenList& t, hipStream_t stream) {
+    if (!t.rejected || t.count == 0) return DYNLP_OK;
+    k_count_rejected<<<(unsigned)std::min<int64_t>(ceil_div(t.count, kBlock), 1024), kBlock, 0, stream>>>(t);
+    return launched();
+}
+
 template <typename O>
 void launch_zeros(O* out, int64_t out_ld, int64_t rows, int dim, hipStream_t stream) {
     constexpr int P = Piece<O>::n;
@@ -276,9 +283,9 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
     const bool pieces = tokens->offsets && tokens->count > kFewPerItem;
     CHECK(check_workspace(call, pieces ? dynlp_embed_workspace(tokens->count, tokens->items, table->dim) : 0));
     if (overlap(*table, *out)) REFUSE("out overlaps the table");
-    if (tokens->items == 0) return DYNLP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const TokenList t = token_list(tokens, table->rows);
+    if (t.items == 0) return launch_count_rejected(t, stream);
     const int dim = table->dim;
     by_type(table->type, dim, [&](auto type, auto width) {
         using T = decltype(type);
@@ -323,9 +330,10 @@ dynlp_status dynlp_embed_grad(const dynlp_matrix* grad, const dynlp_tokens* toke
     const int64_t count = tokens->items == 0 ? 0 : tokens->count;
     CHECK(check_workspace(call, dynlp_embed_grad_workspace(count, tokens->items, grad->dim, out->rows)));
     if (overlap(*grad, *out)) REFUSE("out overlaps grad");
-    if (out->rows == 0) return DYNLP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const TokenList t = token_list(tokens, out->rows);
+    if (count == 0 || out->rows == 0) CHECK(launch_count_rejected(t, stream));
+    if (out->rows == 0) return DYNLP_OK;
     const int dim = grad->dim;
     auto run = [&](auto type, auto width, auto out_type) {
         using T = decltype(type);

@@ -108,3 +108,24 @@ def test_a_gradient_of_h_beside_it_or_in_its_place(kind, rows, dim, classes):
     assert _loss_into(same[1:], same[:rows], W, q, other)[0] == -1 and _loss_into(same[1:], same[:rows], W, q)[0] == -1
     torch.cuda.synchronize()
     assert torch.equal(same, before)
+
+
+@pytest.mark.parametrize("dim", [8, 128])
+@pytest.mark.parametrize("count", [37, 2048, 2049, 8192, 8193])
+def test_every_rejected_id_of_the_list_is_counted(count, dim):
+    """Whether an item has it or not, and also where there is no item, or no row, at all."""
+    P = _api()
+    rng = np.random.default_rng(count)
+    ids = rng.integers(-3, 60, count).astype(np.int32)
+    bad = int((ids >= 50).sum())
+    assert bad > 0
+    table = torch.ones(50, dim, device="cuda")
+    for offsets in ([0, 5, count], [7, 20], [count // 2, count // 2], [0]):
+        o = torch.tensor(offsets, device="cuda")
+        rejected = torch.tensor([3], dtype=torch.int32, device="cuda")
+        P.embed(table, _gpu(ids), o, rejected=rejected)
+        assert int(rejected) == 3 + bad
+        P.embed_grad(torch.ones(len(offsets) - 1, dim, device="cuda"), _gpu(ids), 50, o, rejected=rejected)
+        assert int(rejected) == 3 + 2 * bad
+        P.embed_grad(torch.ones(len(offsets) - 1, dim, device="cuda"), _gpu(ids), 0, o, rejected=rejected)
+        assert int(rejected) == 3 + 2 * bad + int((ids >= 0).sum())
