@@ -147,11 +147,15 @@ int lanes_log2(int pieces) {
     return l;
 }
 
+constexpr int64_t kMostBlocks = 0xffffffff / kBlock;    // workgroups: a launch has fewer than 2^32 threads
 constexpr int64_t kHalfCache = int64_t(128) << 20;  // half the 256 MB before the memory
 
 // ---- embedding --------------------------------------------------------------------------------------------------------
 
 constexpr int64_t kFewPerItem = 2048;  // tokens up to which each item has a workgroup
+
+// Whether items have pieces of the list rather than a workgroup each: long lists, and more items than a launch has workgroups.
+bool in_pieces(int64_t count, int64_t items) { return count > kFewPerItem || (count > 0 && items > kMostBlocks); }
 
 // Rows of 256 bytes and more have waves of their own (k_wave_sum).
 bool wide_rows(int32_t type, int dim) { return (int64_t)dim * type_size(type) >= 256; }
@@ -267,8 +271,7 @@ void launch_zeros(O* out, int64_t out_ld, int64_t rows, int dim, hipStream_t str
 extern "C" {
 
 int64_t dynlp_embed_workspace(int64_t count, int64_t items, int32_t dim) {
-    (void)items;
-    if (count <= kFewPerItem || count > kMostRows || dim < 1) return 0;
+    if (!in_pieces(count, items) || count > kMostRows || dim < 1) return 0;
     return sum_space_bytes(count, dim, -1);
 }
 
@@ -280,7 +283,7 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
     if (out->dim != table->dim) REFUSE("out has rows of %d elements, the table of %d", out->dim, table->dim);
     if (out->rows != tokens->items) REFUSE("out has %lld rows for %lld items", (long long)out->rows, (long long)tokens->items);
     if (tokens->count > 0 && table->rows == 0) REFUSE("%lld tokens and a table without rows", (long long)tokens->count);
-    const bool pieces = tokens->offsets && tokens->count > kFewPerItem;
+    const bool pieces = tokens->offsets && in_pieces(tokens->count, tokens->items);
     CHECK(check_workspace(call, pieces ? dynlp_embed_workspace(tokens->count, tokens->items, table->dim) : 0));
     if (overlap(*table, *out)) REFUSE("out overlaps the table");
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
@@ -293,7 +296,9 @@ dynlp_status dynlp_embed(const dynlp_matrix* table, const dynlp_tokens* tokens, 
         const T* rows = static_cast<const T*>(table->data);
         T* to = static_cast<T*>(out->data);
         const int64_t n = ceil_div(dim, V);
-        if (!t.offsets) {
+        if (t.count == 0) {
+            launch_zeros(to, out->stride, t.items, dim, stream);
+        } else if (!t.offsets) {
             k_embed_rows<T, V><<<(unsigned)ceil_div(t.count * n, kBlock * kRowsAhead), kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, (int)n);
         } else if (!pieces) {
             k_embed_items<T, V><<<(unsigned)t.items, kBlock, 0, stream>>>(t, rows, table->stride, to, out->stride, dim, lanes_log2((int)n));

@@ -129,3 +129,23 @@ def test_every_rejected_id_of_the_list_is_counted(count, dim):
         assert int(rejected) == 3 + 2 * bad
         P.embed_grad(torch.ones(len(offsets) - 1, dim, device="cuda"), _gpu(ids), 0, o, rejected=rejected)
         assert int(rejected) == 3 + 2 * bad + int((ids >= 0).sum())
+
+
+@pytest.mark.parametrize("count", [0, 37, 2048])
+def test_more_items_than_a_launch_has_workgroups(count):
+    """2^24 + 1 items with few tokens: 2^32 threads, where an item has a workgroup."""
+    rng = np.random.default_rng(count)
+    items = 2 ** 24 + 1
+    table, exact = _random(rng, 40, 4, torch.float32)
+    ids = _ids(rng, count, 40)
+    with_tokens = np.unique(np.concatenate([[0, items - 1], rng.integers(0, items, 20)]))
+    cuts = np.concatenate([[0], np.sort(rng.integers(0, count + 1, len(with_tokens) - 1)), [count]])
+    offsets = torch.zeros(items + 1, dtype=torch.int64, device="cuda")
+    offsets[_gpu(with_tokens + 1)] = _gpu(np.diff(cuts))
+    torch.cumsum(offsets, 0, out=offsets)
+    out = torch.full((items, 4), float("nan"), device="cuda")
+    _embed_into(out, table, _gpu(ids), offsets)
+    want, magnitude, terms = S.embed(exact, ids, cuts)
+    _hold_sum(out[_gpu(with_tokens)], want, magnitude, terms)
+    out[_gpu(with_tokens)] = 0.0
+    assert not out.any()
