@@ -26,7 +26,7 @@ struct AdamwTensor {
     float keep;       // 1 - lr * weight_decay
     uint32_t key;     // of the dither
     int32_t types;    // param | grad << 4 | copy << 8
-    int32_t block;    // first workgroup
+    int32_t block;    // first workgroup; below 0 for the rest of a tensor that a launch before this one began
 };
 
 struct AdamwBatch {

@@ -641,11 +641,15 @@ dynlp_status dynlp_adamw_step(int32_t count, const dynlp_adamw_tensor* tensors, 
         const dynlp_adamw_tensor& t = tensors[k];
         if (t.n == 0) continue;
         const int64_t mine = ceil_div(t.n, kStateBlock * (kBlock / kWave));
-        if (b.count == kAdamwTensors || blocks + mine > 0x7fffffff) launch();
-        AdamwTensor& d = b.t[b.count++];
-        d = AdamwTensor{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (float)(1.0 - o->lr * (double)t.weight_decay),
-                        dither_mix(key ^ (uint32_t)k), t.param_type | t.grad_type << 4 | t.copy_type << 8, (int32_t)blocks};
-        blocks += mine;
+        // a tensor that fills a launch goes on in the next, where its first workgroup (2^30 at most) lies before the launch's
+        for (int64_t done = 0; done < mine;) {
+            if (b.count == kAdamwTensors || blocks == kMostBlocks) launch();
+            b.t[b.count++] = AdamwTensor{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, (float)(1.0 - o->lr * (double)t.weight_decay),
+                                         dither_mix(key ^ (uint32_t)k), t.param_type | t.grad_type << 4 | t.copy_type << 8, (int32_t)(blocks - done)};
+            const int64_t now = std::min(mine - done, kMostBlocks - blocks);
+            blocks += now;
+            done += now;
+        }
     }
     launch();
     return launched();

@@ -149,3 +149,26 @@ def test_more_items_than_a_launch_has_workgroups(count):
     _hold_sum(out[_gpu(with_tokens)], want, magnitude, terms)
     out[_gpu(with_tokens)] = 0.0
     assert not out.any()
+
+
+def test_a_tensor_of_more_workgroups_than_a_launch_has():
+    """2^34 + 1,030 elements, 2^24 + 2 workgroups: a step changes what has a gradient, at the ends of the launches too, and nothing else."""
+    if torch.cuda.mem_get_info()[0] < 140e9:
+        pytest.skip("103 GB of states, gradients and parameters, and room to look at them")
+    P = _api()
+    n, launch = 2 ** 34 + 1030, (2 ** 24 - 1) * 1024
+    at = torch.tensor([0, 5, 2 ** 32 + 3, launch - 1, launch, launch + 1024, 2 ** 34 - 1, 2 ** 34, n - 1], device="cuda")
+    params, grads = ([torch.zeros(k, dtype=torch.bfloat16, device="cuda") for k in (n, 300)] for _ in range(2))
+    states = [P.adamw_state(p, bits=8) for p in params]
+    grads[0][at] = grads[1][:len(at)] = torch.linspace(-0.5, 0.75, len(at), device="cuda").bfloat16()
+    P.adamw_step(params, grads, states, step=1, lr=0.01, seed=3)
+
+    def others(t):
+        return sum(int(c.count_nonzero()) for c in t.split(2 ** 30)) - int(t[torch.unique(at if len(t) == n else at // 256)].count_nonzero())
+
+    assert torch.equal(params[0][at], params[1][:len(at)]) and bool((params[0][at] != 0).all()) and others(params[0]) == 0
+    for codes, scales in (states[0][::2], states[0][1::2]):
+        codes = codes.view(torch.uint8)
+        assert bool((codes[at] != 0).all()) and others(codes) == 0 and bool((scales[at // 256] != 0).all()) and others(scales) == 0
+    del params, grads, states, codes, scales
+    torch.cuda.empty_cache()
