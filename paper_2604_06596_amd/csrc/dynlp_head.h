@@ -481,11 +481,11 @@ __device__ inline bool head_dz(const Loss& g, int64_t row, int64_t rows, const R
 }
 
 // Loss, dz and dh of a tile of rows: logits, softmax and the product with W, without leaving the registers.  For heads whose W and dweight do
-// not fit a workgroup, and where no dweight is asked for.
+// not fit a workgroup, and where no dweight is asked for.  Rows from row0 on.
 template <typename T, int CT>
-__global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g) {
+__global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g, int64_t row0) {
     constexpr int NT = kHeadTiles;
-    const int64_t first = (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
+    const int64_t first = row0 + (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
     if (first >= a.rows) return;
     const int q = lane_id() >> 4, r = lane_id() & 15;
     const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
@@ -860,26 +860,29 @@ inline int64_t fused_bytes(int dim) {
     return all > slots ? all : slots;
 }
 
-// Sums the parts: 16 neighbouring elements per workgroup, 16 groups of lanes taking turns on the parts, then joined in order.
+// Sums the parts: 16 neighbouring elements per turn of a workgroup, 16 groups of lanes taking turns on the parts, then joined in order.
 __global__ __launch_bounds__(kBlock) void k_head_join(const float* part, int splits, int classes, int dim, float* dweight, float* dbias) {
     __shared__ float sums[16][17];
     const int e = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t size = (int64_t)classes * (dim + 1);
-    const int64_t at = (int64_t)blockIdx.x * 16 + e;
-    float s = 0.f;
-    if (at < size)
+    for (int64_t first = (int64_t)blockIdx.x * 16; first < size; first += (int64_t)gridDim.x * 16) {
+        const int64_t at = first + e;
+        float s = 0.f;
+        if (at < size)
 #pragma unroll 8
-        for (int k = g; k < splits; k += 16) s += part[k * size + at];
-    sums[g][e] = s;
-    __syncthreads();
-    if (g == 0 && at < size) {
-        for (int k = 1; k < 16; ++k) s += sums[k][e];
-        const int c = (int)(at / (dim + 1)), k = (int)(at - (int64_t)c * (dim + 1));
-        if (k < dim) {
-            if (dweight) dweight[(int64_t)c * dim + k] = s;
-        } else if (dbias) {
-            dbias[c] = s;
+            for (int k = g; k < splits; k += 16) s += part[k * size + at];
+        sums[g][e] = s;
+        __syncthreads();
+        if (g == 0 && at < size) {
+            for (int k = 1; k < 16; ++k) s += sums[k][e];
+            const int c = (int)(at / (dim + 1)), k = (int)(at - (int64_t)c * (dim + 1));
+            if (k < dim) {
+                if (dweight) dweight[(int64_t)c * dim + k] = s;
+            } else if (dbias) {
+                dbias[c] = s;
+            }
         }
+        __syncthreads();
     }
 }
 

@@ -571,15 +571,16 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
                 fused(Tiles<1>());
             }
         } else if (a.rows > 0) {
-            k_head_loss<T, CT><<<(unsigned)ceil_div(a.rows, kHeadRows), kBlock, 0, stream>>>(a, g);
+            for (int64_t row = 0; row < a.rows; row += kMostBlocks * kHeadRows)
+                k_head_loss<T, CT><<<(unsigned)std::min(ceil_div(a.rows - row, kHeadRows), kMostBlocks), kBlock, 0, stream>>>(a, g, row);
         }
         if (!bytes) return;
         if (a.rows > 0 && !s.fused) {
             const Outer o{a.h, s.dz, s.kept, s.part, a.ld_h, a.rows, s.per_wave, a.dim, a.classes};
             k_head_outer<T, CT><<<dim3((unsigned)s.splits, (unsigned)ceil_div(a.dim, 16 * Piece<T>::n)), kBlock, 0, stream>>>(o);
         }
-        k_head_join<<<(unsigned)ceil_div((int64_t)a.classes * (a.dim + 1), 16), kBlock, 0, stream>>>(s.part, a.rows > 0 ? s.splits : 0, a.classes,
-                                                                                                     a.dim, dweight, dbias);
+        k_head_join<<<(unsigned)std::min(ceil_div((int64_t)a.classes * (a.dim + 1), 16), kMostBlocks), kBlock, 0, stream>>>(
+            s.part, a.rows > 0 ? s.splits : 0, a.classes, a.dim, dweight, dbias);
     });
     return launched();
 }

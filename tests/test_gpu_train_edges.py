@@ -172,3 +172,55 @@ def test_a_tensor_of_more_workgroups_than_a_launch_has():
         assert bool((codes[at] != 0).all()) and others(codes) == 0 and bool((scales[at // 256] != 0).all()) and others(scales) == 0
     del params, grads, states, codes, scales
     torch.cuda.empty_cache()
+
+
+def test_a_head_of_four_million_columns():
+    """dweight's 2^28 elements and more are joined 16 to a workgroup: 2^32 threads.  h is zero but for 16 columns, so that a logit has 17 roundings."""
+    P = _api()
+    rng = np.random.default_rng(8)
+    dim, classes = 2 ** 22 + 70, 64
+    some = _gpu(np.concatenate([np.arange(8), dim - 8 + np.arange(8)]))
+    h = torch.zeros(2, dim, device="cuda")
+    h[:, some] = _random(rng, 2, 16, torch.float32)[0]
+    W = torch.randn(classes, dim, device="cuda")
+    label = np.array([3, 63])
+    got = dict(zip(("loss", "dh", "dweight", "dbias"), P.head_loss(h, W, None, _gpu(label.astype(np.int32)))))
+    eh, eW = (x[:, some].double().cpu().numpy() for x in (h, W))
+    ref = S.head_loss(eh, eW, None, hard=label)
+    off = 19 * U * (np.abs(eh) @ np.abs(eW).T).max(axis=1, keepdims=True)
+    p, dz = ref["soft"], np.abs(ref["dz"])
+    ddz = p * (np.exp(2 * off) - 1 + (classes + 16) * U) + 4 * U * (p + ref["target"]) + (classes + 4) * U * dz
+    hold(got["dbias"], ref["dbias"], (ddz + 2 * U * dz).sum(axis=0))
+    hold(got["dweight"][:, some], ref["dweight"], (ddz + 2 * U * dz).T @ np.abs(eh))
+    got["dweight"][:, some] = 0.0
+    assert not got["dweight"].any()
+    wide = W.double()
+    hold(got["dh"], (_gpu(ref["dz"]) @ wide).cpu().numpy(), (_gpu(ddz) @ wide.abs()).cpu().numpy())
+
+
+def test_the_loss_of_as_many_rows_as_there_may_be():
+    """2^31 - 2 rows: 2^24 workgroups of 128 rows.  2 (D + 3) u |h W| + (C + 16) u (1 + |lse - z|) is below 40 u for the last row."""
+    P = _api()
+    rows = 2 ** 31 - 2
+    h, hard = torch.zeros(rows, 1, dtype=torch.float16, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    h[-1], hard[-1] = 2.0, 1
+    loss = P.head_loss(h, torch.tensor([[0.0], [1.0]], dtype=torch.float16, device="cuda"), None, hard, grads=False)[0]
+    hold(loss[-1:], np.log1p(np.exp([-2.0])), 40 * U)
+    loss[-1] = loss[0]
+    hold(torch.stack([loss.min(), loss.max()]), np.full(2, np.log(2.0)), 40 * U)
+
+
+def test_rows_of_sixteen_million_columns():
+    """A wave has 256 columns of a piece of the list, and so has a wave that joins runs: 65,538 of them side by side."""
+    P = _api()
+    rng = np.random.default_rng(9)
+    count, dim = 2049, 2 ** 24 + 300
+    table = torch.randn(3, dim, device="cuda")
+    ids, w = _ids(rng, count, 3), rng.random(count).astype(np.float32)
+    offsets = np.array([0, 1001, count])
+    args = _gpu(ids), _gpu(offsets), _gpu(w)
+    factor, _, terms = S.embed(np.eye(3), ids, offsets, w)  # a row's factor in an item
+    out = P.embed(table, *args)
+    for part in (slice(0, 4096), slice(2 ** 23, 2 ** 23 + 4096), slice(dim - 4096, dim)):
+        rows = table[:, part].double().cpu().numpy()
+        _hold_sum(out[:, part], factor @ rows, factor @ np.abs(rows), terms)
