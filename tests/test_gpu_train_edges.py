@@ -151,6 +151,41 @@ def test_more_items_than_a_launch_has_workgroups(count):
     assert not out.any()
 
 
+def _least_ms(f, turns=4):
+    f()
+    times = []
+    for _ in range(turns):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        f()
+        end.record()
+        end.synchronize()
+        times.append(begin.elapsed_time(end))
+    return min(times)
+
+
+@pytest.mark.parametrize("kind, dim, empty, most_ms", [("bfloat16", 128, 1_000_000, 20.0), ("float32", 16, 8_000_000, 5.0)])
+def test_a_long_run_of_items_without_tokens(kind, dim, empty, most_ms):
+    """Two texts with a million or more empty items between them.  The zeros are 256 and 512 MB, 0.1 ms; a search for the next text takes some tens of reads
+    one after the other.  A look at one item after the other by a wave takes 0.2 us and more each (200 ms), by a workgroup 256 at a time 15 ms."""
+    P = _api()
+    rng = np.random.default_rng(dim)
+    count = 9001
+    ids, w = _ids(rng, count, 300), rng.standard_normal(count).astype(np.float32)
+    table, exact = _random(rng, 300, dim, TYPES[kind])
+    offsets = torch.full((empty + 3,), 4003, dtype=torch.int64, device="cuda")
+    offsets[0], offsets[-1] = 0, count
+    args = _gpu(ids), offsets, _gpu(w)
+    out = P.embed(table, *args)
+    assert out.shape == (empty + 2, dim) and not out[1:-1].any()
+    _hold_sum(out[[0, -1]], *S.embed(exact, ids, [0, 4003, count], w))
+    assert _least_ms(lambda: P.embed(table, *args)) < most_ms
+    out.normal_()
+    g = P.embed_grad(out, args[0], 300, *args[1:])
+    _hold_sum(g, *S.embed_grad(out[[0, -1]].double().cpu().numpy(), ids, 300, [0, 4003, count], w))
+    assert _least_ms(lambda: P.embed_grad(out, args[0], 300, *args[1:])) < most_ms
+
+
 def test_a_tensor_of_more_workgroups_than_a_launch_has():
     """2^34 + 1,030 elements, 2^24 + 2 workgroups: a step changes what has a gradient, at the ends of the launches too, and nothing else."""
     if torch.cuda.mem_get_info()[0] < 140e9:
