@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_items(TokenList t, const T* ta
             *w = t.weights ? t.weights[begin + i] : 1.f;
             return id;
         },
-        t.scale, out + b * out_ld);
+        begin < end ? t.scale : 0.f, out + b * out_ld);  // zeros without tokens, whatever the scale
 }
 
 constexpr int kFewTokens = 8192;     // 32 for each thread of a workgroup

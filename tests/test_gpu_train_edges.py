@@ -186,6 +186,20 @@ def test_a_long_run_of_items_without_tokens(kind, dim, empty, most_ms):
     assert _least_ms(lambda: P.embed_grad(out, args[0], 300, *args[1:])) < most_ms
 
 
+@pytest.mark.parametrize("dim", [16, 128])
+@pytest.mark.parametrize("count", [60, 9001])
+def test_items_without_tokens_are_zeros_whatever_the_scale(count, dim):
+    P = _api()
+    table = torch.ones(5, dim, device="cuda")
+    ids = torch.zeros(count, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, 0, 30, 30, count, count], device="cuda")
+    for scale in (float("inf"), float("nan"), -2.0):
+        out = P.embed(table, ids, offsets, None, scale)
+        assert torch.equal(out[[0, 2, 4]], torch.zeros(3, dim, device="cuda"))
+        want = torch.full((2, dim), scale, device="cuda") * torch.tensor([[30.0], [count - 30.0]], device="cuda")
+        assert torch.equal(out[[1, 3]].nan_to_num(7.0), want.nan_to_num(7.0))
+
+
 def test_a_tensor_of_more_workgroups_than_a_launch_has():
     """2^34 + 1,030 elements, 2^24 + 2 workgroups: a step changes what has a gradient, at the ends of the launches too, and nothing else."""
     if torch.cuda.mem_get_info()[0] < 140e9:
