@@ -154,7 +154,7 @@ typedef struct dynlp_adamw_tensor {
     int32_t param_type, grad_type, copy_type; /* dynlp_type */
 } dynlp_adamw_tensor;
 typedef struct dynlp_adamw_options {
-    double lr, beta1, beta2, eps; /* lr >= 0 and finite, 0 <= beta < 1, eps > 0 */
+    double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps > 0; eps, lr / (1 - beta1^step) and lr weight_decay finite, and eps > 0, in 32 bits */
     int64_t step;                 /* 1 for the first step */
     const float* grad_scale;      /* one float32 on the device, or NULL */
     uint32_t seed;

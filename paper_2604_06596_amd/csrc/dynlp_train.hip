@@ -597,21 +597,6 @@ dynlp_status dynlp_adamw_step(int32_t count, const dynlp_adamw_tensor* tensors, 
     if (!(o->eps > 0.0) || !std::isfinite(o->eps)) REFUSE("eps = %g", o->eps);
     if (o->step < 1) REFUSE("step = %lld: the first is 1", (long long)o->step);
     if (o->state_bits != 32 && o->state_bits != 8) REFUSE("states of %d bits: 32 or 8 are possible", o->state_bits);
-    const bool bits8 = o->state_bits == 8;
-    auto aligned = [](const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size == 0; };
-    for (int32_t k = 0; k < count; ++k) {
-        const dynlp_adamw_tensor& t = tensors[k];
-        if (t.n < 0 || t.n > (int64_t(1) << 40)) REFUSE("tensor %d: %lld elements", k, (long long)t.n);
-        if (t.param_type < DYNLP_FLOAT32 || t.param_type > DYNLP_FLOAT16 || t.grad_type < DYNLP_FLOAT32 || t.grad_type > DYNLP_FLOAT16 ||
-            (t.copy && (t.copy_type < DYNLP_FLOAT32 || t.copy_type > DYNLP_FLOAT16)))
-            REFUSE("tensor %d: a type is not a dynlp_type", k);
-        if (!std::isfinite(t.weight_decay) || t.weight_decay < 0.f) REFUSE("tensor %d: weight_decay = %g", k, t.weight_decay);
-        if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (bits8 && (!t.m_scale || !t.v_scale)))) REFUSE("tensor %d: an array is NULL", k);
-        if (!aligned(t.param, type_size(t.param_type)) || !aligned(t.grad, type_size(t.grad_type)) || (t.copy && !aligned(t.copy, type_size(t.copy_type))) ||
-            (bits8 ? !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4) : !aligned(t.m, 4) || !aligned(t.v, 4)))
-            REFUSE("tensor %d: an array is not aligned to its elements", k);
-    }
-    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     AdamwBatch b{};
     b.grad_scale = o->grad_scale;
     b.beta1 = (float)o->beta1;
@@ -621,6 +606,24 @@ dynlp_status dynlp_adamw_step(int32_t count, const dynlp_adamw_tensor* tensors, 
     b.step_size = (float)(o->lr / (1.0 - std::pow(o->beta1, (double)o->step)));
     b.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o->beta2, (double)o->step)));
     b.eps = (float)o->eps;
+    if (!(b.eps > 0.f) || !std::isfinite(b.eps)) REFUSE("eps = %g is %g in 32 bits", o->eps, b.eps);
+    if (!std::isfinite(b.step_size)) REFUSE("lr = %g makes a step of %g in 32 bits", o->lr, b.step_size);
+    const bool bits8 = o->state_bits == 8;
+    auto aligned = [](const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size == 0; };
+    for (int32_t k = 0; k < count; ++k) {
+        const dynlp_adamw_tensor& t = tensors[k];
+        if (t.n < 0 || t.n > (int64_t(1) << 40)) REFUSE("tensor %d: %lld elements", k, (long long)t.n);
+        if (t.param_type < DYNLP_FLOAT32 || t.param_type > DYNLP_FLOAT16 || t.grad_type < DYNLP_FLOAT32 || t.grad_type > DYNLP_FLOAT16 ||
+            (t.copy && (t.copy_type < DYNLP_FLOAT32 || t.copy_type > DYNLP_FLOAT16)))
+            REFUSE("tensor %d: a type is not a dynlp_type", k);
+        if (!std::isfinite(t.weight_decay) || t.weight_decay < 0.f) REFUSE("tensor %d: weight_decay = %g", k, t.weight_decay);
+        if (!std::isfinite((float)(o->lr * (double)t.weight_decay))) REFUSE("tensor %d: weight_decay = %g with lr = %g", k, t.weight_decay, o->lr);
+        if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v || (bits8 && (!t.m_scale || !t.v_scale)))) REFUSE("tensor %d: an array is NULL", k);
+        if (!aligned(t.param, type_size(t.param_type)) || !aligned(t.grad, type_size(t.grad_type)) || (t.copy && !aligned(t.copy, type_size(t.copy_type))) ||
+            (bits8 ? !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4) : !aligned(t.m, 4) || !aligned(t.v, 4)))
+            REFUSE("tensor %d: an array is not aligned to its elements", k);
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const uint32_t key = dither_mix(dither_mix(o->seed) ^ (uint32_t)o->step);
     // Arrays that are larger than half the cache before the memory leave nothing of use in it: they are read and written past the caches (24M elements,
     // 32 bits: 119 us, 132 us through the caches; 256M, 8 bits: 876 and 894 us)

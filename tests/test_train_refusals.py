@@ -1,7 +1,8 @@
-"""What the student's operators refuse before anything is enqueued: outputs in the memory of inputs.  Addresses are never looked at: these run without
-a GPU, and none of them is a call that would be accepted."""
+"""What the student's operators refuse before anything is enqueued: outputs in the memory of inputs, numbers that 32 bits do not hold.  Addresses are
+never looked at: these run without a GPU, and none of them is a call that would be accepted."""
 import itertools
 
+import numpy as np
 import pytest
 
 from paper_2604_06596_amd import train as T
@@ -68,3 +69,14 @@ def test_other_outputs_in_the_memory_of_inputs_are_refused():
     _refused(L.dynlp_embed_grad(T._Matrix(A, 5, 16, 16, 1), tokens, T._Matrix(A + 64, 50, 16, 16, 0), call), "out overlaps grad")
     huge = T._Matrix(A, 2 ** 31 - 2, 1 << 40, 16, 0)  # rows times stride pass 64 bits
     _refused(L.dynlp_embed(huge, tokens, T._Matrix(A + (1 << 50), 5, 1 << 40, 16, 0), call), "out overlaps the table")
+
+
+@pytest.mark.parametrize("option, decay, word", [(dict(eps=1e-50), 0.0, "eps"), (dict(eps=1e39), 0.0, "eps"), (dict(lr=1e39), 0.0, "lr"),
+                                                 (dict(lr=1e35, beta1=0.99999), 0.0, "lr"), (dict(lr=1e30), 1e30, "weight_decay")])
+def test_adamw_refuses_what_32_bits_do_not_hold(option, decay, word):
+    """eps that is nothing in 32 bits would divide a zero gradient's step by zero; a step or a decay that is infinite leaves no parameter."""
+    table = np.zeros(1, dtype=T._ADAMW_TENSOR)
+    for name, value in dict(n=10, param=A, grad=A << 1, m=A << 2, v=A << 3, weight_decay=decay).items():
+        table[name] = value
+    o = dict(dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=None, seed=0, state_bits=32), **option)
+    _refused(T._library().dynlp_adamw_step(1, table.ctypes.data, T._AdamwOptions(**o), T._Call(None, None, 0)), word)
