@@ -3,6 +3,10 @@
 Arguments are torch tensors on one GPU (only their addresses are used).  Calls run on torch's current stream of that GPU, return
 without waiting for it, and raise ``DynLPError`` for what the library refuses.  Outputs and scratch memory come from torch's
 allocator; under HIP graph capture the calls allocate from the capture's pool and can be replayed.
+
+Nothing here is part of torch's autograd: outputs have no history, also where inputs require gradients.  ``head_loss`` and
+``embed_grad`` return the gradients, and ``adamw_step`` counts as a change of its tensors, so that a backward pass that has
+saved one of them says so.
 """
 from __future__ import annotations
 
@@ -10,6 +14,7 @@ import ctypes as ct
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from .binding import DynLPError, load_library
 
@@ -283,3 +288,5 @@ def adamw_step(params, grads, states, *, step, lr, betas=(0.9, 0.999), eps=1e-8,
     L = _library()
     call, _ = _call(device)
     _check(_run(device, L.dynlp_adamw_step, count, table.ctypes.data, o, call))
+    # what autograd has saved of these tensors is no longer theirs
+    increment_version([*params, *(t for s in states for t in s), *(copies or ())])

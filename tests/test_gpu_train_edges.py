@@ -200,6 +200,25 @@ def test_items_without_tokens_are_zeros_whatever_the_scale(count, dim):
         assert torch.equal(out[[1, 3]].nan_to_num(7.0), want.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_is_a_change_of_its_tensors(bits):
+    """torch counts changes of a tensor, and refuses a backward pass through one that has changed since: a step is such a change, of copies too."""
+    P = _api()
+    p, c = torch.ones(300, device="cuda", requires_grad=True), torch.ones(300, device="cuda", requires_grad=True)
+    state = P.adamw_state(p, bits)
+    before = [t._version for t in (p, c) + state]
+    saved = [(p * p).sum(), (c * c).sum()]
+    P.adamw_step([p], [torch.ones(300, device="cuda")], [state], step=1, lr=0.1, copies=[c])
+    assert all(t._version > v for t, v in zip((p, c) + state, before))
+    for s in saved:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            s.backward()
+    with torch.inference_mode():
+        q = torch.ones(300, device="cuda")
+        P.adamw_step([q], [torch.ones(300, device="cuda")], [P.adamw_state(q, bits)], step=1, lr=0.1)
+    assert torch.equal(q, p)
+
+
 def test_a_tensor_of_more_workgroups_than_a_launch_has():
     """2^34 + 1,030 elements, 2^24 + 2 workgroups: a step changes what has a gradient, at the ends of the launches too, and nothing else."""
     if torch.cuda.mem_get_info()[0] < 140e9:
