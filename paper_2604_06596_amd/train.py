@@ -99,7 +99,7 @@ def _matrix(t, name, device):
         _refuse(f"{name} is on {t.device}, not on {device}")
     rows, dim = t.shape
     stride, step = t.stride()
-    if dim > 1 and step != 1:
+    if rows and dim > 1 and step != 1:  # without rows strides say nothing, and are zeros where numpy made the tensor
         _refuse(f"{name}: the elements of a row have to be contiguous")
     return _Matrix(t.data_ptr(), rows, stride if rows > 1 else max(dim, 1), dim, _TYPES[t.dtype])
 

@@ -292,3 +292,18 @@ def test_rows_of_sixteen_million_columns():
     for part in (slice(0, 4096), slice(2 ** 23, 2 ** 23 + 4096), slice(dim - 4096, dim)):
         rows = table[:, part].double().cpu().numpy()
         _hold_sum(out[:, part], factor @ rows, factor @ np.abs(rows), terms)
+
+
+def test_matrices_without_rows():
+    """Whatever their strides, which numpy's are zeros of."""
+    P = _api()
+    none = torch.from_numpy(np.zeros((0, 8), dtype=np.float32)).cuda()
+    W = torch.ones(3, 8, device="cuda")
+    no_ids, no_offsets = torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    for empty in (none, torch.empty_strided((0, 8), (1, 4), device="cuda"), W[:0]):
+        soft, hard = P.head_labels(empty, W)
+        assert soft.shape == (0, 3) and hard.shape == (0,)
+        loss, dh, dweight, dbias = P.head_loss(empty, W, None, soft)
+        assert loss.shape == (0,) and dh.shape == (0, 8) and torch.equal(dweight, torch.zeros_like(W)) and not dbias.any()
+        assert P.embed(empty, no_ids).shape == (0, 8) and P.embed(empty, no_ids, no_offsets).shape == (0, 8)
+        assert torch.equal(P.embed_grad(empty, no_ids, 5, no_offsets), torch.zeros(5, 8, device="cuda"))
