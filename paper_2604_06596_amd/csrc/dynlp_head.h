@@ -10,8 +10,8 @@
 //   dh       dh^T = W^T dz^T.  The right operand (k = class, column = row r) is what the lane holds after the softmax.  The left one
 //            needs W by columns: pieces of W's rows, for two-byte types transposed between registers.  Result: row r, n consecutive columns.
 //   dweight  dz^T h.  Both operands are read row by row of h and dz, h in pieces, transposed between registers where needed.
-// Precision: products of bfloat16 and float16 values are exact in the matrix cores, sums are float32; dz, which is float32, is taken in bfloat16 terms
-// (two for dh, three for dweight), or the product is made in float32 (float32 and float16 heads).
+// Precision: products of bfloat16 and float16 values are exact in the matrix cores, sums are float32; dz, which is float32, is taken in three
+// bfloat16 terms, which hold all of it, or the product is made in float32 (float32 and float16 heads).
 // What bounds it: h is read once (from memory; for dweight again, from the L2) and dh written once.  1M rows x 256 bfloat16, 50 classes, with soft
 // targets: 378 us (3.3 TB/s of what has to move; the first kernels, with dz through memory and h read twice, 905 us).  100,000 x 64 float32, 10
 // classes: 24 us, of which each workgroup spends half on its start and end.
@@ -322,15 +322,14 @@ struct Loss {
     uint8_t* kept;   // rows: 0 if left out
 };
 
-// Two values rounded to bfloat16, the first in the low half; TERMS of them hold 8 TERMS bits of the values.
+// Two values rounded to bfloat16, the first in the low half; three such terms hold all 24 bits of the values.
 __device__ inline uint32_t bf16_pair(float x, float y) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
 }
-template <int TERMS>
-__device__ inline void bf16_terms(float x, float y, uint32_t (&term)[TERMS]) {
-    for (int k = 0; k < TERMS; ++k) {
+__device__ inline void bf16_terms(float x, float y, uint32_t (&term)[3]) {
+    for (int k = 0; k < 3; ++k) {
         term[k] = bf16_pair(x, y);
         x -= __uint_as_float(term[k] << 16);
         y -= __uint_as_float(term[k] & 0xffff0000u);
@@ -359,9 +358,9 @@ __device__ inline void store_dh(const Head& a, int64_t first, int base, const f3
     }
 }
 // dz of a lane's row and classes 16 t + 4 q + i in bfloat16 terms: pairs (i = 0, 1) and (2, 3).
-template <int CT, int TERMS>
+template <int CT>
 struct DzTerms {
-    uint32_t v[CT][2][TERMS];
+    uint32_t v[CT][2][3];
     __device__ inline void make(const f32x4 (&dz)[CT]) {
         for (int t = 0; t < CT; ++t)
             for (int k = 0; k < 2; ++k) bf16_terms(dz[t][2 * k], dz[t][2 * k + 1], v[t][k]);
@@ -373,9 +372,10 @@ struct DzTerms {
         return u32x4{v[2 * p][0][term], v[2 * p][1][term], two ? v[o][0][term] : 0u, two ? v[o][1][term] : 0u};
     }
 };
-// In bfloat16 dh takes two terms of dz, which leave out 2^-17 of it: far below the rounding of dh itself.
-template <int CT, int NT, int TERMS, typename W>
-__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const DzTerms<CT, TERMS> (&dz)[NT], const bool (&kept)[NT], bf16* dh,
+// Two terms would leave out 2^-17 of dz, which shows in dh where classes cancel, as what W's rows have in common always does (dz sums to nothing over
+// the classes of a row).  The third costs 1 to 3% of a step: 1M x 256, 50 classes, 399 us with two, 410 with three.
+template <int CT, int NT, typename W>
+__device__ inline void head_dh(const Head& a, const W& w, int64_t first, const DzTerms<CT> (&dz)[NT], const bool (&kept)[NT], bf16* dh,
                                int64_t ld_dh) {
     constexpr int P = (CT + 1) / 2;
     const int q = lane_id() >> 4, r = lane_id() & 15;
@@ -396,10 +396,8 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const D
             }
             for (int t = 0; t < 4; ++t) {
                 const u32x4 left = column_of(x, t);
-                for (int m = 0; m < NT; ++m) {
-                    acc[m][t] = mma(left, dz[m].operand(p, 1), acc[m][t], bf16());
-                    acc[m][t] = mma(left, dz[m].operand(p, 0), acc[m][t], bf16());
-                }
+                for (int m = 0; m < NT; ++m)
+                    for (int k = 2; k >= 0; --k) acc[m][t] = mma(left, dz[m].operand(p, k), acc[m][t], bf16());
             }
         }
         store_dh<CT, NT>(a, first, base, acc, kept, dh, ld_dh);
@@ -504,7 +502,7 @@ __global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g, int64_t ro
     }
     if (!g.dh) return;
     if constexpr (__is_same(T, bf16)) {
-        DzTerms<CT, 2> terms[NT];
+        DzTerms<CT> terms[NT];
         for (int m = 0; m < NT; ++m) terms[m].make(z[m]);
         head_dh<CT, NT>(a, w, first, terms, kept, static_cast<T*>(g.dh), g.ld_dh);
     } else {
@@ -655,7 +653,7 @@ struct SharedDz<bf16, CT> {
     static constexpr int ld = fused_rows(CT) + 8, bytes = 3 * 16 * CT * ld * 2;
     float* p;
     __device__ inline bf16* at(int term, int c, int row) const { return reinterpret_cast<bf16*>(p) + (term * 16 * CT + c) * ld + row; }
-    __device__ inline void put(int row, int q, const DzTerms<CT, 3>& z) {
+    __device__ inline void put(int row, int q, const DzTerms<CT>& z) {
         for (int t = 0; t < CT; ++t)
             for (int k = 0; k < 2; ++k)
                 for (int term = 0; term < 3; ++term) {
@@ -783,7 +781,7 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
                     for (int t = 0; t < CT; ++t) dz.put(row, t, q, z[m][t]);
             }
             if constexpr (__is_same(T, bf16)) {
-                DzTerms<CT, 3> terms[NT];
+                DzTerms<CT> terms[NT];
                 for (int m = 0; m < NT; ++m) {
                     terms[m].make(z[m]);
                     dz.put(mine + 16 * m + r, q, terms[m]);

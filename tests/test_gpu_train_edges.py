@@ -7,6 +7,7 @@ import pytest
 
 from oracle import student as S
 from rounding import hold
+from test_gpu_train_head import SHAPES, _bars
 
 pytestmark = pytest.mark.gpu
 
@@ -219,6 +220,25 @@ def test_a_step_is_a_change_of_its_tensors(bits):
     assert torch.equal(q, p)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows, dim", [(200, 24), (200, 64), (64, 520)])
+def test_gradients_of_classes_that_cancel(rows, dim, kind):
+    """W's rows are 64 and a little, and dz sums to nothing: 64 of dz must cancel to what float32 holds.  All logits are 0, so that exponentials and their sum
+    are exact: dz is a division, a product and a difference away from the definition, 3 u (p + q), and dh's products and sums add (C + 4) u |dz| |W|."""
+    P = _api()
+    rng = np.random.default_rng(dim)
+    classes = 3
+    W = 64.0 + 0.5 * rng.integers(0, 2, (classes, dim))
+    q = rng.random((rows, classes)).astype(np.float32)
+    q /= q.sum(axis=1, keepdims=True)
+    h = torch.zeros(rows, dim, dtype=TYPES[kind], device="cuda")
+    dh = P.head_loss(h, _gpu(W).to(TYPES[kind]), None, _gpu(q))[1]
+    exact = q.astype(np.float64)
+    p = 1.0 / classes
+    dz = exact.sum(axis=1, keepdims=True) * p - exact
+    hold(dh, dz @ W, (3 * U * (exact.sum(axis=1, keepdims=True) * p + exact) + (classes + 4) * U * np.abs(dz)) @ W)
+
+
 def test_a_tensor_of_more_workgroups_than_a_launch_has():
     """2^34 + 1,030 elements, 2^24 + 2 workgroups: a step changes what has a gradient, at the ends of the launches too, and nothing else."""
     if torch.cuda.mem_get_info()[0] < 140e9:
@@ -292,6 +312,19 @@ def test_rows_of_sixteen_million_columns():
     for part in (slice(0, 4096), slice(2 ** 23, 2 ** 23 + 4096), slice(dim - 4096, dim)):
         rows = table[:, part].double().cpu().numpy()
         _hold_sum(out[:, part], factor @ rows, factor @ np.abs(rows), terms)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows, dim, classes", SHAPES)
+def test_gradients_of_h_are_those_of_32_bits(rows, dim, classes, kind):
+    """dh of every type within the bars of a float32 dz: those of test_gpu_train_head.py without the 2^-16 of dz that it leaves to bfloat16."""
+    P = _api()
+    rng = np.random.default_rng(5 * rows + dim)
+    (h, eh), (W, eW) = _random(rng, rows, dim, TYPES[kind]), _random(rng, classes, dim, TYPES[kind], 2.0 / np.sqrt(dim))
+    q = rng.random((rows, classes)).astype(np.float32)
+    ref = S.head_loss(eh, eW, None, q)
+    bar = _bars(eh, eW, None, ref, np.ones(rows), 1.0)["dh"] - 2.0 ** -16 * np.abs(ref["dz"]) @ np.abs(eW)
+    hold(P.head_loss(h, W, None, _gpu(q))[1], ref["dh"], bar)
 
 
 def test_matrices_without_rows():
