@@ -4,7 +4,8 @@ them and labels texts the graph has never held.
     python examples/student.py [--items 20000] [--steps 300] [--bits 8]
 
 Synthetic texts: every class has its own frequent words.  The graph joins texts of the same class more often than others
-(``workloads.sbm``).  One process, one GPU; everything stays on it: ``DynLP.get_labels`` returns the soft rows that ``head_loss`` takes.
+(``workloads.sbm``).  One process, one GPU.  ``DynLP.get_labels`` returns the soft rows that ``head_loss`` takes: here as numpy arrays, as the graph is one of these (a
+context made with ``device_ptrs=True`` takes and returns tensors on the GPU).
 """
 import argparse
 import math

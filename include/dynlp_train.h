@@ -98,7 +98,7 @@ int64_t dynlp_embed_grad_workspace(int64_t count, int64_t items, int32_t dim, in
  * lowest class winning ties (int32; or NULL), as dynlp_get_labels gives them.
  *   h       rows x dim; weight: classes x dim, of h's type, 1 .. DYNLP_MAX_CLASSES classes; bias: classes float32, or NULL
  * A class whose logit is -infinity has probability 0; a row with no other logit is 1/C everywhere, hard label 0.  A logit that is
- * not a number makes the row's soft labels so; it never wins the hard label.
+ * not a number makes the row's soft labels so; for the hard label it counts as -infinity.
  */
 dynlp_status dynlp_head_labels(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, float* soft, int32_t* hard,
                                const dynlp_call* call);

@@ -1,6 +1,6 @@
 """DynLP on AMD MI355X: dynamic batched label propagation behind a C-ABI HIP library.
 
-``build()`` compiles ``csrc/dynlp.hip`` for gfx950 into ``libdynlp.so`` next to this file;
+``build()`` compiles ``csrc/dynlp.hip`` and ``csrc/dynlp_train.hip`` for gfx950 into ``libdynlp.so`` next to this file;
 ``DynLP`` (see ``binding``) is a thin ctypes wrapper with the same call names as the C ABI in
 ``include/dynlp.h``; ``embed``, ``embed_grad``, ``head_labels``, ``head_loss`` and ``adamw_step`` (see ``train``) are those of
 ``include/dynlp_train.h``, which train and ask a student of the labels.  All computation happens in the HIP kernels; there is no CPU path, and

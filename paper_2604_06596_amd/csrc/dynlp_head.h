@@ -12,8 +12,10 @@
 //   dweight  dz^T h.  Both operands are read row by row of h and dz, h in pieces, transposed between registers where needed.
 // Precision: products of bfloat16 and float16 values are exact in the matrix cores, sums are float32; dz, which is float32, is taken in three
 // bfloat16 terms, which hold all of it, or the product is made in float32 (float32 and float16 heads).
+// Terms in float16 would need scales of their own: dz, with a grad_scale of one in a million rows, lies below what float16 holds.  The float32 instruction has
+// an eighth of the rate (153 TFLOP/s, 1,190 in bfloat16), which bounds float16 heads: 1M x 256, 50 classes, 816 us, 410 in bfloat16 in the same run.
 // What bounds it: h is read once (from memory; for dweight again, from the L2) and dh written once.  1M rows x 256 bfloat16, 50 classes, with soft
-// targets: 378 us (3.3 TB/s of what has to move; the first kernels, with dz through memory and h read twice, 905 us).  100,000 x 64 float32, 10
+// targets: 385 us (3.2 TB/s of what has to move; the first kernels, with dz through memory and h read twice, 905 us).  100,000 x 64 float32, 10
 // classes: 24 us, of which each workgroup spends half on its start and end.
 #pragma once
 
@@ -628,9 +630,13 @@ __global__ __launch_bounds__(kBlock) void k_head_outer(Outer o) {
 constexpr int kFusedColumns = 64;  // of a group: a wave's part of dweight
 constexpr int kFusedMost = kFusedColumns * 8;
 
-// Up to 32 classes a wave needs few enough registers for four waves on a SIMD: eight waves with 16 rows each.  Beyond that: four waves with 32 rows
-// each, two on a SIMD (in bfloat16 with 50 classes of 256 columns, 1M rows: 423 us; eight waves 467 us, and 656 us when held to 128 registers.  In
-// float32 with 10 classes of 64 columns, 100,000 rows: 25.7 us with eight waves, 28.2 us with four).
+// Waves of a workgroup, 16 rows each: eight up to 32 classes, four on a SIMD; beyond that four, two on a SIMD.  us with eight and with four waves:
+//   up to 16 classes (128 registers are enough): 100,000 x 64, 10 classes: float32 28.0 and 31.1, bfloat16 22.0 and 25.4; 1M x 256 bfloat16 262 and 280
+//   17 to 32 (8, 44 and 100 bytes a lane go to scratch in float16, float32 and bfloat16): 1M x 256, 29 classes: bfloat16 325 and 310, float32 667 and 687,
+//     float16 444 and 464; 1M x 64 float32, 20 classes: 226 and 241
+//   beyond 32: 1M x 256, 50 classes: bfloat16 436 and 410, float16 879 and 816, but float32 1,037 and 1,303; 200,000 x 128 float32, 64 classes: 167 and 145
+// Where more than 256 columns make a wave of the four hold two groups of dweight's columns, one wave is on a SIMD: 500,000 x 512 bfloat16, 50 classes,
+// 571 us, which eight waves would take 392 for.
 __host__ __device__ constexpr int fused_waves(int class_tiles) { return class_tiles <= 2 ? 8 : 4; }
 __host__ __device__ constexpr int fused_rows(int class_tiles) { return 16 * fused_waves(class_tiles); }  // of a tile
 
@@ -739,10 +745,11 @@ __host__ __device__ inline int fused_splits(int groups, int waves) {
     return splits;
 }
 
-// Logits, loss, dz, dh and dweight of a tile of rows, one after the other: switched off one at a time (1M x 256, 50 classes, 379 us), dweight is worth 83 us, dh
-// 103, the logits 63: with two waves to a SIMD they hardly overlap, and registers (233) and shared memory (62 KB) leave room for no third.
+// Logits, loss, dz, dh and dweight of a tile of rows, one after the other: switched off one at a time (1M x 256, 50 classes, then 379 us, with dh from two terms
+// of dz), dweight was worth 83 us, dh 103, the logits 63: with two waves to a SIMD they hardly overlap, and registers (238) and shared memory (62 KB) leave room
+// for no third.
 // Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight (GPW groups of 64, a quad for each of 16 lanes) in registers
-// over all tiles of 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
+// over all tiles of 64 or 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
 template <typename T, int CT, int GPW>
 __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) void k_head_fused(Head a, Loss g, float* part) {
     constexpr int kCols = kFusedColumns, kWaves = fused_waves(CT), NT = 1, kFusedRows = fused_rows(CT);

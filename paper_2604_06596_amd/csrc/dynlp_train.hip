@@ -160,9 +160,9 @@ bool in_pieces(int64_t count, int64_t items) { return count > kFewPerItem || (co
 // Rows of 256 bytes and more have waves of their own (k_wave_sum).
 bool wide_rows(int32_t type, int dim) { return (int64_t)dim * type_size(type) >= 256; }
 
-// Entries of a piece of the list.  Pieces enough for 16,384 waves, or groups of lanes for 8,192, where the list has so many entries (32 waves fit
-// each of the 256 CUs); not so few entries that the two parts a piece may leave weigh much against the rows it reads, and not above 512, so that a run
-// over many pieces is joined soon.
+// Entries of a piece of the list.  Pieces enough for 8,192 to 16,384 waves, or groups of lanes for as many as 8,192 waves, where the list has so many entries
+// (5 to 8 waves of k_wave_sum fit each of 1,024 SIMDs, by its registers); not so few entries that the two parts a piece may leave weigh much against the
+// rows it reads, and not above 512, so that a run over many pieces is joined soon.
 int piece_length(int64_t count, int dim, bool wide) {
     const int64_t lanes = std::min<int64_t>(ceil_div(dim, 8), 64);
     if (wide) {
@@ -625,8 +625,10 @@ dynlp_status dynlp_adamw_step(int32_t count, const dynlp_adamw_tensor* tensors, 
     }
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
     const uint32_t key = dither_mix(dither_mix(o->seed) ^ (uint32_t)o->step);
-    // Arrays that are larger than half the cache before the memory leave nothing of use in it: they are read and written past the caches (24M elements,
-    // 32 bits: 119 us, 132 us through the caches; 256M, 8 bits: 876 and 894 us)
+    // Arrays larger than half the cache before the memory are read and written past the caches, which keep what a training step reads next (24M elements,
+    // 32 bits: 119 us, 132 us through the caches; 256M, 8 bits: 876 and 894 us; three sets of 256 MB in turn: 85 and 92).  Up to the cache's size a set that
+    // is stepped with little in between stays in it: alone, 256 MB, 83 us past and 69 through.  A student's whole step, arrays of 180 MB: 198 and 189 us with
+    // 8,192 items of 64 columns, 455 and 469 with 65,536 of 256; of 250 MB: 220 and 227, 486 and 512
     int64_t bytes = 0, blocks = 0;
     for (int32_t k = 0; k < count; ++k)
         bytes += tensors[k].n * (type_size(tensors[k].param_type) + type_size(tensors[k].grad_type) + (bits8 ? 2 : 8) + (tensors[k].copy ? type_size(tensors[k].copy_type) : 0));
