@@ -340,3 +340,20 @@ def test_matrices_without_rows():
         assert loss.shape == (0,) and dh.shape == (0, 8) and torch.equal(dweight, torch.zeros_like(W)) and not dbias.any()
         assert P.embed(empty, no_ids).shape == (0, 8) and P.embed(empty, no_ids, no_offsets).shape == (0, 8)
         assert torch.equal(P.embed_grad(empty, no_ids, 5, no_offsets), torch.zeros(5, 8, device="cuda"))
+
+
+@pytest.mark.parametrize("kind, rows, dim, classes", [("float32", 700, 64, 10), ("bfloat16", 700, 200, 50), ("float16", 300, 520, 20)])
+def test_dbias_alone_with_a_gradient_in_the_place_of_h(kind, rows, dim, classes):
+    """The kernels that make dbias read h again for a dweight that nobody asked for; dbias and dh are what they are apart from h."""
+    from paper_2604_06596_amd import train as T
+
+    rng = np.random.default_rng(4)
+    h, _ = _random(rng, rows, dim, TYPES[kind])
+    W, _ = _random(rng, classes, dim, TYPES[kind], 2.0 / np.sqrt(dim))
+    q = torch.softmax(_random(rng, rows, classes, torch.float32)[0], 1)
+    _, dh, _, dbias = _api().head_loss(h, W, None, q)
+    L, got = T._library(), torch.empty(classes, device="cuda")
+    m, w = T._matrix(h, "h", h.device), T._matrix(W, "weight", h.device)
+    call, space = T._call(h.device, L.dynlp_head_loss_workspace(m.rows, m.dim, w.rows, m.type))
+    T._check(L.dynlp_head_loss(m, w, None, T._Targets(q.data_ptr(), None, None, None, 1.0), None, m, None, got.data_ptr(), call))
+    assert torch.equal(h, dh) and torch.equal(got, dbias)
