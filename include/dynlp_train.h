@@ -9,6 +9,10 @@
  *   dynlp_head_loss    cross entropy against soft rows (what dynlp_get_labels returns) or hard labels, with its gradients
  *   dynlp_embed_grad   gradient of the table
  *   dynlp_adamw_step   one AdamW step over many tensors, states in 32 or 8 bits
+ * How sure labels are, and what a student learns from the best classes of a teacher alone; heads of any number of classes:
+ *   dynlp_row_scores   log probabilities of given classes, entropy and first classes of rows of logits or of propagated labels
+ *   dynlp_head_scores  the same of the head's answers
+ *   dynlp_head_distill divergence of the head from a teacher's first classes, with its gradients
  *
  * Conventions (those of dynlp.h, and where they differ)
  *   - Array arguments are DEVICE pointers on the calling thread's current device.  Structs and scalars are host memory.
@@ -127,6 +131,70 @@ typedef struct dynlp_targets {
 dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_targets* targets,
                              float* loss, const dynlp_matrix* dh, float* dweight, float* dbias, const dynlp_call* call);
 int64_t dynlp_head_loss_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type);
+
+/*
+ * What rows of one value per class say, without the distribution itself: with p = softmax(x), or (probabilities) x / sum of x, as propagated labels are,
+ *   log_given[n][k] = log p[classes[n][k]];  a negative class is padding and gives 0, so does one that is not below the row's classes, and it is counted in *rejected
+ *   entropy[n]      = - sum over c of p[c] log p[c], 0 where p is 0
+ *   top_classes[n]  = the `top` first classes by their values, of equal ones the lowest, from the first on;  log_top[n] = their log p
+ * classes: rows x given int32; outputs rows x given and rows x top without padding; entropy, top_classes and log_top may each be NULL.
+ * 0 <= given <= DYNLP_MAX_GIVEN, 0 <= top <= DYNLP_MAX_TOP and the classes there are.
+ * A logit of -infinity (a probability of 0) has log p = -infinity; a row of nothing else is 1/C everywhere.  A value that is not a number
+ * makes log p and entropy of its row so, as does a logit of +infinity; for the order it counts as -infinity.  Probabilities are not negative.
+ * The order is that of the values, also where log p is the same.
+ */
+#define DYNLP_MAX_TOP 128
+#define DYNLP_MAX_GIVEN (1 << 20)
+#define DYNLP_MAX_WIDE_CLASSES (1 << 22) /* of the heads below */
+#define DYNLP_MAX_WIDE_DIM (1 << 16)
+typedef struct dynlp_scores {
+    int32_t given, top;
+    const int32_t* classes;
+    float* log_given;
+    float* entropy;
+    int32_t* top_classes;
+    float* log_top;
+    int32_t* rejected; /* one int32 that grows, or NULL */
+} dynlp_scores;
+dynlp_status dynlp_row_scores(const dynlp_matrix* x, int32_t probabilities, const dynlp_scores* scores, const dynlp_call* call);
+int64_t dynlp_row_scores_workspace(int64_t rows, int32_t classes, int32_t top);
+
+/*
+ * The same of the head's logits z = h W^T + bias, which are not kept: h, weight and bias as in dynlp_head_labels, but of up to DYNLP_MAX_WIDE_CLASSES classes and
+ * DYNLP_MAX_WIDE_DIM elements of a row.  A class whose bias is -infinity has that logit whatever h holds.
+ */
+dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_scores* scores, const dynlp_call* call);
+int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type);
+
+/*
+ * Learning from a teacher of which each row keeps some classes with their logits (log probabilities do as well: a constant of the row does not matter).
+ * q = softmax(logits / temperature) over a row's list, 0 for classes that are not in it; p = softmax(z / temperature) over all classes of the head:
+ *   loss[n] = r[n] temperature^2 sum over c of q[n][c] (log q[n][c] - log p[n][c])
+ *   dz = grad_scale r[n] temperature (p[n] - q[n]);  dh = dz W,  dweight = dz^T h,  dbias = sum_n dz[n]
+ *   classes, logits  rows x kept, 1 <= kept <= DYNLP_MAX_TOP.  A negative class is no entry, nor is one that is not below the head's classes, which is counted in
+ *                    *rejected (int32, or NULL).  A class that is named several times has the sum of its probabilities.  One class alone
+ *                    is a hard label, and the loss its cross entropy.
+ *   row_weight       r, float32, or NULL for 1.  A row with weight 0 is left out (loss 0, dh 0, nothing in the other gradients, whatever h and its list hold), and so is
+ *                    one without an entry whose logit is more than -infinity, and one whose own logits are all -infinity.
+ *   loss             rows float32; dh: rows x dim, of h's type; dweight: classes x dim, float32 or of h's type; dbias: classes float32.  Each of the four may be NULL (a
+ *                    matrix with data NULL, too).
+ * An entry's logit that is not a number, or +infinity, makes its row's loss and gradients so.  Heads as in dynlp_head_scores.
+ * Gradients that are rounded to 16 bits are made from dz in 16 bits (bfloat16; float16 with a power of two that the largest r gives); dweight in float32,
+ * and all gradients of float32 heads, from all of it.
+ */
+typedef struct dynlp_teacher {
+    const int32_t* classes;
+    const float* logits;
+    const float* row_weight;
+    int32_t* rejected;
+    int32_t kept;
+    float temperature; /* > 0; it, its inverse and its square finite in 32 bits, as is grad_scale times it */
+    float grad_scale;
+} dynlp_teacher;
+dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_teacher* teacher, float* loss,
+                                const dynlp_matrix* dh, const dynlp_matrix* dweight, float* dbias, const dynlp_call* call);
+/* grad_type: of dweight (h's where there is none), or -1 where the loss alone is asked for. */
+int64_t dynlp_head_distill_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t kept, int32_t type, int32_t grad_type);
 
 /*
  * One step of AdamW with decoupled weight decay over `count` tensors:

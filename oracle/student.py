@@ -114,3 +114,55 @@ def state_neighbours(y):
     at = np.searchsorted(FORMAT, y, side="right") - 1
     low = FORMAT[np.clip(at, 0, 126)]
     return low, np.where(low == y, y, FORMAT[np.clip(at + 1, 0, 126)])
+
+
+# ---- scores and learning from a teacher's first classes ------------------------------------------------------------------
+
+def scores(x, probabilities=False):
+    """(log probabilities, entropy, order of the classes) of rows of logits, or of probabilities."""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        z = np.log(x) if probabilities else x
+        top = z.max(axis=1, keepdims=True)  # not a number where one is
+        finite = np.where(np.isneginf(top), 0.0, top)
+        log_s = np.log(np.where(np.isneginf(z), 0.0, np.exp(z - finite)).sum(axis=1, keepdims=True))
+        log_p = np.where(np.isneginf(top), -np.log(z.shape[1]), (z - finite) - log_s)
+        p = np.exp(log_p)
+        entropy = -np.where(p == 0.0, 0.0, p * np.where(p == 0.0, 0.0, log_p)).sum(axis=1)
+    order = np.argsort(np.where(np.isnan(x), np.inf, -x), axis=1, kind="stable")
+    return log_p, entropy, order
+
+
+def distill(h, weight, bias, classes, logits, temperature=1.0, row_weight=None, grad_scale=1.0):
+    """dict of loss, dh, dweight, dbias, dz, left_out, target (dense), soft (at the temperature), logits (divided by it)."""
+    h, weight = np.asarray(h, dtype=np.float64), np.asarray(weight, dtype=np.float64)
+    n, count = len(h), len(weight)
+    r = np.ones(n) if row_weight is None else np.asarray(row_weight, dtype=np.float64)
+    target, entropy = np.zeros((n, count)), np.zeros(n)
+    out = r == 0.0
+    for i in range(n):
+        real = (classes[i] >= 0) & (classes[i] < count)
+        u = np.asarray(logits[i], dtype=np.float64)[real] / temperature
+        if out[i] or len(u) == 0 or np.isneginf(u).all():
+            out[i] = True
+            continue
+        with np.errstate(invalid="ignore"):
+            e = np.exp(u - u.max())
+            q = e / e.sum()
+            np.add.at(target[i], classes[i][real], q)
+            entropy[i] = np.where(q == 0.0, 0.0, q * np.log(np.where(q == 0.0, 1.0, q))).sum()
+    z, p, _ = head(np.where(out[:, None], 0.0, h), weight, bias)
+    out = out | np.isneginf(z).all(axis=1)
+    z = z / temperature
+    top = np.where(out, 0.0, z.max(axis=1, initial=-np.inf))
+    with np.errstate(divide="ignore", invalid="ignore"):
+        e = np.exp(z - top[:, None])
+        total = e.sum(axis=1)
+        p = e / total[:, None]
+        lse = np.log(total) + top
+        loss = entropy + np.where(target != 0.0, target * (lse[:, None] - z), 0.0).sum(axis=1)
+        dz = grad_scale * r[:, None] * temperature * (p - target)
+    dz[out] = 0.0
+    return {"loss": np.where(out, 0.0, r * temperature ** 2 * loss), "dh": np.where(out[:, None], 0.0, dz @ weight),
+            "dweight": dz.T @ np.where(out[:, None], 0.0, h), "dbias": dz.sum(axis=0), "dz": dz, "left_out": out, "target": target, "soft": p,
+            "logits": z, "lse": lse}

@@ -6,7 +6,7 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
-_SRC = [os.path.join(_HERE, "csrc", name) for name in ("dynlp.hip", "dynlp_train.hip")]
+_SRC = [os.path.join(_HERE, "csrc", name) for name in ("dynlp.hip", "dynlp_train.hip", "dynlp_teach.hip")]
 _SO = os.path.join(_HERE, "libdynlp.so")
 
 

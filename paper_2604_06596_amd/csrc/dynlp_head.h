@@ -20,7 +20,7 @@
 #pragma once
 
 #include "dynlp_device.h"
-#include "dynlp_types.h"
+#include "dynlp_matrix.h"
 
 namespace dynlp {
 
@@ -34,45 +34,6 @@ struct Head {
     int64_t rows;
     int dim, classes;
 };
-
-// acc += left * right over a piece of each.
-__device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 c, bf16) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 c, f16) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-__device__ inline f32x4 mma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 mma(u32x4 a, u32x4 b, f32x4 c, float) {
-    for (int k = 0; k < 4; ++k) c = mma4(__uint_as_float(a[k]), __uint_as_float(b[k]), c);
-    return c;
-}
-
-// The piece at columns col .. col + n - 1 of a row of dim elements; columns from dim on are zeros.
-template <typename T>
-__device__ inline u32x4 load_columns(const T* row, int col, int dim) {
-    constexpr int n = Piece<T>::n;
-    if (col + n <= dim) return load_piece(row + col);
-    u32x4 v = {};
-    for (int k = 0; k < n; ++k)
-        if (col + k < dim) {
-            if constexpr (sizeof(T) == 2)
-                v[k / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, row[col + k]) << (16 * (k & 1));
-            else
-                v[k] = __float_as_uint(row[col + k]);
-        }
-    return v;
-}
-template <typename T>
-__device__ inline void store_columns(T* row, int col, int dim, const float (&f)[Piece<T>::n]) {
-    constexpr int n = Piece<T>::n;
-    if (col + n <= dim) {
-        store_values<n>(row + col, f);
-    } else {
-        for (int k = 0; k < n; ++k)
-            if (col + k < dim) row[col + k] = (T)f[k];
-    }
-}
 
 // Four columns of a row: 16 bytes or 8.
 template <typename T>
@@ -223,25 +184,6 @@ __device__ inline void head_logits(const Head& a, const W& w, int64_t first, f32
     }
 }
 
-// Over the four lanes that share a row.
-__device__ inline float row_sum(float v) {
-    v += __shfl_xor(v, 16, kWave);
-    return v + __shfl_xor(v, 32, kWave);
-}
-__device__ inline float row_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16, kWave));
-    return fmaxf(v, __shfl_xor(v, 32, kWave));
-}
-
-// e^x for x <= 0, or not a number: 2^y for y = x log2(e) as it is rounded, times 1 + ln(2) (what the rounding took).  Values below 2^-126 may be 0.
-__device__ inline float exp_below_0(float x) {
-    x = x < -150.f ? -150.f : x;
-    const float y = x * 1.44269502f;
-    const float rest = __builtin_fmaf(x, 1.44269502f, -y) + x * 1.92596299e-8f;
-    const float p = __builtin_amdgcn_exp2f(y);
-    return __builtin_fmaf(p, rest * 0.693147182f, p);
-}
-
 // z becomes exp(z - max); returns the sum, and the largest logit.  A NaN among the logits makes the sum one.
 template <int CT>
 __device__ inline float head_exp(f32x4 (&z)[CT], float* top) {
@@ -323,20 +265,6 @@ struct Loss {
     float* dz;       // rows x (16 tiles), or NULL; rows that are left out: zeros
     uint8_t* kept;   // rows: 0 if left out
 };
-
-// Two values rounded to bfloat16, the first in the low half; three such terms hold all 24 bits of the values.
-__device__ inline uint32_t bf16_pair(float x, float y) {
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
-}
-__device__ inline void bf16_terms(float x, float y, uint32_t (&term)[3]) {
-    for (int k = 0; k < 3; ++k) {
-        term[k] = bf16_pair(x, y);
-        x -= __uint_as_float(term[k] << 16);
-        y -= __uint_as_float(term[k] & 0xffff0000u);
-    }
-}
 
 // dh of the tile's rows from their dz, 64 columns at a time.  Quads of W's rows are the left operand; in bfloat16 a lane's 8 x 4 block (8 classes, 4
 // columns) is transposed by v_perm.

@@ -1,0 +1,455 @@
+// libdynlp: host side of scores and of learning from a teacher's first classes (include/dynlp_train.h): checks, launch sizes, C ABI.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <type_traits>
+
+#include "dynlp_host.h"
+#include "dynlp_scores.h"
+#include "dynlp_teach.h"
+
+using namespace dynlp;
+
+namespace {
+
+constexpr int64_t kMostBlocks = 0xffffffff / kBlock;  // workgroups: a launch has fewer than 2^32 threads
+constexpr int64_t kMostStride = 1 << 22;              // elements: 32 bits hold the bytes of a tile's rows
+constexpr int64_t kLogitsBytes = int64_t(256) << 20;  // of logits in memory at a time
+constexpr int64_t kTermsBytes = int64_t(4) << 30;     // of dz in memory at a time
+constexpr int64_t kMostTeachRows = 1 << 24;           // at a time: a launch has fewer than 2^32 threads
+
+// ---- products ---------------------------------------------------------------------------------------------------------
+
+struct Tiling {
+    int tm, tn, wm, wn;
+};
+// m: the fast index of the result.
+Tiling tiling(int64_t m, int64_t n) {
+    if (n <= 16) return {256, 16, 4, 1};
+    if (n <= 64) return {256, 64, 4, 1};
+    if (m <= 64) return {64, 256, 1, 4};
+    return {256, 128, 2, 2};
+}
+template <bool TA, bool TB, typename F>
+void by_tiling(const Tiling& t, F f) {
+    if (t.tn == 16) f(Shape<256, 16, 4, 1, TA, TB>());
+    else if (t.tn == 64) f(Shape<256, 64, 4, 1, TA, TB>());
+    else if (t.tm == 64) f(Shape<64, 256, 1, 4, TA, TB>());
+    else f(Shape<256, 128, 2, 2, TA, TB>());
+}
+
+template <typename T, bool TA, bool TB, typename E>
+void launch_product(Wide g, const Tiling& t, int64_t m, int64_t n, int splits, const E& e, hipStream_t stream) {
+    g.tiles_m = (int)ceil_div(m, t.tm);
+    g.tiles_n = (int)ceil_div(n, t.tn);
+    g.per_split = (int)ceil_div((int64_t)g.pairs * g.steps, splits);
+    g.splits = (int)ceil_div((int64_t)g.pairs * g.steps, g.per_split);
+    by_tiling<TA, TB>(t, [&](auto shape) {
+        using S = decltype(shape);
+        static std::atomic<uint64_t> allowed{0};
+        allow_shared(k_wide<T, S, E>, allowed);
+        k_wide<T, S, E><<<(unsigned)((int64_t)g.tiles_m * g.tiles_n * g.splits), kBlock, kStages * S::stage, stream>>>(g, e);
+    });
+}
+
+// Pairs of terms, the smallest products first.
+void set_pairs(Wide* g, int terms_a, int terms_b) {
+    g->pairs = 0;
+    g->pair = 0;
+    for (int sum = 2; sum >= 0; --sum)
+        for (int a = 0; a < terms_a; ++a) {
+            const int b = sum - a;
+            if (b >= 0 && b < terms_b) g->pair |= (uint32_t)(a | b << 2) << (4 * g->pairs++);
+        }
+}
+
+// Splits of a sum so that the chip has two workgroups for each CU, none shorter than 8 steps.
+int splits_of(int64_t m, int64_t n, int64_t steps) {
+    const Tiling t = tiling(m, n);
+    const int64_t tiles = ceil_div(m, t.tm) * ceil_div(n, t.tn);
+    return (int)std::max<int64_t>(std::min(512 / tiles, steps / 8), 1);
+}
+
+// ---- operands ---------------------------------------------------------------------------------------------------------
+
+// A matrix as 16-bit terms whose rows are whole steps and begin at multiples of 16 bytes: as it lies, or laid out anew.
+struct Laid {
+    const void* p;
+    int64_t ld, term;  // elements; bytes
+    int terms;
+};
+int terms_in(int32_t type) { return type == DYNLP_FLOAT32 ? 3 : 1; }
+int64_t laid_ld(int64_t dim) { return round_up(dim, kStep); }
+bool lies_well(const dynlp_matrix& m) {
+    return m.type != DYNLP_FLOAT32 && reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && m.dim % kStep == 0 &&
+           (m.rows == 1 || (m.stride % 8 == 0 && m.stride < kMostStride));
+}
+Laid lay_out(const dynlp_matrix& m, uint16_t* to, hipStream_t stream) {
+    if (!to) return {m.data, m.rows == 1 ? m.dim : m.stride, 0, 1};
+    const int64_t ld = laid_ld(m.dim), term = m.rows * ld, blocks = std::min<int64_t>(ceil_div(m.rows * (ld / 8), kBlock), 8192);
+    if (m.type == DYNLP_FLOAT32)
+        k_lay_out<float><<<(unsigned)blocks, kBlock, 0, stream>>>(static_cast<const float*>(m.data), m.stride, m.rows, m.dim, to, ld, term);
+    else  // bits alone matter
+        k_lay_out<bf16><<<(unsigned)blocks, kBlock, 0, stream>>>(static_cast<const bf16*>(m.data), m.stride, m.rows, m.dim, to, ld, term);
+    return {to, ld, 2 * term, terms_in(m.type)};
+}
+uint16_t* take_laid(Carve& c, int64_t rows, int64_t dim, int32_t type) { return c.take<uint16_t>(rows * laid_ld(dim) * terms_in(type)); }
+
+dynlp_matrix rows_of(const dynlp_matrix& m, int64_t first, int64_t rows) {
+    dynlp_matrix r = m;
+    r.data = static_cast<char*>(m.data) + first * m.stride * type_size(m.type);
+    r.rows = rows;
+    return r;
+}
+
+Wide logits_product(const Laid& weight, int64_t classes, const Laid& h, int64_t rows, int dim) {
+    Wide g{};
+    g.a = weight.p, g.ld_a = weight.ld, g.term_a = weight.term, g.m = (int)classes;
+    g.b = h.p, g.ld_b = h.ld, g.term_b = h.term, g.n = (int)rows;
+    g.k = dim;
+    g.steps = (int)(laid_ld(dim) / kStep);
+    set_pairs(&g, weight.terms, h.terms);
+    return g;
+}
+
+// F is called with a value of the type that the products of a matrix's terms are made in.
+template <typename F>
+void by_terms(int32_t type, F f) {
+    if (type == DYNLP_FLOAT16) f(f16());
+    else f(bf16());
+}
+
+dynlp_status check_wide_head(const dynlp_matrix* h, const dynlp_matrix* weight) {
+    CHECK(check_matrix(h, "h"));
+    CHECK(check_matrix(weight, "weight"));
+    if (weight->type != h->type) REFUSE("weight has type %d, h %d", weight->type, h->type);
+    if (weight->dim != h->dim) REFUSE("weight has rows of %d elements, h of %d", weight->dim, h->dim);
+    if (weight->rows < 1 || weight->rows > DYNLP_MAX_WIDE_CLASSES) REFUSE("%lld classes: 1 .. %d are possible", (long long)weight->rows, DYNLP_MAX_WIDE_CLASSES);
+    if (h->dim > DYNLP_MAX_WIDE_DIM) REFUSE("rows of %d elements: %d are possible", h->dim, DYNLP_MAX_WIDE_DIM);
+    return DYNLP_OK;
+}
+
+// ---- scores -----------------------------------------------------------------------------------------------------------
+
+dynlp_status check_scores(const dynlp_scores* s, int64_t rows, int64_t classes) {
+    if (!s) REFUSE("scores is NULL");
+    if (s->given < 0 || s->given > DYNLP_MAX_GIVEN) REFUSE("%d given classes: 0 .. %d are possible", s->given, DYNLP_MAX_GIVEN);
+    if (s->top < 0 || s->top > DYNLP_MAX_TOP) REFUSE("the first %d classes: 0 .. %d are possible", s->top, DYNLP_MAX_TOP);
+    if (s->top > classes) REFUSE("the first %d of %lld classes", s->top, (long long)classes);
+    if (rows > 0 && s->given > 0 && (!s->classes || !s->log_given)) REFUSE("given classes without %s", s->classes ? "log_given" : "classes");
+    return DYNLP_OK;
+}
+
+Scores scores_of(const dynlp_scores* s) {
+    return Scores{s->classes, s->log_given, s->entropy, s->top_classes, s->log_top, s->rejected, s->given, s->top_classes || s->log_top ? s->top : 0};
+}
+
+template <typename T, bool PROB>
+void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& o, int64_t row0, hipStream_t stream) {
+    k_row_scores<T, PROB><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
+}
+
+// Rows whose logits are in memory at a time.
+int64_t logits_rows(int64_t rows, int64_t classes) {
+    const int64_t most = std::max<int64_t>(kLogitsBytes / (round_up(classes, 16) * 4) / 256 * 256, 256);
+    return std::min(rows, most);
+}
+
+struct ScoreSpace {
+    uint16_t *h, *weight;
+    float* z;
+    int64_t rows;  // at a time
+};
+int64_t score_space(char* base, int64_t rows, int64_t dim, int64_t classes, int32_t type, bool lay_h, bool lay_weight, ScoreSpace* s) {
+    Carve c{base};
+    s->rows = logits_rows(rows, classes);
+    s->z = c.take<float>(s->rows * round_up(classes, 16));
+    s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
+    s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
+    return c.used;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t dynlp_row_scores_workspace(int64_t rows, int32_t classes, int32_t top) {
+    (void)rows, (void)classes, (void)top;
+    return 0;
+}
+
+dynlp_status dynlp_row_scores(const dynlp_matrix* x, int32_t probabilities, const dynlp_scores* scores, const dynlp_call* call) {
+    CHECK(check_matrix(x, "x"));
+    CHECK(check_scores(scores, x->rows, x->dim));
+    CHECK(check_workspace(call, dynlp_row_scores_workspace(x->rows, x->dim, scores->top)));
+    if (x->rows == 0) return DYNLP_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
+    const Scores o = scores_of(scores);
+    auto run = [&](auto type) {
+        using T = decltype(type);
+        const T* p = static_cast<const T*>(x->data);
+        if (probabilities) launch_scores<T, true>(p, x->stride, x->rows, x->dim, o, 0, stream);
+        else launch_scores<T, false>(p, x->stride, x->rows, x->dim, o, 0, stream);
+    };
+    if (x->type == DYNLP_FLOAT32) run(float());
+    else if (x->type == DYNLP_BFLOAT16) run(bf16());
+    else run(f16());
+    return launched();
+}
+
+int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type) {
+    if (rows < 1 || rows > kMostRows || dim < 1 || dim > DYNLP_MAX_WIDE_DIM || classes < 1 || classes > DYNLP_MAX_WIDE_CLASSES) return 0;
+    ScoreSpace s{};
+    return score_space(nullptr, rows, dim, classes, type, true, true, &s);
+}
+
+dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_scores* scores, const dynlp_call* call) {
+    CHECK(check_wide_head(h, weight));
+    CHECK(check_scores(scores, h->rows, weight->rows));
+    const int classes = (int)weight->rows;
+    CHECK(check_workspace(call, dynlp_head_scores_workspace(h->rows, h->dim, classes, h->type)));
+    if (h->rows == 0) return DYNLP_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
+    ScoreSpace s{};
+    score_space(static_cast<char*>(call->workspace), h->rows, h->dim, classes, h->type, !lies_well(*h), !lies_well(*weight), &s);
+    const Scores o = scores_of(scores);
+    const Laid w = lay_out(*weight, s.weight, stream);
+    const int64_t ld = round_up(classes, 16);
+    for (int64_t row = 0; row < h->rows; row += s.rows) {
+        const int64_t rows = std::min(s.rows, h->rows - row);
+        const Laid x = lay_out(rows_of(*h, row, rows), s.h, stream);
+        const Wide g = logits_product(w, classes, x, rows, h->dim);
+        const Logits e{s.z, ld, bias, (int)rows, classes};
+        by_terms(h->type, [&](auto type) { launch_product<decltype(type), false, false>(g, tiling(classes, rows), classes, rows, 1, e, stream); });
+        launch_scores<float, false>(s.z, ld, rows, classes, o, row, stream);
+    }
+    return launched();
+}
+
+}  // extern "C"
+
+// ---- distillation -----------------------------------------------------------------------------------------------------
+
+namespace {
+
+// Terms of dz: one where the gradients are rounded to 16 bits anyway, else as many as hold 24 bits of it (22 in float16).
+int dz_terms(int32_t type, int32_t grad_type) { return type == DYNLP_FLOAT32 ? 3 : grad_type != DYNLP_FLOAT32 ? 1 : type == DYNLP_BFLOAT16 ? 3 : 2; }
+
+struct TeachSpace {
+    int64_t rows;  // at a time
+    int64_t ld;    // of dz
+    uint16_t *h, *weight, *dz;
+    uint32_t *zeros, *largest, *kept;
+    float* undo;
+    Lists lists;
+    float *top, *sum, *picked, *lse, *factor;
+    float *bias_part, *part, *dweight;
+    int64_t part_ld;   // of top, sum and picked
+    int terms, parts;
+    int splits_h, splits_w;
+};
+
+// grad_type: of dweight, or -1 where no gradient is asked for.
+int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int kept, int32_t type, int32_t grad_type, bool lay_h, bool lay_weight, TeachSpace* s) {
+    Carve c{base};
+    const bool grads = grad_type >= 0;
+    s->terms = dz_terms(type, grad_type);
+    s->ld = laid_ld(classes);
+    const int64_t most = std::max<int64_t>(kTermsBytes / (s->ld * 2 * s->terms) / 256 * 256, 256);
+    s->rows = std::min({rows, most, kMostTeachRows});
+    const Tiling t = tiling(classes, s->rows);
+    s->parts = (int)ceil_div(classes, t.tm) * t.wm;
+    s->part_ld = round_up(s->rows, 64);
+    s->zeros = c.take<uint32_t>(128);
+    s->largest = c.take<uint32_t>(1);
+    s->undo = c.take<float>(1);
+    s->kept = c.take<uint32_t>(ceil_div(s->rows, 32));
+    s->lists.classes = c.take<int32_t>(s->rows * kept);
+    s->lists.q = c.take<float>(s->rows * kept);
+    s->lists.entropy = c.take<float>(s->rows);
+    s->lists.weight = c.take<float>(s->rows);
+    s->lse = c.take<float>(s->rows);
+    s->factor = c.take<float>(s->rows);
+    s->top = c.take<float>(s->parts * s->part_ld);
+    s->sum = c.take<float>(s->parts * s->part_ld);
+    s->picked = c.take<float>(s->parts * s->part_ld);
+    s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
+    s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
+    if (grads) {
+        const int pairs = type == DYNLP_FLOAT32 ? 6 : 1;
+        s->dz = c.take<uint16_t>(s->rows * s->ld * s->terms);
+        s->bias_part = c.take<float>(ceil_div(s->rows, t.tn) * t.wn * s->ld);
+        s->splits_h = splits_of(dim, s->rows, pairs * (s->ld / kStep));
+        s->splits_w = splits_of(dim, classes, (pairs == 6 ? 6 : s->terms) * ceil_div(s->rows, kStep));
+        const int64_t part_h = s->splits_h > 1 ? s->splits_h * s->rows * dim : 0, part_w = s->splits_w > 1 ? s->splits_w * classes * dim : 0;
+        s->part = c.take<float>(std::max(part_h, part_w));
+        s->dweight = rows > s->rows && grad_type != DYNLP_FLOAT32 ? c.take<float>(classes * dim) : nullptr;
+    }
+    return c.used;
+}
+
+template <typename O>
+void launch_join(const float* part, int splits, int64_t rows, int dim, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
+                 hipStream_t stream) {
+    k_wide_join<O><<<(unsigned)std::min<int64_t>(ceil_div(rows * dim, kBlock), 16384), kBlock, 0, stream>>>(part, splits, rows * dim, rows, dim, alpha, undo, kept,
+                                                                                                           static_cast<O*>(out), ld, add);
+}
+
+// The product to `out`, by parts where its sum is split.
+template <typename T, bool TA, bool TB, typename O>
+void launch_gradient(const Wide& g, int64_t m, int64_t n, int splits, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
+                     hipStream_t stream) {
+    if (splits > 1) {
+        const int64_t total = (int64_t)g.pairs * g.steps, per = ceil_div(total, splits);
+        const Store<float> e{part, m, n * m, (int)n, (int)m, 1.f, nullptr, nullptr, false};
+        launch_product<T, TA, TB>(g, tiling(m, n), m, n, splits, e, stream);
+        launch_join<O>(part, (int)ceil_div(total, per), n, (int)m, alpha, undo, kept, out, ld, add, stream);
+    } else {
+        const Store<O> e{static_cast<O*>(out), ld, 0, (int)n, (int)m, alpha, undo, kept, add};
+        launch_product<T, TA, TB>(g, tiling(m, n), m, n, 1, e, stream);
+    }
+}
+
+template <typename F>
+void by_type(int32_t type, F f) {
+    if (type == DYNLP_FLOAT32) f(float());
+    else if (type == DYNLP_BFLOAT16) f(bf16());
+    else f(f16());
+}
+
+dynlp_status check_teacher(const dynlp_teacher* t, int64_t rows) {
+    if (!t) REFUSE("teacher is NULL");
+    if (t->kept < 1 || t->kept > DYNLP_MAX_TOP) REFUSE("lists of %d classes: 1 .. %d are possible", t->kept, DYNLP_MAX_TOP);
+    if (rows > 0 && (!t->classes || !t->logits)) REFUSE("a teacher without %s", t->classes ? "logits" : "classes");
+    if (!(t->temperature > 0.f) || !std::isfinite(t->temperature) || !std::isfinite(1.f / t->temperature) || !std::isfinite(t->temperature * t->temperature))
+        REFUSE("temperature = %g", t->temperature);
+    if (!std::isfinite(t->grad_scale * t->temperature)) REFUSE("grad_scale = %g with temperature = %g", t->grad_scale, t->temperature);
+    return DYNLP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t dynlp_head_distill_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t kept, int32_t type, int32_t grad_type) {
+    if (rows < 1 || rows > kMostRows || dim < 1 || dim > DYNLP_MAX_WIDE_DIM || classes < 1 || classes > DYNLP_MAX_WIDE_CLASSES || kept < 1 || kept > DYNLP_MAX_TOP) return 0;
+    TeachSpace s{};
+    return teach_space(nullptr, rows, dim, classes, kept, type, grad_type, true, true, &s);
+}
+
+dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_teacher* teacher, float* loss,
+                                const dynlp_matrix* dh, const dynlp_matrix* dweight, float* dbias, const dynlp_call* call) {
+    CHECK(check_wide_head(h, weight));
+    CHECK(check_teacher(teacher, h->rows));
+    const bool want_h = dh && dh->data, want_w = dweight && dweight->data;
+    if (want_h) {
+        CHECK(check_matrix(dh, "dh"));
+        if (dh->type != h->type || dh->dim != h->dim || dh->rows != h->rows) REFUSE("dh has another shape or type than h");
+        if (overlap(*h, *dh)) REFUSE("dh overlaps h");
+        if (overlap(*weight, *dh)) REFUSE("dh overlaps weight");
+    }
+    if (want_w) {
+        CHECK(check_matrix(dweight, "dweight"));
+        if (dweight->type != h->type && dweight->type != DYNLP_FLOAT32) REFUSE("dweight has type %d: float32 or h's (%d) are possible", dweight->type, h->type);
+        if (dweight->dim != weight->dim || dweight->rows != weight->rows) REFUSE("dweight has another shape than weight");
+        if (overlap(*h, *dweight)) REFUSE("dweight overlaps h");
+        if (overlap(*weight, *dweight)) REFUSE("dweight overlaps weight");
+        if (want_h && overlap(*dh, *dweight)) REFUSE("dweight overlaps dh");
+    }
+    const int classes = (int)weight->rows, dim = h->dim;
+    const bool grads = want_h || want_w || dbias;
+    const int32_t grad_type = want_w ? dweight->type : grads ? h->type : -1;
+    CHECK(check_workspace(call, dynlp_head_distill_workspace(h->rows, dim, classes, teacher->kept, h->type, grad_type)));
+    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
+    if (h->rows == 0) {
+        if (want_w)
+            by_type(dweight->type, [&](auto type) {
+                using O = decltype(type);
+                k_teach_zeros<O><<<(unsigned)std::min<int64_t>(ceil_div((int64_t)classes * dim, kBlock), 8192), kBlock, 0, stream>>>(
+                    static_cast<O*>(dweight->data), dweight->stride, classes, dim);
+            });
+        if (dbias) k_teach_zeros<float><<<(unsigned)ceil_div(classes, kBlock), kBlock, 0, stream>>>(dbias, classes, 1, classes);
+        return launched();
+    }
+    TeachSpace s{};
+    teach_space(static_cast<char*>(call->workspace), h->rows, dim, classes, teacher->kept, h->type, grad_type, !lies_well(*h), !lies_well(*weight), &s);
+    const Laid w = lay_out(*weight, s.weight, stream);
+    const float exponent = 1.44269504f / teacher->temperature, alpha = teacher->grad_scale * teacher->temperature;
+    const bool scaled = h->type == DYNLP_FLOAT16;
+    int group = 0;
+    while (group < 6 && (1 << group) < teacher->kept) ++group;
+    for (int64_t row = 0; row < h->rows; row += s.rows) {
+        const int64_t rows = std::min(s.rows, h->rows - row);
+        const bool add = row > 0;
+        const Laid x = lay_out(rows_of(*h, row, rows), s.h, stream);
+        k_teach_begin<<<1, kBlock, 0, stream>>>(s.zeros, s.largest);
+        Lists lists = s.lists;
+        lists.largest = scaled ? s.largest : nullptr;
+        const Teacher t{teacher->classes, teacher->logits, teacher->row_weight, teacher->rejected, teacher->kept, classes, 1.f / teacher->temperature};
+        const unsigned blocks = (unsigned)ceil_div(rows << group, kBlock);
+        if (teacher->kept > kWave) k_teach_lists<2><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);
+        else k_teach_lists<1><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);
+        const Wide g = logits_product(w, classes, x, rows, dim);
+        const Tiling tile = tiling(classes, s.rows);  // of all chunks: its parts have a size
+        const int parts = (int)ceil_div(classes, tile.tm) * tile.wm;
+        by_terms(h->type, [&](auto type) {
+            using T = decltype(type);
+            const Stats stats{bias, lists.classes, lists.q, s.top, s.sum, s.picked, s.part_ld, exponent, (int)rows, classes, teacher->kept};
+            launch_product<T, false, false>(g, tile, classes, rows, 1, stats, stream);
+            const RowJoin join{s.top, s.sum, s.picked, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.lse, s.factor, s.kept,
+                               s.undo, exponent, teacher->temperature, (int)rows, parts};
+            k_teach_rows<<<(unsigned)ceil_div(rows, 32), kBlock, 0, stream>>>(join);
+            if (!grads) return;
+            const int64_t term = rows * s.ld;
+            auto gradient = [&](auto terms) {
+                const Gradient<T, decltype(terms)::value> e{bias, lists.classes, lists.q, s.lse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes,
+                                                            teacher->kept};
+                launch_product<T, false, false>(g, tile, classes, rows, 1, e, stream);
+            };
+            if (s.terms == 1) gradient(std::integral_constant<int, 1>());
+            else if constexpr (__is_same(T, f16)) gradient(std::integral_constant<int, 2>());
+            else gradient(std::integral_constant<int, 3>());
+            if (dbias)
+                k_teach_bias<<<(unsigned)ceil_div(classes, 64), kBlock, 0, stream>>>(s.bias_part, s.ld, (int)ceil_div(rows, tile.tn) * tile.wn, classes, alpha, s.undo, dbias,
+                                                                                    add);
+            if (want_h) {
+                Wide p{};
+                p.a = w.p, p.ld_a = w.ld, p.term_a = w.term, p.m = (int)laid_ld(dim);
+                p.b = s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)rows;
+                p.k = classes;
+                p.steps = (int)(s.ld / kStep);
+                set_pairs(&p, w.terms, w.terms == 1 ? 1 : s.terms);
+                void* to = static_cast<char*>(dh->data) + row * dh->stride * type_size(dh->type);
+                auto run = [&](auto out) {
+                    launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.splits_h, s.part, alpha, s.undo, s.kept, to, dh->stride, false, stream);
+                };
+                if (h->type == DYNLP_FLOAT32) {
+                    if constexpr (__is_same(T, bf16)) run(float());
+                } else {
+                    run(T());
+                }
+            }
+            if (want_w) {
+                Wide p{};
+                p.a = x.p, p.ld_a = x.ld, p.term_a = x.term, p.m = (int)laid_ld(dim);
+                p.b = s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)s.ld;
+                p.k = (int)rows;
+                p.steps = (int)ceil_div(rows, kStep);
+                p.kept = s.kept;
+                p.zeros = s.zeros;
+                set_pairs(&p, x.terms, s.terms);
+                if (dweight->type == DYNLP_FLOAT32) {
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, add, stream);
+                } else if (s.dweight) {
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, s.dweight, dim, add, stream);
+                    if (row + rows == h->rows) launch_join<T>(s.dweight, 1, classes, dim, 1.f, nullptr, nullptr, dweight->data, dweight->stride, false, stream);
+                } else {
+                    launch_gradient<T, true, true, T>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, false, stream);
+                }
+            }
+        });
+    }
+    return launched();
+}
+
+}  // extern "C"

@@ -11,6 +11,7 @@ saved one of them says so.
 from __future__ import annotations
 
 import ctypes as ct
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -22,6 +23,7 @@ STATE_BLOCK = 256  # elements of an 8-bit state that share a scale
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INVALID = -1
+_MOST = 0x7FFFFFFF
 
 
 class _Matrix(ct.Structure):
@@ -42,6 +44,16 @@ class _Targets(ct.Structure):
                 ("grad_scale", ct.c_float)]
 
 
+class _Scores(ct.Structure):
+    _fields_ = [("given", ct.c_int32), ("top", ct.c_int32), ("classes", ct.c_void_p), ("log_given", ct.c_void_p), ("entropy", ct.c_void_p),
+                ("top_classes", ct.c_void_p), ("log_top", ct.c_void_p), ("rejected", ct.c_void_p)]
+
+
+class _Teacher(ct.Structure):
+    _fields_ = [("classes", ct.c_void_p), ("logits", ct.c_void_p), ("row_weight", ct.c_void_p), ("rejected", ct.c_void_p), ("kept", ct.c_int32),
+                ("temperature", ct.c_float), ("grad_scale", ct.c_float)]
+
+
 class _AdamwOptions(ct.Structure):
     _fields_ = [("lr", ct.c_double), ("beta1", ct.c_double), ("beta2", ct.c_double), ("eps", ct.c_double), ("step", ct.c_int64),
                 ("grad_scale", ct.c_void_p), ("seed", ct.c_uint32), ("state_bits", ct.c_int32)]
@@ -52,7 +64,8 @@ _ADAMW_TENSOR = np.dtype([("n", "i8"), ("param", "u8"), ("grad", "u8"), ("m", "u
                           ("copy_type", "i4")])
 
 EXPORTS = ["dynlp_embed", "dynlp_embed_workspace", "dynlp_embed_grad", "dynlp_embed_grad_workspace", "dynlp_head_labels",
-           "dynlp_head_loss", "dynlp_head_loss_workspace", "dynlp_adamw_step"]
+           "dynlp_head_loss", "dynlp_head_loss_workspace", "dynlp_adamw_step", "dynlp_row_scores", "dynlp_row_scores_workspace",
+           "dynlp_head_scores", "dynlp_head_scores_workspace", "dynlp_head_distill", "dynlp_head_distill_workspace"]
 
 _lib = None
 
@@ -70,11 +83,18 @@ def _library():
         L.dynlp_head_labels.argtypes = [m, m, p, p, p, call]
         L.dynlp_head_loss.argtypes = [m, m, p, ct.POINTER(_Targets), p, m, p, p, call]
         L.dynlp_adamw_step.argtypes = [i32, p, ct.POINTER(_AdamwOptions), call]
-        for name in ("dynlp_embed", "dynlp_embed_grad", "dynlp_head_labels", "dynlp_head_loss", "dynlp_adamw_step"):
+        L.dynlp_row_scores.argtypes = [m, i32, ct.POINTER(_Scores), call]
+        L.dynlp_head_scores.argtypes = [m, m, p, ct.POINTER(_Scores), call]
+        L.dynlp_head_distill.argtypes = [m, m, p, ct.POINTER(_Teacher), p, m, m, p, call]
+        for name in ("dynlp_embed", "dynlp_embed_grad", "dynlp_head_labels", "dynlp_head_loss", "dynlp_adamw_step", "dynlp_row_scores",
+                     "dynlp_head_scores", "dynlp_head_distill"):
             getattr(L, name).restype = ct.c_int
         L.dynlp_embed_workspace.argtypes = [i64, i64, i32]
         L.dynlp_embed_grad_workspace.argtypes = [i64, i64, i32, i64]
         L.dynlp_head_loss_workspace.argtypes = [i64, i32, i32, i32]
+        L.dynlp_row_scores_workspace.argtypes = [i64, i32, i32]
+        L.dynlp_head_scores_workspace.argtypes = [i64, i32, i32, i32]
+        L.dynlp_head_distill_workspace.argtypes = [i64, i32, i32, i32, i32, i32]
         for name in EXPORTS:
             if name.endswith("_workspace"):
                 getattr(L, name).restype = i64
@@ -228,6 +248,88 @@ def head_loss(h, weight, bias, target, *, row_weight=None, grad_scale=1.0, grads
     call, space = _call(device, L.dynlp_head_loss_workspace(m.rows, m.dim, w.rows, m.type))
     to = _Matrix(dh.data_ptr(), m.rows, max(m.dim, 1), m.dim, m.type)
     _check(_run(device, L.dynlp_head_loss, m, w, b, t, loss.data_ptr(), to, dweight.data_ptr(), dbias.data_ptr(), call))
+    return loss, dh, dweight, dbias
+
+
+class Scores(NamedTuple):
+    """What ``row_scores`` and ``head_scores`` return; what was not asked for is None."""
+
+    log_given: Optional[torch.Tensor]  # of the given classes' shape, float32
+    entropy: Optional[torch.Tensor]  # [N] float32
+    top: Optional[torch.Tensor]  # [N, top] int32
+    log_top: Optional[torch.Tensor]  # [N, top] float32
+
+
+def _scores(like, rows, given, top, entropy, rejected, device):
+    """(dynlp_scores, what it points to)."""
+    count = 0
+    if given is not None:
+        if given.dim() not in (1, 2) or given.shape[0] != rows:
+            _refuse(f"given: classes of {rows} rows are wanted, one or several for each")
+        count = 1 if given.dim() == 1 else given.shape[1]
+    if top < 0:
+        _refuse(f"the first {top} classes")
+    out = Scores(None if given is None else like.new_empty(given.shape, dtype=torch.float32),
+                 like.new_empty(rows, dtype=torch.float32) if entropy else None,
+                 like.new_empty((rows, top), dtype=torch.int32) if top else None,
+                 like.new_empty((rows, top), dtype=torch.float32) if top else None)
+    at = [None if t is None else t.data_ptr() for t in out]
+    return _Scores(count, top, _vector(given, "given", torch.int32, rows * count, device), at[0] if count else None, at[1], at[2], at[3],
+                   _vector(rejected, "rejected", torch.int32, 1, device)), out
+
+
+def row_scores(x, *, given=None, top=0, probabilities=False, entropy=True, rejected=None):
+    """dynlp_row_scores.  x [N, C]: rows of logits, or with probabilities=True of probabilities (what ``DynLP.get_labels`` returns first).
+    given [N] or [N, G] int32 (negative: padding, 0 comes back).  Returns ``Scores``.  rejected: an int32 tensor of one element that grows by the number
+    of given classes that are not below C, or None."""
+    device = _device(x, "x")
+    L = _library()
+    m = _matrix(x, "x", device)
+    s, out = _scores(x, m.rows, given, top, entropy, rejected, device)
+    call, space = _call(device, L.dynlp_row_scores_workspace(m.rows, m.dim, top))
+    _check(_run(device, L.dynlp_row_scores, m, bool(probabilities), s, call))
+    return out
+
+
+def head_scores(h, weight, bias=None, *, given=None, top=0, entropy=True, rejected=None):
+    """dynlp_head_scores: ``row_scores`` of the head's logits.  h [N, D], weight [C, D] of h's type, bias [C] float32 or None."""
+    device = _device(h, "h")
+    L = _library()
+    m, w = _matrix(h, "h", device), _matrix(weight, "weight", device)
+    b = _vector(bias, "bias", torch.float32, w.rows, device)
+    s, out = _scores(h, m.rows, given, top, entropy, rejected, device)
+    call, space = _call(device, L.dynlp_head_scores_workspace(m.rows, m.dim, min(w.rows, _MOST), m.type))
+    _check(_run(device, L.dynlp_head_scores, m, w, b, s, call))
+    return out
+
+
+def head_distill(h, weight, bias, classes, logits, *, temperature=1.0, row_weight=None, grad_scale=1.0, grads=True, dtype=torch.float32, rejected=None):
+    """dynlp_head_distill.  classes [N, K] int32 and logits [N, K] float32: the teacher's lists, as ``row_scores`` and ``head_scores`` return them (negative
+    class: no entry).  Returns (loss [N] float32, dh [N, D] of h's type, dweight [C, D] of ``dtype``, float32 or h's, dbias [C] float32); the last three are
+    None with grads=False."""
+    device = _device(h, "h")
+    L = _library()
+    m, w = _matrix(h, "h", device), _matrix(weight, "weight", device)
+    b = _vector(bias, "bias", torch.float32, w.rows, device)
+    if classes.dim() != 2 or classes.shape[0] != m.rows:
+        _refuse(f"classes: lists of {m.rows} rows are wanted")
+    kept = classes.shape[1]
+    t = _Teacher(_vector(classes, "classes", torch.int32, m.rows * kept, device), _vector(logits, "logits", torch.float32, m.rows * kept, device),
+                 _vector(row_weight, "row_weight", torch.float32, m.rows, device), _vector(rejected, "rejected", torch.int32, 1, device), min(kept, _MOST),
+                 float(temperature), float(grad_scale))
+    if dtype not in _TYPES:
+        _refuse("dtype: float32, bfloat16 or float16 is wanted")
+    loss = h.new_empty(m.rows, dtype=torch.float32)
+    to = dw = None
+    dh = dweight = dbias = None
+    if grads:
+        dh = h.new_empty((m.rows, m.dim))
+        dweight = h.new_empty((w.rows, m.dim), dtype=dtype)
+        dbias = h.new_empty(w.rows, dtype=torch.float32)
+        to = _Matrix(dh.data_ptr(), m.rows, max(m.dim, 1), m.dim, m.type)
+        dw = _Matrix(dweight.data_ptr(), w.rows, max(m.dim, 1), m.dim, _TYPES[dtype])
+    call, space = _call(device, L.dynlp_head_distill_workspace(m.rows, m.dim, min(w.rows, _MOST), t.kept, m.type, _TYPES[dtype] if grads else -1))
+    _check(_run(device, L.dynlp_head_distill, m, w, b, t, loss.data_ptr(), to, dw, None if dbias is None else dbias.data_ptr(), call))
     return loss, dh, dweight, dbias
 
 
