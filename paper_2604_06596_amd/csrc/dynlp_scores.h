@@ -27,104 +27,381 @@ __device__ inline uint32_t order_of(float x) {
 __device__ inline uint64_t key_of(float x, int column) { return (uint64_t)order_of(x) << 32 | (uint32_t)~column; }
 __device__ inline int column_of_key(uint64_t key) { return (int)~(uint32_t)key; }
 
-// Sums over a row: m and s, t as above (PROB: m is not used).
+__device__ inline float value_of(uint64_t key) {
+    const uint32_t o = (uint32_t)(key >> 32);
+    return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
+}
+
+// f over the 64 lanes, by moves between neighbours (16 lanes, then rows of them); the result is in every lane.
+template <typename F>
+__device__ inline uint32_t over_wave(uint32_t v, F f) {
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x121, 0xf, 0xf, false));  // rotated by 1, 2, 4, 8
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x122, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x124, 0xf, 0xf, false));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x128, 0xf, 0xf, false));
+    const uint32_t a = f((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
+    const uint32_t b = f((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48));
+    return f(a, b);
+}
+__device__ inline float lanes_max(float v) {
+    return __uint_as_float(over_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+__device__ inline float lanes_sum(float v) {
+    return __uint_as_float(over_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ inline uint32_t lanes_max(uint32_t v) {
+    return over_wave(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ inline uint32_t lanes_min(uint32_t v) {
+    return over_wave(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+__device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+
+// ---- sums -------------------------------------------------------------------------------------------------------------
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// m and s as above, and t in logarithms of two.  PROB: m is not used.
 struct RowSums {
     float m, s, t;
     __device__ static RowSums none() { return {-INFINITY, 0.f, 0.f}; }
-};
-template <bool PROB>
-__device__ inline void add_value(RowSums& a, float x) {
-    if constexpr (PROB) {
-        a.s += x;
-        a.t += x == 0.f ? 0.f : x * logf(x);
-    } else {
-        if (x > a.m) {
-            const float d = a.m - x, f = a.m == -INFINITY ? 0.f : expf(d);
-            a.t = a.m == -INFINITY ? a.t : f * (a.t + a.s * d);
-            a.s *= a.m == -INFINITY ? 1.f : f;
-            a.m = x;
-        }
-        const float d = x - a.m, e = expf(d);
-        if (x != -INFINITY) a.s += e, a.t += e == 0.f ? 0.f : e * d;
-    }
-}
-// Sums of two parts of a row.
-template <bool PROB>
-__device__ inline RowSums joined(const RowSums& a, const RowSums& b) {
-    if constexpr (PROB) return {0.f, a.s + b.s, a.t + b.t};
-    RowSums r{fmaxf(a.m, b.m), 0.f, 0.f};
-    for (const RowSums* x : {&a, &b}) {
-        const float d = x->m - r.m;
-        if (x->m == -INFINITY) {
-            r.s += x->s, r.t += x->t;  // nothing, or not a number
-        } else {
-            const float f = expf(d);
-            r.s += f * x->s;
-            r.t += f == 0.f ? 0.f : f * (x->t + x->s * d);
-        }
-    }
-    return r;
-}
-// Log probability of value x of a row.  A row of nothing but -infinity (zeros) has 1/C everywhere.
-template <bool PROB>
-__device__ inline float log_of(float x, const RowSums& a, float log_s, int dim) {
-    if (a.s == 0.f) return -logf((float)dim);
-    return PROB ? logf(x) - log_s : (x - a.m) - log_s;
-}
-template <bool PROB>
-__device__ inline float entropy_of(const RowSums& a, float log_s, int dim) {
-    return a.s == 0.f ? logf((float)dim) : log_s - a.t / a.s;
-}
-
-template <typename V, typename F>
-__device__ inline V over_block(V v, V* space, F f) {
-    for (int d = 1; d < kWave; d <<= 1) {
-        constexpr int n = sizeof(V) / 4;
-        int word[n];
-        __builtin_memcpy(word, &v, sizeof v);
-        for (int k = 0; k < n; ++k) word[k] = __shfl_xor(word[k], d, kWave);
-        V o;
-        __builtin_memcpy(&o, word, sizeof o);
-        v = lane_id() & d ? f(o, v) : f(v, o);
-    }
-    __syncthreads();
-    if (lane_id() == 0) space[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = space[0];
-    for (int w = 1; w < (int)blockDim.x / kWave; ++w) v = f(v, space[w]);
-    return v;
-}
-
-// A workgroup per row.
-template <typename T, bool PROB>
-__global__ __launch_bounds__(kBlock) void k_row_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
-    __shared__ RowSums sums[kBlock / kWave];
-    __shared__ uint64_t best[kBlock / kWave];
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const T* p = x + row * ld;
-        RowSums a = RowSums::none();
-        for (int c = threadIdx.x; c < dim; c += kBlock) add_value<PROB>(a, to_float(p[c]));
-        a = over_block(a, sums, [](const RowSums& u, const RowSums& v) { return joined<PROB>(u, v); });
-        const float log_s = logf(a.s);
-        const int64_t to = row0 + row;
-        if (threadIdx.x == 0 && o.entropy) o.entropy[to] = entropy_of<PROB>(a, log_s, dim);
-        for (int k = threadIdx.x; k < o.given; k += kBlock) {
-            const int c = o.classes[to * o.given + k];
-            if (c >= dim && o.rejected) atomicAdd(o.rejected, 1);
-            o.log_given[to * o.given + k] = c >= 0 && c < dim ? log_of<PROB>(to_float(p[c]), a, log_s, dim) : 0.f;
-        }
-        uint64_t last = ~uint64_t(0);
-        for (int k = 0; k < o.top; ++k) {
-            uint64_t mine = 0;
-            for (int c = threadIdx.x; c < dim; c += kBlock) {
-                const uint64_t key = key_of(to_float(p[c]), c);
-                if (key < last && key > mine) mine = key;
+    // Values v, of which those that are not there are -infinity.  What is -infinity adds nothing, what is not a number makes s so.
+    template <bool PROB, int N>
+    __device__ void add(const float (&v)[N]) {
+        if constexpr (PROB) {
+            for (int k = 0; k < N; ++k) {
+                const float x = v[k] == -INFINITY ? 0.f : v[k];
+                s += x;
+                t += x == 0.f ? 0.f : x * __builtin_amdgcn_logf(x);
             }
-            last = over_block(mine, best, [](uint64_t u, uint64_t v) { return u > v ? u : v; });
-            if (threadIdx.x == 0) {
-                const int c = column_of_key(last);
-                if (o.top_classes) o.top_classes[to * o.top + k] = c;
-                if (o.log_top) o.log_top[to * o.top + k] = log_of<PROB>(to_float(p[c]), a, log_s, dim);
+        } else {
+            float top = m;
+            for (int k = 0; k < N; ++k) top = fmaxf(top, v[k]);
+            rescale(top);
+            const float base = fmaxf(m, -3e38f);  // a row of nothing but -infinity stays at 0
+            for (int k = 0; k < N; ++k) {
+                const float y = (v[k] - base) * kLog2e, e = __builtin_amdgcn_exp2f(y);
+                s += e;
+                t += e * fmaxf(y, -1e30f);
+            }
+        }
+    }
+    __device__ void rescale(float top) {
+        const float y = (m - top) * kLog2e;
+        if (m == -INFINITY) {
+            // nothing yet, or not a number
+        } else if (y != 0.f) {
+            const float f = __builtin_amdgcn_exp2f(y);
+            t = f * (t + s * fmaxf(y, -1e30f));
+            s *= f;
+        }
+        m = top;
+    }
+    template <bool PROB>
+    __device__ void over_lanes() {
+        if constexpr (!PROB) rescale(lanes_max(m));
+        s = lanes_sum(s);
+        t = lanes_sum(t);
+    }
+    template <bool PROB>
+    __device__ void join(RowSums o) {
+        if constexpr (!PROB) {
+            const float top = fmaxf(m, o.m);
+            rescale(top);
+            o.rescale(top);
+        }
+        s += o.s;
+        t += o.t;
+    }
+};
+// What the sums of a whole row say.  A row of nothing but -infinity (zeros) has 1/C everywhere.
+template <bool PROB>
+struct RowLog {
+    float m, log_s, entropy, uniform;
+    bool none;
+    __device__ RowLog(const RowSums& a, int dim) {
+        m = a.m;
+        none = a.s == 0.f;
+        log_s = logf(a.s);
+        uniform = none ? logf((float)dim) : 0.f;
+        entropy = none ? uniform : log_s - a.t / a.s * kLn2;
+    }
+    __device__ float of(float x) const { return none ? -uniform : PROB ? logf(x) - log_s : (x - m) - log_s; }
+};
+
+// ---- the first classes ------------------------------------------------------------------------------------------------
+
+// A number such that at least k of the wave's `order(j)`, j < n, are not below it, and seldom many more: the interval between the least and the largest is halved up to
+// `most` times.  Orders that are not there are 0; there are k others.
+template <typename O>
+__device__ inline uint32_t threshold(int n, int k, int most, O order) {
+    const uint32_t least = order_of(-INFINITY);
+    uint32_t high = 0, low = ~0u;
+    int count = 0;
+    for (int j = 0; j < n; ++j) {
+        const uint32_t o = order(j);
+        high = max(high, o);
+        low = min(low, o > least ? o : ~0u);
+        count += __popcll(__ballot(o > least));
+    }
+    if (count < k) return least;
+    high = lanes_max(high);
+    low = lanes_min(low);
+    for (int step = 0; step < most && low < high; ++step) {
+        const uint32_t middle = low + ((high - low) >> 1) + 1;
+        count = 0;
+        for (int j = 0; j < n; ++j) count += __popcll(__ballot(order(j) >= middle));
+        if (count >= k) low = middle;
+        else high = middle - 1;
+        if (count == k) break;
+    }
+    return low;
+}
+
+// A wave's candidates in shared memory, in no order; those that cannot be among the first k are no longer there.
+struct Candidates {
+    uint64_t* key;
+    int count;       // the same for all lanes
+    uint32_t above;  // what is not above it in order is none
+    float over;      // the same as a value, for a first look
+    __device__ void none(uint64_t* space) {
+        key = space;
+        count = 0;
+        above = 0;
+        over = -INFINITY;
+    }
+    __device__ void raise(uint32_t order) {
+        above = order;
+        const float v = value_of((uint64_t)order << 32);
+        over = order < 0x00800000u || v != v ? -INFINITY : v == 0.f ? -1e-37f : v;  // -0 comes before 0
+    }
+    __device__ void put(float x, int column, bool there) {
+        const uint32_t o = order_of(x);
+        const bool hit = there && o > above;
+        const uint64_t mask = __ballot(hit);
+        if (mask == 0) return;
+        if (hit) key[count + lanes_before(mask)] = (uint64_t)o << 32 | (uint32_t)~column;
+        count += __popcll(mask);
+    }
+    // Leaves those whose key is not below `least`.
+    __device__ void keep(uint64_t least) {
+        int to = 0;
+        for (int at = 0; at < count; at += kWave) {
+            const int i = at + lane_id();
+            const uint64_t k = i < count ? key[i] : 0;
+            const bool stays = i < count && k >= least;
+            const uint64_t mask = __ballot(stays);
+            if (stays) key[to + lanes_before(mask)] = k;
+            to += __popcll(mask);
+        }
+        count = to;
+    }
+    // Leaves k at least and `most` at most; k <= most.
+    __device__ void cut(int k, int most) {
+        if (count <= k) return;
+        const int n = (count + kWave - 1) / kWave;
+        uint32_t least = threshold(n, k, 14, [&](int j) { return (int)(j * kWave + lane_id()) < count ? (uint32_t)(key[j * kWave + lane_id()] >> 32) : 0u; });
+        keep((uint64_t)least << 32);
+        if (count > most) {  // equal or nearly equal values: exactly k, bit by bit
+            const int left = (count + kWave - 1) / kWave;
+            uint64_t exact = 0;
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t next = exact | uint64_t(1) << bit;
+                int above_it = 0;
+                for (int j = 0; j < left; ++j) {
+                    const int i = j * kWave + lane_id();
+                    above_it += __popcll(__ballot(i < count && key[i] >= next));
+                }
+                if (above_it >= k) exact = next;
+            }
+            keep(exact);
+            raise((uint32_t)(exact >> 32));  // those that come have higher columns
+        } else {
+            raise(max(least, 1u) - 1u);
+        }
+    }
+};
+
+constexpr int kCandidates = 384;  // that a wave has before the list is cut; DYNLP_MAX_TOP is less
+
+// One wave's part of a row: turns of P pieces per lane, `waves` of them taking turns.
+template <typename T, bool PROB, int P>
+struct RowScan {
+    static constexpr int E = Piece<T>::n, N = P * E, turn = N * kWave;
+    __device__ static void load(const T* row, int from, int dim, float (&v)[N]) {
+        u32x4 piece[P];
+        if (from + turn <= dim) {
+            for (int p = 0; p < P; ++p) piece[p] = load_piece(row + from + (p * kWave + lane_id()) * E);
+        } else {
+            for (int p = 0; p < P; ++p) {
+                const int col = from + (p * kWave + lane_id()) * E;
+                piece[p] = col < dim ? load_columns(row, col, dim) : u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+        for (int p = 0; p < P; ++p) {
+            float f[E];
+            widen(piece[p], f, T());
+            for (int e = 0; e < E; ++e) v[p * E + e] = f[e];
+        }
+        if (from + turn > dim)
+            for (int p = 0; p < P; ++p)
+                for (int e = 0; e < E; ++e)
+                    if (from + (p * kWave + (int)lane_id()) * E + e >= dim) v[p * E + e] = -INFINITY;
+    }
+    __device__ static void run(const T* row, int dim, int wave, int waves, int top, RowSums& sums, Candidates& c) {
+#pragma unroll 1
+        for (int from = wave * turn; from < dim; from += waves * turn) {
+            float v[N];
+            load(row, from, dim, v);
+            sums.add<PROB>(v);
+            if (top == 0) continue;
+            if (from == wave * turn) {
+                // of 128 groups of values the k-th largest maximum: k values are not below it
+                float best[2] = {-INFINITY, -INFINITY};
+                for (int k = 0; k < N; ++k) best[k / ((N + 1) / 2)] = fmaxf(best[k / ((N + 1) / 2)], v[k]);
+                const uint32_t order[2] = {order_of(best[0]), order_of(best[1])};
+                c.raise(max(threshold(2, top, 14, [&](int j) { return order[j]; }), 1u) - 1u);
+            }
+            float best = -INFINITY;
+            for (int k = 0; k < N; ++k) best = fmaxf(best, v[k]);
+            if (!__any(best > c.over || c.over == -INFINITY)) continue;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int col = from + (p * kWave + (int)lane_id()) * E + e;
+                    c.put(v[p * E + e], col, col < dim);
+                }
+                if (c.count > kCandidates) c.cut(top, kCandidates);
+            }
+        }
+    }
+};
+
+constexpr int row_lists(int waves) { return waves == 1 ? kBlock / kWave : waves; }
+template <typename T>
+constexpr int row_space(int waves) {
+    return row_lists(waves) * ((kCandidates + kWave * Piece<T>::n) * 8 + (int)sizeof(RowSums) + 4);
+}
+// WAVES waves for each row; four rows to a workgroup where it is one.
+template <typename T, bool PROB, int P, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+    using Scan = RowScan<T, PROB, P>;
+    constexpr int kLists = row_lists(WAVES), kSpace = kCandidates + kWave * Scan::E;
+    extern __shared__ char space[];
+    uint64_t* keys = reinterpret_cast<uint64_t*>(space);
+    RowSums* parts = reinterpret_cast<RowSums*>(keys + kLists * kSpace);
+    int* counts = reinterpret_cast<int*>(parts + kLists);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * kLists + wave : blockIdx.x, step = WAVES == 1 ? (int64_t)gridDim.x * kLists : gridDim.x;
+    for (int64_t row = first; row < rows; row += step) {
+        const T* p = x + row * ld;
+        const int64_t to = row0 + row;
+        RowSums sums = RowSums::none();
+        Candidates c;
+        c.none(keys + wave * kSpace);
+        Scan::run(p, dim, WAVES == 1 ? 0 : wave, WAVES, o.top, sums, c);
+        sums.over_lanes<PROB>();
+        if constexpr (WAVES > 1) {
+            if (o.top) c.cut(o.top, kCandidates);
+            if (lane_id() == 0) parts[wave] = sums, counts[wave] = c.count;
+            uint64_t mine[kCandidates / kWave];
+            for (int j = 0; j < kCandidates / kWave; ++j) mine[j] = j * kWave + (int)lane_id() < c.count ? c.key[j * kWave + lane_id()] : 0;
+            __syncthreads();
+            sums = parts[0];
+            for (int w = 1; w < WAVES; ++w) sums.join<PROB>(parts[w]);
+            int before = 0, all = 0;
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) before += counts[w];
+                all += counts[w];
+            }
+            for (int j = 0; j < kCandidates / kWave; ++j)
+                if (j * kWave + (int)lane_id() < c.count) keys[before + j * kWave + lane_id()] = mine[j];
+            __syncthreads();
+            c.key = keys;
+            c.count = all;
+        }
+        const RowLog<PROB> log(sums, dim);
+        if (threadIdx.x % (WAVES * kWave) == 0 && o.entropy) o.entropy[to] = log.entropy;
+        for (int k = threadIdx.x % (WAVES * kWave); k < o.given; k += WAVES * kWave) {
+            const int g = o.classes[to * o.given + k];
+            if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
+            o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
+        }
+        if (o.top && (WAVES == 1 || wave == 0)) {
+            c.cut(o.top, kCandidates);
+            // the place of a candidate is how many come before it
+            for (int at = 0; at < c.count; at += kWave) {
+                const int i = at + lane_id();
+                const uint64_t key = i < c.count ? c.key[i] : 0;
+                int place = 0;
+                for (int j = 0; j < c.count; ++j) place += c.key[j] > key;
+                if (i < c.count && place < o.top) {
+                    if (o.top_classes) o.top_classes[to * o.top + place] = column_of_key(key);
+                    if (o.log_top) o.log_top[to * o.top + place] = log.of(value_of(key));
+                }
+            }
+        }
+        if constexpr (WAVES > 1) __syncthreads();
+    }
+}
+
+// Rows of up to 64 values: 16 lanes for each, four values in a lane.  The first classes are taken one after the other.
+template <typename T, bool PROB>
+__global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+    const int r = threadIdx.x & 15, col = 4 * r;
+    for (int64_t first = (int64_t)blockIdx.x * (kBlock / 16); first < rows; first += (int64_t)gridDim.x * (kBlock / 16)) {
+        const int64_t row = first + threadIdx.x / 16, to = row0 + row;
+        const bool there = row < rows;
+        const T* p = x + min(row, rows - 1) * ld;
+        float v[4];
+        if (col + 4 <= dim) {
+            Columns<T, 4> d;
+            __builtin_memcpy(d.d, p + col, sizeof d.d);
+            for (int k = 0; k < 4; ++k) v[k] = d.get(k);
+        } else {
+            for (int k = 0; k < 4; ++k) v[k] = col + k < dim ? to_float(p[col + k]) : -INFINITY;
+        }
+        auto turn = [](uint32_t u, int d) {
+            const int w = (int)u;
+            return (uint32_t)(d == 1   ? __builtin_amdgcn_update_dpp(w, w, 0x121, 0xf, 0xf, false)
+                              : d == 2 ? __builtin_amdgcn_update_dpp(w, w, 0x122, 0xf, 0xf, false)
+                              : d == 4 ? __builtin_amdgcn_update_dpp(w, w, 0x124, 0xf, 0xf, false)
+                                       : __builtin_amdgcn_update_dpp(w, w, 0x128, 0xf, 0xf, false));
+        };
+        auto turned = [&](float u, int d) { return __uint_as_float(turn(__float_as_uint(u), d)); };
+        RowSums a = RowSums::none();
+        a.add<PROB>(v);
+        if constexpr (!PROB) {
+            float top = a.m;
+            for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, turned(top, d));
+            a.rescale(top);
+        }
+        for (int d = 1; d < 16; d <<= 1) a.s += turned(a.s, d), a.t += turned(a.t, d);
+        const RowLog<PROB> log(a, dim);
+        if (there && r == 0 && o.entropy) o.entropy[to] = log.entropy;
+        if (there)
+            for (int k = r; k < o.given; k += 16) {
+                const int g = o.classes[to * o.given + k];
+                if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
+                o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
+            }
+        if (o.top == 0) continue;
+        uint32_t order[4];
+        for (int k = 0; k < 4; ++k) order[k] = col + k < dim ? order_of(v[k]) : 0u;
+        for (int place = 0; place < o.top; ++place) {
+            uint32_t best = order[0], at = col;
+            for (int k = 1; k < 4; ++k)
+                if (order[k] > best) best = order[k], at = col + k;
+            for (int d = 1; d < 16; d <<= 1) {
+                const uint32_t other = turn(best, d), other_at = turn(at, d);
+                if (other > best || (other == best && other_at < at)) best = other, at = other_at;
+            }
+            for (int k = 0; k < 4; ++k)
+                if ((int)at == col + k) order[k] = 0u;
+            if (there && r == (place & 15)) {
+                if (o.top_classes) o.top_classes[to * o.top + place] = (int)at;
+                if (o.log_top) o.log_top[to * o.top + place] = log.of(value_of((uint64_t)best << 32));
             }
         }
     }

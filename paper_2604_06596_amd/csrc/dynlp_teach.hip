@@ -146,7 +146,23 @@ Scores scores_of(const dynlp_scores* s) {
 
 template <typename T, bool PROB>
 void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& o, int64_t row0, hipStream_t stream) {
-    k_row_scores<T, PROB><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
+    auto scan = [&](auto pieces, auto waves) {
+        constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
+        const int64_t blocks = W == 1 ? ceil_div(rows, kBlock / kWave) : rows;
+        static std::atomic<uint64_t> allowed{0};
+        allow_shared(k_row_scores<T, PROB, P, W>, allowed);
+        k_row_scores<T, PROB, P, W><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), W == 1 ? kBlock : W * kWave, row_space<T>(W), stream>>>(x, ld, rows, dim, o, row0);
+    };
+    using std::integral_constant;
+    constexpr int E = Piece<T>::n, most = 32 / E;  // pieces of a lane: 2,048 values of a wave
+    const int need = (int)std::min<int64_t>(ceil_div(dim, E * kWave), most);
+    if (dim <= 64) k_short_scores<T, PROB><<<(unsigned)std::min<int64_t>(ceil_div(rows, kBlock / 16), 1 << 20), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
+    else if (need == 1) scan(integral_constant<int, 1>(), integral_constant<int, 1>());
+    else if (need == 2) scan(integral_constant<int, 2>(), integral_constant<int, 1>());
+    else if (dim <= 1024 && most > 4) scan(integral_constant<int, 4>(), integral_constant<int, 1>());
+    else if (dim <= 2048) scan(integral_constant<int, most>(), integral_constant<int, 1>());
+    else if (rows > 512) scan(integral_constant<int, most>(), integral_constant<int, 4>());
+    else scan(integral_constant<int, most>(), integral_constant<int, 16>());
 }
 
 // Rows whose logits are in memory at a time.
