@@ -21,6 +21,7 @@
 
 #include "dynlp_device.h"
 #include "dynlp_matrix.h"
+#include "dynlp_teacher.h"
 
 namespace dynlp {
 
@@ -353,13 +354,15 @@ __device__ inline void head_dh(const Head& a, const W& w, int64_t first, const f
 }
 
 // What a lane needs of row `row` beside its logits, asked for before them.
+struct NoMore {};
 template <int CT>
 struct RowTarget {
+    using More = NoMore;
     f32x4 y[CT];
     float weight;
     bool use;
     // inner (the same for all lanes): 64 rows follow, so that a whole tile of classes may be read from every row.
-    __device__ inline void ask(const Head& a, const Loss& g, int64_t row, bool inner) {
+    __device__ inline void ask(const Head& a, const Loss& g, const NoMore&, int64_t row, bool inner) {
         const int q = lane_id() >> 4;
         const bool inside = row < a.rows;
         const int64_t at = inside ? row : a.rows - 1;
@@ -381,11 +384,104 @@ struct RowTarget {
             }
         }
     }
+    __device__ inline void make(const NoMore&, int64_t, f32x4 (&)[CT]) {}
+    __device__ inline float whole(const NoMore&, float loss) const { return loss; }
+};
+
+// The same of a teacher's list: q = softmax of its entries over T, z over T, and T^2 (sum of q log q + cross entropy) for the loss.  The four lanes of a row have every
+// fourth entry each, of the first 16 asked for before the logits; for the distribution each lane looks at all of them and takes those of its classes.
+template <int CT>
+struct RowList {
+    using More = Teacher;
+    static constexpr int kAhead = 4;
+    int c[kAhead];
+    float u[kAhead];
+    f32x4 y[CT];
+    float weight, entropy;
+    bool use;
+    __device__ inline static void entry(const Teacher& t, int64_t row, int k, int& c, float& u) {
+        c = -1, u = -INFINITY;
+        if (k < t.kept) {
+            c = t.classes[row * t.kept + k];
+            u = t.logits[row * t.kept + k];
+        }
+    }
+    // What is no class is no entry; `counts`: whether it is counted.
+    __device__ inline static void check(const Teacher& t, bool counts, int& c, float& u) {
+        if (c >= t.count) {
+            if (counts && t.rejected) atomicAdd(t.rejected, 1);
+            c = -1;
+        }
+        if (c < 0) u = -INFINITY;
+    }
+    __device__ inline void ask(const Head& a, const Loss&, const Teacher& t, int64_t row, bool) {
+        const int q = lane_id() >> 4;
+        const int64_t at = min(row, a.rows - 1);
+        use = row < a.rows;
+        weight = t.row_weight ? t.row_weight[at] : 1.f;
+        for (int k = 0; k < kAhead; ++k) entry(t, at, 4 * k + q, c[k], u[k]);
+    }
+    // f(entries of all lanes) for 16 entries at a time.
+    template <typename F>
+    __device__ inline void each(const Teacher& t, int64_t at, F f) {
+        f(c, u);
+#pragma unroll 1
+        for (int from = 4 * kAhead; from < t.kept; from += 4 * kAhead) {
+            int more_c[kAhead];
+            float more_u[kAhead];
+            for (int k = 0; k < kAhead; ++k) {
+                entry(t, at, from + 4 * k + (lane_id() >> 4), more_c[k], more_u[k]);
+                check(t, false, more_c[k], more_u[k]);
+            }
+            f(more_c, more_u);
+        }
+    }
+    __device__ inline void make(const Teacher& t, int64_t at, f32x4 (&z)[CT]) {
+        const int q = lane_id() >> 4, r = lane_id() & 15;
+        for (int k = 0; k < kAhead; ++k) check(t, use, c[k], u[k]);
+        if (use)  // the others are counted once
+            for (int k = 4 * kAhead + q; k < t.kept; k += 4) {
+                int more_c;
+                float more_u;
+                entry(t, at, k, more_c, more_u);
+                check(t, true, more_c, more_u);
+            }
+        float top = -INFINITY, sum = 0.f;
+        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead]) {
+            for (int k = 0; k < kAhead; ++k) top = fmaxf(top, v[k]);
+        });
+        top = row_max(top);
+        auto power = [&](float v) { return v == -INFINITY ? 0.f : exp_below_0((v - top) * t.inverse); };
+        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead]) {
+            for (int k = 0; k < kAhead; ++k) sum += power(v[k]);
+        });
+        sum = row_sum(sum);
+        use = use && sum != 0.f;
+        const float log_sum = logf(sum), inverse = sum != 0.f ? 1.f / sum : 0.f;
+        entropy = 0.f;
+        for (int i = 0; i < CT; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        each(t, at, [&](const int (&cs)[kAhead], const float (&v)[kAhead]) {
+            for (int k = 0; k < kAhead; ++k) {
+                const float mine = power(v[k]) * inverse;
+                if (mine != 0.f) entropy += mine * ((v[k] - top) * t.inverse - log_sum);
+                for (int from = 0; from < 4; ++from) {
+                    const int other = __shfl(cs[k], 16 * from + r, kWave);
+                    const float p = __shfl(mine, 16 * from + r, kWave);
+                    for (int m = 0; m < CT; ++m)
+                        for (int i = 0; i < 4; ++i) y[m][i] += other == 16 * m + 4 * q + i ? p : 0.f;
+                }
+            }
+        });
+        entropy = row_sum(entropy);
+        for (int m = 0; m < CT; ++m)
+            for (int i = 0; i < 4; ++i) z[m][i] *= t.inverse;
+    }
+    __device__ inline float whole(const Teacher& t, float loss) const { return t.square * (entropy + loss); }
 };
 
 // From the logits z of row `row` of a lane (first + 16 m + r): its loss is stored, z becomes dz.  Returns whether the row takes part.
-template <int CT>
-__device__ inline bool head_dz(const Loss& g, int64_t row, int64_t rows, const RowTarget<CT>& target, f32x4 (&z)[CT]) {
+template <int CT, typename R>
+__device__ inline bool head_dz(const Loss& g, const typename R::More& more, int64_t row, int64_t rows, const R& target, f32x4 (&z)[CT]) {
     f32x4 e[CT];
     for (int t = 0; t < CT; ++t) e[t] = z[t];
     float top;
@@ -404,27 +500,28 @@ __device__ inline bool head_dz(const Loss& g, int64_t row, int64_t rows, const R
     const float scale = g.grad_scale * target.weight, part = total / sum;
     for (int t = 0; t < CT; ++t)
         for (int i = 0; i < 4; ++i) z[t][i] = use ? scale * (part * e[t][i] - target.y[t][i]) : 0.f;
-    if (row < rows && lane_id() < 16 && g.loss) g.loss[row] = use ? target.weight * loss : 0.f;
+    if (row < rows && lane_id() < 16 && g.loss) g.loss[row] = use ? target.weight * target.whole(more, loss) : 0.f;
     return use;
 }
 
 // Loss, dz and dh of a tile of rows: logits, softmax and the product with W, without leaving the registers.  For heads whose W and dweight do
 // not fit a workgroup, and where no dweight is asked for.  Rows from row0 on.
-template <typename T, int CT>
-__global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g, int64_t row0) {
+template <typename T, int CT, typename R>
+__global__ __launch_bounds__(kBlock) void k_head_loss(Head a, Loss g, typename R::More more, int64_t row0) {
     constexpr int NT = kHeadTiles;
     const int64_t first = row0 + (int64_t)blockIdx.x * kHeadRows + (threadIdx.x / kWave) * (NT * 16);
     if (first >= a.rows) return;
     const int q = lane_id() >> 4, r = lane_id() & 15;
     const WeightRows<T> w{static_cast<const T*>(a.weight), a.bias, a.ld_w, a.dim, a.classes};
     f32x4 z[NT][CT];
-    RowTarget<CT> target[NT];
+    R target[NT];
     bool kept[NT];
-    for (int m = 0; m < NT; ++m) target[m].ask(a, g, first + 16 * m + r, first + 16 * NT + 64 <= a.rows);
+    for (int m = 0; m < NT; ++m) target[m].ask(a, g, more, first + 16 * m + r, first + 16 * NT + 64 <= a.rows);
     head_logits<T, CT, NT, 2>(a, w, first, z);
     for (int m = 0; m < NT; ++m) {
         const int64_t row = first + 16 * m + r;
-        kept[m] = head_dz(g, row, a.rows, target[m], z[m]);
+        target[m].make(more, min(row, a.rows - 1), z[m]);
+        kept[m] = head_dz(g, more, row, a.rows, target[m], z[m]);
         if (row < a.rows && g.dz) {
             if (q == 0) g.kept[row] = kept[m] ? 1 : 0;
             for (int t = 0; t < CT; ++t) *reinterpret_cast<f32x4*>(g.dz + row * (16 * CT) + 16 * t + 4 * q) = z[m][t];
@@ -678,8 +775,8 @@ __host__ __device__ inline int fused_splits(int groups, int waves) {
 // for no third.
 // Workgroups stay: W is copied to shared memory once, and a wave keeps its columns of dweight (GPW groups of 64, a quad for each of 16 lanes) in registers
 // over all tiles of 64 or 128 rows.  Where there are fewer groups of columns than waves, several waves share the rows.
-template <typename T, int CT, int GPW>
-__global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) void k_head_fused(Head a, Loss g, float* part) {
+template <typename T, int CT, int GPW, typename R>
+__global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) void k_head_fused(Head a, Loss g, typename R::More more, float* part) {
     constexpr int kCols = kFusedColumns, kWaves = fused_waves(CT), NT = 1, kFusedRows = fused_rows(CT);
     extern __shared__ char space[];
     const int q = lane_id() >> 4, r = lane_id() & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -703,13 +800,14 @@ __global__ __launch_bounds__(kWave * fused_waves(CT), CT <= 2 ? 4 : 3 - GPW) voi
     for (int64_t tile = (int64_t)blockIdx.x * kFusedRows; tile < a.rows; tile += (int64_t)gridDim.x * kFusedRows) {
         {
             f32x4 z[NT][CT];
-            RowTarget<CT> target[NT];
+            R target[NT];
             bool use[NT];
-            for (int m = 0; m < NT; ++m) target[m].ask(a, g, tile + mine + 16 * m + r, tile + kFusedRows + 64 <= a.rows);
+            for (int m = 0; m < NT; ++m) target[m].ask(a, g, more, tile + mine + 16 * m + r, tile + kFusedRows + 64 <= a.rows);
             head_logits<T, CT, NT, 2>(a, w, tile + mine, z);
             for (int m = 0; m < NT; ++m) {
                 const int row = mine + 16 * m + r;
-                use[m] = head_dz(g, tile + row, a.rows, target[m], z[m]);
+                target[m].make(more, min(tile + row, a.rows - 1), z[m]);
+                use[m] = head_dz(g, more, tile + row, a.rows, target[m], z[m]);
                 const uint16_t bits = (uint16_t)__ballot(use[m]);
                 if (lane_id() == 0) kept16[wave * NT + m] = bits;
                 if constexpr (!__is_same(T, bf16))
@@ -794,7 +892,8 @@ inline int64_t fused_bytes(int dim) {
 }
 
 // Sums the parts: 16 neighbouring elements per turn of a workgroup, 16 groups of lanes taking turns on the parts, then joined in order.
-__global__ __launch_bounds__(kBlock) void k_head_join(const float* part, int splits, int classes, int dim, float* dweight, float* dbias) {
+template <typename O>
+__global__ __launch_bounds__(kBlock) void k_head_join(const float* part, int splits, int classes, int dim, O* dweight, int64_t ld, float* dbias) {
     __shared__ float sums[16][17];
     const int e = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t size = (int64_t)classes * (dim + 1);
@@ -810,7 +909,7 @@ __global__ __launch_bounds__(kBlock) void k_head_join(const float* part, int spl
             for (int k = 1; k < 16; ++k) s += sums[k][e];
             const int c = (int)(at / (dim + 1)), k = (int)(at - (int64_t)c * (dim + 1));
             if (k < dim) {
-                if (dweight) dweight[(int64_t)c * dim + k] = s;
+                if (dweight) dweight[c * ld + k] = (O)s;
             } else if (dbias) {
                 dbias[c] = s;
             }

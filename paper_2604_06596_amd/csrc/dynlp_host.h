@@ -17,6 +17,12 @@ namespace dynlp {
 
 std::string& thread_error();  // what dynlp_last_error(NULL) returns; dynlp.hip
 
+// Learning from a teacher's first classes with a head of up to DYNLP_MAX_CLASSES classes, arguments checked (dynlp_train.hip).
+struct Teacher;
+void distill_few_classes(const dynlp_matrix& h, const dynlp_matrix& weight, const float* bias, const Teacher& teacher, float grad_scale, float* loss,
+                         const dynlp_matrix* dh, const dynlp_matrix* dweight, float* dbias, const dynlp_call* call);
+int64_t distill_few_classes_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type);
+
 namespace {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -6,6 +6,7 @@
 // with W and h (k_wide, classes as its fast index m, rows as n).  A head's own rounding needs one term; dweight in 32 bits takes as many as hold dz.
 #pragma once
 
+#include "dynlp_teacher.h"
 #include "dynlp_wide.h"
 
 namespace dynlp {
@@ -89,14 +90,6 @@ struct Logits {
 
 // ---- the teacher's lists ----------------------------------------------------------------------------------------------
 
-struct Teacher {
-    const int32_t* classes;  // rows x kept
-    const float* logits;
-    const float* row_weight; // or NULL
-    int32_t* rejected;       // or NULL
-    int kept, count;         // of a list; classes of the head
-    float inverse;           // 1 / T
-};
 // Lists that each name a class once (others: -1), their probabilities, sum of q log q and weight of the row (0: left out).
 struct Lists {
     int32_t* classes;

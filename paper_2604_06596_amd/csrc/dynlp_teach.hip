@@ -349,6 +349,7 @@ extern "C" {
 
 int64_t dynlp_head_distill_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t kept, int32_t type, int32_t grad_type) {
     if (rows < 1 || rows > kMostRows || dim < 1 || dim > DYNLP_MAX_WIDE_DIM || classes < 1 || classes > DYNLP_MAX_WIDE_CLASSES || kept < 1 || kept > DYNLP_MAX_TOP) return 0;
+    if (classes <= DYNLP_MAX_CLASSES) return grad_type < 0 ? 0 : distill_few_classes_workspace(rows, dim, classes, type);
     TeachSpace s{};
     return teach_space(nullptr, rows, dim, classes, kept, type, grad_type, true, true, &s);
 }
@@ -387,6 +388,12 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         if (dbias) k_teach_zeros<float><<<(unsigned)ceil_div(classes, kBlock), kBlock, 0, stream>>>(dbias, classes, 1, classes);
         return launched();
     }
+    const Teacher t{teacher->classes, teacher->logits, teacher->row_weight, teacher->rejected, teacher->kept, classes, 1.f / teacher->temperature,
+                    teacher->temperature * teacher->temperature};
+    if (classes <= DYNLP_MAX_CLASSES) {
+        distill_few_classes(*h, *weight, bias, t, teacher->grad_scale * teacher->temperature, loss, want_h ? dh : nullptr, want_w ? dweight : nullptr, dbias, call);
+        return launched();
+    }
     TeachSpace s{};
     teach_space(static_cast<char*>(call->workspace), h->rows, dim, classes, teacher->kept, h->type, grad_type, !lies_well(*h), !lies_well(*weight), &s);
     const Laid w = lay_out(*weight, s.weight, stream);
@@ -401,7 +408,6 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         k_teach_begin<<<1, kBlock, 0, stream>>>(s.zeros, s.largest);
         Lists lists = s.lists;
         lists.largest = scaled ? s.largest : nullptr;
-        const Teacher t{teacher->classes, teacher->logits, teacher->row_weight, teacher->rejected, teacher->kept, classes, 1.f / teacher->temperature};
         const unsigned blocks = (unsigned)ceil_div(rows << group, kBlock);
         if (teacher->kept > kWave) k_teach_lists<2><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);
         else k_teach_lists<1><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);

@@ -388,6 +388,53 @@ int64_t loss_space(char* base, int64_t rows, int dim, int classes, int32_t type,
     return c.used;
 }
 
+// Enqueues loss and gradients of rows whose targets are R's; bytes: of the workspace that gradients of the head take, 0 where none is asked for.
+template <template <int> typename R, typename M>
+void launch_head_loss(const dynlp_matrix& h, const dynlp_matrix& weight, const float* bias, Loss g, const M& more, const dynlp_matrix* dh, void* dweight,
+                      int64_t ld_dweight, int32_t dweight_type, float* dbias, int64_t bytes, const dynlp_call* call) {
+    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
+    const Head a = head_of(&h, &weight, bias);
+    LossSpace s{};
+    if (bytes) loss_space(static_cast<char*>(call->workspace), a.rows, a.dim, a.classes, h.type, a.ld_h < kMostFusedStride, &s);
+    by_head(h.type, weight.rows, [&](auto type, auto tiles) {
+        using T = decltype(type);
+        constexpr int CT = decltype(tiles)::v;
+        g.dh = dh ? dh->data : nullptr;
+        g.ld_dh = dh ? dh->stride : 0;
+        g.dz = s.dz;
+        g.kept = s.kept;
+        if (a.rows > 0 && s.fused) {
+            auto fused = [&](auto per_wave) {
+                constexpr int GPW = decltype(per_wave)::v;
+                static std::atomic<uint64_t> allowed{0};
+                allow_shared(k_head_fused<T, CT, GPW, R<CT>>, allowed);
+                k_head_fused<T, CT, GPW, R<CT>><<<(unsigned)s.splits, kWave * fused_waves(CT), (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, more, s.part);
+            };
+            if constexpr (fused_waves(CT) < 8) {
+                if (a.dim > kFusedColumns * fused_waves(CT)) fused(Tiles<2>());
+                else fused(Tiles<1>());
+            } else {
+                fused(Tiles<1>());
+            }
+        } else if (a.rows > 0) {
+            for (int64_t row = 0; row < a.rows; row += kMostBlocks * kHeadRows)
+                k_head_loss<T, CT, R<CT>><<<(unsigned)std::min(ceil_div(a.rows - row, kHeadRows), kMostBlocks), kBlock, 0, stream>>>(a, g, more, row);
+        }
+        if (!bytes) return;
+        if (a.rows > 0 && !s.fused) {
+            const Outer o{a.h, s.dz, s.kept, s.part, a.ld_h, a.rows, s.per_wave, a.dim, a.classes};
+            k_head_outer<T, CT><<<dim3((unsigned)s.splits, (unsigned)ceil_div(a.dim, 16 * Piece<T>::n)), kBlock, 0, stream>>>(o);
+        }
+        auto join = [&](auto out) {
+            using O = decltype(out);
+            k_head_join<O><<<(unsigned)std::min(ceil_div((int64_t)a.classes * (a.dim + 1), 16), kMostBlocks), kBlock, 0, stream>>>(
+                s.part, a.rows > 0 ? s.splits : 0, a.classes, a.dim, static_cast<O*>(dweight), ld_dweight, dbias);
+        };
+        if (dweight && dweight_type != DYNLP_FLOAT32) join(T());
+        else join(float());
+    });
+}
+
 }  // namespace
 
 extern "C" {
@@ -437,42 +484,28 @@ dynlp_status dynlp_head_loss(const dynlp_matrix* h, const dynlp_matrix* weight, 
     }
     const int64_t bytes = dweight || dbias ? dynlp_head_loss_workspace(h->rows, h->dim, (int32_t)weight->rows, h->type) : 0;
     CHECK(check_workspace(call, bytes));
-    const hipStream_t stream = static_cast<hipStream_t>(call->stream);
-    const Head a = head_of(h, weight, bias);
-    LossSpace s{};
-    if (bytes) loss_space(static_cast<char*>(call->workspace), a.rows, a.dim, a.classes, h->type, a.ld_h < kMostFusedStride, &s);
-    by_head(h->type, weight->rows, [&](auto type, auto tiles) {
-        using T = decltype(type);
-        constexpr int CT = decltype(tiles)::v;
-        const Loss g{targets->soft, targets->hard, targets->row_weight, targets->rejected, targets->grad_scale, loss,
-                     dh ? dh->data : nullptr, dh ? dh->stride : 0, s.dz, s.kept};
-        if (a.rows > 0 && s.fused) {
-            auto fused = [&](auto per_wave) {
-                constexpr int GPW = decltype(per_wave)::v;
-                static std::atomic<uint64_t> allowed{0};
-                allow_shared(k_head_fused<T, CT, GPW>, allowed);
-                k_head_fused<T, CT, GPW><<<(unsigned)s.splits, kWave * fused_waves(CT), (size_t)fused_bytes<T, CT>(a.dim), stream>>>(a, g, s.part);
-            };
-            if constexpr (fused_waves(CT) < 8) {
-                if (a.dim > kFusedColumns * fused_waves(CT)) fused(Tiles<2>());
-                else fused(Tiles<1>());
-            } else {
-                fused(Tiles<1>());
-            }
-        } else if (a.rows > 0) {
-            for (int64_t row = 0; row < a.rows; row += kMostBlocks * kHeadRows)
-                k_head_loss<T, CT><<<(unsigned)std::min(ceil_div(a.rows - row, kHeadRows), kMostBlocks), kBlock, 0, stream>>>(a, g, row);
-        }
-        if (!bytes) return;
-        if (a.rows > 0 && !s.fused) {
-            const Outer o{a.h, s.dz, s.kept, s.part, a.ld_h, a.rows, s.per_wave, a.dim, a.classes};
-            k_head_outer<T, CT><<<dim3((unsigned)s.splits, (unsigned)ceil_div(a.dim, 16 * Piece<T>::n)), kBlock, 0, stream>>>(o);
-        }
-        k_head_join<<<(unsigned)std::min(ceil_div((int64_t)a.classes * (a.dim + 1), 16), kMostBlocks), kBlock, 0, stream>>>(
-            s.part, a.rows > 0 ? s.splits : 0, a.classes, a.dim, dweight, dbias);
-    });
+    const Loss g{targets->soft, targets->hard, targets->row_weight, targets->rejected, targets->grad_scale, loss, nullptr, 0, nullptr, nullptr};
+    launch_head_loss<RowTarget>(*h, *weight, bias, g, NoMore(), dh, dweight, h->dim, DYNLP_FLOAT32, dbias, bytes, call);
     return launched();
 }
+
+}  // extern "C"
+
+namespace dynlp {
+
+int64_t distill_few_classes_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type) { return dynlp_head_loss_workspace(rows, dim, classes, type); }
+
+void distill_few_classes(const dynlp_matrix& h, const dynlp_matrix& weight, const float* bias, const Teacher& teacher, float grad_scale, float* loss,
+                         const dynlp_matrix* dh, const dynlp_matrix* dweight, float* dbias, const dynlp_call* call) {
+    const int64_t bytes = dweight || dbias ? dynlp_head_loss_workspace(h.rows, h.dim, (int32_t)weight.rows, h.type) : 0;
+    const Loss g{nullptr, nullptr, nullptr, nullptr, grad_scale, loss, nullptr, 0, nullptr, nullptr};
+    launch_head_loss<RowList>(h, weight, bias, g, teacher, dh, dweight ? dweight->data : nullptr, dweight ? dweight->stride : 0,
+                              dweight ? dweight->type : DYNLP_FLOAT32, dbias, bytes, call);
+}
+
+}  // namespace dynlp
+
+extern "C" {
 
 // ---- AdamW ------------------------------------------------------------------------------------------------------------
 
