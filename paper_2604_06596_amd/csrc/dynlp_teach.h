@@ -48,18 +48,24 @@ __global__ __launch_bounds__(kBlock) void k_lay_out(const T* in, int64_t ld, int
 
 // ---- logits -----------------------------------------------------------------------------------------------------------
 
-// The tile's bias in shared memory: -infinity, which makes a logit so whatever h holds, for what is not a class.
+// The tile's bias, times a factor, in shared memory: -infinity, which makes a logit so whatever h holds, for what is not a class.  Returns whether there is any such.
 template <typename S>
-__device__ inline const float* tile_bias(const float* bias, int first, int classes, char* space) {
+__device__ inline bool tile_bias(const float* bias, float factor, int first, int classes, char* space) {
     float* b = reinterpret_cast<float*>(space);
-    for (int k = threadIdx.x; k < S::TM; k += kBlock) b[k] = first + k >= classes ? -INFINITY : bias ? bias[first + k] : 0.f;
-    __syncthreads();
-    return b;
+    bool shut = false;
+    for (int k = threadIdx.x; k < S::TM; k += kBlock) {
+        b[k] = first + k >= classes ? -INFINITY : bias ? bias[first + k] * factor : 0.f;
+        shut |= b[k] == -INFINITY;
+    }
+    return __syncthreads_or(shut);
 }
-__device__ inline void add_bias(const float* b, float (&v)[16]) {
+// v = v factor + bias.
+__device__ inline void add_bias(const float* b, float factor, bool shut, float (&v)[16]) {
     for (int k = 0; k < 16; k += 4) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(b + k);
-        for (int i = 0; i < 4; ++i) v[k + i] = x[i] == -INFINITY ? x[i] : v[k + i] + x[i];
+        for (int i = 0; i < 4; ++i) v[k + i] = __builtin_fmaf(v[k + i], factor, x[i]);
+        if (shut)
+            for (int i = 0; i < 4; ++i) v[k + i] = x[i] == -INFINITY ? x[i] : v[k + i];
     }
 }
 
@@ -71,7 +77,8 @@ struct Logits {
     int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        const float* b = tile_bias<S>(bias, at.tile_m * S::TM, classes, space) + at.wave_m * (16 * S::MI);
+        const bool shut = tile_bias<S>(bias, 1.f, at.tile_m * S::TM, classes, space);
+        const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const int q = lane_id() >> 4, r = lane_id() & 15;
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
@@ -81,7 +88,7 @@ struct Logits {
                 if (m >= ld) continue;
                 float v[16];
                 sixteen(acc[i], j, v);
-                add_bias(b + 64 * j + 16 * q, v);
+                add_bias(b + 64 * j + 16 * q, 1.f, shut, v);
                 store_values<16>(z + n * ld + m, v);
             }
         }
@@ -90,13 +97,15 @@ struct Logits {
 
 // ---- the teacher's lists ----------------------------------------------------------------------------------------------
 
-// Lists that each name a class once (others: -1), their probabilities, sum of q log q and weight of the row (0: left out).
+// Entries of 16 rows, ordered by the tile of classes that they lie in: their row and class there, and q.  A class that a row names several times is one entry.
+constexpr int kListRows = 16, kListClasses = 256;
 struct Lists {
-    int32_t* classes;
-    float* q;
-    float* entropy;
-    float* weight;
+    uint2* entry;       // [16 rows][16 kept]: row << 8 | class, bits of q
+    uint32_t* start;    // [16 rows][tiles + 1]
+    float* entropy;     // sum of q log q of a row
+    float* weight;      // of a row; 0: left out
     uint32_t* largest;  // bits of the largest finite |weight|, or NULL
+    int kept, tiles;
 };
 
 // zeros: 512 bytes of them.
@@ -105,18 +114,30 @@ __global__ __launch_bounds__(kBlock) inline void k_teach_begin(uint32_t* zeros, 
     if (threadIdx.x == 0) *largest = 0;
 }
 
-// 1 << log2 lanes per row, E entries for each.
+__device__ inline float over_16(float v, bool sum) {
+    for (int d = 1; d < 16; d <<= 1) {
+        const float o = __shfl_xor(v, d, kWave);
+        v = sum ? v + o : fmaxf(v, o);
+    }
+    return v;
+}
+
+// 16 rows to a workgroup, 16 lanes and E entries in each lane for a row.
 template <int E>
-__global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, int64_t row0, int64_t rows, int log2) {
-    const int group = 1 << log2, me = threadIdx.x & (group - 1);
-    const int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) >> log2;
+__global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, int64_t row0, int64_t rows) {
+    extern __shared__ char space[];
+    uint32_t* count = reinterpret_cast<uint32_t*>(space);  // of each tile, then its next place
+    __shared__ uint32_t sums[kBlock];
+    const int me = threadIdx.x & 15, in = threadIdx.x >> 4;
+    const int64_t row = (int64_t)blockIdx.x * kListRows + in;
     const bool there = row < rows;
     const int64_t at = there ? row0 + row : row0;
+    for (int k = threadIdx.x; k < out.tiles; k += kBlock) count[k] = 0;
     int c[E];
     float u[E], q[E];
     float top = -INFINITY;
     for (int e = 0; e < E; ++e) {
-        const int k = e * group + me;
+        const int k = e * 16 + me;
         c[e] = -1, u[e] = -INFINITY;
         if (there && k < t.kept) {
             c[e] = t.classes[at * t.kept + k];
@@ -129,45 +150,59 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
         if (c[e] < 0) u[e] = -INFINITY;
         top = fmaxf(top, u[e]);
     }
-    for (int d = 1; d < group; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    top = over_16(top, false);
     float sum = 0.f;
     for (int e = 0; e < E; ++e) {
         q[e] = u[e] == -INFINITY ? 0.f : expf((u[e] - top) * t.inverse);
         sum += q[e];
     }
-    for (int d = 1; d < group; d <<= 1) sum += __shfl_xor(sum, d, kWave);
+    sum = over_16(sum, true);
     const float log_sum = logf(sum);
     float entropy = 0.f;
     for (int e = 0; e < E; ++e) {
         if (sum != 0.f) q[e] /= sum;
         if (q[e] != 0.f) entropy += q[e] * ((u[e] - top) * t.inverse - log_sum);
     }
-    for (int d = 1; d < group; d <<= 1) entropy += __shfl_xor(entropy, d, kWave);
-    // classes that are named several times: the first gets all of it
+    entropy = over_16(entropy, true);
+    // a class that is named several times: the first gets all of it
     float all[E];
     bool first[E];
     for (int e = 0; e < E; ++e) all[e] = 0.f, first[e] = true;
-    for (int k = 0; k < t.kept; ++k) {
-        int other = c[0];
-        float more = q[0];
-        if (E > 1 && k >= group) other = c[E - 1], more = q[E - 1];
-        other = __shfl(other, k & (group - 1), group);
-        more = __shfl(more, k & (group - 1), group);
-        for (int e = 0; e < E; ++e)
-            if (other == c[e]) {
-                if (k < e * group + me) first[e] = false;
-                all[e] += more;
-            }
-    }
-    if (!there) return;
-    for (int e = 0; e < E; ++e) {
-        const int k = e * group + me;
-        if (k < t.kept) {
-            out.classes[row * t.kept + k] = first[e] ? c[e] : -1;
-            out.q[row * t.kept + k] = all[e];
+    for (int from = 0; from < E; ++from)
+        for (int k = 0; k < 16 && from * 16 + k < t.kept; ++k) {
+            const int other = __shfl(c[from], k, 16);
+            const float more = __shfl(q[from], k, 16);
+            for (int e = 0; e < E; ++e)
+                if (other == c[e]) {
+                    if (from * 16 + k < e * 16 + me) first[e] = false;
+                    all[e] += more;
+                }
         }
+    __syncthreads();
+    for (int e = 0; e < E; ++e)
+        if (c[e] >= 0 && first[e]) atomicAdd(count + c[e] / kListClasses, 1u);
+    __syncthreads();
+    // where each tile's entries begin
+    const int per = (out.tiles + kBlock - 1) / kBlock;
+    uint32_t mine = 0;
+    for (int k = threadIdx.x * per; k < min((int)(threadIdx.x + 1) * per, out.tiles); ++k) mine += count[k];
+    sums[threadIdx.x] = mine;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int k = 0; k < (int)threadIdx.x; ++k) before += sums[k];
+    uint32_t* start = out.start + (int64_t)blockIdx.x * (out.tiles + 1);
+    for (int k = threadIdx.x * per; k < min((int)(threadIdx.x + 1) * per, out.tiles); ++k) {
+        const uint32_t n = count[k];
+        start[k] = count[k] = before;
+        before += n;
+        if (k + 1 == out.tiles) start[k + 1] = before;
     }
-    if (me == 0) {
+    __syncthreads();
+    uint2* entry = out.entry + (int64_t)blockIdx.x * (kListRows * t.kept);
+    for (int e = 0; e < E; ++e)
+        if (c[e] >= 0 && first[e])  // in whatever order: no two are for the same row and class
+            entry[atomicAdd(count + c[e] / kListClasses, 1u)] = make_uint2((uint32_t)in << 8 | (uint32_t)(c[e] % kListClasses), __float_as_uint(all[e]));
+    if (there && me == 0) {
         const float r = t.row_weight ? t.row_weight[at] : 1.f;
         const float weight = sum == 0.f ? 0.f : r;
         out.weight[row] = weight;
@@ -185,20 +220,12 @@ struct ListTile {
     __device__ void clear() const {
         for (int k = lane_id() * 4; k < 16 * ld; k += kWave * 4) *reinterpret_cast<f32x4*>(p + k) = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // Puts there, or takes away, what rows n .. n + 15 keep of classes m0 on.  Returns whether there is any.
-    __device__ bool put(const int32_t* classes, const float* q, int kept, int n, int rows, int m0, bool away) const {
-        const int r = lane_id() & 15;
-        bool any = false;
-        if (n + r < rows)
-            for (int k = lane_id() >> 4; k < kept; k += 4) {
-                const int64_t at = (int64_t)(n + r) * kept + k;
-                const int c = classes[at] - m0;
-                if (c >= 0 && c < 16 * S::MI && classes[at] >= 0) {
-                    p[r * ld + c] = away ? 0.f : q[at];
-                    any = true;
-                }
-            }
-        return __any(any);
+    // Puts there, or takes away, a lane's entry where it is one of the wave's classes.  Returns whether any lane's is.
+    __device__ bool put(uint2 entry, bool there, int wave_m, bool away) const {
+        const int c = (int)(entry.x & 255) - wave_m * (16 * S::MI);
+        const bool hit = there && c >= 0 && c < 16 * S::MI;
+        if (hit) p[(entry.x >> 8) * ld + c] = away ? 0.f : __uint_as_float(entry.y);
+        return __any(hit);
     }
     __device__ void get(int column, float (&v)[16]) const {
         for (int k = 0; k < 16; k += 4) {
@@ -210,54 +237,83 @@ struct ListTile {
 // A wave's own accesses of shared memory, in order.
 __device__ inline void wave_meets() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// The entries of a wave's rows: the first 64 of each 16 rows are asked for at once.
 template <typename S>
-constexpr int list_space() {
-    return 4 * S::TM + 4 * ListTile<S>::bytes;
-}
+struct WaveLists {
+    ListTile<S> tile;
+    const uint2* entry[S::NI];
+    int count[S::NI];
+    uint2 ahead[S::NI];
+    int wave_m;
+    __device__ WaveLists(const Lists& l, const Place& at, int rows, char* space) : wave_m(at.wave_m) {
+        tile.p = reinterpret_cast<float*>(space + 4 * S::TM + (at.wave_m + S::WM * at.wave_n) * ListTile<S>::bytes);
+        tile.clear();
+        for (int i = 0; i < S::NI; ++i) {
+            const int n = at.n0 + 16 * i;
+            count[i] = 0;
+            entry[i] = l.entry;
+            if (n < rows) {
+                const int64_t block = n / kListRows;
+                const uint32_t* start = l.start + block * (l.tiles + 1) + at.tile_m;
+                entry[i] = l.entry + block * (kListRows * l.kept) + start[0];
+                count[i] = (int)(start[1] - start[0]);
+            }
+            ahead[i] = (int)lane_id() < count[i] ? entry[i][lane_id()] : make_uint2(0, 0);
+        }
+    }
+    __device__ bool put(int i, bool away) const {
+        bool any = tile.put(ahead[i], (int)lane_id() < count[i], wave_m, away);
+        for (int k = kWave; k < count[i]; k += kWave) {
+            const bool there = k + (int)lane_id() < count[i];
+            any |= tile.put(there ? entry[i][k + lane_id()] : make_uint2(0, 0), there, wave_m, away);
+        }
+        wave_meets();
+        return any;
+    }
+};
 
-// Sums of the softmax: for every 16 MI classes and every row the largest logit m, sum of exp((z - m) / T), sum of q z.
+// Sums of the softmax: for every 16 MI classes and every row the largest y = z log2(e) / T, sum of 2^(y - largest), sum of q y.
 struct Stats {
     const float* bias;
-    const int32_t* classes;
-    const float* q;
+    Lists lists;
     float *top, *sum, *picked;  // [part][ld]
     int64_t ld;
     float exponent;             // log2(e) / T
-    int rows, count, kept;
+    int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        const float* b = tile_bias<S>(bias, at.tile_m * S::TM, count, space) + at.wave_m * (16 * S::MI);
-        const ListTile<S> lists{reinterpret_cast<float*>(space + 4 * S::TM + (at.wave_m + S::WM * at.wave_n) * ListTile<S>::bytes)};
-        lists.clear();
+        const bool shut = tile_bias<S>(bias, exponent, at.tile_m * S::TM, classes, space);
+        const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
+        const WaveLists<S> wave(lists, at, rows, space);
         const int lane_q = lane_id() >> 4, r = lane_id() & 15;
+        wave_meets();
+#pragma unroll
         for (int i = 0; i < S::NI; ++i) {
-            const int n = at.n0 + 16 * i;
-            wave_meets();
-            const bool any = lists.put(classes, q, kept, n, rows, at.m0, false);
-            wave_meets();
-            float m = -INFINITY, pick = 0.f, z[S::MI / 4][16];
+            const int n = at.n0 + 16 * i + r;
+            const bool any = wave.put(i, false);
+            float m = -INFINITY, pick = 0.f, y[S::MI / 4][16];
             for (int j = 0; j < S::MI / 4; ++j) {
-                sixteen(acc[i], j, z[j]);
-                add_bias(b + 64 * j + 16 * lane_q, z[j]);
-                for (int k = 0; k < 16; ++k) m = fmaxf(m, z[j][k]);
+                sixteen(acc[i], j, y[j]);
+                add_bias(b + 64 * j + 16 * lane_q, exponent, shut, y[j]);
+                for (int k = 0; k < 16; ++k) m = fmaxf(m, y[j][k]);
                 if (any) {
-                    float y[16];
-                    lists.get(64 * j + 16 * lane_q, y);
-                    for (int k = 0; k < 16; ++k) pick += y[k] != 0.f ? y[k] * z[j][k] : 0.f;
+                    float q[16];
+                    wave.tile.get(64 * j + 16 * lane_q, q);
+                    for (int k = 0; k < 16; ++k) pick += q[k] != 0.f ? q[k] * y[j][k] : 0.f;
                 }
             }
+            if (any) wave.put(i, true);
             m = row_max(m);
+            const float base = fmaxf(m, -3e38f);  // nothing but -infinity stays at 0
             float s = 0.f;
             for (int j = 0; j < S::MI / 4; ++j)
-                for (int k = 0; k < 16; ++k) s += z[j][k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((z[j][k] - m) * exponent);
+                for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(y[j][k] - base);
             s = row_sum(s);
             pick = row_sum(pick);
-            if (lane_q == 0 && n + r < rows) {
-                const int64_t to = (int64_t)(at.tile_m * S::WM + at.wave_m) * ld + n + r;
+            if (lane_q == 0 && n < rows) {
+                const int64_t to = (int64_t)(at.tile_m * S::WM + at.wave_m) * ld + n;
                 top[to] = m, sum[to] = s, picked[to] = pick;
             }
-            wave_meets();
-            if (any) lists.put(classes, q, kept, n, rows, at.m0, true);
         }
     }
 };
@@ -272,7 +328,7 @@ struct RowJoin {
     float* factor;                    // weight times a power of two; 0 where the row is left out
     uint32_t* kept;                   // a bit per row
     float* undo;                      // one over that power
-    float exponent, temperature;
+    float temperature;
     int rows, parts;
 };
 // The parts of 32 rows, by 8 threads each, in order.  The power of two brings the largest weight to 2^14 .. 2^15, so that float16 holds dz's terms.
@@ -285,7 +341,7 @@ __global__ __launch_bounds__(kBlock) inline void k_teach_rows(RowJoin g) {
         const float pm = g.top[p * g.ld + at], ps = g.sum[p * g.ld + at];
         pick += g.picked[p * g.ld + at];
         const float all = fmaxf(m, pm);
-        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - all) * g.exponent)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f((pm - all) * g.exponent));
+        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(m - all)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f(pm - all));
         m = all;
     }
     tops[k][r] = m, sums[k][r] = s, picks[k][r] = pick;
@@ -294,7 +350,7 @@ __global__ __launch_bounds__(kBlock) inline void k_teach_rows(RowJoin g) {
     for (int p = 1; p < 8; ++p) {
         const float pm = tops[p][r], ps = sums[p][r], all = fmaxf(m, pm);
         pick += picks[p][r];
-        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - all) * g.exponent)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f((pm - all) * g.exponent));
+        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(m - all)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f(pm - all));
         m = all;
     }
     const float weight = g.weight[at];
@@ -310,83 +366,102 @@ __global__ __launch_bounds__(kBlock) inline void k_teach_rows(RowJoin g) {
     const uint32_t bits = (uint32_t)__ballot(use);
     if (r == 0) g.kept[blockIdx.x] = bits;
     if (row >= g.rows) return;
-    const float base = m * g.exponent, log2_s = log2f(s);
-    g.lse[row] = base + log2_s;
+    const float log2_s = log2f(s);
+    g.lse[row] = m + log2_s;
     g.factor[row] = use ? weight * scale : 0.f;
     if (g.loss) {
         // of the largest logit's distance and not of the logits, so that large ones do not cancel
-        const float t = g.temperature, part = g.entropy[row] + (m - pick) / t + log2_s * 0.693147181f;
+        const float t = g.temperature, part = g.entropy[row] + ((m - pick) + log2_s) * 0.693147181f;
         g.loss[row] = use ? weight * t * t * part : 0.f;
     }
+}
+
+// Two values rounded to T, the first in the low half, and what of them is left.
+__device__ inline uint32_t pair_of(float x, float y, bf16) { return bf16_pair(x, y); }
+__device__ inline uint32_t pair_of(float x, float y, f16) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), f16x2));
+}
+template <typename T>
+__device__ inline float half_of(uint32_t pair, int k) {
+    return to_float(__builtin_bit_cast(T, (uint16_t)(pair >> (16 * k))));
 }
 
 // dz as 16-bit terms [term][row][ld], and its sums over the rows of a wave's part.
 template <typename T, int TERMS>
 struct Gradient {
     const float* bias;
-    const int32_t* classes;
-    const float* q;
+    Lists lists;
     const float *lse, *factor;
     uint16_t* dz;
     int64_t ld, term;
     float* sums;  // [part][ld]
     float exponent;
-    int rows, count, kept;
-    __device__ static uint16_t narrow(float x) {
-        if constexpr (__is_same(T, bf16)) return (uint16_t)bf16_pair(x, 0.f);
-        else return __builtin_bit_cast(uint16_t, (f16)x);
-    }
-    __device__ static float widened(uint16_t x) { return to_float(__builtin_bit_cast(T, x)); }
+    int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        const float* b = tile_bias<S>(bias, at.tile_m * S::TM, count, space) + at.wave_m * (16 * S::MI);
-        const ListTile<S> lists{reinterpret_cast<float*>(space + 4 * S::TM + (at.wave_m + S::WM * at.wave_n) * ListTile<S>::bytes)};
-        lists.clear();
+        const bool shut = tile_bias<S>(bias, exponent, at.tile_m * S::TM, classes, space);
+        const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
+        const WaveLists<S> wave(lists, at, rows, space);
         const int lane_q = lane_id() >> 4, r = lane_id() & 15;
-        float total[S::MI / 4][16];
+        float total[S::MI / 4][16], f[S::NI], l[S::NI];
         for (int j = 0; j < S::MI / 4; ++j)
             for (int k = 0; k < 16; ++k) total[j][k] = 0.f;
         for (int i = 0; i < S::NI; ++i) {
-            const int n = at.n0 + 16 * i;
-            wave_meets();
-            const bool any = lists.put(classes, q, kept, n, rows, at.m0, false);
-            wave_meets();
-            const bool there = n + r < rows;
-            const float f = there ? factor[n + r] : 0.f, l = there ? lse[n + r] : 0.f;
+            const int n = at.n0 + 16 * i + r;
+            f[i] = n < rows ? factor[n] : 0.f, l[i] = n < rows ? lse[n] : 0.f;
+        }
+        wave_meets();
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i) {
+            const int n = at.n0 + 16 * i + r;
+            const bool any = wave.put(i, false);
+#pragma unroll
             for (int j = 0; j < S::MI / 4; ++j) {
                 const int m = at.m0 + 64 * j + 16 * lane_q;
-                float v[16], y[16];
+                float v[16];
                 sixteen(acc[i], j, v);
-                add_bias(b + 64 * j + 16 * lane_q, v);
+                add_bias(b + 64 * j + 16 * lane_q, exponent, shut, v);
+                for (int k = 0; k < 16; ++k) v[k] = __builtin_amdgcn_exp2f(v[k] - l[i]);
                 if (any) {
-                    lists.get(64 * j + 16 * lane_q, y);
-                } else {
-                    for (int k = 0; k < 16; ++k) y[k] = 0.f;
+                    float q[16];
+                    wave.tile.get(64 * j + 16 * lane_q, q);
+                    for (int k = 0; k < 16; ++k) v[k] -= q[k];
                 }
-                for (int k = 0; k < 16; ++k) {
-                    const float p = __builtin_amdgcn_exp2f(v[k] * exponent - l);
-                    v[k] = f != 0.f && m + k < count ? f * (p - y[k]) : 0.f;
-                    total[j][k] += v[k];
-                }
-                if (there && m < ld)
+                // a row that is left out has zeros whatever its logits, and so have the columns behind the classes
+                for (int k = 0; k < 16; ++k) v[k] = f[i] != 0.f ? v[k] * f[i] : 0.f;
+                if (shut)
+                    for (int k = 0; k < 16; ++k) v[k] = m + k < classes ? v[k] : 0.f;
+                for (int k = 0; k < 16; ++k) total[j][k] += v[k];
+                if (n < rows && m < ld) {
+#pragma unroll
                     for (int t = 0; t < TERMS; ++t) {
                         u32x4 out[2];
+#pragma unroll
                         for (int k = 0; k < 16; k += 2) {
-                            const uint16_t x = narrow(v[k]), y2 = narrow(v[k + 1]);
-                            out[k / 8][k / 2 & 3] = x | (uint32_t)y2 << 16;
-                            if (t + 1 < TERMS) v[k] -= widened(x), v[k + 1] -= widened(y2);
+                            const uint32_t pair = pair_of(v[k], v[k + 1], T());
+                            out[k / 8][k / 2 & 3] = pair;
+                            if (t + 1 < TERMS) v[k] -= half_of<T>(pair, 0), v[k + 1] -= half_of<T>(pair, 1);
                         }
-                        u32x4* to = reinterpret_cast<u32x4*>(dz + t * term + (n + r) * ld + m);
+                        u32x4* to = reinterpret_cast<u32x4*>(dz + t * term + n * ld + m);
                         to[0] = out[0], to[1] = out[1];
                     }
+                }
             }
-            wave_meets();
-            if (any) lists.put(classes, q, kept, n, rows, at.m0, true);
+            if (any) wave.put(i, true);
         }
         for (int j = 0; j < S::MI / 4; ++j) {
             const int m = at.m0 + 64 * j + 16 * lane_q;
-            for (int k = 0; k < 16; ++k)
-                for (int d = 1; d < 16; d <<= 1) total[j][k] += __shfl_xor(total[j][k], d, kWave);
+            for (int k = 0; k < 16; ++k) {
+                uint32_t v = __float_as_uint(total[j][k]);
+                auto add = [](uint32_t x, int y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float((uint32_t)y)); };
+                v = add(v, __builtin_amdgcn_update_dpp((int)v, (int)v, 0x121, 0xf, 0xf, false));  // of 16 lanes, rotated by 1, 2, 4, 8
+                v = add(v, __builtin_amdgcn_update_dpp((int)v, (int)v, 0x122, 0xf, 0xf, false));
+                v = add(v, __builtin_amdgcn_update_dpp((int)v, (int)v, 0x124, 0xf, 0xf, false));
+                v = add(v, __builtin_amdgcn_update_dpp((int)v, (int)v, 0x128, 0xf, 0xf, false));
+                total[j][k] = __uint_as_float(v);
+            }
             if (r == 0 && m < ld) store_values<16>(sums + (at.tile_n * S::WN + at.wave_n) * ld + m, total[j]);
         }
     }

@@ -17,6 +17,7 @@ constexpr int64_t kMostStride = 1 << 22;              // elements: 32 bits hold 
 constexpr int64_t kLogitsBytes = int64_t(256) << 20;  // of logits in memory at a time
 constexpr int64_t kTermsBytes = int64_t(4) << 30;     // of dz in memory at a time
 constexpr int64_t kMostTeachRows = 1 << 24;           // at a time: a launch has fewer than 2^32 threads
+static_assert(DYNLP_MAX_WIDE_CLASSES / kListClasses * 4 <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
 
 // ---- products ---------------------------------------------------------------------------------------------------------
 
@@ -280,8 +281,10 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->largest = c.take<uint32_t>(1);
     s->undo = c.take<float>(1);
     s->kept = c.take<uint32_t>(ceil_div(s->rows, 32));
-    s->lists.classes = c.take<int32_t>(s->rows * kept);
-    s->lists.q = c.take<float>(s->rows * kept);
+    s->lists.kept = kept;
+    s->lists.tiles = (int)ceil_div(classes, kListClasses);
+    s->lists.entry = c.take<uint2>(round_up(s->rows, kListRows) * kept);
+    s->lists.start = c.take<uint32_t>(ceil_div(s->rows, kListRows) * (s->lists.tiles + 1));
     s->lists.entropy = c.take<float>(s->rows);
     s->lists.weight = c.take<float>(s->rows);
     s->lse = c.take<float>(s->rows);
@@ -399,8 +402,6 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
     const Laid w = lay_out(*weight, s.weight, stream);
     const float exponent = 1.44269504f / teacher->temperature, alpha = teacher->grad_scale * teacher->temperature;
     const bool scaled = h->type == DYNLP_FLOAT16;
-    int group = 0;
-    while (group < 6 && (1 << group) < teacher->kept) ++group;
     for (int64_t row = 0; row < h->rows; row += s.rows) {
         const int64_t rows = std::min(s.rows, h->rows - row);
         const bool add = row > 0;
@@ -408,24 +409,28 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         k_teach_begin<<<1, kBlock, 0, stream>>>(s.zeros, s.largest);
         Lists lists = s.lists;
         lists.largest = scaled ? s.largest : nullptr;
-        const unsigned blocks = (unsigned)ceil_div(rows << group, kBlock);
-        if (teacher->kept > kWave) k_teach_lists<2><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);
-        else k_teach_lists<1><<<blocks, kBlock, 0, stream>>>(t, lists, row, rows, group);
+        auto read_lists = [&](auto entries) {
+            constexpr int E = decltype(entries)::value;
+            k_teach_lists<E><<<(unsigned)ceil_div(rows, kListRows), kBlock, lists.tiles * 4, stream>>>(t, lists, row, rows);
+        };
+        if (teacher->kept <= 16) read_lists(std::integral_constant<int, 1>());
+        else if (teacher->kept <= 32) read_lists(std::integral_constant<int, 2>());
+        else if (teacher->kept <= 64) read_lists(std::integral_constant<int, 4>());
+        else read_lists(std::integral_constant<int, 8>());
         const Wide g = logits_product(w, classes, x, rows, dim);
         const Tiling tile = tiling(classes, s.rows);  // of all chunks: its parts have a size
         const int parts = (int)ceil_div(classes, tile.tm) * tile.wm;
         by_terms(h->type, [&](auto type) {
             using T = decltype(type);
-            const Stats stats{bias, lists.classes, lists.q, s.top, s.sum, s.picked, s.part_ld, exponent, (int)rows, classes, teacher->kept};
+            const Stats stats{bias, lists, s.top, s.sum, s.picked, s.part_ld, exponent, (int)rows, classes};
             launch_product<T, false, false>(g, tile, classes, rows, 1, stats, stream);
             const RowJoin join{s.top, s.sum, s.picked, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.lse, s.factor, s.kept,
-                               s.undo, exponent, teacher->temperature, (int)rows, parts};
+                               s.undo, teacher->temperature, (int)rows, parts};
             k_teach_rows<<<(unsigned)ceil_div(rows, 32), kBlock, 0, stream>>>(join);
             if (!grads) return;
             const int64_t term = rows * s.ld;
             auto gradient = [&](auto terms) {
-                const Gradient<T, decltype(terms)::value> e{bias, lists.classes, lists.q, s.lse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes,
-                                                            teacher->kept};
+                const Gradient<T, decltype(terms)::value> e{bias, lists, s.lse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes};
                 launch_product<T, false, false>(g, tile, classes, rows, 1, e, stream);
             };
             if (s.terms == 1) gradient(std::integral_constant<int, 1>());
