@@ -69,6 +69,15 @@ __device__ inline void add_bias(const float* b, float factor, bool shut, float (
     }
 }
 
+// Four of them, v = v factor + bias.
+__device__ inline void add_bias(const float* b, float factor, bool shut, float (&v)[4]) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(b);
+    for (int i = 0; i < 4; ++i) {
+        v[i] = __builtin_fmaf(v[i], factor, x[i]);
+        if (shut) v[i] = x[i] == -INFINITY ? x[i] : v[i];
+    }
+}
+
 // Logits to memory; ld is a multiple of 16, and what lies behind the classes becomes -infinity.
 struct Logits {
     float* z;
@@ -77,19 +86,19 @@ struct Logits {
     int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
+        static_assert(!S::WOVEN, "fours");
         const bool shut = tile_bias<S>(bias, 1.f, at.tile_m * S::TM, classes, space);
         const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const int q = lane_id() >> 4, r = lane_id() & 15;
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
             if (n >= rows) continue;
-            for (int j = 0; j < S::MI / 4; ++j) {
-                const int m = at.m0 + 64 * j + 16 * q;
+            for (int j = 0; j < S::MI; ++j) {
+                const int m = at.m0 + 16 * j + 4 * q;
                 if (m >= ld) continue;
-                float v[16];
-                sixteen(acc[i], j, v);
-                add_bias(b + 64 * j + 16 * q, 1.f, shut, v);
-                store_values<16>(z + n * ld + m, v);
+                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                add_bias(b + 16 * j + 4 * q, 1.f, shut, v);
+                store_values<4>(z + n * ld + m, v);
             }
         }
     }
@@ -483,23 +492,6 @@ __global__ __launch_bounds__(kBlock) inline void k_teach_bias(const float* sums,
         for (int p = 1; p < 4; ++p) v += s[p][threadIdx.x];
         v *= alpha * *undo;
         dbias[c] = add ? dbias[c] + v : v;
-    }
-}
-
-// out = factor times the sum of parts (rows x dim each, rows without padding), rounded; zeros for rows that are left out.
-template <typename O>
-__global__ __launch_bounds__(kBlock) void k_wide_join(const float* part, int splits, int64_t stride, int64_t rows, int dim, float alpha, const float* undo,
-                                                      const uint32_t* kept, O* out, int64_t ld, bool add) {
-    const float factor = undo ? alpha * *undo : alpha;
-    const int64_t total = rows * dim;
-    for (int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x; at < total; at += (int64_t)gridDim.x * kBlock) {
-        const int64_t row = at / dim;
-        float v = 0.f;
-        for (int k = 0; k < splits; ++k) v += part[k * stride + at];
-        v *= factor;
-        if (kept && !(kept[row >> 5] >> (row & 31) & 1)) v = 0.f;
-        O* to = out + row * ld + (at - row * dim);
-        *to = (O)(add ? (float)*to + v : v);
     }
 }
 

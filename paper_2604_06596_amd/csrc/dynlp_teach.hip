@@ -31,26 +31,46 @@ Tiling tiling(int64_t m, int64_t n) {
     if (m <= 64) return {64, 256, 1, 4};
     return {256, 128, 2, 2};
 }
-template <bool TA, bool TB, typename F>
+template <bool TA, bool TB, bool WOVEN, typename F>
 void by_tiling(const Tiling& t, F f) {
-    if (t.tn == 16) f(Shape<256, 16, 4, 1, TA, TB>());
-    else if (t.tn == 64) f(Shape<256, 64, 4, 1, TA, TB>());
-    else if (t.tm == 64) f(Shape<64, 256, 1, 4, TA, TB>());
-    else f(Shape<256, 128, 2, 2, TA, TB>());
+    if (t.tn == 16) f(Shape<256, 16, 4, 1, TA, TB, WOVEN>());
+    else if (t.tn == 64) f(Shape<256, 64, 4, 1, TA, TB, WOVEN>());
+    else if (t.tm == 64) f(Shape<64, 256, 1, 4, TA, TB, WOVEN>());
+    else f(Shape<256, 128, 2, 2, TA, TB, WOVEN>());
 }
 
-template <typename T, bool TA, bool TB, typename E>
-void launch_product(Wide g, const Tiling& t, int64_t m, int64_t n, int splits, const E& e, hipStream_t stream) {
-    g.tiles_m = (int)ceil_div(m, t.tm);
-    g.tiles_n = (int)ceil_div(n, t.tn);
-    g.per_split = (int)ceil_div((int64_t)g.pairs * g.steps, splits);
-    g.splits = (int)ceil_div((int64_t)g.pairs * g.steps, g.per_split);
-    by_tiling<TA, TB>(t, [&](auto shape) {
+// g.whole, g.splits and g.per_split may be set by split_tiles().
+template <typename T, bool TA, bool TB, bool WOVEN, typename E>
+void launch_product(Wide g, const Tiling& t, int64_t m, int64_t n, const E& e, hipStream_t stream) {
+    if (g.tiles_m == 0) {
+        g.tiles_m = (int)ceil_div(m, t.tm);
+        g.tiles_n = (int)ceil_div(n, t.tn);
+        g.whole = g.tiles_m * g.tiles_n;
+    }
+    by_tiling<TA, TB, WOVEN>(t, [&](auto shape) {
         using S = decltype(shape);
         static std::atomic<uint64_t> allowed{0};
         allow_shared(k_wide<T, S, E>, allowed);
-        k_wide<T, S, E><<<(unsigned)((int64_t)g.tiles_m * g.tiles_n * g.splits), kBlock, kStages * S::stage, stream>>>(g, e);
+        const int others = g.tiles_m * g.tiles_n - g.whole;
+        k_wide<T, S, E><<<(unsigned)(g.whole + others * g.splits), kBlock, kStages * S::stage, stream>>>(g, e);
     });
+}
+
+// The chip has room for two workgroups on each CU: the tiles that do not fill it once more have their sums split, so that all of it has work to the end, but in
+// parts of 8 steps at least.  Returns the elements of their parts.
+constexpr int kRoom = 512;
+int64_t split_tiles(Wide* g, const Tiling& t, int64_t m, int64_t n) {
+    g->tiles_m = (int)ceil_div(m, t.tm);
+    g->tiles_n = (int)ceil_div(n, t.tn);
+    const int64_t tiles = (int64_t)g->tiles_m * g->tiles_n, steps = (int64_t)g->pairs * g->steps;
+    const int64_t others = tiles % kRoom, splits = others ? std::min(kRoom / others, steps / 8) : 1;
+    g->whole = (int)tiles;
+    g->splits = 1;
+    if (splits < 2) return 0;
+    g->whole = (int)(tiles - others);
+    g->per_split = (int)ceil_div(steps, splits);
+    g->splits = (int)ceil_div(steps, g->per_split);
+    return others * g->splits * t.tm * t.tn;
 }
 
 // Pairs of terms, the smallest products first.
@@ -62,13 +82,6 @@ void set_pairs(Wide* g, int terms_a, int terms_b) {
             const int b = sum - a;
             if (b >= 0 && b < terms_b) g->pair |= (uint32_t)(a | b << 2) << (4 * g->pairs++);
         }
-}
-
-// Splits of a sum so that the chip has two workgroups for each CU, none shorter than 8 steps.
-int splits_of(int64_t m, int64_t n, int64_t steps) {
-    const Tiling t = tiling(m, n);
-    const int64_t tiles = ceil_div(m, t.tm) * ceil_div(n, t.tn);
-    return (int)std::max<int64_t>(std::min(512 / tiles, steps / 8), 1);
 }
 
 // ---- operands ---------------------------------------------------------------------------------------------------------
@@ -237,7 +250,7 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
         const Laid x = lay_out(rows_of(*h, row, rows), s.h, stream);
         const Wide g = logits_product(w, classes, x, rows, h->dim);
         const Logits e{s.z, ld, bias, (int)rows, classes};
-        by_terms(h->type, [&](auto type) { launch_product<decltype(type), false, false>(g, tiling(classes, rows), classes, rows, 1, e, stream); });
+        by_terms(h->type, [&](auto type) { launch_product<decltype(type), false, false, false>(g, tiling(classes, rows), classes, rows, e, stream); });
         launch_scores<float, false>(s.z, ld, rows, classes, o, row, stream);
     }
     return launched();
@@ -263,7 +276,6 @@ struct TeachSpace {
     float *bias_part, *part, *dweight;
     int64_t part_ld;   // of top, sum and picked
     int terms, parts;
-    int splits_h, splits_w;
 };
 
 // grad_type: of dweight, or -1 where no gradient is asked for.
@@ -295,37 +307,31 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
     s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
     if (grads) {
-        const int pairs = type == DYNLP_FLOAT32 ? 6 : 1;
         s->dz = c.take<uint16_t>(s->rows * s->ld * s->terms);
         s->bias_part = c.take<float>(ceil_div(s->rows, t.tn) * t.wn * s->ld);
-        s->splits_h = splits_of(dim, s->rows, pairs * (s->ld / kStep));
-        s->splits_w = splits_of(dim, classes, (pairs == 6 ? 6 : s->terms) * ceil_div(s->rows, kStep));
-        const int64_t part_h = s->splits_h > 1 ? s->splits_h * s->rows * dim : 0, part_w = s->splits_w > 1 ? s->splits_w * classes * dim : 0;
-        s->part = c.take<float>(std::max(part_h, part_w));
+        Wide by_h{}, by_w{};
+        set_pairs(&by_h, terms_in(type), type == DYNLP_FLOAT32 ? 3 : 1);
+        set_pairs(&by_w, terms_in(type), s->terms);
+        by_h.steps = (int)(s->ld / kStep);
+        by_w.steps = (int)ceil_div(s->rows, kStep);
+        const int64_t parts = std::max(split_tiles(&by_h, tiling(dim, s->rows), dim, s->rows), split_tiles(&by_w, tiling(dim, classes), dim, classes));
+        s->part = c.take<float>(rows > s->rows ? kRoom * 256 * 128 : parts);  // the most there are, where the last rows are fewer than others
         s->dweight = rows > s->rows && grad_type != DYNLP_FLOAT32 ? c.take<float>(classes * dim) : nullptr;
     }
     return c.used;
 }
 
-template <typename O>
-void launch_join(const float* part, int splits, int64_t rows, int dim, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
-                 hipStream_t stream) {
-    k_wide_join<O><<<(unsigned)std::min<int64_t>(ceil_div(rows * dim, kBlock), 16384), kBlock, 0, stream>>>(part, splits, rows * dim, rows, dim, alpha, undo, kept,
-                                                                                                           static_cast<O*>(out), ld, add);
-}
-
-// The product to `out`, by parts where its sum is split.
+// The product to its output.
 template <typename T, bool TA, bool TB, typename O>
-void launch_gradient(const Wide& g, int64_t m, int64_t n, int splits, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
+void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
                      hipStream_t stream) {
-    if (splits > 1) {
-        const int64_t total = (int64_t)g.pairs * g.steps, per = ceil_div(total, splits);
-        const Store<float> e{part, m, n * m, (int)n, (int)m, 1.f, nullptr, nullptr, false};
-        launch_product<T, TA, TB>(g, tiling(m, n), m, n, splits, e, stream);
-        launch_join<O>(part, (int)ceil_div(total, per), n, (int)m, alpha, undo, kept, out, ld, add, stream);
-    } else {
-        const Store<O> e{static_cast<O*>(out), ld, 0, (int)n, (int)m, alpha, undo, kept, add};
-        launch_product<T, TA, TB>(g, tiling(m, n), m, n, 1, e, stream);
+    const Tiling t = tiling(m, n);
+    const int64_t parts = split_tiles(&g, t, m, n);
+    const Output<O> to{static_cast<O*>(out), ld, (int)n, (int)m, alpha, undo, kept, add};
+    launch_product<T, TA, TB, sizeof(O) == 2>(g, t, m, n, Store<O>{to, part}, stream);
+    if (parts > 0) {
+        const int64_t pieces = parts / g.splits / 4;
+        k_wide_join<O><<<(unsigned)std::min<int64_t>(ceil_div(pieces, kBlock), 16384), kBlock, 0, stream>>>(g, t.tm, t.tn, part, to);
     }
 }
 
@@ -423,7 +429,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         by_terms(h->type, [&](auto type) {
             using T = decltype(type);
             const Stats stats{bias, lists, s.top, s.sum, s.picked, s.part_ld, exponent, (int)rows, classes};
-            launch_product<T, false, false>(g, tile, classes, rows, 1, stats, stream);
+            launch_product<T, false, false, true>(g, tile, classes, rows, stats, stream);
             const RowJoin join{s.top, s.sum, s.picked, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.lse, s.factor, s.kept,
                                s.undo, teacher->temperature, (int)rows, parts};
             k_teach_rows<<<(unsigned)ceil_div(rows, 32), kBlock, 0, stream>>>(join);
@@ -431,7 +437,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             const int64_t term = rows * s.ld;
             auto gradient = [&](auto terms) {
                 const Gradient<T, decltype(terms)::value> e{bias, lists, s.lse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes};
-                launch_product<T, false, false>(g, tile, classes, rows, 1, e, stream);
+                launch_product<T, false, false, true>(g, tile, classes, rows, e, stream);
             };
             if (s.terms == 1) gradient(std::integral_constant<int, 1>());
             else if constexpr (__is_same(T, f16)) gradient(std::integral_constant<int, 2>());
@@ -448,7 +454,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
                 set_pairs(&p, w.terms, w.terms == 1 ? 1 : s.terms);
                 void* to = static_cast<char*>(dh->data) + row * dh->stride * type_size(dh->type);
                 auto run = [&](auto out) {
-                    launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.splits_h, s.part, alpha, s.undo, s.kept, to, dh->stride, false, stream);
+                    launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.part, alpha, s.undo, s.kept, to, dh->stride, false, stream);
                 };
                 if (h->type == DYNLP_FLOAT32) {
                     if constexpr (__is_same(T, bf16)) run(float());
@@ -466,12 +472,14 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
                 p.zeros = s.zeros;
                 set_pairs(&p, x.terms, s.terms);
                 if (dweight->type == DYNLP_FLOAT32) {
-                    launch_gradient<T, true, true, float>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, add, stream);
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, add, stream);
                 } else if (s.dweight) {
-                    launch_gradient<T, true, true, float>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, s.dweight, dim, add, stream);
-                    if (row + rows == h->rows) launch_join<T>(s.dweight, 1, classes, dim, 1.f, nullptr, nullptr, dweight->data, dweight->stride, false, stream);
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, s.dweight, dim, add, stream);
+                    if (row + rows == h->rows)
+                        k_round<T><<<(unsigned)std::min<int64_t>(ceil_div((int64_t)classes * dim, kBlock), 16384), kBlock, 0, stream>>>(
+                            s.dweight, classes, dim, static_cast<T*>(dweight->data), dweight->stride);
                 } else {
-                    launch_gradient<T, true, true, T>(p, dim, classes, s.splits_w, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, false, stream);
+                    launch_gradient<T, true, true, T>(p, dim, classes, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, false, stream);
                 }
             }
         });
