@@ -278,6 +278,22 @@ struct RowScan {
     }
 };
 
+// The first classes of a wave's candidates to the outputs: the place of a candidate is how many come before it.
+template <bool PROB>
+__device__ inline void write_top(Candidates& c, const Scores& o, int64_t row, const RowLog<PROB>& log) {
+    c.cut(o.top, kCandidates);
+    for (int at = 0; at < c.count; at += kWave) {
+        const int i = at + lane_id();
+        const uint64_t key = i < c.count ? c.key[i] : 0;
+        int place = 0;
+        for (int j = 0; j < c.count; ++j) place += c.key[j] > key;
+        if (i < c.count && place < o.top) {
+            if (o.top_classes) o.top_classes[row * o.top + place] = column_of_key(key);
+            if (o.log_top) o.log_top[row * o.top + place] = log.of(value_of(key));
+        }
+    }
+}
+
 constexpr int row_lists(int waves) { return waves == 1 ? kBlock / kWave : waves; }
 template <typename T>
 constexpr int row_space(int waves) {
@@ -328,20 +344,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
             if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
             o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
         }
-        if (o.top && (WAVES == 1 || wave == 0)) {
-            c.cut(o.top, kCandidates);
-            // the place of a candidate is how many come before it
-            for (int at = 0; at < c.count; at += kWave) {
-                const int i = at + lane_id();
-                const uint64_t key = i < c.count ? c.key[i] : 0;
-                int place = 0;
-                for (int j = 0; j < c.count; ++j) place += c.key[j] > key;
-                if (i < c.count && place < o.top) {
-                    if (o.top_classes) o.top_classes[to * o.top + place] = column_of_key(key);
-                    if (o.log_top) o.log_top[to * o.top + place] = log.of(value_of(key));
-                }
-            }
-        }
+        if (o.top && (WAVES == 1 || wave == 0)) write_top<PROB>(c, o, to, log);
         if constexpr (WAVES > 1) __syncthreads();
     }
 }

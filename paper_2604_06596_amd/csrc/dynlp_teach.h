@@ -78,32 +78,6 @@ __device__ inline void add_bias(const float* b, float factor, bool shut, float (
     }
 }
 
-// Logits to memory; ld is a multiple of 16, and what lies behind the classes becomes -infinity.
-struct Logits {
-    float* z;
-    int64_t ld;
-    const float* bias;
-    int rows, classes;
-    template <typename S>
-    __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        static_assert(!S::WOVEN, "fours");
-        const bool shut = tile_bias<S>(bias, 1.f, at.tile_m * S::TM, classes, space);
-        const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
-        const int q = lane_id() >> 4, r = lane_id() & 15;
-        for (int i = 0; i < S::NI; ++i) {
-            const int n = at.n0 + 16 * i + r;
-            if (n >= rows) continue;
-            for (int j = 0; j < S::MI; ++j) {
-                const int m = at.m0 + 16 * j + 4 * q;
-                if (m >= ld) continue;
-                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                add_bias(b + 16 * j + 4 * q, 1.f, shut, v);
-                store_values<4>(z + n * ld + m, v);
-            }
-        }
-    }
-};
-
 // ---- the teacher's lists ----------------------------------------------------------------------------------------------
 
 // Entries of 16 rows, ordered by the tile of classes that they lie in: their row and class there, and q.  A class that a row names several times is one entry.

@@ -4,9 +4,8 @@
 #include <cmath>
 #include <type_traits>
 
+#include "dynlp_ask.h"
 #include "dynlp_host.h"
-#include "dynlp_scores.h"
-#include "dynlp_teach.h"
 
 using namespace dynlp;
 
@@ -133,6 +132,13 @@ void by_terms(int32_t type, F f) {
     else f(bf16());
 }
 
+template <typename F>
+void by_type(int32_t type, F f) {
+    if (type == DYNLP_FLOAT32) f(float());
+    else if (type == DYNLP_BFLOAT16) f(bf16());
+    else f(f16());
+}
+
 dynlp_status check_wide_head(const dynlp_matrix* h, const dynlp_matrix* weight) {
     CHECK(check_matrix(h, "h"));
     CHECK(check_matrix(weight, "weight"));
@@ -156,6 +162,17 @@ dynlp_status check_scores(const dynlp_scores* s, int64_t rows, int64_t classes) 
 
 Scores scores_of(const dynlp_scores* s) {
     return Scores{s->classes, s->log_given, s->entropy, s->top_classes, s->log_top, s->rejected, s->given, s->top_classes || s->log_top ? s->top : 0};
+}
+
+// The scores of rows from `row` on.
+Scores scores_from(const Scores& s, int64_t row) {
+    Scores o = s;
+    if (o.classes) o.classes += row * o.given;
+    if (o.log_given) o.log_given += row * o.given;
+    if (o.entropy) o.entropy += row;
+    if (o.top_classes) o.top_classes += row * o.top;
+    if (o.log_top) o.log_top += row * o.top;
+    return o;
 }
 
 template <typename T, bool PROB>
@@ -185,18 +202,87 @@ int64_t logits_rows(int64_t rows, int64_t classes) {
     return std::min(rows, most);
 }
 
+// Classes of a group: a wave's part of the product.  Few rows have more waves than rows, and smaller parts.
+int group_size(int64_t rows, int64_t classes) {
+    if (rows <= 16) return classes <= 16 * 2048 ? 16 : 64;
+    const Tiling t = tiling(classes, rows);
+    return t.tm / t.wm;
+}
+
 struct ScoreSpace {
     uint16_t *h, *weight;
     float* z;
+    GroupSums* sums;
     int64_t rows;  // at a time
+    int size, groups;
 };
 int64_t score_space(char* base, int64_t rows, int64_t dim, int64_t classes, int32_t type, bool lay_h, bool lay_weight, ScoreSpace* s) {
     Carve c{base};
     s->rows = logits_rows(rows, classes);
+    s->size = group_size(s->rows, classes);
+    s->groups = (int)ceil_div(classes, s->size);
     s->z = c.take<float>(s->rows * round_up(classes, 16));
+    s->sums = c.take<GroupSums>(s->rows * s->groups);
+    if (s->rows <= 16) return c.used;  // rows are read as they lie
     s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
     s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
     return c.used;
+}
+
+void launch_groups(const ScoreSpace& s, int64_t ld, int64_t rows, int classes, const Scores& o, int64_t row0, hipStream_t stream) {
+    const int64_t waves = round_up(s.groups, kWave);
+    if (s.groups > kMostGroups) return launch_scores<float, false>(s.z, ld, rows, classes, o, row0, stream);
+    auto run = [&](auto size) {
+        constexpr int GS = decltype(size)::value;
+        static std::atomic<uint64_t> allowed{0};
+        allow_shared(k_group_scores<GS>, allowed);
+        k_group_scores<GS><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kWave, (kCandidates + kWave * 4) * 8 + waves * 8, stream>>>(s.z, ld, s.sums, s.groups, rows, classes, o,
+                                                                                                                                row0);
+    };
+    if (s.size == 16) run(std::integral_constant<int, 16>());
+    else if (s.size == 64) run(std::integral_constant<int, 64>());
+    else run(std::integral_constant<int, 128>());
+}
+
+// F is called with (T(), number of tiles of 16 classes).
+template <typename F>
+void by_few_classes(int32_t type, int64_t classes, F f) {
+    auto tiles = [&](auto t) {
+        switch ((classes + 15) / 16) {
+            case 1: f(t, std::integral_constant<int, 1>()); break;
+            case 2: f(t, std::integral_constant<int, 2>()); break;
+            case 3: f(t, std::integral_constant<int, 3>()); break;
+            default: f(t, std::integral_constant<int, 4>());
+        }
+    };
+    if (type == DYNLP_FLOAT32) tiles(float());
+    else if (type == DYNLP_BFLOAT16) tiles(bf16());
+    else tiles(f16());
+}
+
+void launch_few_scores(const dynlp_matrix& h, const dynlp_matrix& weight, const float* bias, const Scores& o, hipStream_t stream) {
+    const Head a{h.data, weight.data, bias, h.stride, weight.stride, h.rows, h.dim, (int)weight.rows};
+    by_few_classes(h.type, weight.rows, [&](auto type, auto tiles) {
+        using T = decltype(type);
+        constexpr int CT = decltype(tiles)::value;
+        const int64_t bytes = a.dim <= 1 << 14 ? shared_bytes<T, CT>(a.dim) : kSharedMemory + 1, blocks = ceil_div(a.rows, kLabelRows);
+        // a copy of W pays once a workgroup has several tiles of rows
+        const int64_t stay = 256 * std::min<int64_t>(kSharedMemory / bytes, 4);
+        if (bytes <= kSharedMemory && blocks >= 2 * stay) {
+            static std::atomic<uint64_t> allowed{0};
+            allow_shared(k_few_scores<T, CT, true>, allowed);
+            k_few_scores<T, CT, true><<<(unsigned)stay, kBlock, (size_t)bytes, stream>>>(a, o);
+        } else {
+            for (int64_t row = 0; row < a.rows; row += kMostBlocks * kLabelRows) {
+                Head part = a;
+                part.h = static_cast<const T*>(a.h) + row * a.ld_h;
+                part.rows = std::min(a.rows - row, kMostBlocks * kLabelRows);
+                Scores to = o;
+                if (row > 0) to = scores_from(o, row);
+                k_few_scores<T, CT, false><<<(unsigned)ceil_div(part.rows, kLabelRows), kBlock, 0, stream>>>(part, to);
+            }
+        }
+    });
 }
 
 }  // namespace
@@ -229,6 +315,7 @@ dynlp_status dynlp_row_scores(const dynlp_matrix* x, int32_t probabilities, cons
 
 int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type) {
     if (rows < 1 || rows > kMostRows || dim < 1 || dim > DYNLP_MAX_WIDE_DIM || classes < 1 || classes > DYNLP_MAX_WIDE_CLASSES) return 0;
+    if (classes <= DYNLP_MAX_CLASSES) return 0;
     ScoreSpace s{};
     return score_space(nullptr, rows, dim, classes, type, true, true, &s);
 }
@@ -240,18 +327,35 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
     CHECK(check_workspace(call, dynlp_head_scores_workspace(h->rows, h->dim, classes, h->type)));
     if (h->rows == 0) return DYNLP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(call->stream);
+    const Scores o = scores_of(scores);
+    if (classes <= DYNLP_MAX_CLASSES) {
+        launch_few_scores(*h, *weight, bias, o, stream);
+        return launched();
+    }
     ScoreSpace s{};
     score_space(static_cast<char*>(call->workspace), h->rows, h->dim, classes, h->type, !lies_well(*h), !lies_well(*weight), &s);
-    const Scores o = scores_of(scores);
-    const Laid w = lay_out(*weight, s.weight, stream);
     const int64_t ld = round_up(classes, 16);
+    if (s.rows <= 16) {
+        const Head a{h->data, weight->data, bias, h->stride, weight->stride, h->rows, h->dim, classes};
+        const Logits e{s.z, ld, s.sums, s.groups, bias, (int)h->rows, classes};
+        by_type(h->type, [&](auto type) {
+            using T = decltype(type);
+            const unsigned blocks = (unsigned)ceil_div(s.groups, kBlock / kWave);
+            if (s.size == 16) k_thin_logits<T, 1><<<blocks, kBlock, 0, stream>>>(a, e);
+            else k_thin_logits<T, 4><<<blocks, kBlock, 0, stream>>>(a, e);
+        });
+        launch_groups(s, ld, h->rows, classes, o, 0, stream);
+        return launched();
+    }
+    const Laid w = lay_out(*weight, s.weight, stream);
+    const Tiling tile = tiling(classes, s.rows);  // of all turns: its groups have a size
     for (int64_t row = 0; row < h->rows; row += s.rows) {
         const int64_t rows = std::min(s.rows, h->rows - row);
         const Laid x = lay_out(rows_of(*h, row, rows), s.h, stream);
         const Wide g = logits_product(w, classes, x, rows, h->dim);
-        const Logits e{s.z, ld, bias, (int)rows, classes};
-        by_terms(h->type, [&](auto type) { launch_product<decltype(type), false, false, false>(g, tiling(classes, rows), classes, rows, e, stream); });
-        launch_scores<float, false>(s.z, ld, rows, classes, o, row, stream);
+        const Logits e{s.z, ld, s.sums, s.groups, bias, (int)rows, classes};
+        by_terms(h->type, [&](auto type) { launch_product<decltype(type), false, false, false>(g, tile, classes, rows, e, stream); });
+        launch_groups(s, ld, rows, classes, o, row, stream);
     }
     return launched();
 }
@@ -333,13 +437,6 @@ void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, con
         const int64_t pieces = parts / g.splits / 4;
         k_wide_join<O><<<(unsigned)std::min<int64_t>(ceil_div(pieces, kBlock), 16384), kBlock, 0, stream>>>(g, t.tm, t.tn, part, to);
     }
-}
-
-template <typename F>
-void by_type(int32_t type, F f) {
-    if (type == DYNLP_FLOAT32) f(float());
-    else if (type == DYNLP_BFLOAT16) f(bf16());
-    else f(f16());
 }
 
 dynlp_status check_teacher(const dynlp_teacher* t, int64_t rows) {
