@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kBlock) void k_thin_logits(Head a, Logits o) {
 }
 
 constexpr int kMostGroups = 8192;  // of a row: their largest logits are in shared memory
+constexpr int kSums = 8;           // of a lane, under way
 
 // A wave for each row; GS classes to a group.
 template <int GS>
@@ -89,18 +90,26 @@ __global__ __launch_bounds__(kWave) void k_group_scores(const float* z, int64_t 
     extern __shared__ char space[];
     uint64_t* keys = reinterpret_cast<uint64_t*>(space);
     uint32_t* order = reinterpret_cast<uint32_t*>(keys + kRoomFor);
-    int* chosen = reinterpret_cast<int*>(order + (count + kWave - 1) / kWave * kWave);
+    int* chosen = reinterpret_cast<int*>(order + (count + kSums * kWave - 1) / (kSums * kWave) * (kSums * kWave));
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const float* p = z + row * ld;
         const int64_t to = row0 + row;
         RowSums sums = RowSums::none();
         const int turns = (count + kWave - 1) / kWave;
-        for (int j = 0; j < turns; ++j) {
-            const int g = j * kWave + lane_id();
-            GroupSums s{-INFINITY, 0.f, 0.f, 0.f};
-            if (g < count) s = groups[row * count + g];
-            sums.join<false>(RowSums{s.m, s.s, s.t});
-            order[g] = g < count ? order_of(s.m) : 0u;
+#pragma unroll 1
+        for (int j = 0; j < turns; j += kSums) {
+            f32x4 s[kSums];
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) {
+                const int g = (j + k) * kWave + lane_id();
+                s[k] = *reinterpret_cast<const f32x4*>(groups + row * count + min(g, count - 1));
+            }
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) {
+                const int g = (j + k) * kWave + lane_id();
+                if (g < count) sums.join<false>(RowSums{s[k][0], s[k][1], s[k][2]});
+                order[g] = g < count ? order_of(s[k][0]) : 0u;
+            }
         }
         sums.over_lanes<false>();
         const RowLog<false> log(sums, dim);
@@ -115,14 +124,17 @@ __global__ __launch_bounds__(kWave) void k_group_scores(const float* z, int64_t 
         c.none(keys);
         wave_meets();
         // with fewer groups than classes asked for, all of them
-        if (count >= o.top) c.raise(max(threshold(turns, o.top, 14, [&](int j) { return order[j * kWave + lane_id()]; }), 1u) - 1u);
+        if (count >= o.top) c.raise(max(threshold<kSums>(turns, o.top, 14, [&](int j) { return order[j * kWave + lane_id()]; }), 1u) - 1u);
         int found = 0;
-        for (int j = 0; j < turns; ++j) {
-            const int g = j * kWave + lane_id();
-            const bool hit = g < count && order[g] > c.above;
-            const uint64_t mask = __ballot(hit);
-            if (hit) chosen[found + lanes_before(mask)] = g;
-            found += __popcll(mask);
+        for (int j = 0; j < turns; j += kSums) {
+            uint32_t u[kSums];
+            for (int k = 0; k < kSums; ++k) u[k] = order[(j + k) * kWave + lane_id()];
+            for (int k = 0; k < kSums; ++k) {
+                const bool hit = u[k] > c.above;
+                const uint64_t mask = __ballot(hit);
+                if (hit) chosen[found + lanes_before(mask)] = (j + k) * kWave + lane_id();
+                found += __popcll(mask);
+            }
         }
         wave_meets();
         constexpr int kLanes = GS / 4, kOnce = kWave / kLanes;  // of a group; groups in a piece

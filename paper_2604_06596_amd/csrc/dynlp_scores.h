@@ -132,17 +132,20 @@ struct RowLog {
 // ---- the first classes ------------------------------------------------------------------------------------------------
 
 // A number such that at least k of the wave's `order(j)`, j < n, are not below it, and seldom many more: the interval between the least and the largest is halved up to
-// `most` times.  Orders that are not there are 0; there are k others.
-template <typename O>
+// `most` times.  Orders that are not there are 0; there are k others.  U of them are looked at at a time (n is a multiple of U, or order(j) is 0 beyond it).
+template <int U, typename O>
 __device__ inline uint32_t threshold(int n, int k, int most, O order) {
     const uint32_t least = order_of(-INFINITY);
     uint32_t high = 0, low = ~0u;
     int count = 0;
-    for (int j = 0; j < n; ++j) {
-        const uint32_t o = order(j);
-        high = max(high, o);
-        low = min(low, o > least ? o : ~0u);
-        count += __popcll(__ballot(o > least));
+    for (int j = 0; j < n; j += U) {
+        uint32_t o[U];
+        for (int u = 0; u < U; ++u) o[u] = order(j + u);
+        for (int u = 0; u < U; ++u) {
+            high = max(high, o[u]);
+            low = min(low, o[u] > least ? o[u] : ~0u);
+            count += __popcll(__ballot(o[u] > least));
+        }
     }
     if (count < k) return least;
     high = lanes_max(high);
@@ -150,7 +153,11 @@ __device__ inline uint32_t threshold(int n, int k, int most, O order) {
     for (int step = 0; step < most && low < high; ++step) {
         const uint32_t middle = low + ((high - low) >> 1) + 1;
         count = 0;
-        for (int j = 0; j < n; ++j) count += __popcll(__ballot(order(j) >= middle));
+        for (int j = 0; j < n; j += U) {
+            uint32_t o[U];
+            for (int u = 0; u < U; ++u) o[u] = order(j + u);
+            for (int u = 0; u < U; ++u) count += __popcll(__ballot(o[u] >= middle));
+        }
         if (count >= k) low = middle;
         else high = middle - 1;
         if (count == k) break;
@@ -200,7 +207,7 @@ struct Candidates {
     __device__ void cut(int k, int most) {
         if (count <= k) return;
         const int n = (count + kWave - 1) / kWave;
-        uint32_t least = threshold(n, k, 14, [&](int j) { return (int)(j * kWave + lane_id()) < count ? (uint32_t)(key[j * kWave + lane_id()] >> 32) : 0u; });
+        uint32_t least = threshold<2>(n, k, 14, [&](int j) { return (int)(j * kWave + lane_id()) < count ? (uint32_t)(key[j * kWave + lane_id()] >> 32) : 0u; });
         keep((uint64_t)least << 32);
         if (count > most) {  // equal or nearly equal values: exactly k, bit by bit
             const int left = (count + kWave - 1) / kWave;
@@ -260,7 +267,7 @@ struct RowScan {
                 float best[2] = {-INFINITY, -INFINITY};
                 for (int k = 0; k < N; ++k) best[k / ((N + 1) / 2)] = fmaxf(best[k / ((N + 1) / 2)], v[k]);
                 const uint32_t order[2] = {order_of(best[0]), order_of(best[1])};
-                c.raise(max(threshold(2, top, 14, [&](int j) { return order[j]; }), 1u) - 1u);
+                c.raise(max(threshold<2>(2, top, 14, [&](int j) { return order[j]; }), 1u) - 1u);
             }
             float best = -INFINITY;
             for (int k = 0; k < N; ++k) best = fmaxf(best, v[k]);

@@ -230,13 +230,13 @@ int64_t score_space(char* base, int64_t rows, int64_t dim, int64_t classes, int3
 }
 
 void launch_groups(const ScoreSpace& s, int64_t ld, int64_t rows, int classes, const Scores& o, int64_t row0, hipStream_t stream) {
-    const int64_t waves = round_up(s.groups, kWave);
+    const int64_t places = round_up(s.groups, kSums * kWave);
     if (s.groups > kMostGroups) return launch_scores<float, false>(s.z, ld, rows, classes, o, row0, stream);
     auto run = [&](auto size) {
         constexpr int GS = decltype(size)::value;
         static std::atomic<uint64_t> allowed{0};
         allow_shared(k_group_scores<GS>, allowed);
-        k_group_scores<GS><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kWave, (kCandidates + kWave * 4) * 8 + waves * 8, stream>>>(s.z, ld, s.sums, s.groups, rows, classes, o,
+        k_group_scores<GS><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kWave, (kCandidates + kWave * 4) * 8 + places * 8, stream>>>(s.z, ld, s.sums, s.groups, rows, classes, o,
                                                                                                                                 row0);
     };
     if (s.size == 16) run(std::integral_constant<int, 16>());
