@@ -51,7 +51,7 @@ struct Logits {
                 for (int k = 0; k < 4; ++k) v[4 * j + k] = x[k];
             }
             RowSums a = RowSums::none();
-            a.add<false>(v);
+            a.add<false>(v, largest_of(v));
             a = joined_lanes(a);
             if (q == 0 && n < rows && group < groups) sums[(int64_t)n * groups + group] = GroupSums{a.m, a.s, a.t, 0.f};
         }
@@ -75,41 +75,37 @@ __global__ __launch_bounds__(kBlock) void k_thin_logits(Head a, Logits o) {
         for (int k = 0; k < 4; ++k) v[4 * t + k] = x[k];
     }
     RowSums sums = RowSums::none();
-    sums.add<false>(v);
+    sums.add<false>(v, largest_of(v));
     sums = joined_lanes(sums);
     if (q == 0 && r < a.rows) o.sums[(int64_t)r * o.groups + group] = GroupSums{sums.m, sums.s, sums.t, 0.f};
 }
 
-constexpr int kMostGroups = 8192;  // of a row: their largest logits are in shared memory
-constexpr int kSums = 8;           // of a lane, under way
+constexpr int kTurns = 8;  // of 64 heaps of groups, whose largest logits are in registers
 
-// A wave for each row; GS classes to a group.
-template <int GS>
-__global__ __launch_bounds__(kWave) void k_group_scores(const float* z, int64_t ld, const GroupSums* groups, int count, int64_t rows, int dim, Scores o, int64_t row0) {
-    constexpr int kPiece = kWave * 4, kAhead = 4, kRoomFor = kCandidates + kPiece;
-    extern __shared__ char space[];
-    uint64_t* keys = reinterpret_cast<uint64_t*>(space);
-    uint32_t* order = reinterpret_cast<uint32_t*>(keys + kRoomFor);
-    int* chosen = reinterpret_cast<int*>(order + (count + kSums * kWave - 1) / (kSums * kWave) * (kSums * kWave));
+// A wave for each row.  `merge` groups, a power of two, make a heap, of 1 << log2 fours of classes; there are up to 64 kTurns.
+__global__ __launch_bounds__(kWave) inline void k_group_scores(const float* z, int64_t ld, const GroupSums* groups, int count, int merge, int log2, int64_t rows, int dim,
+                                                               Scores o, int64_t row0) {
+    constexpr int kAhead = 4;
+    __shared__ uint64_t keys[kCandidates + kWave * 4];
+    __shared__ int chosen[kTurns * kWave];
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const float* p = z + row * ld;
         const int64_t to = row0 + row;
         RowSums sums = RowSums::none();
-        const int turns = (count + kWave - 1) / kWave;
-#pragma unroll 1
-        for (int j = 0; j < turns; j += kSums) {
-            f32x4 s[kSums];
+        uint32_t order[kTurns];
+        for (int j = 0; j < kTurns; ++j) order[j] = 0;
+#pragma unroll 2
+        for (int part = 0; part < merge; ++part) {
+            f32x4 s[kTurns];
 #pragma unroll
-            for (int k = 0; k < kSums; ++k) {
-                const int g = (j + k) * kWave + lane_id();
-                s[k] = *reinterpret_cast<const f32x4*>(groups + row * count + min(g, count - 1));
-            }
+            for (int j = 0; j < kTurns; ++j)
+                s[j] = *reinterpret_cast<const f32x4*>(groups + row * count + min((j * kWave + (int)lane_id()) * merge + part, count - 1));
 #pragma unroll
-            for (int k = 0; k < kSums; ++k) {
-                const int g = (j + k) * kWave + lane_id();
-                if (g < count) sums.join<false>(RowSums{s[k][0], s[k][1], s[k][2]});
-                order[g] = g < count ? order_of(s[k][0]) : 0u;
-            }
+            for (int j = 0; j < kTurns; ++j)
+                if ((j * kWave + (int)lane_id()) * merge + part < count) {
+                    sums.join<false>(RowSums{s[j][0], s[j][1], s[j][2]});
+                    order[j] = max(order[j], order_of(s[j][0]));
+                }
         }
         sums.over_lanes<false>();
         const RowLog<false> log(sums, dim);
@@ -122,35 +118,41 @@ __global__ __launch_bounds__(kWave) void k_group_scores(const float* z, int64_t 
         if (o.top == 0) continue;
         Candidates c;
         c.none(keys);
-        wave_meets();
-        // with fewer groups than classes asked for, all of them
-        if (count >= o.top) c.raise(max(threshold<kSums>(turns, o.top, 14, [&](int j) { return order[j * kWave + lane_id()]; }), 1u) - 1u);
+        // orders of m, the largest y of a group, which is its largest logit's rounded once: a heap's largest logit is less than another's only if its m is not more
+        const uint32_t least = threshold<kTurns>(kTurns, o.top, 14, [&](int j) { return order[j]; });
         int found = 0;
-        for (int j = 0; j < turns; j += kSums) {
-            uint32_t u[kSums];
-            for (int k = 0; k < kSums; ++k) u[k] = order[(j + k) * kWave + lane_id()];
-            for (int k = 0; k < kSums; ++k) {
-                const bool hit = u[k] > c.above;
-                const uint64_t mask = __ballot(hit);
-                if (hit) chosen[found + lanes_before(mask)] = (j + k) * kWave + lane_id();
-                found += __popcll(mask);
-            }
+        for (int j = 0; j < kTurns; ++j) {
+            const bool hit = order[j] != 0 && order[j] >= least;
+            const uint64_t mask = __ballot(hit);
+            if (hit) chosen[found + lanes_before(mask)] = j * kWave + lane_id();
+            found += __popcll(mask);
         }
         wave_meets();
-        constexpr int kLanes = GS / 4, kOnce = kWave / kLanes;  // of a group; groups in a piece
+        const int fours = found << log2;
 #pragma unroll 1
-        for (int from = 0; from < found; from += kOnce * kAhead) {
+        for (int from = 0; from < fours; from += kWave * kAhead) {
             f32x4 v[kAhead];
             int col[kAhead];
             for (int j = 0; j < kAhead; ++j) {
-                const int k = from + j * kOnce + lane_id() / kLanes;
-                col[j] = k < found ? chosen[k] * GS + lane_id() % kLanes * 4 : dim;
+                const int k = from + j * kWave + lane_id();
+                col[j] = k < fours ? ((chosen[k >> log2] << log2) + (k & ((1 << log2) - 1))) * 4 : dim;
+                v[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (col[j] < dim) v[j] = *reinterpret_cast<const f32x4*>(p + col[j]);
+            }
+            if (from == 0) {
+                // of 128 pairs of fours the k-th largest maximum, as in RowScan
+                uint32_t best[2];
+                for (int j = 0; j < 2; ++j) {
+                    float top = -INFINITY;
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(v[2 * j][e], v[2 * j + 1][e]));
+                    best[j] = order_of(top);
+                }
+                c.raise(max(threshold<2>(2, o.top, 14, [&](int j) { return best[j]; }), 1u) - 1u);
             }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 for (int e = 0; e < 4; ++e) c.put(v[j][e], col[j] + e, col[j] + e < dim);
-                if (c.count > kCandidates) c.cut(o.top, kCandidates);
+                if (c.count > most_of(o.top)) c.cut(o.top, most_of(o.top));
             }
         }
         write_top<false>(c, o, to, log);
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(kBlock) void k_few_scores(Head a, Scores o) {
         for (int t = 0; t < CT; ++t)
             for (int i = 0; i < 4; ++i) v[4 * t + i] = z[0][t][i];
         RowSums sums = RowSums::none();
-        sums.add<false>(v);
+        sums.add<false>(v, largest_of(v));
         sums = joined_lanes(sums);
         const RowLog<false> log(sums, a.classes);
         if (there && q == 0 && o.entropy) o.entropy[row] = log.entropy;

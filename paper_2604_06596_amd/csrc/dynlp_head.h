@@ -36,26 +36,6 @@ struct Head {
     int dim, classes;
 };
 
-// Four columns of a row: 16 bytes or 8.
-template <typename T>
-using Quad = Columns<T, 4>;
-template <typename T>
-__device__ inline Quad<T> load_quad(const T* row, int col, int dim) {
-    Quad<T> v;
-    if (col + 4 <= dim) {
-        __builtin_memcpy(v.d, row + col, sizeof v.d);
-        return v;
-    }
-    v.zero();
-    for (int k = 0; k < 4; ++k)
-        if (col + k < dim) {
-            if constexpr (sizeof(T) == 2)
-                v.d[k / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, row[col + k]) << (16 * (k & 1));
-            else
-                v.d[k] = __float_as_uint(row[col + k]);
-        }
-    return v;
-}
 // Column t of eight rows' quads, as an operand with these rows for k.
 __device__ inline u32x4 column_of(const Quad<bf16> (&x)[8], int t) {
     u32x4 v;

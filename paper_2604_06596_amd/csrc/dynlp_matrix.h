@@ -45,6 +45,29 @@ __device__ inline void store_columns(T* row, int col, int dim, const float (&f)[
     }
 }
 
+// Four columns of a row: 16 bytes or 8.
+template <typename T>
+using Quad = Columns<T, 4>;
+template <typename T>
+__device__ inline Quad<T> load_quad(const T* row, int col, int dim) {
+    Quad<T> v;
+    if (col + 4 <= dim) {
+        __builtin_memcpy(v.d, row + col, sizeof v.d);
+        return v;
+    }
+    v.zero();
+    for (int k = 0; k < 4; ++k)
+        if (col + k < dim) {
+            if constexpr (sizeof(T) == 2)
+                v.d[k / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, row[col + k]) << (16 * (k & 1));
+            else
+                v.d[k] = __float_as_uint(row[col + k]);
+        }
+    return v;
+}
+// A wave's own accesses of shared memory, in order.
+__device__ inline void wave_meets() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Over the four lanes that share a row.
 __device__ inline float row_sum(float v) {
     v += __shfl_xor(v, 16, kWave);

@@ -32,42 +32,53 @@ __device__ inline float value_of(uint64_t key) {
     return __uint_as_float((int)o < 0 ? o & 0x7fffffffu : ~o);
 }
 
-// f over the 64 lanes, by moves between neighbours (16 lanes, then rows of them); the result is in every lane.
+// f over 16 lanes, by moves between them; the result is in every lane.
+template <typename F>
+__device__ inline uint32_t over_16_lanes(uint32_t v, F f) {
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));  // rotated by 1, 2, 4, 8
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, true));
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));
+    return v;
+}
+// f over the 64 lanes.
 template <typename F>
 __device__ inline uint32_t over_wave(uint32_t v, F f) {
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x121, 0xf, 0xf, false));  // rotated by 1, 2, 4, 8
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x122, 0xf, 0xf, false));
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x124, 0xf, 0xf, false));
-    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x128, 0xf, 0xf, false));
+    v = over_16_lanes(v, f);
     const uint32_t a = f((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
     const uint32_t b = f((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48));
     return f(a, b);
 }
-__device__ inline float lanes_max(float v) {
-    return __uint_as_float(over_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
-}
-__device__ inline float lanes_sum(float v) {
-    return __uint_as_float(over_wave(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
-}
-__device__ inline uint32_t lanes_max(uint32_t v) {
-    return over_wave(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-}
-__device__ inline uint32_t lanes_min(uint32_t v) {
-    return over_wave(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
-}
+struct MaxFloat {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+};
+struct AddFloat {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
+};
+struct Larger {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
+struct Smaller {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a < b ? a : b; }
+};
+__device__ inline float lanes_max(float v) { return __uint_as_float(over_wave(__float_as_uint(v), MaxFloat())); }
+__device__ inline float lanes_sum(float v) { return __uint_as_float(over_wave(__float_as_uint(v), AddFloat())); }
+__device__ inline uint32_t lanes_max(uint32_t v) { return over_wave(v, Larger()); }
+__device__ inline uint32_t lanes_min(uint32_t v) { return over_wave(v, Smaller()); }
 __device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
 // ---- sums -------------------------------------------------------------------------------------------------------------
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// m and s as above, and t in logarithms of two.  PROB: m is not used.
+// With y = x log2(e): m is near the largest y (m of a row of nothing but -infinity is that), s = sum 2^(y - m), t = sum 2^(y - m) (y - m).  m need not be a value's y
+// itself, so that its rounding is no error.  PROB: s = sum x, t = sum x log2(x), and m is not used.
 struct RowSums {
     float m, s, t;
     __device__ static RowSums none() { return {-INFINITY, 0.f, 0.f}; }
-    // Values v, of which those that are not there are -infinity.  What is -infinity adds nothing, what is not a number makes s so.
+    // Values v, of which those that are not there are -infinity, and their largest.  What is -infinity adds nothing, what is not a number makes s so.
     template <bool PROB, int N>
-    __device__ void add(const float (&v)[N]) {
+    __device__ void add(const float (&v)[N], float top) {
         if constexpr (PROB) {
             for (int k = 0; k < N; ++k) {
                 const float x = v[k] == -INFINITY ? 0.f : v[k];
@@ -75,19 +86,30 @@ struct RowSums {
                 t += x == 0.f ? 0.f : x * __builtin_amdgcn_logf(x);
             }
         } else {
-            float top = m;
-            for (int k = 0; k < N; ++k) top = fmaxf(top, v[k]);
-            rescale(top);
-            const float base = fmaxf(m, -3e38f);  // a row of nothing but -infinity stays at 0
-            for (int k = 0; k < N; ++k) {
-                const float y = (v[k] - base) * kLog2e, e = __builtin_amdgcn_exp2f(y);
-                s += e;
-                t += e * fmaxf(y, -1e30f);
+            rescale(fmaxf(m, in_twos(top)));
+            const float base = fmaxf(m, -kMost);  // a row of nothing but -infinity stays at 0
+            if (__any(m == kMost)) {
+                for (int k = 0; k < N; ++k) {
+                    const float y = __builtin_fmaf(v[k], kLog2e, -base);
+                    add_power(v[k] < INFINITY && y > 0.f ? 0.f : y);
+                }
+            } else {
+                for (int k = 0; k < N; ++k) add_power(__builtin_fmaf(v[k], kLog2e, -base));
             }
         }
     }
+    __device__ void add_power(float y) {
+        const float e = __builtin_amdgcn_exp2f(y);
+        s += e;
+        t = __builtin_fmaf(e, fmaxf(y, -1e30f), t);
+    }
+    // The largest y of values whose largest is `top`.  Products that 32 bits do not hold stay at the largest number, where such values are equal; +infinity makes s so.
+    static constexpr float kMost = 3.40282347e38f;
+    __device__ static float in_twos(float top) {
+        return fabsf(top) < INFINITY ? fminf(fmaxf(top * kLog2e, -kMost), kMost) : top > 0.f ? kMost : -INFINITY;
+    }
     __device__ void rescale(float top) {
-        const float y = (m - top) * kLog2e;
+        const float y = m - top;
         if (m == -INFINITY) {
             // nothing yet, or not a number
         } else if (y != 0.f) {
@@ -114,6 +136,12 @@ struct RowSums {
         t += o.t;
     }
 };
+template <int N>
+__device__ inline float largest_of(const float (&v)[N]) {
+    float top = v[0];
+    for (int k = 1; k < N; ++k) top = fmaxf(top, v[k]);
+    return top;
+}
 // What the sums of a whole row say.  A row of nothing but -infinity (zeros) has 1/C everywhere.
 template <bool PROB>
 struct RowLog {
@@ -122,11 +150,16 @@ struct RowLog {
     __device__ RowLog(const RowSums& a, int dim) {
         m = a.m;
         none = a.s == 0.f;
-        log_s = logf(a.s);
+        log_s = PROB ? logf(a.s) : a.s < INFINITY ? log2f(a.s) : NAN;
         uniform = none ? logf((float)dim) : 0.f;
-        entropy = none ? uniform : log_s - a.t / a.s * kLn2;
+        entropy = none ? uniform : PROB ? log_s - a.t / a.s * kLn2 : (log_s - a.t / a.s) * kLn2;
     }
-    __device__ float of(float x) const { return none ? -uniform : PROB ? logf(x) - log_s : (x - m) - log_s; }
+    __device__ float of(float x) const {
+        if (none) return -uniform;
+        if constexpr (PROB) return logf(x) - log_s;
+        const float y = m == RowSums::kMost ? fminf(__builtin_fmaf(x, kLog2e, -m), 0.f) : __builtin_fmaf(x, kLog2e, -m);
+        return (y - log_s) * kLn2;
+    }
 };
 
 // ---- the first classes ------------------------------------------------------------------------------------------------
@@ -170,23 +203,23 @@ struct Candidates {
     uint64_t* key;
     int count;       // the same for all lanes
     uint32_t above;  // what is not above it in order is none
-    float over;      // the same as a value, for a first look
+    float over;      // the same as a value, for a first look: what is not above it is none.  Not a number where all have to be looked at
     __device__ void none(uint64_t* space) {
         key = space;
         count = 0;
         above = 0;
-        over = -INFINITY;
+        over = NAN;
     }
     __device__ void raise(uint32_t order) {
         above = order;
         const float v = value_of((uint64_t)order << 32);
-        over = order < 0x00800000u || v != v ? -INFINITY : v == 0.f ? -1e-37f : v;  // -0 comes before 0
+        over = order <= order_of(-INFINITY) ? NAN : v == 0.f ? -1e-37f : v;  // -0 comes before 0
     }
     __device__ void put(float x, int column, bool there) {
+        if (!__any(!(x <= over))) return;
         const uint32_t o = order_of(x);
         const bool hit = there && o > above;
         const uint64_t mask = __ballot(hit);
-        if (mask == 0) return;
         if (hit) key[count + lanes_before(mask)] = (uint64_t)o << 32 | (uint32_t)~column;
         count += __popcll(mask);
     }
@@ -229,7 +262,10 @@ struct Candidates {
     }
 };
 
-constexpr int kCandidates = 384;  // that a wave has before the list is cut; DYNLP_MAX_TOP is less
+constexpr int kCandidates = 384;  // that a wave has at most when its part is done
+// Candidates beyond which the list is cut: a cut costs as much as some twenty candidates, and each lets fewer through (100,003 values, the first 32: cut
+// at 160 candidates 266 us for 4,099 rows).
+__device__ inline int most_of(int top) { return top + max(top, 32); }
 
 // One wave's part of a row: turns of P pieces per lane, `waves` of them taking turns.
 template <typename T, bool PROB, int P>
@@ -260,26 +296,33 @@ struct RowScan {
         for (int from = wave * turn; from < dim; from += waves * turn) {
             float v[N];
             load(row, from, dim, v);
-            sums.add<PROB>(v);
+            float tops[P];
+            for (int p = 0; p < P; ++p) {
+                tops[p] = v[p * E];
+                for (int e = 1; e < E; ++e) tops[p] = fmaxf(tops[p], v[p * E + e]);
+            }
+            const float best = largest_of(tops);
+            sums.add<PROB>(v, best);
             if (top == 0) continue;
             if (from == wave * turn) {
                 // of 128 groups of values the k-th largest maximum: k values are not below it
-                float best[2] = {-INFINITY, -INFINITY};
-                for (int k = 0; k < N; ++k) best[k / ((N + 1) / 2)] = fmaxf(best[k / ((N + 1) / 2)], v[k]);
-                const uint32_t order[2] = {order_of(best[0]), order_of(best[1])};
+                float half = v[0];
+                for (int k = 1; k < (N + 1) / 2; ++k) half = fmaxf(half, v[k]);
+                float other = v[N / 2];
+                for (int k = N / 2 + 1; k < N; ++k) other = fmaxf(other, v[k]);
+                const uint32_t order[2] = {order_of(half), order_of(other)};
                 c.raise(max(threshold<2>(2, top, 14, [&](int j) { return order[j]; }), 1u) - 1u);
             }
-            float best = -INFINITY;
-            for (int k = 0; k < N; ++k) best = fmaxf(best, v[k]);
-            if (!__any(best > c.over || c.over == -INFINITY)) continue;
+            if (!__any(!(best <= c.over))) continue;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
+                if (!__any(!(tops[p] <= c.over))) continue;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const int col = from + (p * kWave + (int)lane_id()) * E + e;
                     c.put(v[p * E + e], col, col < dim);
                 }
-                if (c.count > kCandidates) c.cut(top, kCandidates);
+                if (c.count > most_of(top)) c.cut(top, most_of(top));
             }
         }
     }
@@ -356,38 +399,108 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
     }
 }
 
-// Rows of up to 64 values: 16 lanes for each, four values in a lane.  The first classes are taken one after the other.
+// Many rows of up to 64 values, of which up to K classes are asked for: a lane for each row, from a copy of 64 rows in shared memory.  A lane keeps its first
+// K in order, so that a value is compared with K others.  1M rows of 50 probabilities, the first 4: with 16 lanes for a row (k_short_scores) 117 us.
+template <typename T, bool PROB, int K>
+__global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+    extern __shared__ char space[];
+    float* copy = reinterpret_cast<float*>(space);
+    const int pitch = dim | 1, lane = threadIdx.x;  // rows begin in different banks
+#pragma unroll 1
+    for (int64_t first = (int64_t)blockIdx.x * kWave; first < rows; first += (int64_t)gridDim.x * kWave) {
+        const T* p = x + first * ld;
+        const int here = (int)min(rows - first, (int64_t)kWave);
+        constexpr int kAhead = 16;
+        for (int from = 0; from < here; from += kAhead) {
+            T v[kAhead];
+            for (int k = 0; k < kAhead; ++k) v[k] = p[min(from + k, here - 1) * ld + min(lane, dim - 1)];
+            for (int k = 0; k < kAhead; ++k)
+                if (lane < dim) copy[min(from + k, here - 1) * pitch + lane] = to_float(v[k]);
+        }
+        wave_meets();
+        const float* mine = copy + min(lane, here - 1) * pitch;
+        RowSums a = RowSums::none();
+        float value[K];
+        int at[K];
+        for (int k = 0; k < K; ++k) value[k] = NAN, at[k] = 0;  // not a number: nothing yet
+        if constexpr (!PROB) {
+            float top = -INFINITY;
+            for (int c = 0; c < dim; ++c) top = fmaxf(top, mine[c]);
+            a.m = RowSums::in_twos(top);
+        }
+        const float base = fmaxf(a.m, -RowSums::kMost);
+        const bool huge = !PROB && __any(a.m == RowSums::kMost);
+#pragma unroll 2
+        for (int c = 0; c < dim; ++c) {
+            const float x1 = mine[c];
+            if constexpr (PROB) {
+                const float u = x1 == -INFINITY ? 0.f : x1;
+                a.s += u;
+                a.t = __builtin_fmaf(u, __builtin_amdgcn_logf(fmaxf(u, 1.17549435e-38f)), a.t);
+            } else {
+                float y = __builtin_fmaf(x1, kLog2e, -base);
+                if (huge) y = x1 < INFINITY && y > 0.f ? 0.f : y;
+                a.add_power(y);
+            }
+            const float u = fmaxf(x1, -INFINITY);  // what is not a number counts as that
+            bool before[K];
+            for (int k = 0; k < K; ++k) before[k] = !(u <= value[k]);
+            for (int k = K - 1; k >= 0; --k) {
+                const float own = before[k] ? u : value[k];
+                const int own_at = before[k] ? c : at[k];
+                value[k] = k > 0 && before[k - 1] ? value[k - 1] : own;
+                at[k] = k > 0 && before[k - 1] ? at[k - 1] : own_at;
+            }
+        }
+        const RowLog<PROB> log(a, dim);
+        const int64_t to = row0 + first + lane;
+        if (lane < here) {
+            if (o.entropy) o.entropy[to] = log.entropy;
+            for (int k = 0; k < o.given; ++k) {
+                const int g = o.classes[to * o.given + k];
+                if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
+                o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(mine[g]) : 0.f;
+            }
+            for (int k = 0; k < K; ++k)
+                if (k < o.top) {
+                    if (o.top_classes) o.top_classes[to * o.top + k] = at[k];
+                    if (o.log_top) o.log_top[to * o.top + k] = log.of(value[k]);
+                }
+        }
+        wave_meets();
+    }
+}
+
+// Rows of up to 64 values: 16 lanes for each, four values in a lane.  The first classes are taken one after the other; lane k mod 16 keeps the k-th until 16 are together.
 template <typename T, bool PROB>
 __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
     const int r = threadIdx.x & 15, col = 4 * r;
-    for (int64_t first = (int64_t)blockIdx.x * (kBlock / 16); first < rows; first += (int64_t)gridDim.x * (kBlock / 16)) {
+    const int64_t step = (int64_t)gridDim.x * (kBlock / 16);
+    Columns<T, 4> ahead;
+    auto ask = [&](int64_t row) {
+        const T* p = x + min(row, rows - 1) * ld;
+        if (col + 4 <= dim) {
+            __builtin_memcpy(ahead.d, p + col, sizeof ahead.d);
+        } else {
+            const Quad<T> some = load_quad(p, min(col, dim), dim);
+            for (int k = 0; k < Columns<T, 4>::words; ++k) ahead.d[k] = some.d[k];
+        }
+    };
+    ask((int64_t)blockIdx.x * (kBlock / 16) + threadIdx.x / 16);
+#pragma unroll 1
+    for (int64_t first = (int64_t)blockIdx.x * (kBlock / 16); first < rows; first += step) {
         const int64_t row = first + threadIdx.x / 16, to = row0 + row;
         const bool there = row < rows;
         const T* p = x + min(row, rows - 1) * ld;
         float v[4];
-        if (col + 4 <= dim) {
-            Columns<T, 4> d;
-            __builtin_memcpy(d.d, p + col, sizeof d.d);
-            for (int k = 0; k < 4; ++k) v[k] = d.get(k);
-        } else {
-            for (int k = 0; k < 4; ++k) v[k] = col + k < dim ? to_float(p[col + k]) : -INFINITY;
-        }
-        auto turn = [](uint32_t u, int d) {
-            const int w = (int)u;
-            return (uint32_t)(d == 1   ? __builtin_amdgcn_update_dpp(w, w, 0x121, 0xf, 0xf, false)
-                              : d == 2 ? __builtin_amdgcn_update_dpp(w, w, 0x122, 0xf, 0xf, false)
-                              : d == 4 ? __builtin_amdgcn_update_dpp(w, w, 0x124, 0xf, 0xf, false)
-                                       : __builtin_amdgcn_update_dpp(w, w, 0x128, 0xf, 0xf, false));
-        };
-        auto turned = [&](float u, int d) { return __uint_as_float(turn(__float_as_uint(u), d)); };
+        for (int k = 0; k < 4; ++k) v[k] = col + k < dim ? ahead.get(k) : -INFINITY;
+        if (first + step < rows) ask(row + step);
         RowSums a = RowSums::none();
-        a.add<PROB>(v);
-        if constexpr (!PROB) {
-            float top = a.m;
-            for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, turned(top, d));
-            a.rescale(top);
-        }
-        for (int d = 1; d < 16; d <<= 1) a.s += turned(a.s, d), a.t += turned(a.t, d);
+        float top = largest_of(v);
+        if constexpr (!PROB) top = __uint_as_float(over_16_lanes(__float_as_uint(top), MaxFloat()));
+        a.add<PROB>(v, top);
+        a.s = __uint_as_float(over_16_lanes(__float_as_uint(a.s), AddFloat()));
+        a.t = __uint_as_float(over_16_lanes(__float_as_uint(a.t), AddFloat()));
         const RowLog<PROB> log(a, dim);
         if (there && r == 0 && o.entropy) o.entropy[to] = log.entropy;
         if (there)
@@ -399,19 +512,21 @@ __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld,
         if (o.top == 0) continue;
         uint32_t order[4];
         for (int k = 0; k < 4; ++k) order[k] = col + k < dim ? order_of(v[k]) : 0u;
-        for (int place = 0; place < o.top; ++place) {
-            uint32_t best = order[0], at = col;
-            for (int k = 1; k < 4; ++k)
-                if (order[k] > best) best = order[k], at = col + k;
-            for (int d = 1; d < 16; d <<= 1) {
-                const uint32_t other = turn(best, d), other_at = turn(at, d);
-                if (other > best || (other == best && other_at < at)) best = other, at = other_at;
+        for (int from = 0; from < o.top; from += 16) {
+            uint32_t my_order = 0, my_class = 0;
+            const int here = min(o.top - from, 16);
+            for (int place = 0; place < here; ++place) {
+                const uint32_t best = over_16_lanes(max(max(order[0], order[1]), max(order[2], order[3])), Larger());
+                uint32_t at = 64;
+                for (int k = 3; k >= 0; --k) at = order[k] == best ? col + k : at;
+                at = over_16_lanes(at, Smaller());
+                for (int k = 0; k < 4; ++k) order[k] = (int)at == col + k ? 0u : order[k];
+                my_order = r == place ? best : my_order;
+                my_class = r == place ? at : my_class;
             }
-            for (int k = 0; k < 4; ++k)
-                if ((int)at == col + k) order[k] = 0u;
-            if (there && r == (place & 15)) {
-                if (o.top_classes) o.top_classes[to * o.top + place] = (int)at;
-                if (o.log_top) o.log_top[to * o.top + place] = log.of(value_of((uint64_t)best << 32));
+            if (there && r < here) {
+                if (o.top_classes) o.top_classes[to * o.top + from + r] = (int)my_class;
+                if (o.log_top) o.log_top[to * o.top + from + r] = log.of(value_of((uint64_t)my_order << 32));
             }
         }
     }

@@ -217,9 +217,6 @@ struct ListTile {
         }
     }
 };
-// A wave's own accesses of shared memory, in order.
-__device__ inline void wave_meets() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
 // The entries of a wave's rows: the first 64 of each 16 rows are asked for at once.
 template <typename S>
 struct WaveLists {

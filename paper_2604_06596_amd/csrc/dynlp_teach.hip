@@ -187,7 +187,16 @@ void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& 
     using std::integral_constant;
     constexpr int E = Piece<T>::n, most = 32 / E;  // pieces of a lane: 2,048 values of a wave
     const int need = (int)std::min<int64_t>(ceil_div(dim, E * kWave), most);
-    if (dim <= 64) k_short_scores<T, PROB><<<(unsigned)std::min<int64_t>(ceil_div(rows, kBlock / 16), 1 << 20), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
+    // a lane for each row pays once there are rows for a wave on each of the 1,024 SIMDs
+    auto lanes = [&](auto first) {
+        constexpr int K = decltype(first)::value;
+        k_lane_scores<T, PROB, K><<<(unsigned)std::min<int64_t>(ceil_div(rows, kWave), 1 << 20), kWave, kWave * (dim | 1) * 4, stream>>>(x, ld, rows, dim, o, row0);
+    };
+    const bool many = dim <= 64 && rows >= 1024 * kWave;
+    if (many && o.top <= 2) lanes(integral_constant<int, 2>());
+    else if (many && o.top <= 4) lanes(integral_constant<int, 4>());
+    else if (many && o.top <= 8) lanes(integral_constant<int, 8>());
+    else if (dim <= 64) k_short_scores<T, PROB><<<(unsigned)std::min<int64_t>(ceil_div(rows, kBlock / 16), 2048), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
     else if (need == 1) scan(integral_constant<int, 1>(), integral_constant<int, 1>());
     else if (need == 2) scan(integral_constant<int, 2>(), integral_constant<int, 1>());
     else if (dim <= 1024 && most > 4) scan(integral_constant<int, 4>(), integral_constant<int, 1>());
@@ -230,18 +239,10 @@ int64_t score_space(char* base, int64_t rows, int64_t dim, int64_t classes, int3
 }
 
 void launch_groups(const ScoreSpace& s, int64_t ld, int64_t rows, int classes, const Scores& o, int64_t row0, hipStream_t stream) {
-    const int64_t places = round_up(s.groups, kSums * kWave);
-    if (s.groups > kMostGroups) return launch_scores<float, false>(s.z, ld, rows, classes, o, row0, stream);
-    auto run = [&](auto size) {
-        constexpr int GS = decltype(size)::value;
-        static std::atomic<uint64_t> allowed{0};
-        allow_shared(k_group_scores<GS>, allowed);
-        k_group_scores<GS><<<(unsigned)std::min<int64_t>(rows, 1 << 20), kWave, (kCandidates + kWave * 4) * 8 + places * 8, stream>>>(s.z, ld, s.sums, s.groups, rows, classes, o,
-                                                                                                                                row0);
-    };
-    if (s.size == 16) run(std::integral_constant<int, 16>());
-    else if (s.size == 64) run(std::integral_constant<int, 64>());
-    else run(std::integral_constant<int, 128>());
+    int merge = 1, log2 = 0;
+    while (ceil_div(s.groups, merge) > kTurns * kWave) merge *= 2;
+    while (4 << log2 < s.size * merge) ++log2;
+    k_group_scores<<<(unsigned)std::min<int64_t>(rows, 1 << 20), kWave, 0, stream>>>(s.z, ld, s.sums, s.groups, merge, log2, rows, classes, o, row0);
 }
 
 // F is called with (T(), number of tiles of 16 classes).
