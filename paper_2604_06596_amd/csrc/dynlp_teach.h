@@ -81,14 +81,14 @@ __device__ inline void add_bias(const float* b, float factor, bool shut, float (
 // ---- the teacher's lists ----------------------------------------------------------------------------------------------
 
 // Entries of 16 rows, ordered by the tile of classes that they lie in: their row and class there, and q.  A class that a row names several times is one entry.
-constexpr int kListRows = 16, kListClasses = 256;
+constexpr int kListRows = 16;
 struct Lists {
     uint2* entry;       // [16 rows][16 kept]: row << 8 | class, bits of q
     uint32_t* start;    // [16 rows][tiles + 1]
     float* entropy;     // sum of q log q of a row
     float* weight;      // of a row; 0: left out
     uint32_t* largest;  // bits of the largest finite |weight|, or NULL
-    int kept, tiles;
+    int kept, tiles, log2;  // tiles of 1 << log2 classes, 256 at most
 };
 
 // zeros: 512 bytes of them.
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
         }
     __syncthreads();
     for (int e = 0; e < E; ++e)
-        if (c[e] >= 0 && first[e]) atomicAdd(count + c[e] / kListClasses, 1u);
+        if (c[e] >= 0 && first[e]) atomicAdd(count + (c[e] >> out.log2), 1u);
     __syncthreads();
     // where each tile's entries begin
     const int per = (out.tiles + kBlock - 1) / kBlock;
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
     uint2* entry = out.entry + (int64_t)blockIdx.x * (kListRows * t.kept);
     for (int e = 0; e < E; ++e)
         if (c[e] >= 0 && first[e])  // in whatever order: no two are for the same row and class
-            entry[atomicAdd(count + c[e] / kListClasses, 1u)] = make_uint2((uint32_t)in << 8 | (uint32_t)(c[e] % kListClasses), __float_as_uint(all[e]));
+            entry[atomicAdd(count + (c[e] >> out.log2), 1u)] = make_uint2((uint32_t)in << 8 | (uint32_t)(c[e] & ((1 << out.log2) - 1)), __float_as_uint(all[e]));
     if (there && me == 0) {
         const float r = t.row_weight ? t.row_weight[at] : 1.f;
         const float weight = sum == 0.f ? 0.f : r;

@@ -16,25 +16,41 @@ constexpr int64_t kMostStride = 1 << 22;              // elements: 32 bits hold 
 constexpr int64_t kLogitsBytes = int64_t(256) << 20;  // of logits in memory at a time
 constexpr int64_t kTermsBytes = int64_t(4) << 30;     // of dz in memory at a time
 constexpr int64_t kMostTeachRows = 1 << 24;           // at a time: a launch has fewer than 2^32 threads
-static_assert(DYNLP_MAX_WIDE_CLASSES / kListClasses * 4 <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
+static_assert(DYNLP_MAX_WIDE_CLASSES / 256 * 4 <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
 
 // ---- products ---------------------------------------------------------------------------------------------------------
 
 struct Tiling {
     int tm, tn, wm, wn;
 };
-// m: the fast index of the result.
-Tiling tiling(int64_t m, int64_t n) {
-    if (n <= 16) return {256, 16, 4, 1};
-    if (n <= 64) return {256, 64, 4, 1};
-    if (m <= 64) return {64, 256, 1, 4};
-    return {256, 128, 2, 2};
+constexpr int kRoom = 512;  // workgroups that the chip has room for: two on each CU, by their shared memory
+// The tile with which the product (m: the fast index of the result) is done soonest: rounds of kRoom tiles, weighed by the products of a tile and by how much longer
+// small ones take for each of them.  `even`: the last round's tiles are split, and it is as long as it is full.
+Tiling tiling(int64_t m, int64_t n, bool even) {
+    struct Weighed {
+        Tiling t;
+        double weight;
+    };
+    static const Weighed all[] = {{{256, 128, 2, 2}, 1.0}, {{256, 64, 4, 1}, 1.6}, {{128, 128, 2, 2}, 1.4}, {{64, 256, 1, 4}, 1.6}, {{256, 16, 4, 1}, 3.0}};
+    const Weighed* best = nullptr;
+    double least = 0.0;
+    for (const Weighed& w : all) {
+        if (w.t.tm < 256 && m > 1024) continue;  // few tiles of classes, which k_teach_lists counts
+        const int64_t tiles = ceil_div(m, w.t.tm) * ceil_div(n, w.t.tn);
+        const double rounds = even ? std::max((double)tiles / kRoom, 1.0) : (double)ceil_div(tiles, kRoom);
+        const double cost = rounds * w.t.tm * w.t.tn * w.weight;
+        if (!best || cost < least) best = &w, least = cost;
+    }
+    return best->t;
 }
+// Of logits: classes by rows.
+Tiling logits_tiling(int64_t classes, int64_t rows) { return tiling(classes, rows, false); }
 template <bool TA, bool TB, bool WOVEN, typename F>
 void by_tiling(const Tiling& t, F f) {
     if (t.tn == 16) f(Shape<256, 16, 4, 1, TA, TB, WOVEN>());
     else if (t.tn == 64) f(Shape<256, 64, 4, 1, TA, TB, WOVEN>());
     else if (t.tm == 64) f(Shape<64, 256, 1, 4, TA, TB, WOVEN>());
+    else if (t.tm == 128) f(Shape<128, 128, 2, 2, TA, TB, WOVEN>());
     else f(Shape<256, 128, 2, 2, TA, TB, WOVEN>());
 }
 
@@ -57,7 +73,6 @@ void launch_product(Wide g, const Tiling& t, int64_t m, int64_t n, const E& e, h
 
 // The chip has room for two workgroups on each CU: the tiles that do not fill it once more have their sums split, so that all of it has work to the end, but in
 // parts of 8 steps at least.  Returns the elements of their parts.
-constexpr int kRoom = 512;
 int64_t split_tiles(Wide* g, const Tiling& t, int64_t m, int64_t n) {
     g->tiles_m = (int)ceil_div(m, t.tm);
     g->tiles_n = (int)ceil_div(n, t.tn);
@@ -214,7 +229,7 @@ int64_t logits_rows(int64_t rows, int64_t classes) {
 // Classes of a group: a wave's part of the product.  Few rows have more waves than rows, and smaller parts.
 int group_size(int64_t rows, int64_t classes) {
     if (rows <= 16) return classes <= 16 * 2048 ? 16 : 64;
-    const Tiling t = tiling(classes, rows);
+    const Tiling t = logits_tiling(classes, rows);
     return t.tm / t.wm;
 }
 
@@ -349,7 +364,7 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
         return launched();
     }
     const Laid w = lay_out(*weight, s.weight, stream);
-    const Tiling tile = tiling(classes, s.rows);  // of all turns: its groups have a size
+    const Tiling tile = logits_tiling(classes, s.rows);  // of all turns: its groups have a size
     for (int64_t row = 0; row < h->rows; row += s.rows) {
         const int64_t rows = std::min(s.rows, h->rows - row);
         const Laid x = lay_out(rows_of(*h, row, rows), s.h, stream);
@@ -391,7 +406,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->ld = laid_ld(classes);
     const int64_t most = std::max<int64_t>(kTermsBytes / (s->ld * 2 * s->terms) / 256 * 256, 256);
     s->rows = std::min({rows, most, kMostTeachRows});
-    const Tiling t = tiling(classes, s->rows);
+    const Tiling t = logits_tiling(classes, s->rows);
     s->parts = (int)ceil_div(classes, t.tm) * t.wm;
     s->part_ld = round_up(s->rows, 64);
     s->zeros = c.take<uint32_t>(128);
@@ -399,7 +414,8 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->undo = c.take<float>(1);
     s->kept = c.take<uint32_t>(ceil_div(s->rows, 32));
     s->lists.kept = kept;
-    s->lists.tiles = (int)ceil_div(classes, kListClasses);
+    s->lists.tiles = (int)ceil_div(classes, t.tm);
+    s->lists.log2 = t.tm == 256 ? 8 : t.tm == 128 ? 7 : 6;
     s->lists.entry = c.take<uint2>(round_up(s->rows, kListRows) * kept);
     s->lists.start = c.take<uint32_t>(ceil_div(s->rows, kListRows) * (s->lists.tiles + 1));
     s->lists.entropy = c.take<float>(s->rows);
@@ -419,7 +435,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
         set_pairs(&by_w, terms_in(type), s->terms);
         by_h.steps = (int)(s->ld / kStep);
         by_w.steps = (int)ceil_div(s->rows, kStep);
-        const int64_t parts = std::max(split_tiles(&by_h, tiling(dim, s->rows), dim, s->rows), split_tiles(&by_w, tiling(dim, classes), dim, classes));
+        const int64_t parts = std::max(split_tiles(&by_h, tiling(dim, s->rows, true), dim, s->rows), split_tiles(&by_w, tiling(dim, classes, true), dim, classes));
         s->part = c.take<float>(rows > s->rows ? kRoom * 256 * 128 : parts);  // the most there are, where the last rows are fewer than others
         s->dweight = rows > s->rows && grad_type != DYNLP_FLOAT32 ? c.take<float>(classes * dim) : nullptr;
     }
@@ -430,7 +446,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
 template <typename T, bool TA, bool TB, typename O>
 void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
                      hipStream_t stream) {
-    const Tiling t = tiling(m, n);
+    const Tiling t = tiling(m, n, true);
     const int64_t parts = split_tiles(&g, t, m, n);
     const Output<O> to{static_cast<O*>(out), ld, (int)n, (int)m, alpha, undo, kept, add};
     launch_product<T, TA, TB, sizeof(O) == 2>(g, t, m, n, Store<O>{to, part}, stream);
@@ -522,7 +538,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         else if (teacher->kept <= 64) read_lists(std::integral_constant<int, 4>());
         else read_lists(std::integral_constant<int, 8>());
         const Wide g = logits_product(w, classes, x, rows, dim);
-        const Tiling tile = tiling(classes, s.rows);  // of all chunks: its parts have a size
+        const Tiling tile = logits_tiling(classes, s.rows);  // of all chunks: its parts have a size
         const int parts = (int)ceil_div(classes, tile.tm) * tile.wm;
         by_terms(h->type, [&](auto type) {
             using T = decltype(type);
