@@ -1,11 +1,12 @@
 """A student of propagated labels: texts as vertices, a kNN-like graph, labels propagated from a few of them, and a classifier that learns
 them and labels texts the graph has never held.
 
-    python examples/student.py [--items 20000] [--steps 300] [--bits 8]
+    python examples/student.py [--items 20000] [--steps 300] [--bits 8] [--keep 3]
 
 Synthetic texts: every class has its own frequent words.  The graph joins texts of the same class more often than others
 (``workloads.sbm``).  One process, one GPU.  ``DynLP.get_labels`` returns the soft rows that ``head_loss`` takes: here as numpy arrays, as the graph is one of these (a
-context made with ``device_ptrs=True`` takes and returns tensors on the GPU).
+context made with ``device_ptrs=True`` takes and returns tensors on the GPU).  With ``--keep K`` only the first K classes of each row are kept
+(``row_scores``) and learnt from (``head_distill``); at the end ``head_scores`` says of which unseen texts the student is least sure.
 """
 import argparse
 import math
@@ -53,10 +54,17 @@ class Student:
     def labels(self, ids, offsets, weights):
         return P.head_labels(P.embed(self.table, ids, offsets, weights), self.weight, self.bias)
 
+    def unsure(self, ids, offsets, weights):
+        """Entropy of each item's answer."""
+        return P.head_scores(P.embed(self.table, ids, offsets, weights), self.weight, self.bias).entropy
+
     def learn(self, ids, offsets, weights, soft, row_weight, lr):
-        """One step; returns the rows' losses."""
+        """One step, on soft rows or on their first classes; returns the rows' losses."""
         h = P.embed(self.table, ids, offsets, weights)
-        loss, dh, dweight, dbias = P.head_loss(h, self.weight, self.bias, soft, row_weight=row_weight, grad_scale=1.0 / len(h))
+        if isinstance(soft, P.Scores):
+            loss, dh, dweight, dbias = P.head_distill(h, self.weight, self.bias, soft.top, soft.log_top, row_weight=row_weight, grad_scale=1.0 / len(h))
+        else:
+            loss, dh, dweight, dbias = P.head_loss(h, self.weight, self.bias, soft, row_weight=row_weight, grad_scale=1.0 / len(h))
         dtable = P.embed_grad(dh, ids, len(self.table), offsets, weights)
         self.steps += 1
         P.adamw_step(self.params, [dtable, dweight, dbias], self.states, step=self.steps, lr=lr, weight_decay=[1e-4, 1e-4, 0.0],
@@ -64,7 +72,7 @@ class Student:
         return loss
 
 
-def run(items=20000, steps=300, bits=8, words=20000, dim=64, classes=10, verbose=True):
+def run(items=20000, steps=300, bits=8, words=20000, dim=64, classes=10, verbose=True, keep=0):
     """Returns (agreement of the propagated, and of the student's, labels of unseen texts with the truth, first and last mean loss)."""
     graph = W.sbm(items, classes, 16.0, 60.0, 0.1, 3)
     with P.DynLP(graph.n, graph.row_ptr, graph.col, graph.w, classes, graph.seed_vertex, graph.seed_class) as d:
@@ -76,10 +84,11 @@ def run(items=20000, steps=300, bits=8, words=20000, dim=64, classes=10, verbose
     texts, unseen = make_texts(true_class, classes, words, 20.0, 1), make_texts(unseen_class, classes, words, 20.0, 2)
     # a row that propagation is unsure of (near 1/C everywhere) counts for little
     sure = ((soft.max(1).values - 1.0 / classes) / (1.0 - 1.0 / classes)).clamp(0.0, 1.0)
+    target = P.row_scores(soft, top=keep, probabilities=True) if keep else soft
     student = Student(words, dim, classes, bits, 5)
     first = last = None
     for k in range(steps):
-        loss = student.learn(*texts, soft, sure, 0.01)
+        loss = student.learn(*texts, target, sure, 0.01)
         if k in (0, steps - 1):
             first, last = (float(loss.mean()) if k == 0 else first), float(loss.mean())
             if verbose:
@@ -87,6 +96,8 @@ def run(items=20000, steps=300, bits=8, words=20000, dim=64, classes=10, verbose
     propagated = float((torch.from_numpy(hard).cuda() == true_class).float().mean())
     learned = float((student.labels(*unseen)[1] == unseen_class).float().mean())
     if verbose:
+        entropy = student.unsure(*unseen)
+        print(f"least sure of: {torch.topk(entropy, 5).indices.tolist()} (entropy up to {float(entropy.max()):.3f}, mean {float(entropy.mean()):.3f})")
         print(f"propagated labels agree with the truth on {propagated:.3f} of the graph, the student's on {learned:.3f} of unseen texts")
     return propagated, learned, first, last
 
@@ -96,5 +107,6 @@ if __name__ == "__main__":
     ap.add_argument("--items", type=int, default=20000)
     ap.add_argument("--steps", type=int, default=300)
     ap.add_argument("--bits", type=int, default=8, choices=(8, 32))
+    ap.add_argument("--keep", type=int, default=0, help="classes of a row that the student learns from (0: all)")
     a = ap.parse_args()
-    run(a.items, a.steps, a.bits)
+    run(a.items, a.steps, a.bits, keep=a.keep)

@@ -91,7 +91,7 @@ struct RowSums {
             if (__any(m == kMost)) {
                 for (int k = 0; k < N; ++k) {
                     const float y = __builtin_fmaf(v[k], kLog2e, -base);
-                    add_power(v[k] < INFINITY && y > 0.f ? 0.f : y);
+                    add_power(m == kMost && v[k] < INFINITY && y > 0.f ? 0.f : y);
                 }
             } else {
                 for (int k = 0; k < N; ++k) add_power(__builtin_fmaf(v[k], kLog2e, -base));
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
             a.m = RowSums::in_twos(top);
         }
         const float base = fmaxf(a.m, -RowSums::kMost);
-        const bool huge = !PROB && __any(a.m == RowSums::kMost);
+        const bool huge = !PROB && a.m == RowSums::kMost;
 #pragma unroll 2
         for (int c = 0; c < dim; ++c) {
             const float x1 = mine[c];

@@ -110,7 +110,8 @@ template <int E>
 __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, int64_t row0, int64_t rows) {
     extern __shared__ char space[];
     uint32_t* count = reinterpret_cast<uint32_t*>(space);  // of each tile, then its next place
-    __shared__ uint32_t sums[kBlock];
+    __shared__ uint32_t sums[kBlock / kWave], most;
+    if (threadIdx.x == 0) most = 0;
     const int me = threadIdx.x & 15, in = threadIdx.x >> 4;
     const int64_t row = (int64_t)blockIdx.x * kListRows + in;
     const bool there = row < rows;
@@ -169,10 +170,15 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
     const int per = (out.tiles + kBlock - 1) / kBlock;
     uint32_t mine = 0;
     for (int k = threadIdx.x * per; k < min((int)(threadIdx.x + 1) * per, out.tiles); ++k) mine += count[k];
-    sums[threadIdx.x] = mine;
+    uint32_t before = mine;  // of the wave's threads up to this one, then of all before it
+    for (int d = 1; d < kWave; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)before, d, kWave);
+        if ((int)lane_id() >= d) before += o;
+    }
+    if (lane_id() == kWave - 1) sums[threadIdx.x / kWave] = before;
     __syncthreads();
-    uint32_t before = 0;
-    for (int k = 0; k < (int)threadIdx.x; ++k) before += sums[k];
+    before -= mine;
+    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) before += sums[w];
     uint32_t* start = out.start + (int64_t)blockIdx.x * (out.tiles + 1);
     for (int k = threadIdx.x * per; k < min((int)(threadIdx.x + 1) * per, out.tiles); ++k) {
         const uint32_t n = count[k];
@@ -190,8 +196,12 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
         const float weight = sum == 0.f ? 0.f : r;
         out.weight[row] = weight;
         out.entropy[row] = entropy;
-        if (out.largest && fabsf(weight) < INFINITY) atomicMax(out.largest, __float_as_uint(fabsf(weight)));
+        if (out.largest && fabsf(weight) < INFINITY) atomicMax(&most, __float_as_uint(fabsf(weight)));
     }
+    if (!out.largest) return;
+    __syncthreads();
+    // one address takes some 10^8 of these a second: those that change nothing do not go there
+    if (threadIdx.x == 0 && most > __hip_atomic_load(out.largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(out.largest, most);
 }
 
 // A wave's part of the lists of 16 rows in shared memory: q of the wave's classes, row by row.
@@ -311,27 +321,29 @@ struct RowJoin {
     float temperature;
     int rows, parts;
 };
-// The parts of 32 rows, by 8 threads each, in order.  The power of two brings the largest weight to 2^14 .. 2^15, so that float16 holds dz's terms.
-__global__ __launch_bounds__(kBlock) inline void k_teach_rows(RowJoin g) {
-    __shared__ float tops[8][32], sums[8][32], picks[8][32];
+// The parts of 32 rows, by K threads each, in order.  The power of two brings the largest weight to 2^14 .. 2^15, so that float16 holds dz's terms.
+template <int K>
+__global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
+    __shared__ float tops[K][33], sums[K][33], picks[K][33];
     const int r = threadIdx.x & 31, k = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + r, at = min(row, g.rows - 1);
     float m = -INFINITY, s = 0.f, pick = 0.f;
-    for (int p = k; p < g.parts; p += 8) {
-        const float pm = g.top[p * g.ld + at], ps = g.sum[p * g.ld + at];
-        pick += g.picked[p * g.ld + at];
+    auto take = [&](float pm, float ps) {
         const float all = fmaxf(m, pm);
         s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(m - all)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f(pm - all));
         m = all;
+    };
+#pragma unroll 4
+    for (int p = k; p < g.parts; p += K) {
+        pick += g.picked[p * g.ld + at];
+        take(g.top[p * g.ld + at], g.sum[p * g.ld + at]);
     }
     tops[k][r] = m, sums[k][r] = s, picks[k][r] = pick;
     __syncthreads();
     if (k != 0) return;
-    for (int p = 1; p < 8; ++p) {
-        const float pm = tops[p][r], ps = sums[p][r], all = fmaxf(m, pm);
+    for (int p = 1; p < K; ++p) {
         pick += picks[p][r];
-        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(m - all)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f(pm - all));
-        m = all;
+        take(tops[p][r], sums[p][r]);
     }
     const float weight = g.weight[at];
     const bool use = row < g.rows && weight != 0.f && s != 0.f;
@@ -449,20 +461,23 @@ struct Gradient {
 
 // ---- joins ------------------------------------------------------------------------------------------------------------
 
-// dbias = alpha sum of the parts, or that added to it.
-__global__ __launch_bounds__(kBlock) inline void k_teach_bias(const float* sums, int64_t ld, int parts, int classes, float alpha, const float* undo, float* dbias,
+// dbias = alpha sum of the parts, or that added to it; `each` of them at a time, to one row of dbias (ld elements) for each.
+constexpr int kBiasParts = 64;
+__global__ __launch_bounds__(kBlock) inline void k_teach_bias(const float* sums, int64_t ld, int parts, int each, int classes, float alpha, const float* undo, float* dbias,
                                                               bool add) {
     __shared__ float s[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, first = blockIdx.y * each, end = min(first + each, parts);
     float v = 0.f;
     if (c < classes)
-        for (int p = k; p < parts; p += 4) v += sums[p * ld + c];
+#pragma unroll 4
+        for (int p = first + k; p < end; p += 4) v += sums[p * ld + c];
     s[k][threadIdx.x & 63] = v;
     __syncthreads();
     if (k == 0 && c < classes) {
         for (int p = 1; p < 4; ++p) v += s[p][threadIdx.x];
-        v *= alpha * *undo;
-        dbias[c] = add ? dbias[c] + v : v;
+        v *= undo ? alpha * *undo : alpha;
+        float* to = dbias + blockIdx.y * ld + c;
+        *to = add ? *to + v : v;
     }
 }
 

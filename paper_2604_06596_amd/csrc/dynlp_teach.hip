@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t kMostBlocks = 0xffffffff / kBlock;  // workgroups: a launch has fewer than 2^32 threads
 constexpr int64_t kMostStride = 1 << 22;              // elements: 32 bits hold the bytes of a tile's rows
-constexpr int64_t kLogitsBytes = int64_t(256) << 20;  // of logits in memory at a time
+constexpr int64_t kLogitsBytes = int64_t(1) << 30;    // of logits in memory at a time (8,192 x 32,768: 776 us, with 256 MB 935)
 constexpr int64_t kTermsBytes = int64_t(4) << 30;     // of dz in memory at a time
 constexpr int64_t kMostTeachRows = 1 << 24;           // at a time: a launch has fewer than 2^32 threads
 static_assert(DYNLP_MAX_WIDE_CLASSES / 256 * 4 <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
@@ -24,30 +24,33 @@ struct Tiling {
     int tm, tn, wm, wn;
 };
 constexpr int kRoom = 512;  // workgroups that the chip has room for: two on each CU, by their shared memory
-// The tile with which the product (m: the fast index of the result) is done soonest: rounds of kRoom tiles, weighed by the products of a tile and by how much longer
-// small ones take for each of them.  `even`: the last round's tiles are split, and it is as long as it is full.
-Tiling tiling(int64_t m, int64_t n, bool even) {
+// The tile with which the product (m: the fast index of the result) is done soonest.  Weighed: what a product takes in a tile of a size, relative to the largest (256 x 128:
+// 966 TFLOP/s; 128 x 128: 480 in the same call).  Rounds of kRoom tiles; where sums may be split in parts of 8 steps (steps > 0), the tiles share the chip evenly.
+Tiling tiling(int64_t m, int64_t n, int64_t steps) {
     struct Weighed {
         Tiling t;
         double weight;
     };
-    static const Weighed all[] = {{{256, 128, 2, 2}, 1.0}, {{256, 64, 4, 1}, 1.6}, {{128, 128, 2, 2}, 1.4}, {{64, 256, 1, 4}, 1.6}, {{256, 16, 4, 1}, 3.0}};
+    static const Weighed all[] = {{{256, 128, 2, 2}, 1.0}, {{128, 64, 2, 2}, 1.5}, {{256, 64, 4, 1}, 1.6}, {{128, 128, 2, 2}, 1.8}, {{64, 256, 1, 4}, 1.8}, {{256, 16, 4, 1}, 4.0}};
     const Weighed* best = nullptr;
     double least = 0.0;
     for (const Weighed& w : all) {
-        if (w.t.tm < 256 && m > 1024) continue;  // few tiles of classes, which k_teach_lists counts
+        const bool few = n <= 64;  // rows: bound by reading the other operand
+        if (w.t.tm * w.t.tn == 128 * 64 && !few) continue;
+        if (w.t.tm < 256 && m > (few ? 1 << 20 : 1024)) continue;  // k_teach_lists counts the tiles of classes in 64 KB
         const int64_t tiles = ceil_div(m, w.t.tm) * ceil_div(n, w.t.tn);
-        const double rounds = even ? std::max((double)tiles / kRoom, 1.0) : (double)ceil_div(tiles, kRoom);
+        const double rounds = steps > 0 ? (double)tiles / (double)std::min<int64_t>(kRoom, tiles * std::max<int64_t>(steps / 8, 1)) : (double)ceil_div(tiles, kRoom);
         const double cost = rounds * w.t.tm * w.t.tn * w.weight;
         if (!best || cost < least) best = &w, least = cost;
     }
     return best->t;
 }
 // Of logits: classes by rows.
-Tiling logits_tiling(int64_t classes, int64_t rows) { return tiling(classes, rows, false); }
+Tiling logits_tiling(int64_t classes, int64_t rows) { return tiling(classes, rows, 0); }
 template <bool TA, bool TB, bool WOVEN, typename F>
 void by_tiling(const Tiling& t, F f) {
     if (t.tn == 16) f(Shape<256, 16, 4, 1, TA, TB, WOVEN>());
+    else if (t.tn == 64 && t.tm == 128) f(Shape<128, 64, 2, 2, TA, TB, WOVEN>());
     else if (t.tn == 64) f(Shape<256, 64, 4, 1, TA, TB, WOVEN>());
     else if (t.tm == 64) f(Shape<64, 256, 1, 4, TA, TB, WOVEN>());
     else if (t.tm == 128) f(Shape<128, 128, 2, 2, TA, TB, WOVEN>());
@@ -73,6 +76,7 @@ void launch_product(Wide g, const Tiling& t, int64_t m, int64_t n, const E& e, h
 
 // The chip has room for two workgroups on each CU: the tiles that do not fill it once more have their sums split, so that all of it has work to the end, but in
 // parts of 8 steps at least.  Returns the elements of their parts.
+Tiling gradient_tiling(const Wide& g, int64_t m, int64_t n) { return tiling(m, n, (int64_t)g.pairs * g.steps); }
 int64_t split_tiles(Wide* g, const Tiling& t, int64_t m, int64_t n) {
     g->tiles_m = (int)ceil_div(m, t.tm);
     g->tiles_n = (int)ceil_div(n, t.tn);
@@ -220,9 +224,12 @@ void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& 
     else scan(integral_constant<int, most>(), integral_constant<int, 16>());
 }
 
+// Elements of a row of logits: rows that begin a power of two apart are written to few of the memory's channels (8,192 x 32,768, 256 MB at a time: 935 us, 845 so).
+int64_t logits_ld(int64_t classes) { return round_up(classes, 16) + 32; }
+
 // Rows whose logits are in memory at a time.
 int64_t logits_rows(int64_t rows, int64_t classes) {
-    const int64_t most = std::max<int64_t>(kLogitsBytes / (round_up(classes, 16) * 4) / 256 * 256, 256);
+    const int64_t most = std::max<int64_t>(kLogitsBytes / (logits_ld(classes) * 4) / 256 * 256, 256);
     return std::min(rows, most);
 }
 
@@ -245,7 +252,7 @@ int64_t score_space(char* base, int64_t rows, int64_t dim, int64_t classes, int3
     s->rows = logits_rows(rows, classes);
     s->size = group_size(s->rows, classes);
     s->groups = (int)ceil_div(classes, s->size);
-    s->z = c.take<float>(s->rows * round_up(classes, 16));
+    s->z = c.take<float>(s->rows * logits_ld(classes));
     s->sums = c.take<GroupSums>(s->rows * s->groups);
     if (s->rows <= 16) return c.used;  // rows are read as they lie
     s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
@@ -350,7 +357,7 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
     }
     ScoreSpace s{};
     score_space(static_cast<char*>(call->workspace), h->rows, h->dim, classes, h->type, !lies_well(*h), !lies_well(*weight), &s);
-    const int64_t ld = round_up(classes, 16);
+    const int64_t ld = logits_ld(classes);
     if (s.rows <= 16) {
         const Head a{h->data, weight->data, bias, h->stride, weight->stride, h->rows, h->dim, classes};
         const Logits e{s.z, ld, s.sums, s.groups, bias, (int)h->rows, classes};
@@ -429,14 +436,15 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
     if (grads) {
         s->dz = c.take<uint16_t>(s->rows * s->ld * s->terms);
-        s->bias_part = c.take<float>(ceil_div(s->rows, t.tn) * t.wn * s->ld);
+        const int64_t parts = ceil_div(s->rows, t.tn) * t.wn;
+        s->bias_part = c.take<float>((parts + ceil_div(parts, kBiasParts)) * s->ld);
         Wide by_h{}, by_w{};
         set_pairs(&by_h, terms_in(type), type == DYNLP_FLOAT32 ? 3 : 1);
         set_pairs(&by_w, terms_in(type), s->terms);
-        by_h.steps = (int)(s->ld / kStep);
+        by_h.steps = (int)(laid_ld(classes) / kStep);
         by_w.steps = (int)ceil_div(s->rows, kStep);
-        const int64_t parts = std::max(split_tiles(&by_h, tiling(dim, s->rows, true), dim, s->rows), split_tiles(&by_w, tiling(dim, classes, true), dim, classes));
-        s->part = c.take<float>(rows > s->rows ? kRoom * 256 * 128 : parts);  // the most there are, where the last rows are fewer than others
+        const int64_t split = std::max(split_tiles(&by_h, gradient_tiling(by_h, dim, s->rows), dim, s->rows), split_tiles(&by_w, gradient_tiling(by_w, dim, classes), dim, classes));
+        s->part = c.take<float>(rows > s->rows ? kRoom * 256 * 128 : split);  // the most there are, where the last rows are fewer than others
         s->dweight = rows > s->rows && grad_type != DYNLP_FLOAT32 ? c.take<float>(classes * dim) : nullptr;
     }
     return c.used;
@@ -446,7 +454,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
 template <typename T, bool TA, bool TB, typename O>
 void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
                      hipStream_t stream) {
-    const Tiling t = tiling(m, n, true);
+    const Tiling t = gradient_tiling(g, m, n);
     const int64_t parts = split_tiles(&g, t, m, n);
     const Output<O> to{static_cast<O*>(out), ld, (int)n, (int)m, alpha, undo, kept, add};
     launch_product<T, TA, TB, sizeof(O) == 2>(g, t, m, n, Store<O>{to, part}, stream);
@@ -546,7 +554,8 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             launch_product<T, false, false, true>(g, tile, classes, rows, stats, stream);
             const RowJoin join{s.top, s.sum, s.picked, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.lse, s.factor, s.kept,
                                s.undo, teacher->temperature, (int)rows, parts};
-            k_teach_rows<<<(unsigned)ceil_div(rows, 32), kBlock, 0, stream>>>(join);
+            if (parts <= 64) k_teach_rows<8><<<(unsigned)ceil_div(rows, 32), 256, 0, stream>>>(join);
+            else k_teach_rows<32><<<(unsigned)ceil_div(rows, 32), 1024, 0, stream>>>(join);
             if (!grads) return;
             const int64_t term = rows * s.ld;
             auto gradient = [&](auto terms) {
@@ -556,15 +565,24 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             if (s.terms == 1) gradient(std::integral_constant<int, 1>());
             else if constexpr (__is_same(T, f16)) gradient(std::integral_constant<int, 2>());
             else gradient(std::integral_constant<int, 3>());
-            if (dbias)
-                k_teach_bias<<<(unsigned)ceil_div(classes, 64), kBlock, 0, stream>>>(s.bias_part, s.ld, (int)ceil_div(rows, tile.tn) * tile.wn, classes, alpha, s.undo, dbias,
-                                                                                    add);
+            if (dbias) {
+                int64_t parts_n = ceil_div(rows, tile.tn) * tile.wn;
+                float* from = s.bias_part;
+                const unsigned across = (unsigned)ceil_div(s.ld, 64);
+                if (parts_n > kBiasParts) {  // many rows: first some of them at a time
+                    float* to = from + parts_n * s.ld;
+                    k_teach_bias<<<dim3(across, (unsigned)ceil_div(parts_n, kBiasParts)), kBlock, 0, stream>>>(from, s.ld, (int)parts_n, kBiasParts, (int)s.ld, 1.f, nullptr, to, false);
+                    from = to;
+                    parts_n = ceil_div(parts_n, kBiasParts);
+                }
+                k_teach_bias<<<dim3(across, 1), kBlock, 0, stream>>>(from, s.ld, (int)parts_n, (int)parts_n, classes, alpha, s.undo, dbias, add);
+            }
             if (want_h) {
                 Wide p{};
                 p.a = w.p, p.ld_a = w.ld, p.term_a = w.term, p.m = (int)laid_ld(dim);
                 p.b = s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)rows;
                 p.k = classes;
-                p.steps = (int)(s.ld / kStep);
+                p.steps = (int)(laid_ld(classes) / kStep);
                 set_pairs(&p, w.terms, w.terms == 1 ? 1 : s.terms);
                 void* to = static_cast<char*>(dh->data) + row * dh->stride * type_size(dh->type);
                 auto run = [&](auto out) {

@@ -323,3 +323,39 @@ def test_a_teacher_and_its_student(classes, kept):
     assert torch.allclose(dweight.double(), dense.t().contiguous() @ h.double() / items, rtol=1e-3, atol=1e-6)
     answer = P.head_scores(h, weight, bias, given=lists.top[:, 0].contiguous(), top=2)
     assert torch.allclose(answer.log_given, torch.full((items,), -float(np.log(classes)), device="cuda")) and (answer.top == torch.tensor([0, 1], device="cuda")).all()
+
+
+@pytest.mark.parametrize("rows, dim, classes, kept", [(70, 16, 70, 5), (1, 301, 20011, 16), (3000, 48, 900, 3), (1500, 130, 66, 128), (33, 20, 100003, 2), (5000, 17, 100, 9),
+                                                      (260, 64, 8200, 64)])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_other_shapes_of_heads(rows, dim, classes, kept, kind):
+    """Few rows and many classes, many rows and few classes: each has tiles and joins of its own."""
+    P = _api()
+    rng = np.random.default_rng(rows + dim)
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, TYPES[kind], False)
+    at = rng.integers(0, classes, size=(rows, kept)).astype(np.int32)
+    u = rng.standard_normal((rows, kept)).astype(np.float32)
+    r = np.where(rng.random(rows) < 0.2, 0.0, rng.random(rows)).astype(np.float32)
+    got = _run(P, h, W, b, at, u, temperature=3.0, row_weight=torch.from_numpy(r).cuda(), dtype=TYPES[kind])
+    ref = S.distill(eh, eW, eb, at, u, 3.0, r)
+    bars = _bars(ref, eh, eW, eb, r.astype(np.float64), 3.0, 1.0, kind, kind, u)
+    for name, value in zip(("loss", "dh", "dweight", "dbias"), got):
+        hold(value, ref[name], bars[name], name)
+
+
+def test_the_example_learns_from_lists():
+    """It runs, its numbers are numbers; unsure() is the entropy of labels()."""
+    import importlib.util
+    import os
+
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "student.py")
+    spec = importlib.util.spec_from_file_location("student_example", at)
+    E = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(E)
+    results = E.run(items=2000, steps=3, words=2000, dim=32, keep=3, verbose=True)
+    assert np.isfinite(results).all()
+    student = E.Student(500, 32, 10, 32, 1)
+    student.weight.normal_()
+    texts = E.make_texts(torch.arange(40, device="cuda") % 10, 10, 500, 8.0, 3)
+    soft = student.labels(*texts)[0].double()
+    assert torch.allclose(student.unsure(*texts).double(), -torch.xlogy(soft, soft).sum(1), rtol=1e-4, atol=1e-5)

@@ -274,3 +274,67 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         for a, c in zip((*P.head_scores(h, W, b, given=given, top=8), *P.row_scores(x, given=given, top=8)), (*got, *got_rows)):
             assert torch.equal(a, c), turn
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16", "probabilities"])
+@pytest.mark.parametrize("classes, top", [(1, 1), (5, 2), (29, 4), (50, 8), (63, 3), (64, 5), (64, 0)])
+def test_many_short_rows(classes, top, kind):
+    """So many that each has a lane: a row count that is no multiple of 64, rows with padding behind them, rows that have fewer numbers than classes asked for."""
+    P = _api()
+    g = torch.Generator(device="cuda").manual_seed(classes * 10 + top)
+    rows = 1024 * 64 + 37
+    dtype = TYPES.get(kind, torch.float32)
+    probabilities = kind == "probabilities"
+    x = 3.0 * torch.randn(rows, classes, generator=g, device="cuda")
+    if probabilities:
+        x = torch.softmax(x, 1)
+        x[::7] = torch.nn.functional.one_hot(x[::7].argmax(1), classes).float()
+    else:
+        x[::5, classes // 2:] = -float("inf")
+        x[3] = -float("inf")
+        x[::11] = 1.0
+    wide = torch.full((rows, classes + 3), 9.0, dtype=dtype, device="cuda")
+    wide[:, :classes] = x.to(dtype)
+    t = wide[:, :classes]
+    given = torch.randint(-1, classes, (rows, 2), generator=g, device="cuda", dtype=torch.int32)
+    out = P.row_scores(t, given=given, top=top, probabilities=probabilities)
+    _check(out, t.double().cpu().numpy(), probabilities, given.cpu().numpy(), top)
+    if not probabilities and classes > 2:
+        odd = t[:rows].clone()
+        odd[100, 1], odd[200, 0] = float("nan"), float("inf")
+        got = P.row_scores(odd, top=top)
+        assert torch.isnan(got.entropy[[100, 200]]).all()
+        keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+        keep[[100, 200]] = False
+        assert torch.equal(got.entropy[keep], P.row_scores(t.contiguous(), top=top).entropy[keep])
+        if top:
+            assert torch.isnan(got.log_top[[100, 200]]).all()
+            assert np.array_equal(got.top[[100, 200]].cpu().numpy(), S.scores(odd[[100, 200]].double().cpu().numpy())[2][:, :top])
+            assert torch.equal(got.top[keep], out.top[keep])
+
+
+@pytest.mark.parametrize("lowest", [-3.4028234663852886e38, -1e30])
+def test_masks_of_the_lowest_value(lowest):
+    """Masked classes that hold the type's lowest value: nothing of them is left; where all are, they are equal."""
+    P = _api()
+    for classes in (7, 64, 300, 5000):
+        x = torch.randn(3, classes, device="cuda")
+        x[0, ::2] = lowest
+        x[1] = lowest
+        out = P.row_scores(x, top=2)
+        _check(out, x.double().cpu().numpy(), False, None, 2)
+        h, W = torch.zeros(3, 8, device="cuda"), torch.zeros(classes, 8, device="cuda")
+        b = torch.where(torch.arange(classes, device="cuda") % 2 == 0, torch.full((classes,), lowest, device="cuda"), torch.randn(classes, device="cuda"))
+        _check(P.head_scores(h, W, b, top=2), b.double().cpu().numpy()[None].repeat(3, 0), False, None, 2)
+
+
+@pytest.mark.parametrize("rows, dim, classes", [(20, 40, 100000), (3, 64, 600000), (70, 33, 1100000)])
+def test_heads_of_many_classes(rows, dim, classes):
+    """Groups of groups, and more of them than 64 lanes hold at a time."""
+    P = _api()
+    rng = np.random.default_rng(classes)
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, torch.bfloat16, True)
+    given = rng.integers(0, classes, size=(rows, 3)).astype(np.int32)
+    out = P.head_scores(h, W, b, given=torch.from_numpy(given).cuda(), top=100)
+    z = eh @ eW.T + eb
+    _check(out, z, False, given, 100)
