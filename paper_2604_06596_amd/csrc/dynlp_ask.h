@@ -118,7 +118,6 @@ __global__ __launch_bounds__(kWave) inline void k_group_scores(const float* z, i
         if (o.top == 0) continue;
         Candidates c;
         c.none(keys);
-        // orders of m, the largest y of a group, which is its largest logit's rounded once: a heap's largest logit is less than another's only if its m is not more
         const uint32_t least = threshold<kTurns>(kTurns, o.top, 14, [&](int j) { return order[j]; });
         int found = 0;
         for (int j = 0; j < kTurns; ++j) {

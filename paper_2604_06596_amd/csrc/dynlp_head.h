@@ -401,10 +401,10 @@ struct RowList {
         weight = t.row_weight ? t.row_weight[at] : 1.f;
         for (int k = 0; k < kAhead; ++k) entry(t, at, 4 * k + q, c[k], u[k]);
     }
-    // f(entries of all lanes) for 16 entries at a time.
+    // f(entries of all lanes, of which four each are there) for 16 entries at a time.
     template <typename F>
     __device__ inline void each(const Teacher& t, int64_t at, F f) {
-        f(c, u);
+        f(c, u, (t.kept + 3) / 4);
 #pragma unroll 1
         for (int from = 4 * kAhead; from < t.kept; from += 4 * kAhead) {
             int more_c[kAhead];
@@ -413,7 +413,7 @@ struct RowList {
                 entry(t, at, from + 4 * k + (lane_id() >> 4), more_c[k], more_u[k]);
                 check(t, false, more_c[k], more_u[k]);
             }
-            f(more_c, more_u);
+            f(more_c, more_u, (t.kept - from + 3) / 4);
         }
     }
     __device__ inline void make(const Teacher& t, int64_t at, f32x4 (&z)[CT]) {
@@ -427,12 +427,12 @@ struct RowList {
                 check(t, true, more_c, more_u);
             }
         float top = -INFINITY, sum = 0.f;
-        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead]) {
+        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead], int) {
             for (int k = 0; k < kAhead; ++k) top = fmaxf(top, v[k]);
         });
         top = row_max(top);
         auto power = [&](float v) { return v == -INFINITY ? 0.f : exp_below_0((v - top) * t.inverse); };
-        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead]) {
+        each(t, at, [&](const int (&)[kAhead], const float (&v)[kAhead], int) {
             for (int k = 0; k < kAhead; ++k) sum += power(v[k]);
         });
         sum = row_sum(sum);
@@ -440,8 +440,9 @@ struct RowList {
         const float log_sum = logf(sum), inverse = sum != 0.f ? 1.f / sum : 0.f;
         entropy = 0.f;
         for (int i = 0; i < CT; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        each(t, at, [&](const int (&cs)[kAhead], const float (&v)[kAhead]) {
+        each(t, at, [&](const int (&cs)[kAhead], const float (&v)[kAhead], int there) {
             for (int k = 0; k < kAhead; ++k) {
+                if (k >= there) break;  // the same for all lanes
                 const float mine = power(v[k]) * inverse;
                 if (mine != 0.f) entropy += mine * ((v[k] - top) * t.inverse - log_sum);
                 for (int from = 0; from < 4; ++from) {

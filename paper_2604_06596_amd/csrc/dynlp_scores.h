@@ -71,8 +71,8 @@ __device__ inline int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcn
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// With y = x log2(e): m is near the largest y (m of a row of nothing but -infinity is that), s = sum 2^(y - m), t = sum 2^(y - m) (y - m).  m need not be a value's y
-// itself, so that its rounding is no error.  PROB: s = sum x, t = sum x log2(x), and m is not used.
+// m: the largest x; with y = (x - m) log2(e), s = sum 2^y, t = sum 2^y y.  PROB: s = sum x, t = sum x log2(x), and m is not used.  (One operation less, x log2(e) - m', leaves
+// the rounding of m' = m log2(e) in every y, which is more than 32 bits hold where m is large, as masks are.)
 struct RowSums {
     float m, s, t;
     __device__ static RowSums none() { return {-INFINITY, 0.f, 0.f}; }
@@ -86,30 +86,20 @@ struct RowSums {
                 t += x == 0.f ? 0.f : x * __builtin_amdgcn_logf(x);
             }
         } else {
-            rescale(fmaxf(m, in_twos(top)));
-            const float base = fmaxf(m, -kMost);  // a row of nothing but -infinity stays at 0
-            if (__any(m == kMost)) {
-                for (int k = 0; k < N; ++k) {
-                    const float y = __builtin_fmaf(v[k], kLog2e, -base);
-                    add_power(m == kMost && v[k] < INFINITY && y > 0.f ? 0.f : y);
-                }
-            } else {
-                for (int k = 0; k < N; ++k) add_power(__builtin_fmaf(v[k], kLog2e, -base));
-            }
+            rescale(fmaxf(m, top));
+            const float from = base();
+            for (int k = 0; k < N; ++k) add_power((v[k] - from) * kLog2e);
         }
     }
+    // A row of nothing but -infinity stays at 0.
+    __device__ float base() const { return m == -INFINITY ? 0.f : m; }
     __device__ void add_power(float y) {
         const float e = __builtin_amdgcn_exp2f(y);
         s += e;
         t = __builtin_fmaf(e, fmaxf(y, -1e30f), t);
     }
-    // The largest y of values whose largest is `top`.  Products that 32 bits do not hold stay at the largest number, where such values are equal; +infinity makes s so.
-    static constexpr float kMost = 3.40282347e38f;
-    __device__ static float in_twos(float top) {
-        return fabsf(top) < INFINITY ? fminf(fmaxf(top * kLog2e, -kMost), kMost) : top > 0.f ? kMost : -INFINITY;
-    }
     __device__ void rescale(float top) {
-        const float y = m - top;
+        const float y = (m - top) * kLog2e;
         if (m == -INFINITY) {
             // nothing yet, or not a number
         } else if (y != 0.f) {
@@ -150,16 +140,11 @@ struct RowLog {
     __device__ RowLog(const RowSums& a, int dim) {
         m = a.m;
         none = a.s == 0.f;
-        log_s = PROB ? logf(a.s) : a.s < INFINITY ? log2f(a.s) : NAN;
+        log_s = logf(a.s);
         uniform = none ? logf((float)dim) : 0.f;
-        entropy = none ? uniform : PROB ? log_s - a.t / a.s * kLn2 : (log_s - a.t / a.s) * kLn2;
+        entropy = none ? uniform : log_s - a.t / a.s * kLn2;
     }
-    __device__ float of(float x) const {
-        if (none) return -uniform;
-        if constexpr (PROB) return logf(x) - log_s;
-        const float y = m == RowSums::kMost ? fminf(__builtin_fmaf(x, kLog2e, -m), 0.f) : __builtin_fmaf(x, kLog2e, -m);
-        return (y - log_s) * kLn2;
-    }
+    __device__ float of(float x) const { return none ? -uniform : PROB ? logf(x) - log_s : (x - m) - log_s; }
 };
 
 // ---- the first classes ------------------------------------------------------------------------------------------------
@@ -426,10 +411,9 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
         if constexpr (!PROB) {
             float top = -INFINITY;
             for (int c = 0; c < dim; ++c) top = fmaxf(top, mine[c]);
-            a.m = RowSums::in_twos(top);
+            a.m = top;
         }
-        const float base = fmaxf(a.m, -RowSums::kMost);
-        const bool huge = !PROB && a.m == RowSums::kMost;
+        const float base = a.base();
 #pragma unroll 2
         for (int c = 0; c < dim; ++c) {
             const float x1 = mine[c];
@@ -438,9 +422,7 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
                 a.s += u;
                 a.t = __builtin_fmaf(u, __builtin_amdgcn_logf(fmaxf(u, 1.17549435e-38f)), a.t);
             } else {
-                float y = __builtin_fmaf(x1, kLog2e, -base);
-                if (huge) y = x1 < INFINITY && y > 0.f ? 0.f : y;
-                a.add_power(y);
+                a.add_power((x1 - base) * kLog2e);
             }
             const float u = fmaxf(x1, -INFINITY);  // what is not a number counts as that
             bool before[K];
