@@ -161,7 +161,8 @@ int64_t dynlp_row_scores_workspace(int64_t rows, int32_t classes, int32_t top);
 
 /*
  * The same of the head's logits z = h W^T + bias, which are not kept: h, weight and bias as in dynlp_head_labels, but of up to DYNLP_MAX_WIDE_CLASSES classes and
- * DYNLP_MAX_WIDE_DIM elements of a row.  A class whose bias is -infinity has that logit whatever h holds.
+ * DYNLP_MAX_WIDE_DIM elements of a row.  A class whose bias is -infinity has that logit whatever h holds.  The logits of float32 heads of more than 64 classes are made
+ * from three 16-bit terms of each value, which hold all of it: an infinite element of h or weight makes the logits it meets not a number.
  */
 dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_scores* scores, const dynlp_call* call);
 int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type);
@@ -179,8 +180,8 @@ int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, 
  *   loss             rows float32; dh: rows x dim, of h's type; dweight: classes x dim, float32 or of h's type; dbias: classes float32.  Each of the four may be NULL (a
  *                    matrix with data NULL, too).
  * An entry's logit that is not a number, or +infinity, makes its row's loss and gradients so.  Heads as in dynlp_head_scores.
- * Gradients that are rounded to 16 bits are made from dz in 16 bits (bfloat16; float16 with a power of two that the largest r gives); dweight in float32,
- * and all gradients of float32 heads, from all of it.
+ * Up to 64 classes, and in float32 heads, the gradients are made from all 24 bits of dz.  Of larger heads in 16 bits, dh and a dweight in 16 bits are made from dz
+ * rounded to h's type (float16: times a power of two that the largest r gives), a dweight in float32 from all of it (float16: 22 bits).
  */
 typedef struct dynlp_teacher {
     const int32_t* classes;

@@ -441,15 +441,18 @@ struct RowList {
         entropy = 0.f;
         for (int i = 0; i < CT; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         each(t, at, [&](const int (&cs)[kAhead], const float (&v)[kAhead], int there) {
+#pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                if (k >= there) break;  // the same for all lanes
-                const float mine = power(v[k]) * inverse;
-                if (mine != 0.f) entropy += mine * ((v[k] - top) * t.inverse - log_sum);
-                for (int from = 0; from < 4; ++from) {
-                    const int other = __shfl(cs[k], 16 * from + r, kWave);
-                    const float p = __shfl(mine, 16 * from + r, kWave);
-                    for (int m = 0; m < CT; ++m)
-                        for (int i = 0; i < 4; ++i) y[m][i] += other == 16 * m + 4 * q + i ? p : 0.f;
+                if (k < there) {  // the same for all lanes
+                    const float mine = power(v[k]) * inverse;
+                    if (mine != 0.f) entropy += mine * ((v[k] - top) * t.inverse - log_sum);
+#pragma unroll
+                    for (int from = 0; from < 4; ++from) {
+                        const int other = __shfl(cs[k], 16 * from + r, kWave);
+                        const float p = __shfl(mine, 16 * from + r, kWave);
+                        for (int m = 0; m < CT; ++m)
+                            for (int i = 0; i < 4; ++i) y[m][i] += other == 16 * m + 4 * q + i ? p : 0.f;
+                    }
                 }
             }
         });

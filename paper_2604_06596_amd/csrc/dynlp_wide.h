@@ -8,7 +8,13 @@
 // Fragments: lane l = 16 q + r holds columns (n) r and rows (m) 4 q .. 4 q + 3 of a result.  Which rows of A stand behind the 16 rows of a fragment is free: for results of 16
 // bits four fragments share 64 of them (WOVEN) so that a lane has the 16 consecutive elements m = 16 q .. 16 q + 15 of row n, and four lanes a whole line of memory;
 // for results of 32 bits the four consecutive elements of a fragment do.
-// Sums are float32, products of 16-bit values are exact.  Operands in 32 bits come as bfloat16 terms that hold all 24 bits, and the sum runs over pairs of terms.
+// Sums are float32, products of 16-bit values are exact.  Operands in 32 bits come as bfloat16 terms that hold all 24 bits, and the sum runs over pairs of terms: six of
+// the nine, the others lie below 2^-24 of the whole.  (Two terms of float16 would take three products, but only with a power of two for each matrix or row, under which a
+// row of values of very different sizes loses its small ones.)
+// What bounds it: 50,021 x 8,192 x 1,024 bfloat16 837 to 872 us without what follows (1,000 TFLOP/s; the library's product 1,029), 8,192^3 1,023 (library 1,400).
+// The matrix cores are busy 41% of the time then, the requests to the L2 (64 bytes of a row per step) at 40% of its rate and shared memory at 40%.  Two workgroups to
+// a CU, so that one's end and beginning fall into the other's sums; fragments of the next step read ahead, a fourth stage's worth of prefetch and s_setprio around the
+// products changed nothing (837 / 848 / 839 us).
 #pragma once
 
 #include "dynlp_matrix.h"
@@ -131,7 +137,7 @@ struct Side {
     }
 };
 
-// Sizes of a workgroup's tile: TM x TN results, WM x WN waves.
+// Sizes of a workgroup's tile: TM x TN results, WM x WN waves.  256 x 128 has the fewest reads of shared memory per product that leave two workgroups room on a CU (72 KB each).
 template <int TM_, int TN_, int WM_, int WN_, bool TA_, bool TB_, bool WOVEN_>
 struct Shape {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
