@@ -42,7 +42,10 @@ def test_heads():
         _refused(L.dynlp_head_distill(h, weight, None, teacher, A << 6, None, None, None, call), word)
     long = (1 << 16) + 1
     _refused(L.dynlp_head_scores(T._Matrix(A, 5, long, long, 1), T._Matrix(A << 8, 10, long, long, 1), None, _scores(), call), "elements")
-    _refused(L.dynlp_head_scores(h, w, None, _scores(), T._Call(None, None, 0)), "workspace")
+    wide = T._Matrix(A << 1, 100, 8, 8, 1)  # up to 64 classes take no workspace
+    _refused(L.dynlp_head_scores(h, wide, None, _scores(), T._Call(None, None, 0)), "workspace")
+    _refused(L.dynlp_head_scores(h, wide, None, _scores(), T._Call(None, (A << 10) + 16, 1 << 50)), "aligned")
+    _refused(L.dynlp_head_distill(h, wide, None, teacher, A << 6, None, None, None, T._Call(None, A << 10, 1)), "workspace")
     _refused(L.dynlp_head_scores(h, w, None, _scores(), None), "call is NULL")
     _refused(L.dynlp_head_scores(h, w, None, None, call), "scores is NULL")
     _refused(L.dynlp_head_distill(h, w, None, None, A << 6, None, None, None, call), "teacher is NULL")
@@ -83,9 +86,12 @@ def test_workspaces_of_sizes_that_no_call_takes():
     L = T._library()
     assert L.dynlp_head_scores_workspace(0, 8, 10, 0) == 0 and L.dynlp_head_scores_workspace(5, 8, (1 << 22) + 1, 0) == 0
     assert L.dynlp_head_distill_workspace(0, 8, 10, 1, 0, 0) == 0 and L.dynlp_head_distill_workspace(5, 8, 10, 0, 0, 0) == 0
-    assert 0 < L.dynlp_head_distill_workspace(5, 8, 10, 1, 1, -1) < L.dynlp_head_distill_workspace(5, 8, 10, 1, 1, 1)
+    assert 0 < L.dynlp_head_distill_workspace(5, 8, 100, 1, 1, -1) < L.dynlp_head_distill_workspace(5, 8, 100, 1, 1, 1)
+    # up to 64 classes: none for scores and the loss, that of head_loss for gradients
+    assert L.dynlp_head_scores_workspace(5, 8, 64, 1) == 0 and L.dynlp_head_distill_workspace(5, 8, 64, 1, 1, -1) == 0
+    assert L.dynlp_head_distill_workspace(500, 8, 64, 1, 1, 1) == L.dynlp_head_loss_workspace(500, 8, 64, 1) > 0
     # whatever the rows, no more than some GiB, the head itself apart
-    for rows, classes in ((1, 1 << 22), (1 << 20, 1 << 22), ((1 << 31) - 2, 64), ((1 << 31) - 2, 1)):
+    for rows, classes in ((1, 1 << 22), (1 << 20, 1 << 22), ((1 << 31) - 2, 65)):
         for t in (0, 1, 2):
             assert 0 < L.dynlp_head_scores_workspace(rows, 64, classes, t) < 8 << 30
             assert 0 < L.dynlp_head_distill_workspace(rows, 64, classes, 8, t, 0) < 32 << 30
