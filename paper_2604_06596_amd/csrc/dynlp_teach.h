@@ -4,7 +4,7 @@
 //   loss = r T^2 sum q (log q - log p),   dz = grad_scale r T (p - q),   dh = dz W,   dweight = dz^T h,   dbias = sum of dz over rows
 // Logits do not go through memory: the product h W^T is made twice, for the sums of the softmax and again for dz, of which 16-bit terms are stored for the products
 // with W and h (k_wide, classes as its fast index m, rows as n).  A head's own rounding needs one term (rounding dz once more, to 2^-9 of it on average, adds as much as the
-// result's own rounding: 0.0023 of dh's norm where it alone is 0.0017); dweight in 32 bits takes as many as hold dz.
+// result's own rounding: 0.0023 of dh's norm where it alone is 0.0017; two are used in small calls, where few values decide); dweight in 32 bits takes as many as hold dz.
 // What bounds it: the four products, 8 rows classes dim operations where 6 cannot be done without.  8,192 x 1,024 bfloat16, 50,021 classes: 3.72 ms: sums 926 us, dz 997
 // (837 each without what follows the product), dh 788, dweight 958.  Logits kept in 32 bits between the first two would move 10 bytes each at some 5 TB/s, which
 // is a second product's time at dim = 1,000.

@@ -392,8 +392,16 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
 
 namespace {
 
-// Terms of dz: one where the gradients are rounded to 16 bits anyway, else as many as hold 24 bits of it (22 in float16).
-int dz_terms(int32_t type, int32_t grad_type) { return type == DYNLP_FLOAT32 ? 3 : grad_type != DYNLP_FLOAT32 ? 1 : type == DYNLP_BFLOAT16 ? 3 : 2; }
+// Terms of dz that dweight is made of: as many as hold 24 bits of it (22 in float16), or one where the gradients are rounded to 16 bits anyway.  One term's rounding errors average
+// to what the result's own rounding adds where many values of dz make a gradient; with few rows some values decide, and the error was up to 1.56 times that of the
+// rounding alone.  Two terms are used there, and where the products are short beside the launches.
+bool is_small(int64_t rows, int64_t dim, int64_t classes) { return rows <= 256 || (double)rows * (double)dim * (double)classes <= 2147483648.0; }
+int dz_terms(int32_t type, int32_t grad_type, bool small) {
+    if (type != DYNLP_FLOAT32 && grad_type != DYNLP_FLOAT32) return small ? 2 : 1;
+    return type == DYNLP_FLOAT16 ? 2 : 3;
+}
+// Of these, those that dh is made of.
+int dh_terms(int32_t type, bool small) { return type == DYNLP_FLOAT32 ? 3 : small ? 2 : 1; }
 
 struct TeachSpace {
     int64_t rows;  // at a time
@@ -406,13 +414,15 @@ struct TeachSpace {
     float *bias_part, *part, *dweight;
     int64_t part_ld;   // of top, sum and picked
     int terms, parts;
+    bool small;
 };
 
 // grad_type: of dweight, or -1 where no gradient is asked for.
 int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int kept, int32_t type, int32_t grad_type, bool lay_h, bool lay_weight, TeachSpace* s) {
     Carve c{base};
     const bool grads = grad_type >= 0;
-    s->terms = dz_terms(type, grad_type);
+    s->small = is_small(rows, dim, classes);
+    s->terms = dz_terms(type, grad_type, s->small);
     s->ld = laid_ld(classes);
     const int64_t most = std::max<int64_t>(kTermsBytes / (s->ld * 2 * s->terms) / 256 * 256, 256);
     s->rows = std::min({rows, most, kMostTeachRows});
@@ -442,7 +452,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
         const int64_t parts = ceil_div(s->rows, t.tn) * t.wn;
         s->bias_part = c.take<float>((parts + ceil_div(parts, kBiasParts)) * s->ld);
         Wide by_h{}, by_w{};
-        set_pairs(&by_h, terms_in(type), type == DYNLP_FLOAT32 ? 3 : 1);
+        set_pairs(&by_h, terms_in(type), dh_terms(type, s->small));
         set_pairs(&by_w, terms_in(type), s->terms);
         by_h.steps = (int)(laid_ld(classes) / kStep);
         by_w.steps = (int)ceil_div(s->rows, kStep);
@@ -566,8 +576,8 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
                 launch_product<T, false, false, true>(g, tile, classes, rows, e, stream);
             };
             if (s.terms == 1) gradient(std::integral_constant<int, 1>());
-            else if constexpr (__is_same(T, f16)) gradient(std::integral_constant<int, 2>());
-            else gradient(std::integral_constant<int, 3>());
+            else if (s.terms == 2) gradient(std::integral_constant<int, 2>());
+            else if constexpr (!__is_same(T, f16)) gradient(std::integral_constant<int, 3>());
             if (dbias) {
                 int64_t parts_n = ceil_div(rows, tile.tn) * tile.wn;
                 float* from = s.bias_part;
@@ -586,7 +596,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
                 p.b = s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)rows;
                 p.k = classes;
                 p.steps = (int)(laid_ld(classes) / kStep);
-                set_pairs(&p, w.terms, w.terms == 1 ? 1 : s.terms);
+                set_pairs(&p, w.terms, dh_terms(h->type, s.small));
                 void* to = static_cast<char*>(dh->data) + row * dh->stride * type_size(dh->type);
                 auto run = [&](auto out) {
                     launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.part, alpha, s.undo, s.kept, to, dh->stride, false, stream);

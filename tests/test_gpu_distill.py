@@ -359,3 +359,21 @@ def test_the_example_learns_from_lists():
     texts = E.make_texts(torch.arange(40, device="cuda") % 10, 10, 500, 8.0, 3)
     soft = student.labels(*texts)[0].double()
     assert torch.allclose(student.unsure(*texts).double(), -torch.xlogy(soft, soft).sum(1), rtol=1e-4, atol=1e-5)
+
+
+@pytest.mark.parametrize("rows, dim, classes", [(3, 64, 70), (40, 64, 200), (256, 48, 1000)])
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+def test_small_calls_are_off_by_their_own_rounding(rows, dim, classes, kind):
+    """dz in two terms: what they leave out, 2^-16 of it in bfloat16 and 2^-22 in float16, is little beside the result's rounding."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, TYPES[kind], False)
+    at, u = _lists(rng, rows, classes, 2)
+    got = _run(P, h, W, b, at, u, dtype=TYPES[kind])
+    ref = S.distill(eh, eW, eb, at, u)
+    bars = _bars(ref, eh, eW, eb, np.ones(rows), 1.0, 1.0, "float32", "float32", u)
+    dz = np.abs(ref["dz"])
+    rel, absolute = (2.0 ** -16, 0.0) if kind == "bfloat16" else (2.0 ** -22, 2.0 ** -25 * 2.0 ** -14)
+    more = rel * dz + np.where(dz > 0, absolute, 0.0)
+    hold(got[1], ref["dh"], bars["dh"] + more @ np.abs(eW), "dh")
+    hold(got[2], ref["dweight"], bars["dweight"] + more.T @ np.abs(eh), "dweight")
