@@ -44,10 +44,10 @@ struct Wide {
 // 64 lanes x 16 bytes from base + their offset to consecutive places of shared memory from `to` on (both the same for all lanes).  The compiler
 // does not count these loads: whoever reads them waits by arrived().
 __device__ inline void load_shared(const char* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" ::"s"(base), "v"(offset), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" ::"s"(base), "v"(offset), "s"(to) : "memory", "m0");
 }
 __device__ inline void load_shared(const char* address, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(address), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(address), "s"(to) : "memory", "m0");
 }
 // All but the last N of a wave's loads are in shared memory.
 template <int N>
