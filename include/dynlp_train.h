@@ -140,8 +140,8 @@ int64_t dynlp_head_loss_workspace(int64_t rows, int32_t dim, int32_t classes, in
  * classes: rows x given int32; outputs rows x given and rows x top without padding; entropy, top_classes and log_top may each be NULL.
  * 0 <= given <= DYNLP_MAX_GIVEN, 0 <= top <= DYNLP_MAX_TOP and the classes there are.
  * A logit of -infinity (a probability of 0) has log p = -infinity; a row of nothing else is 1/C everywhere.  A value that is not a number
- * makes log p and entropy of its row so, as does a logit of +infinity; for the order it counts as -infinity.  Probabilities are not negative.
- * The order is that of the values, also where log p is the same.
+ * makes log p and entropy of its row so, as does +infinity; for the order it counts as -infinity.  Probabilities are not negative.
+ * The order is that of the values, also where log p is the same.  Rows of probabilities may have any sum, also one that 32 bits do not hold.
  */
 #define DYNLP_MAX_TOP 128
 #define DYNLP_MAX_GIVEN (1 << 20)

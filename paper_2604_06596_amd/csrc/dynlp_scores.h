@@ -82,17 +82,21 @@ struct RowSums {
     template <bool PROB, int N>
     __device__ void add(const float (&v)[N], float top) {
         if constexpr (PROB) {
-            for (int k = 0; k < N; ++k) {
-                const float x = v[k] == -INFINITY ? 0.f : v[k];
-                s += x;
-                t += x == 0.f ? 0.f : x * __builtin_amdgcn_logf(x);
-            }
+            for (int k = 0; k < N; ++k) add_probability(v[k]);
         } else {
             rescale(fmaxf(m, top));
             const float from = base();
             for (int k = 0; k < N; ++k) add_power((v[k] - from) * kLog2e);
         }
     }
+    // The instruction's logarithm takes a denormal for 0: those, and 0, have that of 2^-126, which is near enough beside a sum of 2^-60 (power_of() sees to others).
+    __device__ void add_probability(float v) {
+        const float x = v == -INFINITY ? 0.f : v;
+        s += x;
+        t = __builtin_fmaf(x, __builtin_amdgcn_logf(fmaxf(x, 1.17549435e-38f)), t);
+    }
+    // A power of two for rows of probabilities whose sum is so small, or so large, that s or t does not hold it: they are summed once more, times that.  1 for all others.
+    __device__ float power_of() const { return s > 0.f && s < 0x1p-60f ? 0x1p90f : s > 0x1p100f ? 0x1p-60f : 1.f; }
     // A row of nothing but -infinity stays at 0.
     __device__ float base() const { return m == -INFINITY ? 0.f : m; }
     __device__ void add_power(float y) {
@@ -134,17 +138,20 @@ __device__ inline float largest_of(const float (&v)[N]) {
     for (int k = 1; k < N; ++k) top = fmaxf(top, v[k]);
     return top;
 }
-// What the sums of a whole row say.  A row of nothing but -infinity (zeros) has 1/C everywhere.
+// What the sums of a whole row (of probabilities: times `power`) say.  A row of nothing but -infinity (zeros) has 1/C everywhere.
 template <bool PROB>
 struct RowLog {
     float m, log_s, entropy, uniform;
     bool none;
-    __device__ RowLog(const RowSums& a, int dim) {
+    __device__ RowLog(const RowSums& a, int dim, float power = 1.f) {
         m = a.m;
         none = a.s == 0.f;
         log_s = logf(a.s);
         uniform = none ? logf((float)dim) : 0.f;
         entropy = none ? uniform : log_s - a.t / a.s * kLn2;
+        if constexpr (PROB) {
+            if (power != 1.f) log_s = a.s == INFINITY ? NAN : log_s - (power > 1.f ? 90.f : -60.f) * kLn2;
+        }
     }
     __device__ float of(float x) const { return none ? -uniform : PROB ? logf(x) - log_s : (x - m) - log_s; }
 };
@@ -278,6 +285,18 @@ struct RowScan {
                 for (int e = 0; e < E; ++e)
                     if (from + (p * kWave + (int)lane_id()) * E + e >= dim) v[p * E + e] = -INFINITY;
     }
+    // The sums alone, of values times a power of two.
+    __device__ static RowSums again(const T* row, int dim, int wave, int waves, float power) {
+        RowSums sums = RowSums::none();
+#pragma unroll 1
+        for (int from = wave * turn; from < dim; from += waves * turn) {
+            float v[N];
+            load(row, from, dim, v);
+            for (int k = 0; k < N; ++k) sums.add_probability(v[k] * power);
+        }
+        sums.over_lanes<true>();
+        return sums;
+    }
     __device__ static void run(const T* row, int dim, int wave, int waves, int top, RowSums& sums, Candidates& c) {
 #pragma unroll 1
         for (int from = wave * turn; from < dim; from += waves * turn) {
@@ -374,7 +393,20 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
             c.key = keys;
             c.count = all;
         }
-        const RowLog<PROB> log(sums, dim);
+        float power = 1.f;
+        if constexpr (PROB) {
+            power = sums.power_of();  // the same for all waves of the row
+            if (power != 1.f) {
+                sums = Scan::again(p, dim, WAVES == 1 ? 0 : wave, WAVES, power);
+                if constexpr (WAVES > 1) {
+                    if (lane_id() == 0) parts[wave] = sums;
+                    __syncthreads();
+                    sums = parts[0];
+                    for (int w = 1; w < WAVES; ++w) sums.join<PROB>(parts[w]);
+                }
+            }
+        }
+        const RowLog<PROB> log(sums, dim, power);
         if (threadIdx.x % (WAVES * kWave) == 0 && o.entropy) o.entropy[to] = log.entropy;
         for (int k = threadIdx.x % (WAVES * kWave); k < o.given; k += WAVES * kWave) {
             const int g = o.classes[to * o.given + k];
@@ -420,9 +452,7 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
         for (int c = 0; c < dim; ++c) {
             const float x1 = mine[c];
             if constexpr (PROB) {
-                const float u = x1 == -INFINITY ? 0.f : x1;
-                a.s += u;
-                a.t = __builtin_fmaf(u, __builtin_amdgcn_logf(fmaxf(u, 1.17549435e-38f)), a.t);
+                a.add_probability(x1);
             } else {
                 a.add_power((x1 - base) * kLog2e);
             }
@@ -436,7 +466,15 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
                 at[k] = k > 0 && before[k - 1] ? at[k - 1] : own_at;
             }
         }
-        const RowLog<PROB> log(a, dim);
+        float power = 1.f;
+        if constexpr (PROB) {
+            power = a.power_of();
+            if (power != 1.f) {
+                a = RowSums::none();
+                for (int c = 0; c < dim; ++c) a.add_probability(mine[c] * power);
+            }
+        }
+        const RowLog<PROB> log(a, dim, power);
         const int64_t to = row0 + first + lane;
         if (lane < here) {
             if (o.entropy) o.entropy[to] = log.entropy;
@@ -483,9 +521,21 @@ __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld,
         float top = largest_of(v);
         if constexpr (!PROB) top = __uint_as_float(over_16_lanes(__float_as_uint(top), MaxFloat()));
         a.add<PROB>(v, top);
-        a.s = __uint_as_float(over_16_lanes(__float_as_uint(a.s), AddFloat()));
-        a.t = __uint_as_float(over_16_lanes(__float_as_uint(a.t), AddFloat()));
-        const RowLog<PROB> log(a, dim);
+        auto join = [&] {
+            a.s = __uint_as_float(over_16_lanes(__float_as_uint(a.s), AddFloat()));
+            a.t = __uint_as_float(over_16_lanes(__float_as_uint(a.t), AddFloat()));
+        };
+        join();
+        float power = 1.f;
+        if constexpr (PROB) {
+            power = a.power_of();
+            if (__any(power != 1.f)) {  // the wave's other rows have the same sums again
+                a = RowSums::none();
+                for (int k = 0; k < 4; ++k) a.add_probability(v[k] * power);
+                join();
+            }
+        }
+        const RowLog<PROB> log(a, dim, power);
         if (there && r == 0 && o.entropy) o.entropy[to] = log.entropy;
         if (there)
             for (int k = r; k < o.given; k += 16) {
