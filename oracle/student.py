@@ -150,6 +150,7 @@ def distill(h, weight, bias, classes, logits, temperature=1.0, row_weight=None, 
             e = np.exp(u - u.max())
             q = e / e.sum()
             np.add.at(target[i], classes[i][real], q)
+            q = target[i]  # of a class, however many entries name it
             entropy[i] = np.where(q == 0.0, 0.0, q * np.log(np.where(q == 0.0, 1.0, q))).sum()
     z, p, _ = head(np.where(out[:, None], 0.0, h), weight, bias)
     out = out | np.isneginf(z).all(axis=1)

@@ -89,7 +89,7 @@ constexpr int kListRows = 16;
 struct Lists {
     uint2* entry;       // [16 rows][16 kept]: row << 8 | class, bits of q
     uint32_t* start;    // [16 rows][tiles + 1]
-    float* entropy;     // sum of q log q of a row
+    float* entropy;     // sum of q log q over the classes of a row
     float* weight;      // of a row; 0: left out
     uint32_t* largest;  // bits of the largest finite |weight|, or NULL
     int kept, tiles, log2;  // tiles of 1 << log2 classes, 256 at most
@@ -147,12 +147,8 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
     }
     sum = over_16(sum, true);
     const float log_sum = logf(sum);
-    float entropy = 0.f;
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < E; ++e)
         if (sum != 0.f) q[e] /= sum;
-        if (q[e] != 0.f) entropy += q[e] * ((u[e] - top) * t.inverse - log_sum);
-    }
-    entropy = over_16(entropy, true);
     // a class that is named several times: the first gets all of it
     float all[E];
     bool first[E];
@@ -167,6 +163,11 @@ __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, in
                     all[e] += more;
                 }
         }
+    // of probabilities of classes, not of entries; an entry that has its class to itself has the logarithm of q from its logit
+    float entropy = 0.f;
+    for (int e = 0; e < E; ++e)
+        if (c[e] >= 0 && first[e] && all[e] != 0.f) entropy += all[e] * (all[e] == q[e] ? (u[e] - top) * t.inverse - log_sum : logf(all[e]));
+    entropy = over_16(entropy, true);
     __syncthreads();
     for (int e = 0; e < E; ++e)
         if (c[e] >= 0 && first[e]) atomicAdd(count + (c[e] >> out.log2), 1u);

@@ -1,0 +1,26 @@
+"""The definition of learning from lists, held to its formula where a list names a class several times."""
+import numpy as np
+import pytest
+
+from oracle import student as S
+
+
+@pytest.mark.parametrize("temperature", [1.0, 2.5])
+def test_a_class_that_is_named_several_times_has_the_sum_of_its_probabilities(temperature):
+    """The divergence of one distribution over classes from another: never below zero, zero where they are the same, and that of the list with each class once."""
+    rng = np.random.default_rng(0)
+    h, W, b = rng.standard_normal((6, 4)), rng.standard_normal((5, 4)), rng.standard_normal(5)
+    at = rng.integers(0, 5, size=(6, 7))
+    u = rng.standard_normal((6, 7))
+    ref = S.distill(h, W, b, at, u, temperature)
+    q, p = ref["target"], ref["soft"]
+    np.testing.assert_allclose(q.sum(axis=1), 1.0)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        want = temperature ** 2 * np.where(q > 0, q * (np.log(q) - np.log(p)), 0.0).sum(axis=1)
+    np.testing.assert_allclose(ref["loss"], want, rtol=1e-12)
+    assert (ref["loss"] > 0).all()
+    once = S.distill(h, W, b, np.tile(np.arange(5), (6, 1)), temperature * np.log(np.maximum(q, 1e-300)), temperature)
+    for name in ("loss", "dh", "dweight", "dbias"):
+        np.testing.assert_allclose(ref[name], once[name], rtol=1e-9, atol=1e-12)
+    sure = np.array([-np.inf, 0.0, -np.inf, -np.inf, -np.inf])
+    assert abs(S.distill(np.zeros((1, 4)), W, sure, np.array([[1, 1, 1]]), rng.standard_normal((1, 3)))["loss"][0]) < 1e-15

@@ -1,0 +1,44 @@
+"""Learning from a teacher's first classes where the numbers themselves are hard.  Bars as in test_gpu_distill."""
+import numpy as np
+import pytest
+
+from oracle import student as S
+from rounding import hold
+from test_gpu_distill import _bars, _lists, _run
+from test_gpu_scores import TYPES, U, _api, _head
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows, classes", [(5, 10), (40, 64), (5, 100), (300, 400)])
+def test_a_class_that_is_named_twice_is_one_class(rows, classes, kind):
+    """The loss is a divergence of distributions over classes: of [c, c] it is that of [c], whichever logits share its probability; nothing where the head is certain of c."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    h, W, b, eh, eW, eb = _head(rng, rows, 32, classes, TYPES[kind], False)
+    y = rng.integers(0, classes, size=(rows, 1)).astype(np.int32)
+    for kept in (2, 5, 33):
+        u = rng.standard_normal((rows, kept)).astype(np.float32)
+        many = np.repeat(y, kept, axis=1)
+        got = _run(P, h, W, b, many, u)
+        ref = S.distill(eh, eW, eb, y, u[:, :1])
+        bars = _bars(ref, eh, eW, eb, np.ones(rows), 1.0, 1.0, kind, "float32", u)
+        for name, value in zip(("loss", "dh", "dweight", "dbias"), got):
+            hold(value, ref[name], bars[name], name)
+        # two classes, the first of them several times: its probabilities' sum
+        other = np.concatenate([many, (y + 1) % classes], axis=1)
+        v = np.concatenate([u, rng.standard_normal((rows, 1)).astype(np.float32)], axis=1)
+        both = np.concatenate([np.log(np.exp(v[:, :-1].astype(np.float64)).sum(axis=1, keepdims=True)), v[:, -1:]], axis=1)
+        got = _run(P, h, W, b, other, v)
+        ref = S.distill(eh, eW, eb, np.concatenate([y, (y + 1) % classes], axis=1), both)
+        bars = _bars(ref, eh, eW, eb, np.ones(rows), 1.0, 1.0, kind, "float32", v)
+        for name, value in zip(("loss", "dh", "dweight", "dbias"), got):
+            hold(value, ref[name], bars[name], name)
+    sure = torch.full((classes,), -float("inf"), device="cuda")
+    sure[1] = 0.0
+    one = torch.ones(rows, 2, dtype=torch.int32, device="cuda")
+    loss = P.head_distill(torch.zeros_like(h), W, sure, one, torch.randn(rows, 2, device="cuda"))[0]
+    assert float(loss.abs().max()) <= 4 * U
