@@ -38,7 +38,7 @@ struct Logits {
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
         static_assert(!S::WOVEN, "fours");
-        const bool shut = tile_bias<S>(bias, 1.f, at.tile_m * S::TM, classes, space);
+        const bool shut = tile_bias<S>(bias, at.tile_m * S::TM, classes, space);
         const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const int q = lane_id() >> 4, r = lane_id() & 15, group = at.tile_m * S::WM + at.wave_m;
 #pragma unroll
@@ -49,7 +49,7 @@ struct Logits {
             for (int j = 0; j < S::MI; ++j) {
                 const int m = at.m0 + 16 * j + 4 * q;
                 float x[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                add_bias(b + 16 * j + 4 * q, 1.f, shut, x);
+                add_bias(b + 16 * j + 4 * q, shut, x);
                 if (n < rows && m < ld) store_values<4>(z + n * ld + m, x);
                 for (int k = 0; k < 4; ++k) v[4 * j + k] = x[k];
             }

@@ -52,33 +52,25 @@ __global__ __launch_bounds__(kBlock) void k_lay_out(const T* in, int64_t ld, int
 
 // ---- logits -----------------------------------------------------------------------------------------------------------
 
-// The tile's bias, times a factor, in shared memory: -infinity, which makes a logit so whatever h holds, for what is not a class.  Returns whether there is any such.
+// The tile's bias in shared memory: -infinity, which makes a logit so whatever h holds, for what is not a class.  Returns whether there is any such.
 template <typename S>
-__device__ inline bool tile_bias(const float* bias, float factor, int first, int classes, char* space) {
+__device__ inline bool tile_bias(const float* bias, int first, int classes, char* space) {
     float* b = reinterpret_cast<float*>(space);
     bool shut = false;
     for (int k = threadIdx.x; k < S::TM; k += kBlock) {
-        b[k] = first + k >= classes ? -INFINITY : bias ? bias[first + k] * factor : 0.f;
+        b[k] = first + k >= classes ? -INFINITY : bias ? bias[first + k] : 0.f;
         shut |= b[k] == -INFINITY;
     }
     return __syncthreads_or(shut);
 }
-// v = v factor + bias.
-__device__ inline void add_bias(const float* b, float factor, bool shut, float (&v)[16]) {
-    for (int k = 0; k < 16; k += 4) {
+// Adds it to consecutive logits.
+template <int N>
+__device__ inline void add_bias(const float* b, bool shut, float (&v)[N]) {
+    for (int k = 0; k < N; k += 4) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(b + k);
-        for (int i = 0; i < 4; ++i) v[k + i] = __builtin_fmaf(v[k + i], factor, x[i]);
+        for (int i = 0; i < 4; ++i) v[k + i] += x[i];
         if (shut)
             for (int i = 0; i < 4; ++i) v[k + i] = x[i] == -INFINITY ? x[i] : v[k + i];
-    }
-}
-
-// Four of them, v = v factor + bias.
-__device__ inline void add_bias(const float* b, float factor, bool shut, float (&v)[4]) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(b);
-    for (int i = 0; i < 4; ++i) {
-        v[i] = __builtin_fmaf(v[i], factor, x[i]);
-        if (shut) v[i] = x[i] == -INFINITY ? x[i] : v[i];
     }
 }
 
@@ -268,17 +260,21 @@ struct WaveLists {
     }
 };
 
-// Sums of the softmax: for every 16 MI classes and every row the largest y = z log2(e) / T, sum of 2^(y - largest), sum of q y.
+// The least that logits are taken relative to: what has none but -infinity stays at 0.
+__device__ inline float base_of(float m) { return fmaxf(m, -3e38f); }
+
+// Sums of the softmax: for every 16 MI classes and every row the largest logit m, sum of exp((z - m) / T), sum of q (z - m), sum of q.  All that is rounded is differences
+// of logits, so that what they share, however large, takes no digits from p.
 struct Stats {
     const float* bias;
     Lists lists;
-    float *top, *sum, *picked;  // [part][ld]
+    float *top, *sum, *picked, *share;  // [part][ld]
     int64_t ld;
     float exponent;             // log2(e) / T
     int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        const bool shut = tile_bias<S>(bias, exponent, at.tile_m * S::TM, classes, space);
+        const bool shut = tile_bias<S>(bias, at.tile_m * S::TM, classes, space);
         const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const WaveLists<S> wave(lists, at, rows, space);
         const int lane_q = lane_id() >> 4, r = lane_id() & 15;
@@ -287,70 +283,76 @@ struct Stats {
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
             const bool any = wave.put(i, false);
-            float m = -INFINITY, pick = 0.f, y[S::MI / 4][16];
+            float m = -INFINITY, z[S::MI / 4][16];
             for (int j = 0; j < S::MI / 4; ++j) {
-                sixteen(acc[i], j, y[j]);
-                add_bias(b + 64 * j + 16 * lane_q, exponent, shut, y[j]);
-                for (int k = 0; k < 16; ++k) m = fmaxf(m, y[j][k]);
-                if (any) {
+                sixteen(acc[i], j, z[j]);
+                add_bias(b + 64 * j + 16 * lane_q, shut, z[j]);
+                for (int k = 0; k < 16; ++k) m = fmaxf(m, z[j][k]);
+            }
+            m = row_max(m);
+            const float base = base_of(m);
+            float s = 0.f, pick = 0.f, all = 0.f;
+            for (int j = 0; j < S::MI / 4; ++j)
+                for (int k = 0; k < 16; ++k) {
+                    z[j][k] -= base;
+                    s += __builtin_amdgcn_exp2f(z[j][k] * exponent);
+                }
+            s = row_sum(s);
+            if (any) {
+                for (int j = 0; j < S::MI / 4; ++j) {
                     float q[16];
                     wave.tile.get(64 * j + 16 * lane_q, q);
-                    for (int k = 0; k < 16; ++k) pick += q[k] != 0.f ? q[k] * y[j][k] : 0.f;
+                    for (int k = 0; k < 16; ++k) {
+                        pick += q[k] != 0.f ? q[k] * z[j][k] : 0.f;
+                        all += q[k];
+                    }
                 }
+                wave.put(i, true);
+                pick = row_sum(pick);
+                all = row_sum(all);
             }
-            if (any) wave.put(i, true);
-            m = row_max(m);
-            const float base = fmaxf(m, -3e38f);  // nothing but -infinity stays at 0
-            float s = 0.f;
-            for (int j = 0; j < S::MI / 4; ++j)
-                for (int k = 0; k < 16; ++k) s += __builtin_amdgcn_exp2f(y[j][k] - base);
-            s = row_sum(s);
-            pick = row_sum(pick);
             if (lane_q == 0 && n < rows) {
                 const int64_t to = (int64_t)(at.tile_m * S::WM + at.wave_m) * ld + n;
-                top[to] = m, sum[to] = s, picked[to] = pick;
+                top[to] = m, sum[to] = s, picked[to] = pick, share[to] = all;
             }
         }
     }
 };
 
 struct RowJoin {
-    const float *top, *sum, *picked;  // [part][ld]
+    const float *top, *sum, *picked, *share;  // [part][ld]
     int64_t ld;
     const float *entropy, *weight;    // of the lists
     const uint32_t* largest;          // of 16-bit floats with 5 bits of exponent, or NULL
     float* loss;                      // or NULL
-    float* lse;                       // log2 of the sum of exp(z / T)
+    float *base, *inverse;            // the largest logit m, and one over the sum of exp((z - m) / T)
     float* factor;                    // weight times a power of two; 0 where the row is left out
     uint32_t* kept;                   // a bit per row
     float* undo;                      // one over that power
-    float temperature;
+    float temperature, exponent;
     int rows, parts;
 };
 // The parts of 32 rows, by K threads each, in order.  The power of two brings the largest weight to 2^14 .. 2^15, so that float16 holds dz's terms.
 template <int K>
 __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
-    __shared__ float tops[K][33], sums[K][33], picks[K][33];
+    __shared__ float tops[K][33], sums[K][33], picks[K][33], shares[K][33];
     const int r = threadIdx.x & 31, k = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + r, at = min(row, g.rows - 1);
-    float m = -INFINITY, s = 0.f, pick = 0.f;
-    auto take = [&](float pm, float ps) {
-        const float all = fmaxf(m, pm);
-        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(m - all)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f(pm - all));
+    float m = -INFINITY, s = 0.f, pick = 0.f, share = 0.f;
+    auto take = [&](float pm, float ps, float pp, float pq) {
+        const float all = fmaxf(m, pm), base = base_of(all);
+        s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - all) * g.exponent)) + (pm == -INFINITY ? ps : ps * __builtin_amdgcn_exp2f((pm - all) * g.exponent));
+        if (share != 0.f) pick += share * (base_of(m) - base);
+        if (pq != 0.f) pick += pp + pq * (base_of(pm) - base);
+        share += pq;
         m = all;
     };
 #pragma unroll 4
-    for (int p = k; p < g.parts; p += K) {
-        pick += g.picked[p * g.ld + at];
-        take(g.top[p * g.ld + at], g.sum[p * g.ld + at]);
-    }
-    tops[k][r] = m, sums[k][r] = s, picks[k][r] = pick;
+    for (int p = k; p < g.parts; p += K) take(g.top[p * g.ld + at], g.sum[p * g.ld + at], g.picked[p * g.ld + at], g.share[p * g.ld + at]);
+    tops[k][r] = m, sums[k][r] = s, picks[k][r] = pick, shares[k][r] = share;
     __syncthreads();
     if (k != 0) return;
-    for (int p = 1; p < K; ++p) {
-        pick += picks[p][r];
-        take(tops[p][r], sums[p][r]);
-    }
+    for (int p = 1; p < K; ++p) take(tops[p][r], sums[p][r], picks[p][r], shares[p][r]);
     const float weight = g.weight[at];
     const bool use = row < g.rows && weight != 0.f && s != 0.f;
     float scale = 1.f;
@@ -364,12 +366,11 @@ __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     const uint32_t bits = (uint32_t)__ballot(use);
     if (r == 0) g.kept[blockIdx.x] = bits;
     if (row >= g.rows) return;
-    const float log2_s = log2f(s);
-    g.lse[row] = m + log2_s;
+    g.base[row] = m;
+    g.inverse[row] = 1.f / s;
     g.factor[row] = use ? weight * scale : 0.f;
     if (g.loss) {
-        // of the largest logit's distance and not of the logits, so that large ones do not cancel
-        const float t = g.temperature, part = g.entropy[row] + ((m - pick) + log2_s) * 0.693147181f;
+        const float t = g.temperature, part = g.entropy[row] + (logf(s) - pick / t);
         g.loss[row] = use ? weight * t * t * part : 0.f;
     }
 }
@@ -391,7 +392,7 @@ template <typename T, int TERMS>
 struct Gradient {
     const float* bias;
     Lists lists;
-    const float *lse, *factor;
+    const float *base, *inverse, *factor;
     uint16_t* dz;
     int64_t ld, term;
     float* sums;  // [part][ld]
@@ -399,16 +400,16 @@ struct Gradient {
     int rows, classes;
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
-        const bool shut = tile_bias<S>(bias, exponent, at.tile_m * S::TM, classes, space);
+        const bool shut = tile_bias<S>(bias, at.tile_m * S::TM, classes, space);
         const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const WaveLists<S> wave(lists, at, rows, space);
         const int lane_q = lane_id() >> 4, r = lane_id() & 15;
-        float total[S::MI / 4][16], f[S::NI], l[S::NI];
+        float total[S::MI / 4][16], f[S::NI], fp[S::NI], top[S::NI];  // of q, and of exp((z - top) / T)
         for (int j = 0; j < S::MI / 4; ++j)
             for (int k = 0; k < 16; ++k) total[j][k] = 0.f;
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
-            f[i] = n < rows ? factor[n] : 0.f, l[i] = n < rows ? lse[n] : 0.f;
+            f[i] = n < rows ? factor[n] : 0.f, fp[i] = n < rows ? inverse[n] * factor[n] : 0.f, top[i] = n < rows ? base[n] : 0.f;
         }
         wave_meets();
 #pragma unroll
@@ -420,15 +421,15 @@ struct Gradient {
                 const int m = at.m0 + 64 * j + 16 * lane_q;
                 float v[16];
                 sixteen(acc[i], j, v);
-                add_bias(b + 64 * j + 16 * lane_q, exponent, shut, v);
-                for (int k = 0; k < 16; ++k) v[k] = __builtin_amdgcn_exp2f(v[k] - l[i]);
+                add_bias(b + 64 * j + 16 * lane_q, shut, v);
+                for (int k = 0; k < 16; ++k) v[k] = __builtin_amdgcn_exp2f((v[k] - top[i]) * exponent) * fp[i];
                 if (any) {
                     float q[16];
                     wave.tile.get(64 * j + 16 * lane_q, q);
-                    for (int k = 0; k < 16; ++k) v[k] -= q[k];
+                    for (int k = 0; k < 16; ++k) v[k] = __builtin_fmaf(-q[k], f[i], v[k]);
                 }
                 // a row that is left out has zeros whatever its logits, and so have the columns behind the classes
-                for (int k = 0; k < 16; ++k) v[k] = f[i] != 0.f ? v[k] * f[i] : 0.f;
+                for (int k = 0; k < 16; ++k) v[k] = f[i] != 0.f ? v[k] : 0.f;
                 if (shut)
                     for (int k = 0; k < 16; ++k) v[k] = m + k < classes ? v[k] : 0.f;
                 for (int k = 0; k < 16; ++k) total[j][k] += v[k];

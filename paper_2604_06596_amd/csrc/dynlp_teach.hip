@@ -410,9 +410,9 @@ struct TeachSpace {
     uint32_t *zeros, *largest, *kept;
     float* undo;
     Lists lists;
-    float *top, *sum, *picked, *lse, *factor;
+    float *top, *sum, *picked, *share, *base, *inverse, *factor;
     float *bias_part, *part, *dweight;
-    int64_t part_ld;   // of top, sum and picked
+    int64_t part_ld;   // of top, sum, picked and share
     int terms, parts;
     bool small;
 };
@@ -440,11 +440,13 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->lists.start = c.take<uint32_t>(ceil_div(s->rows, kListRows) * (s->lists.tiles + 1));
     s->lists.entropy = c.take<float>(s->rows);
     s->lists.weight = c.take<float>(s->rows);
-    s->lse = c.take<float>(s->rows);
+    s->base = c.take<float>(s->rows);
+    s->inverse = c.take<float>(s->rows);
     s->factor = c.take<float>(s->rows);
     s->top = c.take<float>(s->parts * s->part_ld);
     s->sum = c.take<float>(s->parts * s->part_ld);
     s->picked = c.take<float>(s->parts * s->part_ld);
+    s->share = c.take<float>(s->parts * s->part_ld);
     s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
     s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
     if (grads) {
@@ -563,16 +565,16 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         const int parts = (int)ceil_div(classes, tile.tm) * tile.wm;
         by_terms(h->type, [&](auto type) {
             using T = decltype(type);
-            const Stats stats{bias, lists, s.top, s.sum, s.picked, s.part_ld, exponent, (int)rows, classes};
+            const Stats stats{bias, lists, s.top, s.sum, s.picked, s.share, s.part_ld, exponent, (int)rows, classes};
             launch_product<T, false, false, true>(g, tile, classes, rows, stats, stream);
-            const RowJoin join{s.top, s.sum, s.picked, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.lse, s.factor, s.kept,
-                               s.undo, teacher->temperature, (int)rows, parts};
+            const RowJoin join{s.top, s.sum, s.picked, s.share, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.base, s.inverse,
+                               s.factor, s.kept, s.undo, teacher->temperature, exponent, (int)rows, parts};
             if (parts <= 64) k_teach_rows<8><<<(unsigned)ceil_div(rows, 32), 256, 0, stream>>>(join);
             else k_teach_rows<32><<<(unsigned)ceil_div(rows, 32), 1024, 0, stream>>>(join);
             if (!grads) return;
             const int64_t term = rows * s.ld;
             auto gradient = [&](auto terms) {
-                const Gradient<T, decltype(terms)::value> e{bias, lists, s.lse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes};
+                const Gradient<T, decltype(terms)::value> e{bias, lists, s.base, s.inverse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes};
                 launch_product<T, false, false, true>(g, tile, classes, rows, e, stream);
             };
             if (s.terms == 1) gradient(std::integral_constant<int, 1>());

@@ -42,3 +42,37 @@ def test_a_class_that_is_named_twice_is_one_class(rows, classes, kind):
     one = torch.ones(rows, 2, dtype=torch.int32, device="cuda")
     loss = P.head_distill(torch.zeros_like(h), W, sure, one, torch.randn(rows, 2, device="cuda"))[0]
     assert float(loss.abs().max()) <= 4 * U
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("classes", [50, 100, 700])
+@pytest.mark.parametrize("size", [1e3, 1e5, 1e7])
+def test_logits_that_share_a_large_part(size, classes, kind):
+    """Logits on a grid far from zero, exact in 32 bits: the softmax is that of their differences, whose size d is all that it is rounded at.  p is off by (C + 64) u + 4 u d
+    of itself, the loss by T^2 (C + K + 64) u (1 + d + log C)."""
+    P = _api()
+    rng = np.random.default_rng(classes)
+    rows, kept = 70, 3
+    h, W, b, eh, eW, eb = _head(rng, rows, 32, classes, TYPES[kind], True)
+    h.copy_((h * 8).round().clamp(-2, 2))  # integers: the logits' differences are, too
+    W.copy_((W * 8).round().clamp(-3, 3))
+    eh, eW = h.double().cpu().numpy(), W.double().cpu().numpy()
+    for equal in (True, False):
+        if equal:
+            h.zero_()
+            eb = np.full(classes, size)
+        else:
+            h.copy_(torch.from_numpy(eh))
+            eb = size + rng.integers(-3, 3, size=classes)
+        b.copy_(torch.from_numpy(eb))
+        at, u = _lists(rng, rows, classes, kept, pad=False)
+        for temperature in (1.0, 2.0):
+            loss, dh, dweight, dbias = _run(P, h, W, b, at, u, temperature=temperature)
+            ref = S.distill(np.zeros_like(eh) if equal else eh, eW, eb, at, u, temperature)
+            z = ref["logits"]
+            d = (z.max(axis=1) - z.min(axis=1)).max()
+            spread = float(u.max() - u.min()) / temperature
+            p, q = ref["soft"], ref["target"]
+            dp = temperature * (p * ((classes + 64) * U + 4 * U * (d + np.log(classes))) + q * ((kept + 16 + 2 * spread) * U)) + 4 * U * np.abs(ref["dz"])
+            hold(dbias, ref["dbias"], (dp + (rows + 64) * U * np.abs(ref["dz"])).sum(axis=0), "dbias")
+            hold(loss, ref["loss"], temperature ** 2 * (classes + kept + 64) * U * (1 + d + spread + np.log(classes)) * np.ones(rows), "loss")
