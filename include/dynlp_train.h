@@ -181,8 +181,8 @@ int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, 
  *                    matrix with data NULL, too).
  * An entry's logit that is not a number, or +infinity, makes its row's loss and gradients so.  Heads as in dynlp_head_scores.
  * Up to 64 classes, and in float32 heads, the gradients are made from all 24 bits of dz.  Of larger heads in 16 bits, dh and a dweight in 16 bits are made from dz
- * rounded to h's type (float16: times a power of two that the largest r gives), with up to 256 rows, or 2^31 rows times dim times classes, to two such terms; a dweight in
- * float32 is made from all of it (float16: 22 bits).
+ * rounded to h's type, with up to 256 rows, or 2^31 rows times dim times classes, to two such terms; a dweight in float32 is made from all of it (float16: 22 bits).  In
+ * float16 what lies below 2^-39 of a row's r is left out of its dh, and what lies below 2^-39 of the largest r of dweight.
  */
 typedef struct dynlp_teacher {
     const int32_t* classes;

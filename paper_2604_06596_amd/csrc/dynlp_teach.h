@@ -328,11 +328,18 @@ struct RowJoin {
     float *base, *inverse;            // the largest logit m, and one over the sum of exp((z - m) / T)
     float* factor;                    // weight times a power of two; 0 where the row is left out
     uint32_t* kept;                   // a bit per row
-    float* undo;                      // one over that power
+    float *undo_row, *ratio;          // where there is `largest`: one over the row's power, and the largest weight's power over it
+    float* undo;                      // one over the largest weight's power
     float temperature, exponent;
     int rows, parts;
 };
-// The parts of 32 rows, by K threads each, in order.  The power of two brings the largest weight to 2^14 .. 2^15, so that float16 holds dz's terms.
+// What brings a weight to 2^14 .. 2^15, so that float16 holds the terms of its row's dz.
+__device__ inline float power_to_15(float weight) {
+    int e;
+    frexpf(weight, &e);
+    return ldexpf(1.f, min(max(15 - e, -120), 120));
+}
+// The parts of 32 rows, by K threads each, in order.
 template <int K>
 __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     __shared__ float tops[K][33], sums[K][33], picks[K][33], shares[K][33];
@@ -355,12 +362,11 @@ __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     for (int p = 1; p < K; ++p) take(tops[p][r], sums[p][r], picks[p][r], shares[p][r]);
     const float weight = g.weight[at];
     const bool use = row < g.rows && weight != 0.f && s != 0.f;
-    float scale = 1.f;
+    float scale = 1.f, own = 1.f;
     if (g.largest) {
-        int e;
         const float most = __uint_as_float(*g.largest);
-        frexpf(most, &e);
-        if (most > 0.f) scale = ldexpf(1.f, min(max(15 - e, -120), 120));
+        if (most > 0.f) scale = power_to_15(most);
+        own = weight != 0.f && fabsf(weight) < INFINITY ? power_to_15(fabsf(weight)) : scale;
     }
     if (blockIdx.x == 0 && r == 0) *g.undo = 1.f / scale;
     const uint32_t bits = (uint32_t)__ballot(use);
@@ -368,7 +374,8 @@ __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     if (row >= g.rows) return;
     g.base[row] = m;
     g.inverse[row] = 1.f / s;
-    g.factor[row] = use ? weight * scale : 0.f;
+    g.factor[row] = use ? weight * own : 0.f;
+    if (g.largest) g.undo_row[row] = 1.f / own, g.ratio[row] = scale / own;
     if (g.loss) {
         const float t = g.temperature, part = g.entropy[row] + (logf(s) - pick / t);
         g.loss[row] = use ? weight * t * t * part : 0.f;
@@ -387,29 +394,47 @@ __device__ inline float half_of(uint32_t pair, int k) {
     return to_float(__builtin_bit_cast(T, (uint16_t)(pair >> (16 * k))));
 }
 
-// dz as 16-bit terms [term][row][ld], and its sums over the rows of a wave's part.
-template <typename T, int TERMS>
+// dz as 16-bit terms [term][row][ld], and its sums over the rows of a wave's part.  Float16 has OWN terms beside them, for what is made row by row: times the row's power of
+// two and not the largest weight's, so that a row of little weight keeps as many digits as any.
+template <typename T, int TERMS, int OWN>
 struct Gradient {
     const float* bias;
     Lists lists;
-    const float *base, *inverse, *factor;
-    uint16_t* dz;
+    const float *base, *inverse, *factor, *ratio;
+    uint16_t *own, *dz;  // each may be NULL
     int64_t ld, term;
     float* sums;  // [part][ld]
     float exponent;
     int rows, classes;
+    // 16 values of a row, as N terms.
+    template <int N>
+    __device__ void put(uint16_t* to, float (&v)[16]) const {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            u32x4 out[2];
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+                const uint32_t pair = pair_of(v[k], v[k + 1], T());
+                out[k / 8][k / 2 & 3] = pair;
+                if (t + 1 < N) v[k] -= half_of<T>(pair, 0), v[k + 1] -= half_of<T>(pair, 1);
+            }
+            u32x4* p = reinterpret_cast<u32x4*>(to + t * term);
+            p[0] = out[0], p[1] = out[1];
+        }
+    }
     template <typename S>
     __device__ void finish(const Wide&, const Place& at, const f32x4 (&acc)[S::NI][S::MI], char* space) const {
         const bool shut = tile_bias<S>(bias, at.tile_m * S::TM, classes, space);
         const float* b = reinterpret_cast<float*>(space) + at.wave_m * (16 * S::MI);
         const WaveLists<S> wave(lists, at, rows, space);
         const int lane_q = lane_id() >> 4, r = lane_id() & 15;
-        float total[S::MI / 4][16], f[S::NI], fp[S::NI], top[S::NI];  // of q, and of exp((z - top) / T)
+        float total[S::MI / 4][16], f[S::NI], fp[S::NI], top[S::NI], to_all[S::NI];  // f: of q; fp: of exp((z - top) / T)
         for (int j = 0; j < S::MI / 4; ++j)
             for (int k = 0; k < 16; ++k) total[j][k] = 0.f;
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
             f[i] = n < rows ? factor[n] : 0.f, fp[i] = n < rows ? inverse[n] * factor[n] : 0.f, top[i] = n < rows ? base[n] : 0.f;
+            if constexpr (OWN > 0) to_all[i] = n < rows ? ratio[n] : 0.f;
         }
         wave_meets();
 #pragma unroll
@@ -432,21 +457,14 @@ struct Gradient {
                 for (int k = 0; k < 16; ++k) v[k] = f[i] != 0.f ? v[k] : 0.f;
                 if (shut)
                     for (int k = 0; k < 16; ++k) v[k] = m + k < classes ? v[k] : 0.f;
-                for (int k = 0; k < 16; ++k) total[j][k] += v[k];
-                if (n < rows && m < ld) {
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) {
-                        u32x4 out[2];
-#pragma unroll
-                        for (int k = 0; k < 16; k += 2) {
-                            const uint32_t pair = pair_of(v[k], v[k + 1], T());
-                            out[k / 8][k / 2 & 3] = pair;
-                            if (t + 1 < TERMS) v[k] -= half_of<T>(pair, 0), v[k + 1] -= half_of<T>(pair, 1);
-                        }
-                        u32x4* to = reinterpret_cast<u32x4*>(dz + t * term + n * ld + m);
-                        to[0] = out[0], to[1] = out[1];
-                    }
+                const bool there = n < rows && m < ld;
+                if constexpr (OWN > 0) {
+                    float x[16];
+                    for (int k = 0; k < 16; ++k) x[k] = v[k], v[k] *= to_all[i];
+                    if (there && own) put<OWN>(own + n * ld + m, x);
                 }
+                for (int k = 0; k < 16; ++k) total[j][k] += v[k];
+                if (there && dz) put<TERMS>(dz + n * ld + m, v);
             }
             if (any) wave.put(i, true);
         }

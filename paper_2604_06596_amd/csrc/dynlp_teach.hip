@@ -392,7 +392,7 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
 
 namespace {
 
-// Terms of dz that dweight is made of: as many as hold 24 bits of it (22 in float16), or one where the gradients are rounded to 16 bits anyway.  One term's rounding errors average
+// Terms of dz that dweight is made of: as many as hold 24 bits of it (22 in float16, and nothing below 2^-39 of the largest weight), or one where the gradients are rounded to 16 bits anyway.  One term's rounding errors average
 // to what the result's own rounding adds where many values of dz make a gradient; with few rows some values decide, and the error was up to 1.56 times that of the
 // rounding alone.  Two terms are used there, and where the products are short beside the launches.
 bool is_small(int64_t rows, int64_t dim, int64_t classes) { return rows <= 256 || (double)rows * (double)dim * (double)classes <= 2147483648.0; }
@@ -406,14 +406,14 @@ int dh_terms(int32_t type, bool small) { return type == DYNLP_FLOAT32 ? 3 : smal
 struct TeachSpace {
     int64_t rows;  // at a time
     int64_t ld;    // of dz
-    uint16_t *h, *weight, *dz;
+    uint16_t *h, *weight, *own, *dz;
     uint32_t *zeros, *largest, *kept;
-    float* undo;
+    float *undo, *undo_row, *ratio;
     Lists lists;
     float *top, *sum, *picked, *share, *base, *inverse, *factor;
     float *bias_part, *part, *dweight;
     int64_t part_ld;   // of top, sum, picked and share
-    int terms, parts;
+    int terms, own_terms, parts;
     bool small;
 };
 
@@ -423,8 +423,9 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     const bool grads = grad_type >= 0;
     s->small = is_small(rows, dim, classes);
     s->terms = dz_terms(type, grad_type, s->small);
+    s->own_terms = type == DYNLP_FLOAT16 ? dh_terms(type, s->small) : 0;
     s->ld = laid_ld(classes);
-    const int64_t most = std::max<int64_t>(kTermsBytes / (s->ld * 2 * s->terms) / 256 * 256, 256);
+    const int64_t most = std::max<int64_t>(kTermsBytes / (s->ld * 2 * (s->terms + s->own_terms)) / 256 * 256, 256);
     s->rows = std::min({rows, most, kMostTeachRows});
     const Tiling t = logits_tiling(classes, s->rows);
     s->parts = (int)ceil_div(classes, t.tm) * t.wm;
@@ -443,6 +444,8 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->base = c.take<float>(s->rows);
     s->inverse = c.take<float>(s->rows);
     s->factor = c.take<float>(s->rows);
+    s->undo_row = s->own_terms ? c.take<float>(s->rows) : nullptr;
+    s->ratio = s->own_terms ? c.take<float>(s->rows) : nullptr;
     s->top = c.take<float>(s->parts * s->part_ld);
     s->sum = c.take<float>(s->parts * s->part_ld);
     s->picked = c.take<float>(s->parts * s->part_ld);
@@ -450,6 +453,7 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
     s->weight = lay_weight ? take_laid(c, classes, dim, type) : nullptr;
     s->h = lay_h ? take_laid(c, s->rows, dim, type) : nullptr;
     if (grads) {
+        s->own = s->own_terms ? c.take<uint16_t>(s->rows * s->ld * s->own_terms) : nullptr;
         s->dz = c.take<uint16_t>(s->rows * s->ld * s->terms);
         const int64_t parts = ceil_div(s->rows, t.tn) * t.wn;
         s->bias_part = c.take<float>((parts + ceil_div(parts, kBiasParts)) * s->ld);
@@ -467,11 +471,11 @@ int64_t teach_space(char* base, int64_t rows, int64_t dim, int64_t classes, int 
 
 // The product to its output.
 template <typename T, bool TA, bool TB, typename O>
-void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, const float* undo, const uint32_t* kept, void* out, int64_t ld, bool add,
-                     hipStream_t stream) {
+void launch_gradient(Wide g, int64_t m, int64_t n, float* part, float alpha, const float* undo, const float* undo_row, const uint32_t* kept, void* out, int64_t ld,
+                     bool add, hipStream_t stream) {
     const Tiling t = gradient_tiling(g, m, n);
     const int64_t parts = split_tiles(&g, t, m, n);
-    const Output<O> to{static_cast<O*>(out), ld, (int)n, (int)m, alpha, undo, kept, add};
+    const Output<O> to{static_cast<O*>(out), ld, (int)n, (int)m, alpha, undo, undo_row, kept, add};
     launch_product<T, TA, TB, sizeof(O) == 2>(g, t, m, n, Store<O>{to, part}, stream);
     if (parts > 0) {
         const int64_t pieces = parts / g.splits / 4;
@@ -568,18 +572,28 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             const Stats stats{bias, lists, s.top, s.sum, s.picked, s.share, s.part_ld, exponent, (int)rows, classes};
             launch_product<T, false, false, true>(g, tile, classes, rows, stats, stream);
             const RowJoin join{s.top, s.sum, s.picked, s.share, s.part_ld, lists.entropy, lists.weight, lists.largest, loss ? loss + row : nullptr, s.base, s.inverse,
-                               s.factor, s.kept, s.undo, teacher->temperature, exponent, (int)rows, parts};
+                               s.factor, s.kept, s.undo_row, s.ratio, s.undo, teacher->temperature, exponent, (int)rows, parts};
             if (parts <= 64) k_teach_rows<8><<<(unsigned)ceil_div(rows, 32), 256, 0, stream>>>(join);
             else k_teach_rows<32><<<(unsigned)ceil_div(rows, 32), 1024, 0, stream>>>(join);
             if (!grads) return;
             const int64_t term = rows * s.ld;
-            auto gradient = [&](auto terms) {
-                const Gradient<T, decltype(terms)::value> e{bias, lists, s.base, s.inverse, s.factor, s.dz, s.ld, term, s.bias_part, exponent, (int)rows, classes};
+            auto gradient = [&](auto terms, auto own) {
+                constexpr int TERMS = decltype(terms)::value, OWN = decltype(own)::value;
+                const bool shared = OWN == 0;  // by dh and dweight
+                const Gradient<T, TERMS, OWN> e{bias,   lists, s.base,      s.inverse, s.factor,  s.ratio, want_h ? s.own : nullptr, want_w || (want_h && shared) ? s.dz : nullptr,
+                                                s.ld,   term,  s.bias_part, exponent,  (int)rows, classes};
                 launch_product<T, false, false, true>(g, tile, classes, rows, e, stream);
             };
-            if (s.terms == 1) gradient(std::integral_constant<int, 1>());
-            else if (s.terms == 2) gradient(std::integral_constant<int, 2>());
-            else if constexpr (!__is_same(T, f16)) gradient(std::integral_constant<int, 3>());
+            using std::integral_constant;
+            if constexpr (__is_same(T, f16)) {
+                if (s.terms == 1) gradient(integral_constant<int, 1>(), integral_constant<int, 1>());
+                else if (s.own_terms == 1) gradient(integral_constant<int, 2>(), integral_constant<int, 1>());
+                else gradient(integral_constant<int, 2>(), integral_constant<int, 2>());
+            } else {
+                if (s.terms == 1) gradient(integral_constant<int, 1>(), integral_constant<int, 0>());
+                else if (s.terms == 2) gradient(integral_constant<int, 2>(), integral_constant<int, 0>());
+                else gradient(integral_constant<int, 3>(), integral_constant<int, 0>());
+            }
             if (dbias) {
                 int64_t parts_n = ceil_div(rows, tile.tn) * tile.wn;
                 float* from = s.bias_part;
@@ -595,13 +609,13 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             if (want_h) {
                 Wide p{};
                 p.a = w.p, p.ld_a = w.ld, p.term_a = w.term, p.m = (int)laid_ld(dim);
-                p.b = s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)rows;
+                p.b = s.own ? s.own : s.dz, p.ld_b = s.ld, p.term_b = 2 * term, p.n = (int)rows;
                 p.k = classes;
                 p.steps = (int)(laid_ld(classes) / kStep);
                 set_pairs(&p, w.terms, dh_terms(h->type, s.small));
                 void* to = static_cast<char*>(dh->data) + row * dh->stride * type_size(dh->type);
                 auto run = [&](auto out) {
-                    launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.part, alpha, s.undo, s.kept, to, dh->stride, false, stream);
+                    launch_gradient<T, true, false, decltype(out)>(p, dim, rows, s.part, alpha, s.own ? nullptr : s.undo, s.undo_row, s.kept, to, dh->stride, false, stream);
                 };
                 if (h->type == DYNLP_FLOAT32) {
                     if constexpr (__is_same(T, bf16)) run(float());
@@ -619,14 +633,14 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
                 p.zeros = s.zeros;
                 set_pairs(&p, x.terms, s.terms);
                 if (dweight->type == DYNLP_FLOAT32) {
-                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, add, stream);
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, nullptr, dweight->data, dweight->stride, add, stream);
                 } else if (s.dweight) {
-                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, s.dweight, dim, add, stream);
+                    launch_gradient<T, true, true, float>(p, dim, classes, s.part, alpha, s.undo, nullptr, nullptr, s.dweight, dim, add, stream);
                     if (row + rows == h->rows)
                         k_round<T><<<(unsigned)std::min<int64_t>(ceil_div((int64_t)classes * dim, kBlock), 16384), kBlock, 0, stream>>>(
                             s.dweight, classes, dim, static_cast<T*>(dweight->data), dweight->stride);
                 } else {
-                    launch_gradient<T, true, true, T>(p, dim, classes, s.part, alpha, s.undo, nullptr, dweight->data, dweight->stride, false, stream);
+                    launch_gradient<T, true, true, T>(p, dim, classes, s.part, alpha, s.undo, nullptr, nullptr, dweight->data, dweight->stride, false, stream);
                 }
             }
         });

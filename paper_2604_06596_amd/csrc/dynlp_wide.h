@@ -266,7 +266,7 @@ __device__ inline void store_some(O* row, int col, int dim, const float (&v)[N])
     }
 }
 
-// What becomes of a product's sums: times alpha (and *scale), rounded to O; rows that are left out are zeros; added to what is there.
+// What becomes of a product's sums: times alpha (and *scale, and the row's own), rounded to O; rows that are left out are zeros; added to what is there.
 template <typename O>
 struct Output {
     O* out;
@@ -274,9 +274,11 @@ struct Output {
     int rows, dim;
     float alpha;
     const float* scale;     // or NULL
+    const float* of_row;    // a factor per row n, or NULL
     const uint32_t* kept;   // a bit per row n, or NULL
     bool add;
     __device__ float factor() const { return scale ? alpha * *scale : alpha; }
+    __device__ float factor(int n, float of_all) const { return of_row ? of_all * of_row[n] : of_all; }
     template <int N>
     __device__ void put(int n, int m, float factor, float (&v)[N]) const {
         const bool zero = kept && !(kept[n >> 5] >> (n & 31) & 1);
@@ -308,11 +310,12 @@ struct Store {
                 }
             return;
         }
-        const float factor = to.factor();
+        const float of_all = to.factor();
 #pragma unroll
         for (int i = 0; i < S::NI; ++i) {
             const int n = at.n0 + 16 * i + r;
             if (n >= to.rows) continue;
+            const float factor = to.factor(n, of_all);
             if constexpr (S::WOVEN) {
 #pragma unroll
                 for (int j = 0; j < S::MI / 4; ++j) {
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(kBlock) void k_wide_join(Wide g, int tm, int tn, co
 #pragma unroll 4
         for (int k = 1; k < g.splits; ++k) sum += *reinterpret_cast<const f32x4*>(p + (int64_t)k * (tm * tn));
         float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-        to.put(n, m, factor, v);
+        to.put(n, m, to.factor(n, factor), v);
     }
 }
 

@@ -76,3 +76,40 @@ def test_logits_that_share_a_large_part(size, classes, kind):
             dp = temperature * (p * ((classes + 64) * U + 4 * U * (d + np.log(classes))) + q * ((kept + 16 + 2 * spread) * U)) + 4 * U * np.abs(ref["dz"])
             hold(dbias, ref["dbias"], (dp + (rows + 64) * U * np.abs(ref["dz"])).sum(axis=0), "dbias")
             hold(loss, ref["loss"], temperature ** 2 * (classes + kept + 64) * U * (1 + d + spread + np.log(classes)) * np.ones(rows), "loss")
+
+
+@pytest.mark.parametrize("rows, dim, classes", [(40, 64, 200), (300, 64, 130000)])
+def test_rows_of_little_weight_in_16_bits(rows, dim, classes):
+    """A row's dh is as exact as with a call to itself.  Weights that are powers of two change no digit of what it is made from: dh is that of weights of 1 times them, wherever
+    float16 holds both without loss."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, torch.float16, False)
+    at, u = _lists(rng, rows, classes, 3, pad=False)
+    r = 2.0 ** -torch.from_numpy(rng.integers(0, 25, size=rows)).cuda().float()
+    r[3] = 1.0
+    for grad in (torch.float16, torch.float32):
+        want = _run(P, h, W, b, at, u, grad_scale=8192.0, dtype=grad)[1].float() * r[:, None]
+        got = _run(P, h, W, b, at, u, grad_scale=8192.0, dtype=grad, row_weight=r)[1].float()
+        normal = want.abs() >= 2.0 ** -14
+        assert float(normal.float().mean()) > 0.5
+        assert torch.equal(got[normal], want[normal])
+
+
+@pytest.mark.parametrize("rows", [40, 200])
+def test_sums_over_rows_of_all_weights_in_16_bits(rows):
+    """dweight and dbias beside the largest weight: what float16 terms leave out is 2^-22 of dz and 2^-39 of that weight."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    h, W, b, eh, eW, eb = _head(rng, rows, 64, 200, torch.float16, False)
+    at, u = _lists(rng, rows, 200, 3, pad=False)
+    r = (2.0 ** -rng.integers(0, 25, size=rows) * rng.random(rows)).astype(np.float32)
+    for grad in ("float16", "float32"):
+        got = _run(P, h, W, b, at, u, row_weight=torch.from_numpy(r).cuda(), grad_scale=4096.0, dtype=TYPES[grad])
+        ref = S.distill(eh, eW, eb, at, u, 1.0, r, 4096.0)
+        bars = _bars(ref, eh, eW, eb, r.astype(np.float64), 1.0, 4096.0, "float32", "float32", u)
+        dz = np.abs(ref["dz"])
+        weight = 4096.0 * r.astype(np.float64)[:, None]
+        for name, value, more in (("loss", got[0], 0.0), ("dh", got[1], (2.0 ** -22 * dz + 2.0 ** -39 * weight) @ np.abs(eW)),
+                                  ("dweight", got[2], (2.0 ** -22 * dz + np.where(dz > 0, 2.0 ** -39 * weight.max(), 0.0)).T @ np.abs(eh)), ("dbias", got[3], 0.0)):
+            hold(value, ref[name], bars[name] + more, name)
