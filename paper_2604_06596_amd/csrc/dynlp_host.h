@@ -115,13 +115,14 @@ struct Carve {
 constexpr int64_t kSharedMemory = 160 * 1024;  // of a CU
 
 // Shared memory beyond 64 KB is to be asked for, once per kernel and device; `done` has a bit per device (those from the 64th on are asked each time).
+// bytes: without the kernel's own arrays.
 template <typename F>
-void allow_shared(F kernel, std::atomic<uint64_t>& done) {
+void allow_shared(F kernel, std::atomic<uint64_t>& done, int64_t bytes = kSharedMemory) {
     int device = 0;
     if (hipGetDevice(&device) != hipSuccess) return;  // the launch will say so
     const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
     if (done.load(std::memory_order_relaxed) & bit) return;
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedMemory) == hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess)
         done.fetch_or(bit, std::memory_order_relaxed);
     else
         (void)hipGetLastError();  // the launch will say so

@@ -16,7 +16,8 @@ constexpr int64_t kMostStride = 1 << 22;              // elements: 32 bits hold 
 constexpr int64_t kLogitsBytes = int64_t(1) << 30;    // of logits in memory at a time (8,192 x 32,768: 776 us, with 256 MB 935)
 constexpr int64_t kTermsBytes = int64_t(4) << 30;     // of dz in memory at a time
 constexpr int64_t kMostTeachRows = 1 << 24;           // at a time: a launch has fewer than 2^32 threads
-static_assert(DYNLP_MAX_WIDE_CLASSES / 256 * 4 <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
+constexpr int64_t kTilesBytes = DYNLP_MAX_WIDE_CLASSES / 256 * 4;  // of shared memory: k_teach_lists counts the entries of each tile, beside arrays of its own
+static_assert(kTilesBytes <= 64 * 1024 && DYNLP_MAX_TOP <= 8 * 16, "k_teach_lists");
 
 // ---- products ---------------------------------------------------------------------------------------------------------
 
@@ -558,12 +559,15 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         lists.largest = scaled ? s.largest : nullptr;
         auto read_lists = [&](auto entries) {
             constexpr int E = decltype(entries)::value;
+            static std::atomic<uint64_t> allowed{0};
+            allow_shared(k_teach_lists<E>, allowed, kTilesBytes);
             k_teach_lists<E><<<(unsigned)ceil_div(rows, kListRows), kBlock, lists.tiles * 4, stream>>>(t, lists, row, rows);
         };
         if (teacher->kept <= 16) read_lists(std::integral_constant<int, 1>());
         else if (teacher->kept <= 32) read_lists(std::integral_constant<int, 2>());
         else if (teacher->kept <= 64) read_lists(std::integral_constant<int, 4>());
         else read_lists(std::integral_constant<int, 8>());
+        CHECK(launched());  // what follows reads at places that the lists give
         const Wide g = logits_product(w, classes, x, rows, dim);
         const Tiling tile = logits_tiling(classes, s.rows);  // of all chunks: its parts have a size
         const int parts = (int)ceil_div(classes, tile.tm) * tile.wm;

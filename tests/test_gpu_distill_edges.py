@@ -113,3 +113,37 @@ def test_sums_over_rows_of_all_weights_in_16_bits(rows):
         for name, value, more in (("loss", got[0], 0.0), ("dh", got[1], (2.0 ** -22 * dz + 2.0 ** -39 * weight) @ np.abs(eW)),
                                   ("dweight", got[2], (2.0 ** -22 * dz + np.where(dz > 0, 2.0 ** -39 * weight.max(), 0.0)).T @ np.abs(eh)), ("dbias", got[3], 0.0)):
             hold(value, ref[name], bars[name] + more, name)
+
+
+def test_the_largest_number_of_classes():
+    """2^22 classes, whose tiles' counts alone take 64 KB of shared memory.  Sums of the softmax: 2,114 roundings one after the other at most (32 values of a lane, two joins of lanes,
+    65,536 parts by 32 threads and those joined), n u of it; products over classes: 131,072 steps, whose roundings are 2^-7 of the sum of magnitudes; dz in two terms."""
+    P = _api()
+    rows, dim, classes, kept = 20, 32, 1 << 22, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.randn(rows, dim, generator=g, device="cuda").to(torch.bfloat16)
+    W = (0.3 * torch.randn(classes, dim, generator=g, device="cuda")).to(torch.bfloat16)
+    at = torch.randint(0, classes, (rows, kept), generator=g, device="cuda", dtype=torch.int32)
+    at[0] = torch.tensor([classes - 1, 0, classes], dtype=torch.int32)
+    u = torch.randn(rows, kept, generator=g, device="cuda")
+    rejected = torch.zeros(1, dtype=torch.int32, device="cuda")
+    loss, dh, dweight, dbias = P.head_distill(h, W, None, at, u, rejected=rejected)
+    assert int(rejected) == 1
+    u = torch.where(at < classes, u, -float("inf")).double()
+    q = torch.softmax(u, 1)
+    z = h.double() @ W.double().t()
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    picked = z.gather(1, at.long().clamp(max=classes - 1))
+    want = torch.where(q > 0, q * (q.log() - picked + lse), 0.0).sum(1)
+    n = 2114 * U
+    assert ((loss.double() - want).abs() <= n + 64 * U * 20).all()
+    p = z.sub_(lse).exp_()
+    sums = p.sum(0)
+    dz = p.scatter_add_(1, at.long().clamp(max=classes - 1), -q)
+    want = dz.sum(0)
+    assert ((dbias.double() - want).abs() <= (2 * n + 128 * U) * sums + 64 * U * dz.abs().sum(0)).all()
+    want = dz @ W.double()
+    assert ((dh.double() - want).abs() <= (2.0 ** -7 + n) * (dz.abs() @ W.double().abs()) + 2.0 ** -8 * want.abs()).all()
+    want = dz.t().contiguous() @ h.double()
+    bar = (2 * n + 2.0 ** -16) * (dz.abs().t().contiguous() @ h.double().abs())
+    assert ((dweight.double() - want).abs() <= bar + U * want.abs()).all()
