@@ -162,7 +162,8 @@ int64_t dynlp_row_scores_workspace(int64_t rows, int32_t classes, int32_t top);
 /*
  * The same of the head's logits z = h W^T + bias, which are not kept: h, weight and bias as in dynlp_head_labels, but of up to DYNLP_MAX_WIDE_CLASSES classes and
  * DYNLP_MAX_WIDE_DIM elements of a row.  A class whose bias is -infinity has that logit whatever h holds.  The logits of float32 heads of more than 64 classes are made
- * from three 16-bit terms of each value, which hold all of it: an infinite element of h or weight makes the logits it meets not a number.
+ * from three 16-bit terms of each value, which hold all of it, but where up to 16 rows are scored: there an infinite element of h or weight makes infinite logits, as it does in
+ * other heads, and otherwise makes the logits it meets not a number (products that 32 bits do not hold may).
  */
 dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_scores* scores, const dynlp_call* call);
 int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, int32_t type);

@@ -15,13 +15,15 @@
 
 namespace dynlp {
 
-// Rows as 16-bit terms with zeros up to ld_out, a multiple of 32.  Bfloat16 terms of 32-bit values are each the nearest to what is left, and hold all 24 bits.
+// Rows as 16-bit terms with zeros up to ld_out, a multiple of 32.  Bfloat16 terms of 32-bit values are each the nearest to what is left, and hold all 24 bits.  An infinite
+// value is not a number there: as a term it would meet the other side's terms one by one, whose signs and zeros are not those of their sum.
 template <typename T>
 __device__ inline void terms_of(float x, uint16_t (&term)[3]) {
+    if (fabsf(x) == INFINITY) x = NAN;
     for (int k = 0; k < 3; ++k) {
         uint16_t b = (uint16_t)bf16_pair(x, 0.f);
         float v = __uint_as_float((uint32_t)b << 16);
-        if (fabsf(v) == INFINITY && fabsf(x) != INFINITY) {  // a value that rounding makes infinite is cut off instead
+        if (fabsf(v) == INFINITY) {  // a value that rounding makes infinite is cut off instead
             b = (uint16_t)(__float_as_uint(x) >> 16);
             v = __uint_as_float((uint32_t)b << 16);
         }

@@ -51,3 +51,29 @@ def test_infinite_probabilities(rows, classes, top):
     keep = torch.arange(rows, device="cuda") != 2
     for a, b in zip(got, want):
         assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("rows", [16, 17, 60, 300])
+def test_infinite_elements_of_heads_in_32_bits(rows):
+    """Up to 16 rows an infinite element makes logits that are infinite, as in the definition; from 17 rows on every logit that it meets is not a number, whatever the
+    other element is, and its row has no scores."""
+    P = _api()
+    rng = np.random.default_rng(rows)
+    classes, dim = 100, 40
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, torch.float32, False)
+    given = torch.full((rows,), 5, dtype=torch.int32, device="cuda")
+    for at in (1.0 + 2.0 ** -9 + 2.0 ** -18, 1.0, 1.0 + 2.0 ** -9, -1.5):  # three terms of one sign, one, two; another sign
+        h[1:, 7], h[2, 7] = 0.5, at
+        W[5, 7] = -float("inf")
+        out = P.head_scores(h, W, b, given=given, top=3)
+        if rows <= 16:
+            fine = [1] + list(range(3, rows)) + ([2] if at > 0 else [])
+            assert torch.isfinite(out.entropy[fine]).all() and (out.log_given[fine] == -float("inf")).all()
+        else:
+            assert torch.isnan(out.entropy).all() and torch.isnan(out.log_given).all() and torch.isnan(out.log_top).all()
+        W[:, 7] = at
+        h[2, 7] = float("inf")
+        out = P.head_scores(h, W, b, given=given, top=3)
+        assert torch.isfinite(out.entropy[3:]).all()
+        if rows > 16 or at > 0:
+            assert torch.isnan(out.entropy[2]) and torch.isnan(out.log_top[2]).all() and out.top[2].tolist() == [0, 1, 2]
