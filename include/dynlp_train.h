@@ -180,7 +180,7 @@ int64_t dynlp_head_scores_workspace(int64_t rows, int32_t dim, int32_t classes, 
  *                    one without an entry whose logit is more than -infinity, and one whose own logits are all -infinity.
  *   loss             rows float32; dh: rows x dim, of h's type; dweight: classes x dim, float32 or of h's type; dbias: classes float32.  Each of the four may be NULL (a
  *                    matrix with data NULL, too).
- * An entry's logit that is not a number, or +infinity, makes its row's loss and gradients so.  Heads as in dynlp_head_scores.
+ * An entry's logit that is not a number, or +infinity, makes its row's loss and dz so, of all classes.  Heads as in dynlp_head_scores.
  * Up to 64 classes, and in float32 heads, the gradients are made from all 24 bits of dz.  Of larger heads in 16 bits, dh and a dweight in 16 bits are made from dz
  * rounded to h's type, with up to 256 rows, or 2^31 rows times dim times classes, to two such terms; a dweight in float32 is made from all of it (float16: 22 bits).  In
  * float16 what lies below 2^-39 of a row's r is left out of its dh, and what lies below 2^-39 of the largest r of dweight.

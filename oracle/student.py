@@ -162,7 +162,7 @@ def distill(h, weight, bias, classes, logits, temperature=1.0, row_weight=None, 
         p = e / total[:, None]
         lse = np.log(total) + top
         loss = entropy + np.where(target != 0.0, target * (lse[:, None] - z), 0.0).sum(axis=1)
-        dz = grad_scale * r[:, None] * temperature * (p - target)
+        dz = grad_scale * r[:, None] * temperature * (np.where(np.isnan(target).any(axis=1, keepdims=True), np.nan, p) - target)
     dz[out] = 0.0
     return {"loss": np.where(out, 0.0, r * temperature ** 2 * loss), "dh": np.where(out[:, None], 0.0, dz @ weight),
             "dweight": dz.T @ np.where(out[:, None], 0.0, h), "dbias": dz.sum(axis=0), "dz": dz, "left_out": out, "target": target, "soft": p,

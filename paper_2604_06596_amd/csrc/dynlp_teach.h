@@ -376,7 +376,8 @@ __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     if (row >= g.rows) return;
     g.base[row] = m;
     g.inverse[row] = 1.f / s;
-    g.factor[row] = use ? weight * own : 0.f;
+    // a list that holds what is no number says nothing of any class
+    g.factor[row] = !use ? 0.f : g.entropy[row] == g.entropy[row] ? weight * own : NAN;
     if (g.largest) g.undo_row[row] = 1.f / own, g.ratio[row] = scale / own;
     if (g.loss) {
         const float t = g.temperature, part = g.entropy[row] + (logf(s) - pick / t);

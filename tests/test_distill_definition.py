@@ -24,3 +24,16 @@ def test_a_class_that_is_named_several_times_has_the_sum_of_its_probabilities(te
         np.testing.assert_allclose(ref[name], once[name], rtol=1e-9, atol=1e-12)
     sure = np.array([-np.inf, 0.0, -np.inf, -np.inf, -np.inf])
     assert abs(S.distill(np.zeros((1, 4)), W, sure, np.array([[1, 1, 1]]), rng.standard_normal((1, 3)))["loss"][0]) < 1e-15
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_a_list_with_what_is_no_number(bad):
+    """Its row's dz is none for every class; others are what they are without it."""
+    rng = np.random.default_rng(1)
+    h, W, b = rng.standard_normal((3, 4)), rng.standard_normal((6, 4)), rng.standard_normal(6)
+    at, u = np.array([[0, 1], [2, 3], [4, 5]]), rng.standard_normal((3, 2))
+    want = S.distill(h, W, b, at, u)
+    u[1, 0] = bad
+    ref = S.distill(h, W, b, at, u)
+    assert np.isnan(ref["dz"][1]).all() and np.isnan(ref["loss"][1]) and np.isnan(ref["dh"][1]).all() and np.isnan(ref["dweight"]).all()
+    np.testing.assert_array_equal(ref["dz"][[0, 2]], want["dz"][[0, 2]])

@@ -147,3 +147,18 @@ def test_the_largest_number_of_classes():
     want = dz.t().contiguous() @ h.double()
     bar = (2 * n + 2.0 ** -16) * (dz.abs().t().contiguous() @ h.double().abs())
     assert ((dweight.double() - want).abs() <= bar + U * want.abs()).all()
+
+
+@pytest.mark.parametrize("classes", [10, 64, 70, 300])
+def test_lists_with_what_is_no_number(classes):
+    """All of the row's gradients are none then, whatever the head's size."""
+    P = _api()
+    rng = np.random.default_rng(classes)
+    h, W, b, eh, eW, eb = _head(rng, 20, 16, classes, torch.float32, False)
+    for bad in (np.nan, np.inf):
+        at, u = _lists(rng, 20, classes, 3, pad=False)
+        u[4, 1] = bad
+        loss, dh, dweight, dbias = _run(P, h, W, b, at, u)
+        keep = np.arange(20) != 4
+        assert torch.isnan(loss[4]) and torch.isnan(dh[4]).all() and torch.isnan(dweight).all() and torch.isnan(dbias).all()
+        assert torch.isfinite(loss[keep]).all() and torch.isfinite(dh[keep]).all()
