@@ -191,7 +191,7 @@ typedef struct dynlp_teacher {
     const float* row_weight;
     int32_t* rejected;
     int32_t kept;
-    float temperature; /* > 0; it, its inverse and its square finite in 32 bits, as is grad_scale times it */
+    float temperature; /* > 0; it, its square and log2(e) over it finite in 32 bits, as is grad_scale times it */
     float grad_scale;
 } dynlp_teacher;
 dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weight, const float* bias, const dynlp_teacher* teacher, float* loss,

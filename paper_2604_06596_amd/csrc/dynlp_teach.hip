@@ -488,7 +488,7 @@ dynlp_status check_teacher(const dynlp_teacher* t, int64_t rows) {
     if (!t) REFUSE("teacher is NULL");
     if (t->kept < 1 || t->kept > DYNLP_MAX_TOP) REFUSE("lists of %d classes: 1 .. %d are possible", t->kept, DYNLP_MAX_TOP);
     if (rows > 0 && (!t->classes || !t->logits)) REFUSE("a teacher without %s", t->classes ? "logits" : "classes");
-    if (!(t->temperature > 0.f) || !std::isfinite(t->temperature) || !std::isfinite(1.f / t->temperature) || !std::isfinite(t->temperature * t->temperature))
+    if (!(t->temperature > 0.f) || !std::isfinite(t->temperature) || !std::isfinite(1.44269504f / t->temperature) || !std::isfinite(t->temperature * t->temperature))
         REFUSE("temperature = %g", t->temperature);
     if (!std::isfinite(t->grad_scale * t->temperature)) REFUSE("grad_scale = %g with temperature = %g", t->grad_scale, t->temperature);
     return DYNLP_OK;

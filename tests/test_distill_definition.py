@@ -37,3 +37,17 @@ def test_a_list_with_what_is_no_number(bad):
     ref = S.distill(h, W, b, at, u)
     assert np.isnan(ref["dz"][1]).all() and np.isnan(ref["loss"][1]) and np.isnan(ref["dh"][1]).all() and np.isnan(ref["dweight"]).all()
     np.testing.assert_array_equal(ref["dz"][[0, 2]], want["dz"][[0, 2]])
+
+
+@pytest.mark.parametrize("temperature", [2.95e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_that_make_powers_of_two_infinite_are_refused(temperature):
+    """Exponents are multiplied by log2(e) / T, which 32 bits do not hold here although they do 1 / T.  No GPU is needed to be refused."""
+    from paper_2604_06596_amd import train as T
+
+    a = 1 << 20
+    L = T._library()
+    assert np.isfinite(np.float32(1.0) / np.float32(temperature))
+    for classes in (10, 100):
+        status = L.dynlp_head_distill(T._Matrix(a, 5, 8, 8, 1), T._Matrix(a << 1, classes, 8, 8, 1), None, T._Teacher(a << 4, a << 5, None, None, 3, temperature, 1.0), a << 6,
+                                      None, None, None, T._Call(None, a << 10, 0))
+        assert status == -1 and ("temperature" in T._lib.dynlp_last_error(None).decode())
