@@ -476,7 +476,8 @@ struct RowList {
         for (int m = 0; m < CT; ++m)
             for (int i = 0; i < 4; ++i) z[m][i] *= t.inverse;
     }
-    __device__ inline float whole(const Teacher& t, float loss) const { return t.square * (entropy + loss); }
+    // T^2 by itself may lie below what 32 bits hold
+    __device__ inline float whole(const Teacher& t, float loss) const { return t.temperature * (t.temperature * (entropy + loss)); }
 };
 
 // From the logits z of row `row` of a lane (first + 16 m + r): its loss is stored, z becomes dz.  Returns whether the row takes part.

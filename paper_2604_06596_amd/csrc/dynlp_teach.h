@@ -381,7 +381,7 @@ __global__ __launch_bounds__(32 * K) void k_teach_rows(RowJoin g) {
     if (g.largest) g.undo_row[row] = 1.f / own, g.ratio[row] = scale / own;
     if (g.loss) {
         const float t = g.temperature, part = g.entropy[row] + (logf(s) - pick / t);
-        g.loss[row] = use ? weight * t * t * part : 0.f;
+        g.loss[row] = use ? weight * (t * (t * part)) : 0.f;  // T^2 by itself may lie below what 32 bits hold
     }
 }
 

@@ -540,7 +540,7 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
         return launched();
     }
     const Teacher t{teacher->classes, teacher->logits, teacher->row_weight, teacher->rejected, teacher->kept, classes, 1.f / teacher->temperature,
-                    teacher->temperature * teacher->temperature};
+                    teacher->temperature};
     if (classes <= DYNLP_MAX_CLASSES) {
         distill_few_classes(*h, *weight, bias, t, teacher->grad_scale * teacher->temperature, loss, want_h ? dh : nullptr, want_w ? dweight : nullptr, dbias, call);
         return launched();

@@ -12,7 +12,7 @@ struct Teacher {
     int32_t* rejected;       // or NULL
     int kept, count;         // of a list; classes of the head
     float inverse;           // 1 / T
-    float square;            // T^2
+    float temperature;       // T
 };
 
 }  // namespace dynlp

@@ -162,3 +162,19 @@ def test_lists_with_what_is_no_number(classes):
         keep = np.arange(20) != 4
         assert torch.isnan(loss[4]) and torch.isnan(dh[4]).all() and torch.isnan(dweight).all() and torch.isnan(dbias).all()
         assert torch.isfinite(loss[keep]).all() and torch.isfinite(dh[keep]).all()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("classes", [50, 100])
+@pytest.mark.parametrize("temperature", [1e-15, 1e-21, 1e-25, 1e-30])
+def test_losses_at_small_temperatures(temperature, classes, kind):
+    """T^2 leaves 32 bits long before T^2 times the divergence does, which is then about T times a difference of logits."""
+    P = _api()
+    rng = np.random.default_rng(classes)
+    h, W, b, eh, eW, eb = _head(rng, 30, 32, classes, TYPES[kind], False)
+    at, u = _lists(rng, 30, classes, 4, pad=False)
+    temperature = float(np.float32(temperature))
+    loss = _run(P, h, W, b, at, u, temperature=temperature, grads=False)[0]
+    ref = S.distill(eh, eW, eb, at, u, temperature)
+    bars = _bars(ref, eh, eW, eb, np.ones(30), temperature, 1.0, kind, "float32", u)
+    hold(loss, ref["loss"], bars["loss"] - 2.0 ** -140 + 2.0 ** -149, "loss")
