@@ -20,10 +20,12 @@ namespace dynlp {
 template <typename T>
 __device__ inline void terms_of(float x, uint16_t (&term)[3]) {
     if (fabsf(x) == INFINITY) x = NAN;
+    bool cut = false;
     for (int k = 0; k < 3; ++k) {
         uint16_t b = (uint16_t)bf16_pair(x, 0.f);
         float v = __uint_as_float((uint32_t)b << 16);
-        if (fabsf(v) == INFINITY) {  // a value that rounding makes infinite is cut off instead
+        if (cut || fabsf(v) == INFINITY) {  // a value that rounding makes infinite is cut off instead, and so is what is left of it: no sum of some terms is beyond x
+            cut = true;
             b = (uint16_t)(__float_as_uint(x) >> 16);
             v = __uint_as_float((uint32_t)b << 16);
         }

@@ -178,3 +178,35 @@ def test_losses_at_small_temperatures(temperature, classes, kind):
     ref = S.distill(eh, eW, eb, at, u, temperature)
     bars = _bars(ref, eh, eW, eb, np.ones(30), temperature, 1.0, kind, "float32", u)
     hold(loss, ref["loss"], bars["loss"] - 2.0 ** -140 + 2.0 ** -149, "loss")
+
+
+@pytest.mark.parametrize("rows", [3, 20, 150])
+def test_large_and_tiny_values_of_wide_heads(rows):
+    """Operands in 32 bits become bfloat16 terms: values that rounding to bfloat16 would make infinite, and those that have no second or third term."""
+    P = _api()
+    classes = 80
+    h = torch.zeros(rows, 3, device="cuda")
+    W = torch.zeros(classes, 3, device="cuda")
+    h[0] = torch.tensor([3.4028234e38, 1.0, 0.0])
+    h[1] = torch.tensor([1e-30, 2.0 ** -100, 1.0])
+    h[2] = torch.tensor([2.0 ** -60, 1.0 + 2.0 ** -20, 3.0])
+    W[:2] = torch.tensor([[1.0, 2.0, 3.0], [-1.0, 0.0, 1.0]])
+    b = torch.full((classes,), -100.0, device="cuda")
+    b[:2] = 0.0
+    at, u = np.ones((rows, 1), dtype=np.int32), np.zeros((rows, 1), dtype=np.float32)
+    r = np.ones(rows, dtype=np.float32)
+    r[0] = 0.0
+    got = _run(P, h, W, b, at, u, row_weight=torch.from_numpy(r).cuda())
+    eh, eW, eb = (x.double().cpu().numpy() for x in (h, W, b))
+    ref = S.distill(eh, eW, eb, at, u, 1.0, r)
+    # the power of two of a logit 87 to 104 below the largest, a denormal number, is 0: each p is off by 2^-126, of up to `rows` and `classes`, times 3 at most of h or W
+    below = 2.0 ** -126 * rows * classes * 3
+    bars = _bars(ref, eh, eW, eb, r.astype(np.float64), 1.0, 1.0, "float32", "float32", u)
+    for name, value in zip(("loss", "dh", "dweight", "dbias"), got):
+        hold(value, ref[name], bars[name] + below, name)
+    # the row of the large value alone: the head is certain of class 0, and its loss is beyond 32 bits
+    r[:] = 0.0
+    r[0] = 1.0
+    loss, dh, dweight, dbias = _run(P, h, W, b, at, u, row_weight=torch.from_numpy(r).cuda())
+    assert float(loss[0]) == float("inf") and dh[0].tolist() == [2.0, 2.0, 2.0] and dbias[:3].tolist() == [1.0, -1.0, 0.0]
+    assert torch.equal(dweight[0], h[0]) and torch.equal(dweight[1], -h[0]) and (dweight[2:] == 0).all() and (dh[1:] == 0).all() and (loss[1:] == 0).all()
