@@ -77,3 +77,92 @@ def test_infinite_elements_of_heads_in_32_bits(rows):
         assert torch.isfinite(out.entropy[3:]).all()
         if rows > 16 or at > 0:
             assert torch.isnan(out.entropy[2]) and torch.isnan(out.log_top[2]).all() and out.top[2].tolist() == [0, 1, 2]
+
+
+@pytest.mark.parametrize("rows", [3, 20, 150])
+def test_large_and_tiny_values_of_wide_heads(rows):
+    """More than 64 classes and 16 rows, where operands in 32 bits become bfloat16 terms: values that rounding to bfloat16 would make infinite, and those that have no
+    second or third term."""
+    P = _api()
+    classes = 80
+    h = torch.zeros(rows, 3, device="cuda")
+    W = torch.zeros(classes, 3, device="cuda")
+    h[0] = torch.tensor([3.4028234e38, 1.0, 0.0])
+    h[1] = torch.tensor([1e-30, 2.0 ** -100, 1.0])
+    h[2] = torch.tensor([2.0 ** -60, 1.0 + 2.0 ** -20, 3.0])
+    W[:2] = torch.tensor([[1.0, 2.0, 3.0], [-1.0, 0.0, 1.0]])
+    W[2] = torch.tensor([2.0 ** 60, 2.0 ** -120, 0.0])
+    b = torch.full((classes,), -100.0, device="cuda")
+    b[:3] = torch.tensor([0.0, 0.0, -float("inf")])
+    z = h.double() @ W.double().t() + b.double()
+    z[:, 2] = -float("inf")
+    z = z.cpu().numpy()
+    out = P.head_scores(h, W, b, top=3)
+    assert out.top[0].tolist()[:1] == [0] and float(out.log_top[0, 0]) == 0.0 and float(out.log_top[0, 1]) < -1e38
+    log_bar, entropy_bar = _bars(z[1:], False)
+    off = 26 * U * (np.abs(h.double().cpu().numpy()[1:]) @ np.abs(W.double().cpu().numpy())[[0, 1]].T).max(axis=1)
+    log_p, entropy, order = S.scores(z[1:])
+    at = np.arange(rows - 1)[:, None]
+    assert np.array_equal(out.top[1:].cpu().numpy(), order[:, :3])
+    hold(out.log_top[1:], log_p[at, order[:, :3]], log_bar[at, order[:, :3]] + 2 * off[:, None], "log_top")
+    hold(out.entropy[1:], entropy, entropy_bar + off * (2 + 2 * np.abs(np.where(np.isfinite(log_p), log_p, 0.0)).max(axis=1)), "entropy")
+
+
+@pytest.mark.parametrize("kind, rows, dim, classes", [("bfloat16", 3000, 32, 131072), ("float32", 2300, 20, 131000), ("float16", 500, 40, 1500000)])
+def test_turns(kind, rows, dim, classes):
+    """More logits than are in memory at a time (1 GiB), a shorter last turn: every row's scores against the definition, on a grid on which logits are exact."""
+    P = _api()
+    from paper_2604_06596_amd import train as T
+
+    rng = np.random.default_rng(rows)
+    assert T._library().dynlp_head_scores_workspace(rows, dim, classes, T._TYPES[TYPES[kind]]) < 4 * rows * classes  # logits of some rows at a time
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, TYPES[kind], True)
+    given = torch.from_numpy(rng.integers(-1, classes, size=(rows, 2)).astype(np.int32)).cuda()
+    out = P.head_scores(h, W, b, given=given, top=4)
+    w64, b64 = W.double().t().contiguous(), b.double()
+    n = (2 * -(-classes // 64) + 64) * U
+    for at in range(0, rows, 100):
+        some = slice(at, at + 100)
+        z = h[some].double() @ w64 + b64
+        order = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :4]
+        assert torch.equal(out.top[some].long(), order)
+        d = z.amax(1, keepdim=True) - z
+        z -= torch.logsumexp(z, 1, keepdim=True)
+        p = z.exp()
+        mean, square, log_s = (p * d).sum(1), (p * d * d).sum(1), -z.amax(1)
+        log_bar = (n + U * mean + 3 * U * log_s)[:, None] + U * (3 * d - 2 * z)
+        g = given[some].long()
+        real = g >= 0
+        for got, want, bar in ((out.log_top[some], z.gather(1, order), log_bar.gather(1, order)),
+                               (out.log_given[some][real], z.gather(1, g.clamp(min=0))[real], log_bar.gather(1, g.clamp(min=0))[real]),
+                               (out.entropy[some], -(p * z).sum(1), n * (2 + 2 * mean) + U * (5 * mean + 4 * square + 4 * log_s))):
+            assert ((got.double() - want).abs() <= bar + U * want.abs()).all(), at
+        assert (out.log_given[some][~real] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [3, 20])
+def test_the_largest_number_of_classes(rows):
+    """2^22 classes, few rows by themselves and a tile of them, on a grid on which logits are exact; the last classes among the first."""
+    P = _api()
+    classes, dim = 1 << 22, 16
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    h = (torch.randint(-8, 9, (rows, dim), generator=g, device="cuda") / 8.0).to(torch.bfloat16)
+    W = (torch.randint(-32, 33, (classes, dim), generator=g, device="cuda") / 64.0).to(torch.bfloat16)
+    b = torch.randint(-64, 65, (classes,), generator=g, device="cuda") / 64.0
+    b[[0, classes - 1]] = 30.0
+    given = torch.tensor([0, classes - 1, classes, -1], dtype=torch.int32, device="cuda").repeat(rows, 1)
+    rejected = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = P.head_scores(h, W, b, given=given, top=128, rejected=rejected)
+    assert int(rejected) == rows and (out.log_given[:, 2:] == 0).all()
+    z = h.double() @ W.double().t() + b.double()
+    order = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :128]
+    assert torch.equal(out.top.long(), order)
+    d = z.amax(1, keepdim=True) - z
+    z -= torch.logsumexp(z, 1, keepdim=True)
+    p = z.exp()
+    n = (2 * classes // 64 + 64) * U
+    mean, square, log_s = (p * d).sum(1), (p * d * d).sum(1), -z.amax(1)
+    log_bar = (n + U * mean + 3 * U * log_s)[:, None] + U * (3 * d - 3 * z)
+    for got, at in ((out.log_top, order), (out.log_given[:, :2], given[:, :2].long())):
+        assert ((got.double() - z.gather(1, at)).abs() <= log_bar.gather(1, at)).all()
+    assert ((out.entropy.double() + (p * z).sum(1)).abs() <= n * (2 + 2 * mean) + U * (6 * mean + 4 * square + 5 * log_s)).all()
