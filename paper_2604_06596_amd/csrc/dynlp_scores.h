@@ -357,7 +357,7 @@ constexpr int row_space(int waves) {
 }
 // WAVES waves for each row; four rows to a workgroup where it is one.
 template <typename T, bool PROB, int P, int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+__global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o) {
     using Scan = RowScan<T, PROB, P>;
     constexpr int kLists = row_lists(WAVES), kSpace = kCandidates + kWave * Scan::E;
     extern __shared__ char space[];
@@ -368,7 +368,6 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
     const int64_t first = WAVES == 1 ? (int64_t)blockIdx.x * kLists + wave : blockIdx.x, step = WAVES == 1 ? (int64_t)gridDim.x * kLists : gridDim.x;
     for (int64_t row = first; row < rows; row += step) {
         const T* p = x + row * ld;
-        const int64_t to = row0 + row;
         RowSums sums = RowSums::none();
         Candidates c;
         c.none(keys + wave * kSpace);
@@ -407,13 +406,13 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
             }
         }
         const RowLog<PROB> log(sums, dim, power);
-        if (threadIdx.x % (WAVES * kWave) == 0 && o.entropy) o.entropy[to] = log.entropy;
+        if (threadIdx.x % (WAVES * kWave) == 0 && o.entropy) o.entropy[row] = log.entropy;
         for (int k = threadIdx.x % (WAVES * kWave); k < o.given; k += WAVES * kWave) {
-            const int g = o.classes[to * o.given + k];
+            const int g = o.classes[row * o.given + k];
             if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
-            o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
+            o.log_given[row * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
         }
-        if (o.top && (WAVES == 1 || wave == 0)) write_top<PROB>(c, o, to, log);
+        if (o.top && (WAVES == 1 || wave == 0)) write_top<PROB>(c, o, row, log);
         if constexpr (WAVES > 1) __syncthreads();
     }
 }
@@ -421,7 +420,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
 // Many rows of up to 64 values, of which up to K classes are asked for: a lane for each row, from a copy of 64 rows in shared memory.  A lane keeps its first
 // K in order, so that a value is compared with K others.  1M rows of 50 probabilities, the first 4: 75 us; with 16 lanes for a row (k_short_scores) 117.
 template <typename T, bool PROB, int K>
-__global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+__global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o) {
     extern __shared__ char space[];
     float* copy = reinterpret_cast<float*>(space);
     const int pitch = dim | 1, lane = threadIdx.x;  // rows begin in different banks
@@ -475,18 +474,18 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
             }
         }
         const RowLog<PROB> log(a, dim, power);
-        const int64_t to = row0 + first + lane;
+        const int64_t row = first + lane;
         if (lane < here) {
-            if (o.entropy) o.entropy[to] = log.entropy;
+            if (o.entropy) o.entropy[row] = log.entropy;
             for (int k = 0; k < o.given; ++k) {
-                const int g = o.classes[to * o.given + k];
+                const int g = o.classes[row * o.given + k];
                 if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
-                o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(mine[g]) : 0.f;
+                o.log_given[row * o.given + k] = g >= 0 && g < dim ? log.of(mine[g]) : 0.f;
             }
             for (int k = 0; k < K; ++k)
                 if (k < o.top) {
-                    if (o.top_classes) o.top_classes[to * o.top + k] = at[k];
-                    if (o.log_top) o.log_top[to * o.top + k] = log.of(value[k]);
+                    if (o.top_classes) o.top_classes[row * o.top + k] = at[k];
+                    if (o.log_top) o.log_top[row * o.top + k] = log.of(value[k]);
                 }
         }
         wave_meets();
@@ -495,7 +494,7 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
 
 // Rows of up to 64 values: 16 lanes for each, four values in a lane.  The first classes are taken one after the other; lane k mod 16 keeps the k-th until 16 are together.
 template <typename T, bool PROB>
-__global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o, int64_t row0) {
+__global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o) {
     const int r = threadIdx.x & 15, col = 4 * r;
     const int64_t step = (int64_t)gridDim.x * (kBlock / 16);
     Columns<T, 4> ahead;
@@ -511,7 +510,7 @@ __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld,
     ask((int64_t)blockIdx.x * (kBlock / 16) + threadIdx.x / 16);
 #pragma unroll 1
     for (int64_t first = (int64_t)blockIdx.x * (kBlock / 16); first < rows; first += step) {
-        const int64_t row = first + threadIdx.x / 16, to = row0 + row;
+        const int64_t row = first + threadIdx.x / 16;
         const bool there = row < rows;
         const T* p = x + min(row, rows - 1) * ld;
         float v[4];
@@ -536,12 +535,12 @@ __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld,
             }
         }
         const RowLog<PROB> log(a, dim, power);
-        if (there && r == 0 && o.entropy) o.entropy[to] = log.entropy;
+        if (there && r == 0 && o.entropy) o.entropy[row] = log.entropy;
         if (there)
             for (int k = r; k < o.given; k += 16) {
-                const int g = o.classes[to * o.given + k];
+                const int g = o.classes[row * o.given + k];
                 if (g >= dim && o.rejected) atomicAdd(o.rejected, 1);
-                o.log_given[to * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
+                o.log_given[row * o.given + k] = g >= 0 && g < dim ? log.of(to_float(p[g])) : 0.f;
             }
         if (o.top == 0) continue;
         uint32_t order[4];
@@ -559,8 +558,8 @@ __global__ __launch_bounds__(kBlock) void k_short_scores(const T* x, int64_t ld,
                 my_class = r == place ? at : my_class;
             }
             if (there && r < here) {
-                if (o.top_classes) o.top_classes[to * o.top + from + r] = (int)my_class;
-                if (o.log_top) o.log_top[to * o.top + from + r] = log.of(value_of((uint64_t)my_order << 32));
+                if (o.top_classes) o.top_classes[row * o.top + from + r] = (int)my_class;
+                if (o.log_top) o.log_top[row * o.top + from + r] = log.of(value_of((uint64_t)my_order << 32));
             }
         }
     }

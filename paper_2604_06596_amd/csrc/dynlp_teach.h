@@ -17,7 +17,6 @@ namespace dynlp {
 
 // Rows as 16-bit terms with zeros up to ld_out, a multiple of 32.  Bfloat16 terms of 32-bit values are each the nearest to what is left, and hold all 24 bits.  An infinite
 // value is not a number there: as a term it would meet the other side's terms one by one, whose signs and zeros are not those of their sum.
-template <typename T>
 __device__ inline void terms_of(float x, uint16_t (&term)[3]) {
     if (fabsf(x) == INFINITY) x = NAN;
     bool cut = false;
@@ -45,8 +44,8 @@ __global__ __launch_bounds__(kBlock) void k_lay_out(const T* in, int64_t ld, int
             u32x4 v[3];
             for (int k = 0; k < 8; k += 2) {
                 uint16_t a[3], b[3];
-                terms_of<T>(col + k < dim ? in[row * ld + col + k] : 0.f, a);
-                terms_of<T>(col + k + 1 < dim ? in[row * ld + col + k + 1] : 0.f, b);
+                terms_of(col + k < dim ? in[row * ld + col + k] : 0.f, a);
+                terms_of(col + k + 1 < dim ? in[row * ld + col + k + 1] : 0.f, b);
                 for (int t = 0; t < 3; ++t) v[t][k / 2] = a[t] | (uint32_t)b[t] << 16;
             }
             for (int t = 0; t < 3; ++t) *reinterpret_cast<u32x4*>(out + t * term + row * ld_out + col) = v[t];

@@ -196,13 +196,13 @@ Scores scores_from(const Scores& s, int64_t row) {
 }
 
 template <typename T, bool PROB>
-void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& o, int64_t row0, hipStream_t stream) {
+void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& o, hipStream_t stream) {
     auto scan = [&](auto pieces, auto waves) {
         constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
         const int64_t blocks = W == 1 ? ceil_div(rows, kBlock / kWave) : rows;
         static std::atomic<uint64_t> allowed{0};
         allow_shared(k_row_scores<T, PROB, P, W>, allowed);
-        k_row_scores<T, PROB, P, W><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), W == 1 ? kBlock : W * kWave, row_space<T>(W), stream>>>(x, ld, rows, dim, o, row0);
+        k_row_scores<T, PROB, P, W><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), W == 1 ? kBlock : W * kWave, row_space<T>(W), stream>>>(x, ld, rows, dim, o);
     };
     using std::integral_constant;
     constexpr int E = Piece<T>::n, most = 32 / E;  // pieces of a lane: 2,048 values of a wave
@@ -210,13 +210,13 @@ void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& 
     // a lane for each row pays once there are rows for a wave on each of the 1,024 SIMDs
     auto lanes = [&](auto first) {
         constexpr int K = decltype(first)::value;
-        k_lane_scores<T, PROB, K><<<(unsigned)std::min<int64_t>(ceil_div(rows, kWave), 1 << 20), kWave, kWave * (dim | 1) * 4, stream>>>(x, ld, rows, dim, o, row0);
+        k_lane_scores<T, PROB, K><<<(unsigned)std::min<int64_t>(ceil_div(rows, kWave), 1 << 20), kWave, kWave * (dim | 1) * 4, stream>>>(x, ld, rows, dim, o);
     };
     const bool many = dim <= 64 && rows >= 1024 * kWave;
     if (many && o.top <= 2) lanes(integral_constant<int, 2>());
     else if (many && o.top <= 4) lanes(integral_constant<int, 4>());
     else if (many && o.top <= 8) lanes(integral_constant<int, 8>());
-    else if (dim <= 64) k_short_scores<T, PROB><<<(unsigned)std::min<int64_t>(ceil_div(rows, kBlock / 16), 2048), kBlock, 0, stream>>>(x, ld, rows, dim, o, row0);
+    else if (dim <= 64) k_short_scores<T, PROB><<<(unsigned)std::min<int64_t>(ceil_div(rows, kBlock / 16), 2048), kBlock, 0, stream>>>(x, ld, rows, dim, o);
     else if (need == 1) scan(integral_constant<int, 1>(), integral_constant<int, 1>());
     else if (need == 2) scan(integral_constant<int, 2>(), integral_constant<int, 1>());
     else if (dim <= 1024 && most > 4) scan(integral_constant<int, 4>(), integral_constant<int, 1>());
@@ -331,8 +331,8 @@ dynlp_status dynlp_row_scores(const dynlp_matrix* x, int32_t probabilities, cons
     auto run = [&](auto type) {
         using T = decltype(type);
         const T* p = static_cast<const T*>(x->data);
-        if (probabilities) launch_scores<T, true>(p, x->stride, x->rows, x->dim, o, 0, stream);
-        else launch_scores<T, false>(p, x->stride, x->rows, x->dim, o, 0, stream);
+        if (probabilities) launch_scores<T, true>(p, x->stride, x->rows, x->dim, o, stream);
+        else launch_scores<T, false>(p, x->stride, x->rows, x->dim, o, stream);
     };
     if (x->type == DYNLP_FLOAT32) run(float());
     else if (x->type == DYNLP_BFLOAT16) run(bf16());
