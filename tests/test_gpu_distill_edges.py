@@ -164,6 +164,7 @@ def test_lists_with_what_is_no_number(classes):
         assert torch.isfinite(loss[keep]).all() and torch.isfinite(dh[keep]).all()
 
 
+@pytest.mark.filterwarnings("ignore::RuntimeWarning")  # bars of gradients, which are not looked at
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("classes", [50, 100])
 @pytest.mark.parametrize("temperature", [1e-15, 1e-21, 1e-25, 1e-30])
@@ -210,3 +211,85 @@ def test_large_and_tiny_values_of_wide_heads(rows):
     loss, dh, dweight, dbias = _run(P, h, W, b, at, u, row_weight=torch.from_numpy(r).cuda())
     assert float(loss[0]) == float("inf") and dh[0].tolist() == [2.0, 2.0, 2.0] and dbias[:3].tolist() == [1.0, -1.0, 0.0]
     assert torch.equal(dweight[0], h[0]) and torch.equal(dweight[1], -h[0]) and (dweight[2:] == 0).all() and (dh[1:] == 0).all() and (loss[1:] == 0).all()
+
+
+@pytest.mark.parametrize("kind, grad, rows", [("float16", "float16", 16001), ("float16", "float32", 16001), ("bfloat16", "float32", 16001), ("float32", "float32", 11003)])
+def test_turns_of_all_types(kind, grad, rows):
+    """More of dz than is in memory at a time (4 GiB), a shorter last turn: rows are those of calls that are done at once, sums over rows the sum of theirs.  Weights of
+    the first half are far below those of the second, so that the turns' powers of two differ."""
+    P = _api()
+    classes, dim, kept = 70000, 32, 3
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    dtype = TYPES[kind]
+    h = torch.randn(rows, dim, generator=g, device="cuda").to(dtype)
+    W = (0.3 * torch.randn(classes, dim, generator=g, device="cuda")).to(dtype)
+    b = torch.randn(classes, generator=g, device="cuda")
+    at = torch.randint(-1, classes + 1, (rows, kept), generator=g, device="cuda", dtype=torch.int32)
+    u = torch.randn(rows, kept, generator=g, device="cuda")
+    r = torch.rand(rows, generator=g, device="cuda") + 0.5
+    r[torch.rand(rows, generator=g, device="cuda") < 0.1] = 0.0
+    r[:rows // 2] *= 2.0 ** -9
+    rejected = torch.zeros(1, dtype=torch.int32, device="cuda")
+    loss, dh, dweight, dbias = P.head_distill(h, W, b, at, u, row_weight=r, grad_scale=64.0, dtype=TYPES[grad], rejected=rejected)
+    assert int(rejected) == int((at == classes).sum())
+    third = -(-rows // 3)
+    parts = [P.head_distill(h[s], W, b, at[s], u[s], row_weight=r[s], grad_scale=64.0, dtype=torch.float32) for s in (slice(k, min(k + third, rows)) for k in range(0, rows, third))]
+    assert torch.equal(loss, torch.cat([x[0] for x in parts]))
+    # the same dz in the same terms; the order of its sums, of up to 70,000 products with |W| up to 1.5, is what the tiles give: 2^-16 of the row's weight beside a rounding
+    want = torch.cat([x[1] for x in parts]).double()
+    step = {"float32": U, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+    assert ((dh.double() - want).abs() <= 2 * step[kind] * want.abs() + 2.0 ** -15 * 64.0 * r[:, None] + 2.0 ** -24).all()
+    assert (dh[r == 0] == 0).all()
+    for got, want, error in ((dweight.double(), sum(x[2].double() for x in parts), step[grad] + (2.0 ** -16 if grad == "float32" else step[kind])),
+                             (dbias.double(), sum(x[3].double() for x in parts), 2.0 ** -16)):
+        assert float((got - want).norm() / want.norm()) <= error
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_calls_on_two_streams_at_once(kind):
+    """Each with a workspace of its own, over and over, none waiting for the other: the same bits as alone."""
+    P = _api()
+    rng = np.random.default_rng(12)
+    sets = []
+    for rows, classes in ((700, 1500), (90, 5000)):
+        h, W, b, *_ = _head(rng, rows, 64, classes, TYPES[kind], False)
+        at, u = (torch.from_numpy(x).cuda() for x in _lists(rng, rows, classes, 8))
+        sets.append((h, W, b, at, u))
+    call = lambda s: (*P.head_distill(*s), *P.head_scores(*s[:3], given=s[3], top=9), *P.row_scores(s[4], top=3)[1:])  # noqa: E731
+    want = [call(s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(8):
+        for s, stream in zip(sets, streams):
+            with torch.cuda.stream(stream):
+                got.append(call(s))
+    torch.cuda.synchronize()
+    for k, outs in enumerate(got):
+        for a, c in zip(outs, want[k % 2]):
+            assert torch.equal(a, c), k
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_a_batch_with_padding(kind):
+    """A buffer of more rows than there are: rows behind the last one, whose lists are empty or whose weight is 0, change nothing, whatever they hold."""
+    P = _api()
+    rng = np.random.default_rng(13)
+    for rows, classes in ((45, 30), (45, 90), (300, 1000)):
+        h, W, b, eh, eW, eb = _head(rng, rows, 48, classes, TYPES[kind], False)
+        at, u = _lists(rng, rows, classes, 4, pad=False)
+        r = rng.random(rows).astype(np.float32) + 0.5
+        ref = S.distill(eh, eW, eb, at, u, 1.0, r)
+        bars = _bars(ref, eh, eW, eb, r.astype(np.float64), 1.0, 1.0, kind, "float32", u)
+        more = 83
+        big = torch.full((rows + more, 48), float("nan"), dtype=TYPES[kind], device="cuda")
+        big[:rows] = h
+        at = np.concatenate([at, np.full((more, 4), -1, dtype=np.int32)])
+        at[rows + 40:] = 3
+        u = np.concatenate([u, np.full((more, 4), np.nan, dtype=np.float32)])
+        r = np.concatenate([r, np.ones(more, dtype=np.float32)])
+        r[rows + 40:] = 0.0
+        loss, dh, dweight, dbias = _run(P, big, W, b, at, u, row_weight=torch.from_numpy(r).cuda())
+        assert (loss[rows:] == 0).all() and (dh[rows:] == 0).all()
+        for name, value in (("loss", loss[:rows]), ("dh", dh[:rows]), ("dweight", dweight), ("dbias", dbias)):
+            hold(value, ref[name], bars[name], name)
