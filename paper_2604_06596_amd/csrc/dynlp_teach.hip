@@ -222,9 +222,10 @@ void launch_scores(const T* x, int64_t ld, int64_t rows, int dim, const Scores& 
     else if (need == 2) scan(integral_constant<int, 2>(), integral_constant<int, 1>());
     else if (dim <= 1024 && most > 4) scan(integral_constant<int, 4>(), integral_constant<int, 1>());
     else if (dim <= 2048) scan(integral_constant<int, most>(), integral_constant<int, 1>());
-    // a wave's search for a threshold and its last cuts cost as much as some 10,000 values: one wave for a row where there are rows enough (54,734 x 7,308 float16: 284 us,
-    // with four 554; 4,099 x 100,003 bfloat16: 239 and 266; 4,105 x 97,420 float32, which memory bounds: 360 and 310)
-    else if (rows >= 16384 || (sizeof(T) == 2 && rows >= 4096)) scan(integral_constant<int, most>(), integral_constant<int, 1>());
+    // a wave's search for a threshold and its last cuts cost as much as some 10,000 values: one wave for a row where that makes two for each of the 1,024 SIMDs.  us with
+    // one and with four, the first 32: 1,024 rows of 5,000 bfloat16 21 and 19, of 100,003 120 and 80, float32 114 and 87; 2,048 rows 23 and 32, 140 and 147, 157 and 160; 4,099
+    // rows 31 and 54, 187 and 242, 297 and 301; 16,400 rows of 20,011 bfloat16 197 and 350, float32 247 and 287
+    else if (rows >= 2048) scan(integral_constant<int, most>(), integral_constant<int, 1>());
     else if (rows > 512) scan(integral_constant<int, most>(), integral_constant<int, 4>());
     else scan(integral_constant<int, most>(), integral_constant<int, 16>());
 }

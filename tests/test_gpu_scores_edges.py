@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-PATHS = [(65536 + 5, 50, 4), (40, 50, 4), (40, 50, 20), (5, 3, 1), (40, 300, 5), (40, 1500, 70), (600, 3001, 5), (9, 9000, 5)]  # a lane, 16 lanes, 1, 4 and 16 waves for a row
+PATHS = [(65536 + 5, 50, 4), (40, 50, 4), (40, 50, 20), (5, 3, 1), (40, 300, 5), (40, 1500, 70), (600, 3001, 5), (9, 9000, 5), (2050, 4100, 40)]  # a lane, 16 lanes, 1, 4, 16 waves and 1 for a row
 
 
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
@@ -166,3 +166,38 @@ def test_the_largest_number_of_classes(rows):
     for got, at in ((out.log_top, order), (out.log_given[:, :2], given[:, :2].long())):
         assert ((got.double() - z.gather(1, at)).abs() <= log_bar.gather(1, at)).all()
     assert ((out.entropy.double() + (p * z).sum(1)).abs() <= n * (2 + 2 * mean) + U * (6 * mean + 4 * square + 5 * log_s)).all()
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16", "probabilities"])
+@pytest.mark.parametrize("rows, classes, top, given", [(2048, 2049, 128, 1), (2050, 5003, 9, 2), (2047, 5003, 32, 0)])
+def test_many_long_rows(rows, classes, top, given, kind):
+    """A wave for each row that takes several turns through it (2,047 rows: four waves): equal values, rising and falling ones, masks, rows of nothing."""
+    P = _api()
+    g = torch.Generator(device="cuda").manual_seed(rows + classes)
+    probabilities = kind == "probabilities"
+    dtype = TYPES.get(kind, torch.float32)
+    x = 3.0 * torch.randn(rows, classes, generator=g, device="cuda")
+    at = torch.arange(classes, device="cuda").float()
+    x[0], x[1], x[2] = 0.0, at / 64.0, -at / 64.0
+    x[3] = torch.where(at > classes - 300, 5.0 + at % 7, -1.0)
+    x[4] = at * 7 % 5
+    if probabilities:
+        x = torch.softmax(x, 1)
+        x[5] = 0.0
+    else:
+        x[5:300, classes // 3:classes // 2] = -float("inf")
+        x[6] = -float("inf")
+        x[7, :-1] = -float("inf")
+    wide = torch.zeros(rows, classes + 3, dtype=dtype, device="cuda")
+    wide[:, :classes] = x.to(dtype)
+    t = wide[:, :classes]
+    ids = torch.randint(-1, classes, (rows, given), generator=g, device="cuda", dtype=torch.int32) if given else None
+    out = P.row_scores(t, given=ids, top=top, probabilities=probabilities)
+    some = np.concatenate([np.arange(310), np.arange(310, rows, 29), [rows - 1]])
+    e = t[torch.from_numpy(some).cuda()].double().cpu().numpy()
+    keep = some != 5 if probabilities else np.ones(len(some), bool)  # a row of zeros has bars of no size
+    pick = torch.from_numpy(some[keep]).cuda()
+    _check(type(out)(None if ids is None else out.log_given[pick], out.entropy[pick], out.top[pick], out.log_top[pick]), e[keep], probabilities,
+           None if ids is None else ids[pick].cpu().numpy(), top)
+    if probabilities:
+        assert out.top[5].tolist() == list(range(top)) and torch.allclose(out.entropy[5], torch.tensor(float(np.log(classes)), device="cuda"), rtol=4 * U, atol=0)
