@@ -293,3 +293,29 @@ def test_a_batch_with_padding(kind):
         assert (loss[rows:] == 0).all() and (dh[rows:] == 0).all()
         for name, value in (("loss", loss[:rows]), ("dh", dh[:rows]), ("dweight", dweight), ("dbias", dbias)):
             hold(value, ref[name], bars[name], name)
+
+
+@pytest.mark.parametrize("rows, dim, classes", [(100, 32, 300), (300, 40, 200000)])
+def test_float16_gradients_one_at_a_time(rows, dim, classes):
+    """dh has terms of its own there: each gradient by itself is what it is with the others, in one term and in two."""
+    from paper_2604_06596_amd import train as T
+
+    P = _api()
+    rng = np.random.default_rng(14)
+    L = T._library()
+    h, W, b, *_ = _head(rng, rows, dim, classes, torch.float16, False)
+    at, u = (torch.from_numpy(x).cuda() for x in _lists(rng, rows, classes, 4))
+    r = 2.0 ** -torch.from_numpy(rng.integers(0, 12, size=rows)).cuda().float()
+    m, w = T._matrix(h, "h", h.device), T._matrix(W, "W", h.device)
+    t = T._Teacher(at.data_ptr(), u.data_ptr(), r.data_ptr(), None, 4, 1.0, 512.0)
+    for dtype in (torch.float16, torch.float32):
+        _, dh, dweight, dbias = P.head_distill(h, W, b, at, u, row_weight=r, grad_scale=512.0, dtype=dtype)
+        outs = [torch.full((rows + 1, dim), 7.0, dtype=torch.float16, device="cuda"), torch.full((classes + 1, dim), 7.0, dtype=dtype, device="cuda"),
+                torch.full((classes + 1,), 7.0, device="cuda")]
+        for which in range(3):
+            grad = T._TYPES[dtype]
+            call, space = T._call(h.device, L.dynlp_head_distill_workspace(rows, dim, classes, 4, m.type, grad))
+            T._check(L.dynlp_head_distill(m, w, b.data_ptr(), t, None, T._Matrix(outs[0].data_ptr(), rows, dim, dim, m.type) if which == 0 else None,
+                                          T._Matrix(outs[1].data_ptr(), classes, dim, dim, grad) if which == 1 else None, outs[2].data_ptr() if which == 2 else None, call))
+            value, want = outs[which], (dh, dweight, dbias)[which]
+            assert torch.equal(value[:-1], want) and (value[-1] == 7).all()
