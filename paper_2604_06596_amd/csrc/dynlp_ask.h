@@ -3,9 +3,9 @@
 // Up to 64 classes: logits and what they say, in registers (k_few_scores).  More: a product makes logits (k_wide, or k_thin_logits for up to 16 rows) and leaves with them
 // what each group of classes of a row adds to its sums, and its largest logit.  The k-th largest of these is not above the row's k-th largest logit, so
 // that k_group_scores looks at some k groups of a row again and not at all of it.
-// What bounds it: 8,192 x 1,024 bfloat16, 32,768 classes: 752 us, the product some 685 of them (800 TFLOP/s with 1.07 GB of logits stored; without stores and sums
-// 930).
-// 64 x 1,024, 131,072 classes: 80 us: the head once, 63 (4.3 TB/s), the groups 16, a wave for each row.  20,011 x 200 float16, 29 classes: 15 us, the host's call; 9 on the GPU.
+// What bounds it: 8,192 x 1,024 bfloat16, 32,768 classes: 756 us in two turns, whose products take 693 (770 TFLOP/s with 1.04 GB of logits stored; without stores and sums 930)
+// and 39 (256 rows), the groups 48 and 16.
+// 64 x 1,024, 131,072 classes: 78 us: the head once, 63 (4.3 TB/s), the groups 16, a wave for each row.  20,011 x 200 float16, 29 classes: 15 us, the host's call; 9 on the GPU.
 #pragma once
 
 #include "dynlp_head.h"

@@ -4,7 +4,7 @@
 // Of rows of probabilities, which need not sum to one: s = sum x, t = sum x log x:     log p = log x - log s,   entropy = log s - t / s.
 // Classes are ordered by a key of 64 bits: the value's order above the class's, so that keys differ and of equal values the lowest class is the first.
 // What bounds it: 4,099 x 100,003 bfloat16, the first 32: 185 us (4.4 TB/s, a copy 4.7), one pass over the rows with a threshold that some k values pass (k searches through
-// a row: 16,969).  1M x 50 float32 probabilities, the first 4: 75 us (3.2 TB/s), half of it arithmetic: the logarithms and 20 operations a value for the order.
+// a row: 16,969).  1M x 50 float32 probabilities, the first 4: 75 us (3.1 TB/s), half of it arithmetic: the logarithms and 20 operations a value for the order.
 #pragma once
 
 #include "dynlp_matrix.h"

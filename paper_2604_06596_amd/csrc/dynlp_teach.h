@@ -5,8 +5,8 @@
 // Logits do not go through memory: the product h W^T is made twice, for the sums of the softmax and again for dz, of which 16-bit terms are stored for the products
 // with W and h (k_wide, classes as its fast index m, rows as n).  A head's own rounding needs one term (rounding dz once more, to 2^-9 of it on average, adds as much as the
 // result's own rounding: 0.0023 of dh's norm where it alone is 0.0017; two are used in small calls, where few values decide); dweight in 32 bits takes as many as hold dz.
-// What bounds it: the four products, 8 rows classes dim operations where 6 cannot be done without.  8,192 x 1,024 bfloat16, 50,021 classes: 3.72 ms: sums 926 us, dz 997
-// (837 each without what follows the product), dh 788, dweight 958.  Logits kept in 32 bits between the first two would move 10 bytes each at some 5 TB/s, which
+// What bounds it: the four products, 8 rows classes dim operations where 6 cannot be done without.  8,192 x 1,024 bfloat16, 50,021 classes: 3.76 ms: sums 905 us, dz 998
+// (837 each without what follows the product), dh 764, dweight 935; in float16, whose dh has terms of its own, 4% more.  Logits kept in 32 bits between the first two would move 10 bytes each at some 5 TB/s, which
 // is a second product's time at dim = 1,000.
 #pragma once
 
@@ -105,7 +105,7 @@ __device__ inline float over_16(float v, bool sum) {
 }
 
 // 16 rows to a workgroup, 16 lanes and E entries in each lane for a row.  8,192 rows of 32: 8 us.  Ordered, an epilogue reads the few entries of its own 16 rows and classes
-// (8,192 x 50,021: sums 1,202 us and dz 1,277 with a search through all of a row's, 949 and 1,035 so).
+// (8,192 x 50,021: sums 1,202 us and dz 1,277 with a search through all of a row's, 949 and 1,035 so when that was done).
 template <int E>
 __global__ __launch_bounds__(kBlock) void k_teach_lists(Teacher t, Lists out, int64_t row0, int64_t rows) {
     extern __shared__ char space[];
