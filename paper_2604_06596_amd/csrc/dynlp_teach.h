@@ -6,8 +6,8 @@
 // with W and h (k_wide, classes as its fast index m, rows as n).  A head's own rounding needs one term (rounding dz once more, to 2^-9 of it on average, adds as much as the
 // result's own rounding: 0.0023 of dh's norm where it alone is 0.0017; two are used in small calls, where few values decide); dweight in 32 bits takes as many as hold dz.
 // What bounds it: the four products, 8 rows classes dim operations where 6 cannot be done without.  8,192 x 1,024 bfloat16, 50,021 classes: 3.76 ms: sums 905 us, dz 998
-// (837 each without what follows the product), dh 764, dweight 935; in float16, whose dh has terms of its own, 4% more.  Logits kept in 32 bits between the first two would move 10 bytes each at some 5 TB/s, which
-// is a second product's time at dim = 1,000.
+// (837 each without what follows the product), dh 764, dweight 935; in float16, whose dh has terms of its own, 4% more.
+// Logits kept in 32 bits between the first two would move 10 bytes each at some 5 TB/s, which is a second product's time at dim = 1,000.
 #pragma once
 
 #include "dynlp_teacher.h"

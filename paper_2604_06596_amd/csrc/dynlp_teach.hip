@@ -395,9 +395,9 @@ dynlp_status dynlp_head_scores(const dynlp_matrix* h, const dynlp_matrix* weight
 
 namespace {
 
-// Terms of dz that dweight is made of: as many as hold 24 bits of it (22 in float16, and nothing below 2^-39 of the largest weight), or one where the gradients are rounded to 16 bits anyway.  One term's rounding errors average
-// to what the result's own rounding adds where many values of dz make a gradient; with few rows some values decide, and the error was up to 1.56 times that of the
-// rounding alone.  Two terms are used there, and where the products are short beside the launches.
+// Terms of dz that dweight is made of: as many as hold 24 bits of it (22 in float16, and nothing below 2^-39 of the largest weight), or one where the gradients are rounded to
+// 16 bits anyway.  One term's rounding errors average to what the result's own rounding adds where many values of dz make a gradient; with few rows some values decide, and the
+// error was up to 1.56 times that of the rounding alone.  Two terms are used there, and where the products are short beside the launches.
 bool is_small(int64_t rows, int64_t dim, int64_t classes) { return rows <= 256 || (double)rows * (double)dim * (double)classes <= 2147483648.0; }
 int dz_terms(int32_t type, int32_t grad_type, bool small) {
     if (type != DYNLP_FLOAT32 && grad_type != DYNLP_FLOAT32) return small ? 2 : 1;
@@ -586,8 +586,8 @@ dynlp_status dynlp_head_distill(const dynlp_matrix* h, const dynlp_matrix* weigh
             auto gradient = [&](auto terms, auto own) {
                 constexpr int TERMS = decltype(terms)::value, OWN = decltype(own)::value;
                 const bool shared = OWN == 0;  // by dh and dweight
-                const Gradient<T, TERMS, OWN> e{bias,   lists, s.base,      s.inverse, s.factor,  s.ratio, want_h ? s.own : nullptr, want_w || (want_h && shared) ? s.dz : nullptr,
-                                                s.ld,   term,  s.bias_part, exponent,  (int)rows, classes};
+                const Gradient<T, TERMS, OWN> e{bias, lists, s.base, s.inverse, s.factor, s.ratio, want_h ? s.own : nullptr, want_w || (want_h && shared) ? s.dz : nullptr, s.ld, term,
+                                                s.bias_part, exponent, (int)rows, classes};
                 launch_product<T, false, false, true>(g, tile, classes, rows, e, stream);
             };
             using std::integral_constant;
