@@ -418,7 +418,8 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * kWave) void k_row_sco
 }
 
 // Many rows of up to 64 values, of which up to K classes are asked for: a lane for each row, from a copy of 64 rows in shared memory.  A lane keeps its first
-// K in order, so that a value is compared with K others.  1M rows of 50 probabilities, the first 4: 75 us; with 16 lanes for a row (k_short_scores) 117.
+// K in order, so that a value is compared with K others.  1M rows of 50, the first 4: probabilities 75 us, logits 77, in 16 bits 69; with 16 lanes for a row (k_short_scores) 173, 166
+// and 150; 70,000 rows of 10, the first 2: 15.5 and 16.5.
 template <typename T, bool PROB, int K>
 __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, int64_t rows, int dim, Scores o) {
     extern __shared__ char space[];
@@ -430,10 +431,17 @@ __global__ __launch_bounds__(kWave) void k_lane_scores(const T* x, int64_t ld, i
         const int here = (int)min(rows - first, (int64_t)kWave);
         constexpr int kAhead = 16;
         for (int from = 0; from < here; from += kAhead) {
-            T v[kAhead];
-            for (int k = 0; k < kAhead; ++k) v[k] = p[min(from + k, here - 1) * ld + min(lane, dim - 1)];
+            uint32_t v[kAhead];  // bits: as values of 16 bits two would share a register, and each load wait for the one before it
+            for (int k = 0; k < kAhead; ++k) {
+                const T one = p[min(from + k, here - 1) * ld + min(lane, dim - 1)];
+                if constexpr (sizeof(T) == 2) v[k] = __builtin_bit_cast(uint16_t, one);
+                else v[k] = __float_as_uint(one);
+            }
             for (int k = 0; k < kAhead; ++k)
-                if (lane < dim) copy[min(from + k, here - 1) * pitch + lane] = to_float(v[k]);
+                if (lane < dim) {
+                    if constexpr (sizeof(T) == 2) copy[min(from + k, here - 1) * pitch + lane] = to_float(__builtin_bit_cast(T, (uint16_t)v[k]));
+                    else copy[min(from + k, here - 1) * pitch + lane] = __uint_as_float(v[k]);
+                }
         }
         wave_meets();
         const float* mine = copy + min(lane, here - 1) * pitch;
