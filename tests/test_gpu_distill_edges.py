@@ -319,3 +319,51 @@ def test_float16_gradients_one_at_a_time(rows, dim, classes):
                                           T._Matrix(outs[1].data_ptr(), classes, dim, dim, grad) if which == 1 else None, outs[2].data_ptr() if which == 2 else None, call))
             value, want = outs[which], (dh, dweight, dbias)[which]
             assert torch.equal(value[:-1], want) and (value[-1] == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float32"])
+def test_rows_that_lie_far_apart(kind):
+    """Strides of more than 2^22 elements, of inputs and outputs: offsets within a tile of rows pass 32 bits."""
+    from paper_2604_06596_amd import train as T
+
+    P = _api()
+    rng = np.random.default_rng(15)
+    rows, dim, classes, stride = 140, 64, 90, (1 << 22) + (1 << 20) + 8
+    h, W, b, *_ = _head(rng, rows, dim, classes, TYPES[kind], False)
+    at, u = (torch.from_numpy(x).cuda() for x in _lists(rng, rows, classes, 4))
+    want = P.head_distill(h, W, b, at, u, dtype=TYPES[kind])
+    scores = P.head_scores(h, W, b, top=5)
+    far = torch.zeros(rows * stride, dtype=TYPES[kind], device="cuda").view(rows, stride)
+    far_h, far_w = far[:, :dim], far[:classes, dim:2 * dim]
+    far_h.copy_(h)
+    far_w.copy_(W)
+    got = P.head_distill(far_h, far_w, b, at, u, dtype=TYPES[kind])
+    for a, c in zip(want, got):
+        assert torch.equal(a, c)
+    for a, c in zip(scores[1:], P.head_scores(far_h, far_w, b, top=5)[1:]):
+        assert torch.equal(a, c)
+    for a, c in zip(P.row_scores(h, top=5)[1:], P.row_scores(far_h, top=5)[1:]):
+        assert torch.equal(a, c)
+    # outputs there, too
+    L = T._library()
+    m = T._matrix(far_h, "h", h.device)
+    out_h, out_w = far[:, 2 * dim:3 * dim], far[:classes, 3 * dim:4 * dim]
+    call, space = T._call(h.device, L.dynlp_head_distill_workspace(rows, dim, classes, 4, m.type, m.type))
+    t = T._Teacher(at.data_ptr(), u.data_ptr(), None, None, 4, 1.0, 1.0)
+    T._check(L.dynlp_head_distill(m, T._matrix(far_w, "weight", h.device), b.data_ptr(), t, None, T._matrix(out_h, "dh", h.device), T._matrix(out_w, "dweight", h.device), None, call))
+    assert torch.equal(out_h, want[1]) and torch.equal(out_w, want[2])
+    assert (far[:, 4 * dim:] == 0).all() and (far[classes:, 3 * dim:4 * dim] == 0).all()
+
+
+@pytest.mark.parametrize("kind, grad", [("float32", "float32"), ("bfloat16", "bfloat16"), ("float16", "float32")])
+@pytest.mark.parametrize("rows, dim, classes", [(1, 1, 65), (18, 1, 66), (33, 2, 200), (260, 31, 70), (20, 65, 4097)])
+def test_heads_of_few_columns(rows, dim, classes, kind, grad):
+    P = _api()
+    rng = np.random.default_rng(rows + dim)
+    h, W, b, eh, eW, eb = _head(rng, rows, dim, classes, TYPES[kind], False)
+    at, u = _lists(rng, rows, classes, 3)
+    got = _run(P, h, W, b, at, u, dtype=TYPES[grad])
+    ref = S.distill(eh, eW, eb, at, u)
+    bars = _bars(ref, eh, eW, eb, np.ones(rows), 1.0, 1.0, kind, grad, u)
+    for name, value in zip(("loss", "dh", "dweight", "dbias"), got):
+        hold(value, ref[name], bars[name], name)
